@@ -303,6 +303,76 @@ int jz_lars_mp_update_presummed_dyn(const jz_param_set* ps, const jz_lars_hparam
                                     jz_loss_scale_state* state_dev, int* found_inf_dev, void* ws, size_t ws_bytes,
                                     void* hip_stream);
 
+/* ---- residual blocks: clipping by the global norm, norms around a block, gated feed-forward block -------------------
+ * What a training step of a network of gated feed-forward residual blocks needs next to the operations above, and its
+ * serving forms.  Element types of these entry points: */
+enum { JZ_F16 = 0, JZ_BF16 = 1, JZ_F32 = 2 };
+
+/* Global norm of the gradients of many tensors, and clipping by it, on gradients that carry a loss scale S:
+ *   norm = sqrt( sum over all tensors and elements of g^2 ) / S       (squares of eight elements added in FP32, or in FP64 where they leave
+ *                                                                      its range; everything above in FP64; fixed order)
+ *   out  = RNE( c * g ),  c = max_norm / norm where norm > max_norm, else 1: the loss scale stays in the gradients
+ * found_inf_dev (DEVICE int): 1 if an element is +-Inf or NaN, else 0; with 1 (the norm is then Inf or NaN) and whenever
+ * c = 1 the gradients are not scaled: out receives a copy, in place nothing is written.  norm_dev: DEVICE float.  S is state_dev->scale when
+ * state_dev (DEVICE, as in jz_lars_mp_update_dyn) is not NULL, else loss_scale (> 0).  Clip before the optimiser sees the
+ * gradients: before jz_lars_mp_update[_dyn], or before jz_lars_grad_sumsq (a sink that a producing kernel filled holds the norm
+ * from before the clipping).  max_norm >= 0; +Inf never clips.
+ *   jz_grad_clip_prepare  writes the table of the tensors into `ws` (a blocking host-to-device copy on `hip_stream`).  Once per
+ *                         list; `ws` must then be kept intact and passed to every call with the same list.
+ *   jz_grad_norm          norm and flag only.            jz_grad_clip   norm, flag and the clipped gradients: two launches.
+ * A tensor is contiguous and aligned to its own elements (JZ_ERR_ALIGN otherwise): gradients may lie anywhere in a fused
+ * buffer.  An output is its own gradient (out == NULL, or out[t] == grads[t]) or overlaps no gradient, no other output and not the workspace
+ * (JZ_ERR_ALIAS, from jz_grad_clip_prepare).  The kernels check the table in `ws` against the list: if it is not the one prepared,
+ * *found_inf_dev = -1, *norm_dev is NaN and nothing else is written. */
+typedef struct {
+  int64_t num_tensors;      /* T >= 0 */
+  const void* const* grads; /* HOST [T] of DEVICE pointers */
+  void* const* out;         /* HOST [T] of DEVICE pointers, or NULL: in place */
+  const int64_t* numel;     /* HOST [T], >= 0 (pointers of empty tensors may be NULL) */
+  const int* dtypes;        /* HOST [T], JZ_F16 / JZ_BF16 / JZ_F32 */
+} jz_grad_list;
+int jz_grad_clip_workspace_bytes(const jz_grad_list* list, size_t* bytes);
+int jz_grad_clip_prepare(const jz_grad_list* list, void* ws, size_t ws_bytes, void* hip_stream);
+int jz_grad_norm(const jz_grad_list* list, float loss_scale, const jz_loss_scale_state* state_dev, float* norm_dev, int* found_inf_dev,
+                 void* ws, size_t ws_bytes, void* hip_stream);
+int jz_grad_clip(const jz_grad_list* list, float max_norm, float loss_scale, const jz_loss_scale_state* state_dev, float* norm_dev,
+                 int* found_inf_dev, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* The norms before and after a residual block, fused with the block's gate and the residual sum.  With
+ * rstd(v) = 1 / sqrt(mean over channels of v^2 + eps), row by row:
+ *   p     = y * rstd(y) * w_post               (the norm after the block; p = y where w_post is NULL)
+ *   r_out = res_scale * r + branch_scale * gate * p          (gate: one row of channels for each group of rows; 1 where NULL)
+ *   n     = r_out * rstd(r_out) * w_pre        (the norm before the next block)
+ * FP32 arithmetic and sums, one rounding to the type of each output; n is formed from the unrounded r_out.
+ *   r, r_out: DEVICE [rows][channels] res_dtype, the residual stream.  r_out may be r.  y, n: DEVICE [rows][channels] dtype.
+ *   w_post, w_pre: DEVICE FP32 [channels], gate: DEVICE FP32 [groups][channels] (master precision)
+ *   rstd_post, rstd_pre: DEVICE FP32 [rows], written forward, read backward; each may be NULL where its norm is not asked for
+ * Forms: r_out == NULL (with y, w_post, gate ignored or NULL): the norm of r alone, n = r * rstd(r) * w_pre.  n == NULL (with w_pre,
+ * rstd_pre): the sum alone, behind the last block.
+ * jz_norm_residual_bwd: the gradients of those outputs' inputs from dr_out (res_dtype; NULL: none arrives) and dn (dtype; NULL:
+ *   there is no n):
+ *     R  = dr_out + rstd_pre * (w_pre dn - r^ mean(w_pre dn r^)),  r^ = r_out rstd_pre          dw_pre = sum over rows of dn r^
+ *     dr = res_scale * R                                              dgate = sum over the group's rows of branch_scale p R
+ *     dp = branch_scale gate R,   dw_post = sum over rows of dp y^,   dy = rstd_post * (w_post dp - y^ mean(w_post dp y^)),  y^ = y rstd_post
+ *   (dy = dp without a post-norm).  r_out is the tensor that the forward call wrote (r itself for the norm alone, with dy == NULL).
+ *   dr: res_dtype, may be dr_out.  dy: dtype.  dw_post, dgate, dw_pre: dtype, as an optimiser's gradient buffer takes them (they carry whatever
+ *   loss scale dr_out and dn carry); required where w_post, gate, dn are given.  The sums over rows are FP32 in a fixed order.
+ * Shapes: rows >= 0 (no rows: parameter gradients are zeros), channels from 1 to 16384, any number (odd ones too); res_dtype is dtype
+ * or JZ_F32.  rows_per_group divides rows; 0 is one group.  JZ_ERR_SHAPE / JZ_ERR_UNSUPPORTED otherwise. */
+typedef struct {
+  int64_t rows;
+  int channels;
+  int64_t rows_per_group;
+  int dtype, res_dtype;
+  float eps, res_scale, branch_scale;
+} jz_norm_residual_desc;
+int jz_norm_residual_fwd(const jz_norm_residual_desc* desc, const void* r, const void* y, const float* w_post, const float* gate,
+                         const float* w_pre, void* r_out, void* n, float* rstd_post, float* rstd_pre, void* hip_stream);
+int jz_norm_residual_bwd_workspace_bytes(const jz_norm_residual_desc* desc, size_t* bytes);
+int jz_norm_residual_bwd(const jz_norm_residual_desc* desc, const void* y, const void* r_out, const float* w_post, const float* gate,
+                         const float* w_pre, const float* rstd_post, const float* rstd_pre, const void* dr_out, const void* dn, void* dr,
+                         void* dy, void* dw_post, void* dgate, void* dw_pre, void* ws, size_t ws_bytes, void* hip_stream);
+
 /* Backward-data of a convolution together with the backward pass of the batch normalization + ReLU that produced the
  * convolution's input (Section 4.2's layer; the counterpart of jz_conv2d_bn_relu_fwd):  y = relu(bn(c)) was the input of
  * this convolution in the forward pass.  One call computes

@@ -32,6 +32,7 @@ JZ_ERR_ALIGN, JZ_ERR_ALIAS, JZ_ERR_LAUNCH, JZ_ERR_NOT_PREPARED = -5, -6, -7, -8
 JZ_FWD, JZ_BWD_DATA, JZ_BWD_WEIGHT = 0, 1, 2
 JZ_BESIDE = 16
 JZ_SET_MAX = 11
+JZ_F16, JZ_BF16, JZ_F32 = 0, 1, 2
 JZ_PARAM_WEIGHT_DECAY, JZ_PARAM_LARS, JZ_PARAM_GRAD_PRESUMMED = 1, 2, 4
 
 EXPORTS = [
@@ -45,6 +46,8 @@ EXPORTS = [
     "jz_bias_grad", "jz_softmax_xent_bwd", "jz_conv2d_bn_relu_fwd_workspace_bytes", "jz_conv2d_bn_relu_fwd",
     "jz_conv2d_bwd_data_bn_relu_bwd_workspace_bytes", "jz_conv2d_bwd_data_bn_relu_bwd", "jz_conv2d_bwd_data_block_end_bwd",
     "jz_bn_workspace_bytes", "jz_bn_relu_fwd", "jz_bn_relu_bwd", "jz_bn_bwd_block_end", "jz_bn_tune_wait",
+    "jz_grad_clip_workspace_bytes", "jz_grad_clip_prepare", "jz_grad_norm", "jz_grad_clip",
+    "jz_norm_residual_fwd", "jz_norm_residual_bwd_workspace_bytes", "jz_norm_residual_bwd",
     "jz_status_string", "jz_version",
 ]
 
@@ -93,6 +96,16 @@ class jz_param_set(ctypes.Structure):
         ("grad16", ctypes.c_void_p),
         ("weight16", ctypes.c_void_p),
     ]
+
+
+class jz_grad_list(ctypes.Structure):
+    _fields_ = [("num_tensors", ctypes.c_int64), ("grads", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_void_p),
+                ("dtypes", ctypes.c_void_p)]
+
+
+class jz_norm_residual_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("channels", ctypes.c_int), ("rows_per_group", ctypes.c_int64), ("dtype", ctypes.c_int),
+                ("res_dtype", ctypes.c_int), ("eps", ctypes.c_float), ("res_scale", ctypes.c_float), ("branch_scale", ctypes.c_float)]
 
 
 _lib = None
@@ -164,6 +177,14 @@ def lib() -> ctypes.CDLL:
         L.jz_conv2d_bwd_data_bn_relu_bwd_workspace_bytes.argtypes = [dp, ctypes.POINTER(sz)]
         L.jz_conv2d_bwd_data_bn_relu_bwd.argtypes = [dp] + [vp] * 12 + [sz, vp]
         L.jz_conv2d_bwd_data_block_end_bwd.argtypes = [dp] + [vp] * 13 + [sz, vp]
+        gp, np_ = ctypes.POINTER(jz_grad_list), ctypes.POINTER(jz_norm_residual_desc)
+        L.jz_grad_clip_workspace_bytes.argtypes = [gp, ctypes.POINTER(sz)]
+        L.jz_grad_clip_prepare.argtypes = [gp, vp, sz, vp]
+        L.jz_grad_norm.argtypes = [gp, cf, vp, vp, vp, vp, sz, vp]
+        L.jz_grad_clip.argtypes = [gp, cf, cf, vp, vp, vp, vp, sz, vp]
+        L.jz_norm_residual_fwd.argtypes = [np_] + [vp] * 10
+        L.jz_norm_residual_bwd_workspace_bytes.argtypes = [np_, ctypes.POINTER(sz)]
+        L.jz_norm_residual_bwd.argtypes = [np_] + [vp] * 15 + [sz, vp]
         L.jz_status_string.argtypes = [ci]
         L.jz_status_string.restype = ctypes.c_char_p
         L.jz_version.argtypes = []
@@ -860,3 +881,106 @@ def jz_conv2d_bwd_data_block_end_bwd(desc, dy16, w16, dyb16, bn_x16, y_out16, ga
     (no ReLU, input bn_x16) of dy = g16."""
     bind_conv2d_bwd_data_block_end_bwd(desc, dy16, w16, dyb16, bn_x16, y_out16, gamma, save_mean, save_invstd, g16, bn_dx16, dgamma16,
                                        dbeta16, ws)(stream)
+
+
+# ---------------------------------------------------------------------------------------------
+# residual blocks: clipping by the global norm, norms around a block, gated feed-forward block
+# ---------------------------------------------------------------------------------------------
+_DTYPES = {torch.float16: JZ_F16, torch.bfloat16: JZ_BF16, torch.float32: JZ_F32}
+_TORCH_TYPES = (torch.float16, torch.bfloat16, torch.float32)
+
+
+def dtype_of(dtype: torch.dtype) -> int:
+    """JZ_F16, JZ_BF16 or JZ_F32."""
+    if dtype not in _DTYPES:
+        raise TypeError("no kernels for %s: float16, bfloat16 or float32" % dtype)
+    return _DTYPES[dtype]
+
+
+class GradList:
+    """A jz_grad_list with its host tables: gradients on the GPU (contiguous, float16, bfloat16 or float32, mixed as they come) and
+    where their clipped values go (None: in place).  Keeps the tensors alive."""
+
+    def __init__(self, grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]] = None):
+        self.grads, self.out = tuple(grads), tuple(out) if out is not None else None
+        T = len(self.grads)
+        if self.out is not None and len(self.out) != T:
+            raise ValueError("one output for each gradient")
+        for i, g in enumerate(self.grads):
+            dtype_of(g.dtype)
+            _dev_ptr(g, g.dtype, None, "gradient %d" % i)
+            if self.out is not None:
+                _dev_ptr(self.out[i], g.dtype, g.numel(), "output %d" % i)
+        ptrs = lambda ts: np.array([t.data_ptr() for t in ts], dtype=np.uint64)
+        self._tables = (ptrs(self.grads), ptrs(self.out) if self.out is not None else None,
+                        np.array([g.numel() for g in self.grads], dtype=np.int64), np.array([_DTYPES[g.dtype] for g in self.grads], dtype=np.int32))
+        self.c = jz_grad_list(T, *(None if a is None else a.ctypes.data for a in self._tables))
+
+
+def jz_grad_clip_workspace_bytes(grads: GradList) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().jz_grad_clip_workspace_bytes(ctypes.byref(grads.c), ctypes.byref(n)), "jz_grad_clip_workspace_bytes")
+    return n.value
+
+
+def jz_grad_clip_prepare(grads: GradList, ws: torch.Tensor, stream=None):
+    wp, wn = _ws(ws)
+    _check(lib().jz_grad_clip_prepare(ctypes.byref(grads.c), wp, wn, _stream(stream)), "jz_grad_clip_prepare")
+
+
+def jz_grad_norm(grads: GradList, norm: torch.Tensor, found_inf: torch.Tensor, ws: torch.Tensor, loss_scale: float = 1.0,
+                 state: Optional[torch.Tensor] = None, stream=None):
+    """norm (float32[1]) of the un-scaled gradients and the overflow flag (int32[1])."""
+    wp, wn = _ws(ws)
+    _check(lib().jz_grad_norm(ctypes.byref(grads.c), float(loss_scale), _ls_state(state) if state is not None else None,
+                              _dev_ptr(norm, torch.float32, 1, "norm"), _flag(found_inf), wp, wn, _stream(stream)), "jz_grad_norm")
+
+
+def jz_grad_clip(grads: GradList, max_norm: float, norm: torch.Tensor, found_inf: torch.Tensor, ws: torch.Tensor, loss_scale: float = 1.0,
+                 state: Optional[torch.Tensor] = None, stream=None):
+    """jz_grad_norm, then the gradients scaled by max_norm / norm where norm > max_norm, into the list's outputs or in place."""
+    wp, wn = _ws(ws)
+    _check(lib().jz_grad_clip(ctypes.byref(grads.c), float(max_norm), float(loss_scale), _ls_state(state) if state is not None else None,
+                              _dev_ptr(norm, torch.float32, 1, "norm"), _flag(found_inf), wp, wn, _stream(stream)), "jz_grad_clip")
+
+
+def norm_residual_desc(rows: int, channels: int, rows_per_group: int = 0, dtype: int = JZ_F16, res_dtype: Optional[int] = None, eps: float = 1e-5,
+                       res_scale: float = 1.0, branch_scale: float = 1.0) -> jz_norm_residual_desc:
+    return jz_norm_residual_desc(rows, channels, rows_per_group, dtype, dtype if res_dtype is None else res_dtype, eps, res_scale, branch_scale)
+
+
+def _norm_types(d):
+    """(element type, residual type, elements, gate groups) of a descriptor; a type that does not exist is the library's to refuse."""
+    t = _TORCH_TYPES[d.dtype] if 0 <= d.dtype <= 2 else None
+    rt = _TORCH_TYPES[d.res_dtype] if 0 <= d.res_dtype <= 2 else None
+    return t, rt, d.rows * d.channels, d.rows // d.rows_per_group if d.rows_per_group > 0 else 1
+
+
+def jz_norm_residual_fwd(desc, r, y, w_post, gate, w_pre, r_out, n, rstd_post=None, rstd_pre=None, stream=None):
+    """r_out = res_scale * r + branch_scale * gate * norm(y) * w_post and n = norm(r_out) * w_pre; r_out None: n from r alone; n None:
+    the sum alone; w_post None: y as it is; gate None: 1."""
+    t, rt, e, groups = _norm_types(desc)
+    C, f = desc.channels, torch.float32
+    _check(lib().jz_norm_residual_fwd(ctypes.byref(desc), _dev_ptr(r, rt, e, "r"), _dev_ptr(y, t, e, "y"), _dev_ptr(w_post, f, C, "w_post"),
+                                      _dev_ptr(gate, f, groups * C, "gate"), _dev_ptr(w_pre, f, C, "w_pre"), _dev_ptr(r_out, rt, e, "r_out"),
+                                      _dev_ptr(n, t, e, "n"), _dev_ptr(rstd_post, f, desc.rows, "rstd_post"),
+                                      _dev_ptr(rstd_pre, f, desc.rows, "rstd_pre"), _stream(stream)), "jz_norm_residual_fwd")
+
+
+def jz_norm_residual_bwd_workspace_bytes(desc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().jz_norm_residual_bwd_workspace_bytes(ctypes.byref(desc), ctypes.byref(n)), "jz_norm_residual_bwd_workspace_bytes")
+    return n.value
+
+
+def jz_norm_residual_bwd(desc, y, r_out, w_post, gate, w_pre, rstd_post, rstd_pre, dr_out, dn, dr, dy, dw_post, dgate, dw_pre, ws, stream=None):
+    """dr, dy, dw_post, dgate, dw_pre from dr_out (None: none arrives) and dn (None: there was no n); dy None: the norm of r alone."""
+    t, rt, e, groups = _norm_types(desc)
+    C, f = desc.channels, torch.float32
+    wp, wn = _ws(ws)
+    _check(lib().jz_norm_residual_bwd(ctypes.byref(desc), _dev_ptr(y, t, e, "y"), _dev_ptr(r_out, rt, e, "r_out"), _dev_ptr(w_post, f, C, "w_post"),
+                                      _dev_ptr(gate, f, groups * C, "gate"), _dev_ptr(w_pre, f, C, "w_pre"),
+                                      _dev_ptr(rstd_post, f, desc.rows, "rstd_post"), _dev_ptr(rstd_pre, f, desc.rows, "rstd_pre"),
+                                      _dev_ptr(dr_out, rt, e, "dr_out"), _dev_ptr(dn, t, e, "dn"), _dev_ptr(dr, rt, e, "dr"), _dev_ptr(dy, t, e, "dy"),
+                                      _dev_ptr(dw_post, t, C, "dw_post"), _dev_ptr(dgate, t, groups * C, "dgate"), _dev_ptr(dw_pre, t, C, "dw_pre"),
+                                      wp, wn, _stream(stream)), "jz_norm_residual_bwd")
