@@ -373,6 +373,38 @@ int jz_norm_residual_bwd(const jz_norm_residual_desc* desc, const void* y, const
                          const float* w_pre, const float* rstd_post, const float* rstd_pre, const void* dr_out, const void* dn, void* dr,
                          void* dy, void* dw_post, void* dgate, void* dw_pre, void* ws, size_t ws_bytes, void* hip_stream);
 
+/* Gated feed-forward block on rows (tokens) of features, FP16 or BF16 storage, FP32 sums:
+ *   gate = x W_gate^T,  up = x W_up^T,  h = act(gate) * up,  y = h W_down^T
+ * x [rows][in_features], W_gate and W_up [hidden][in_features], W_down [out_features][hidden], y [rows][out_features], all
+ * DEVICE, dtype JZ_F16 or JZ_BF16 (JZ_F32: JZ_ERR_UNSUPPORTED).  The two projections, the activation and the product are one
+ * kernel; the product is formed from the FP32 sums and rounded once.
+ *   h         [rows][hidden] out: what the second product reads, and the backward pass
+ *   gate, up  [rows][hidden] out, both or neither: the projections, rounded, for the backward pass; NULL when none follows
+ * jz_ffn_bwd, with dh = dy W_down and act evaluated at the rounded gate:
+ *   dup = RNE(dh act(gate)),  dgate = RNE(dh up act'(gate)),  dx = RNE(dgate W_gate + dup W_up)  (one FP32 sum),
+ *   dW_gate = RNE(dgate^T x),  dW_up = RNE(dup^T x),  dW_down = RNE(dy^T h)
+ *   dx may be NULL (the first block); dw_gate, dw_up, dw_down all or none (frozen weights; x and h may then be NULL).
+ * Activations: SILU v sigmoid(v); GELU v Phi(v) by the error function; GELU_TANH its tanh form; RELU with derivative 0 at 0.
+ * Sizes: any positive feature counts (multiples of 8 with strides that are multiples of 8 take the LDS-direct kernels), rows >= 0
+ * (without rows the weight gradients are zeros).  *_stride: elements from one row to the next of x, y, dx, dy; 0 is dense, below the feature
+ * count is JZ_ERR_SHAPE; h, gate, up and the weights are dense.  Feature counts and strides up to 2^24, rows up to 2^31.
+ * Workspace: dgate and dup, and partial sums (FP32) of reductions that are split where there are few rows or few features; with less
+ * than the backward call's dgate and dup need: JZ_ERR_WORKSPACE, with less than reported otherwise fewer splits. */
+enum { JZ_ACT_SILU = 0, JZ_ACT_GELU = 1, JZ_ACT_GELU_TANH = 2, JZ_ACT_RELU = 3 };
+typedef struct {
+  int64_t rows;
+  int in_features, hidden, out_features;
+  int act, dtype;
+  int64_t x_stride, y_stride, dx_stride, dy_stride;
+} jz_ffn_desc;
+int jz_ffn_fwd_workspace_bytes(const jz_ffn_desc* desc, size_t* bytes);
+int jz_ffn_fwd(const jz_ffn_desc* desc, const void* x, const void* w_gate, const void* w_up, const void* w_down, void* h, void* gate,
+               void* up, void* y, void* ws, size_t ws_bytes, void* hip_stream);
+int jz_ffn_bwd_workspace_bytes(const jz_ffn_desc* desc, size_t* bytes);
+int jz_ffn_bwd(const jz_ffn_desc* desc, const void* x, const void* w_gate, const void* w_up, const void* w_down, const void* gate,
+               const void* up, const void* h, const void* dy, void* dx, void* dw_gate, void* dw_up, void* dw_down, void* ws, size_t ws_bytes,
+               void* hip_stream);
+
 /* Backward-data of a convolution together with the backward pass of the batch normalization + ReLU that produced the
  * convolution's input (Section 4.2's layer; the counterpart of jz_conv2d_bn_relu_fwd):  y = relu(bn(c)) was the input of
  * this convolution in the forward pass.  One call computes

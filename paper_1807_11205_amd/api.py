@@ -33,6 +33,7 @@ JZ_FWD, JZ_BWD_DATA, JZ_BWD_WEIGHT = 0, 1, 2
 JZ_BESIDE = 16
 JZ_SET_MAX = 11
 JZ_F16, JZ_BF16, JZ_F32 = 0, 1, 2
+JZ_ACT_SILU, JZ_ACT_GELU, JZ_ACT_GELU_TANH, JZ_ACT_RELU = 0, 1, 2, 3
 JZ_PARAM_WEIGHT_DECAY, JZ_PARAM_LARS, JZ_PARAM_GRAD_PRESUMMED = 1, 2, 4
 
 EXPORTS = [
@@ -48,6 +49,7 @@ EXPORTS = [
     "jz_bn_workspace_bytes", "jz_bn_relu_fwd", "jz_bn_relu_bwd", "jz_bn_bwd_block_end", "jz_bn_tune_wait",
     "jz_grad_clip_workspace_bytes", "jz_grad_clip_prepare", "jz_grad_norm", "jz_grad_clip",
     "jz_norm_residual_fwd", "jz_norm_residual_bwd_workspace_bytes", "jz_norm_residual_bwd",
+    "jz_ffn_fwd_workspace_bytes", "jz_ffn_fwd", "jz_ffn_bwd_workspace_bytes", "jz_ffn_bwd",
     "jz_status_string", "jz_version",
 ]
 
@@ -106,6 +108,12 @@ class jz_grad_list(ctypes.Structure):
 class jz_norm_residual_desc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("channels", ctypes.c_int), ("rows_per_group", ctypes.c_int64), ("dtype", ctypes.c_int),
                 ("res_dtype", ctypes.c_int), ("eps", ctypes.c_float), ("res_scale", ctypes.c_float), ("branch_scale", ctypes.c_float)]
+
+
+class jz_ffn_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("in_features", ctypes.c_int), ("hidden", ctypes.c_int), ("out_features", ctypes.c_int),
+                ("act", ctypes.c_int), ("dtype", ctypes.c_int), ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64),
+                ("dx_stride", ctypes.c_int64), ("dy_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -185,6 +193,10 @@ def lib() -> ctypes.CDLL:
         L.jz_norm_residual_fwd.argtypes = [np_] + [vp] * 10
         L.jz_norm_residual_bwd_workspace_bytes.argtypes = [np_, ctypes.POINTER(sz)]
         L.jz_norm_residual_bwd.argtypes = [np_] + [vp] * 15 + [sz, vp]
+        fp = ctypes.POINTER(jz_ffn_desc)
+        L.jz_ffn_fwd_workspace_bytes.argtypes = L.jz_ffn_bwd_workspace_bytes.argtypes = [fp, ctypes.POINTER(sz)]
+        L.jz_ffn_fwd.argtypes = [fp] + [vp] * 9 + [sz, vp]
+        L.jz_ffn_bwd.argtypes = [fp] + [vp] * 13 + [sz, vp]
         L.jz_status_string.argtypes = [ci]
         L.jz_status_string.restype = ctypes.c_char_p
         L.jz_version.argtypes = []
@@ -984,3 +996,57 @@ def jz_norm_residual_bwd(desc, y, r_out, w_post, gate, w_pre, rstd_post, rstd_pr
                                       _dev_ptr(dr_out, rt, e, "dr_out"), _dev_ptr(dn, t, e, "dn"), _dev_ptr(dr, rt, e, "dr"), _dev_ptr(dy, t, e, "dy"),
                                       _dev_ptr(dw_post, t, C, "dw_post"), _dev_ptr(dgate, t, groups * C, "dgate"), _dev_ptr(dw_pre, t, C, "dw_pre"),
                                       wp, wn, _stream(stream)), "jz_norm_residual_bwd")
+
+
+def ffn_desc(rows: int, in_features: int, hidden: int, out_features: int, act: int = JZ_ACT_SILU, dtype: int = JZ_F16, x_stride: int = 0,
+             y_stride: int = 0, dx_stride: int = 0, dy_stride: int = 0) -> jz_ffn_desc:
+    """Strides are elements from one row to the next, 0: dense."""
+    return jz_ffn_desc(rows, in_features, hidden, out_features, act, dtype, x_stride, y_stride, dx_stride, dy_stride)
+
+
+def _rows_ptr(t: Optional[torch.Tensor], dtype, rows: int, cols: int, stride: int, what: str) -> Optional[int]:
+    """A [rows][cols] tensor whose rows are `stride` elements apart (0: dense)."""
+    if t is None or stride in (0, cols):
+        return _dev_ptr(t, dtype, rows * cols, what)
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 2:
+        raise TypeError("%s must be a two-dimensional %s tensor on the GPU" % (what, dtype))
+    if t.shape != (rows, cols) or (rows and t.stride(1) != 1 and cols > 1) or (rows > 1 and t.stride(0) != stride):
+        raise ValueError("%s must be [%d, %d] with rows %d elements apart" % (what, rows, cols, stride))
+    return t.data_ptr() if t.numel() else None
+
+
+def jz_ffn_fwd_workspace_bytes(desc: jz_ffn_desc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().jz_ffn_fwd_workspace_bytes(ctypes.byref(desc), ctypes.byref(n)), "jz_ffn_fwd_workspace_bytes")
+    return n.value
+
+
+def jz_ffn_bwd_workspace_bytes(desc: jz_ffn_desc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().jz_ffn_bwd_workspace_bytes(ctypes.byref(desc), ctypes.byref(n)), "jz_ffn_bwd_workspace_bytes")
+    return n.value
+
+
+def _ffn_type(d):
+    return _TORCH_TYPES[d.dtype] if 0 <= d.dtype <= 2 else None
+
+
+def jz_ffn_fwd(desc, x, w_gate, w_up, w_down, h, y, gate=None, up=None, ws=None, stream=None):
+    """h = act(x w_gate^T) * (x w_up^T), y = h w_down^T; gate and up receive the projections where a backward pass follows."""
+    d, t = desc, _ffn_type(desc)
+    M, D, F, O = d.rows, d.in_features, d.hidden, d.out_features
+    wp, wn = _ws(ws)
+    _check(lib().jz_ffn_fwd(ctypes.byref(d), _rows_ptr(x, t, M, D, d.x_stride, "x"), _dev_ptr(w_gate, t, F * D, "w_gate"), _dev_ptr(w_up, t, F * D, "w_up"),
+                            _dev_ptr(w_down, t, O * F, "w_down"), _dev_ptr(h, t, M * F, "h"), _dev_ptr(gate, t, M * F, "gate"), _dev_ptr(up, t, M * F, "up"),
+                            _rows_ptr(y, t, M, O, d.y_stride, "y"), wp, wn, _stream(stream)), "jz_ffn_fwd")
+
+
+def jz_ffn_bwd(desc, x, w_gate, w_up, w_down, gate, up, h, dy, dx, dw_gate, dw_up, dw_down, ws=None, stream=None):
+    """The gradients of jz_ffn_fwd; dx may be None, and the three weight gradients together."""
+    d, t = desc, _ffn_type(desc)
+    M, D, F, O = d.rows, d.in_features, d.hidden, d.out_features
+    wp, wn = _ws(ws)
+    _check(lib().jz_ffn_bwd(ctypes.byref(d), _rows_ptr(x, t, M, D, d.x_stride, "x"), _dev_ptr(w_gate, t, F * D, "w_gate"), _dev_ptr(w_up, t, F * D, "w_up"),
+                            _dev_ptr(w_down, t, O * F, "w_down"), _dev_ptr(gate, t, M * F, "gate"), _dev_ptr(up, t, M * F, "up"), _dev_ptr(h, t, M * F, "h"),
+                            _rows_ptr(dy, t, M, O, d.dy_stride, "dy"), _rows_ptr(dx, t, M, D, d.dx_stride, "dx"), _dev_ptr(dw_gate, t, F * D, "dw_gate"),
+                            _dev_ptr(dw_up, t, F * D, "dw_up"), _dev_ptr(dw_down, t, O * F, "dw_down"), wp, wn, _stream(stream)), "jz_ffn_bwd")

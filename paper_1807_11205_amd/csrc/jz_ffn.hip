@@ -1,0 +1,195 @@
+// Gated feed-forward block, forward and backward (include/jz.h: jz_ffn_fwd, jz_ffn_bwd): planning and entry points; the products are
+// in jz_ffn_gemm.h.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "jz_internal.h"
+
+namespace {
+
+#include "jz_lds_dma.h"
+#include "jz_vec.h"
+#include "jz_ffn_gemm.h"
+
+struct FfnTensor {
+  const void* p;
+  size_t bytes;
+  bool out;
+};
+int ffn_look_over(const FfnTensor* t, int n, const void* ws, size_t ws_bytes) {
+  for (int i = 0; i < n; ++i)
+    if (t[i].p && !jz::aligned16(t[i].p)) return JZ_ERR_ALIGN;
+  for (int i = 0; i < n; ++i) {
+    if (jz::overlaps(t[i].p, t[i].bytes, ws, ws_bytes)) return JZ_ERR_ALIAS;
+    for (int j = i + 1; j < n; ++j)
+      if ((t[i].out || t[j].out) && jz::overlaps(t[i].p, t[i].bytes, t[j].p, t[j].bytes)) return JZ_ERR_ALIAS;
+  }
+  return JZ_OK;
+}
+
+struct FfnShape {
+  int64_t M, D, F, O, ldx, ldy, lddx, lddy;
+};
+int ffn_shape(const jz_ffn_desc* d, FfnShape* s) {
+  if (!d) return JZ_ERR_NULL;
+  if (d->rows < 0 || d->in_features <= 0 || d->hidden <= 0 || d->out_features <= 0 || d->act < JZ_ACT_SILU || d->act > JZ_ACT_RELU || d->dtype < JZ_F16 ||
+      d->dtype > JZ_F32)
+    return JZ_ERR_SHAPE;
+  const int64_t in = d->in_features, out = d->out_features;
+  *s = {d->rows, in, d->hidden, out, d->x_stride ? d->x_stride : in, d->y_stride ? d->y_stride : out, d->dx_stride ? d->dx_stride : in,
+        d->dy_stride ? d->dy_stride : out};
+  if (s->ldx < in || s->ldy < out || s->lddx < in || s->lddy < out) return JZ_ERR_SHAPE;
+  // a tensor's bytes stay far inside 64 bits, tile counts inside a grid
+  const int64_t most = int64_t(1) << 24;
+  if (d->dtype == JZ_F32 || d->rows > (int64_t(1) << 31) || in > most || d->hidden > most || out > most || std::max(std::max(s->ldx, s->ldy), std::max(s->lddx, s->lddy)) > most)
+    return JZ_ERR_UNSUPPORTED;
+  return JZ_OK;
+}
+// bytes from the first to the last element of rows x cols with a row pitch
+size_t span(int64_t rows, int64_t cols, int64_t ld) { return rows ? ((size_t)(rows - 1) * ld + cols) * 2 : 0; }
+
+template <int BM, int BN>
+void set_tiles(GemmArgs* a, int epi) {
+  for (int i = 0; i < a->products; ++i) {
+    a->p[i].tiles_m = (int)((a->p[i].M + BM - 1) / BM);
+    const int64_t cols = epi == EPI_GLU ? 2 * ((a->p[i].N + 31) / 32 * 32) : a->p[i].N;
+    a->p[i].tiles_n = (int)((cols + BN - 1) / BN);
+  }
+}
+int tile_count(const GemmArgs& a) {
+  int n = 0;
+  for (int i = 0; i < a.products; ++i) n += a.p[i].tiles_m * a.p[i].tiles_n;
+  return n;
+}
+
+template <class T, bool KCA, bool KCB, int EPI>
+int gemm(GemmArgs a, hipStream_t st) {
+  set_tiles<128, 128>(&a, EPI);
+  a.splits = 1;
+  a.tiles_per_split = 0x7fffffff;
+  const int tiles = tile_count(a);
+  if (tiles > 0) ffn_gemm_any<T, KCA, KCB, EPI, 128, 128><<<tiles, 256, 0, st>>>(a);
+  return jz::launch_status();
+}
+
+Product product(const void* a, int64_t lda, const void* b, int64_t ldb, void* c, int64_t ldc, int64_t M, int64_t N, int64_t K) {
+  Product p = {};
+  p.a[0] = p.a[1] = a;
+  p.b[0] = p.b[1] = b;
+  p.c = c;
+  p.lda = lda;
+  p.ldb = ldb;
+  p.ldc = ldc;
+  p.M = M;
+  p.N = N;
+  p.K = K;
+  return p;
+}
+GemmArgs one(const Product& p, int act) {
+  GemmArgs a = {};
+  a.p[0] = p;
+  a.products = a.parts = 1;
+  a.act = act;
+  return a;
+}
+
+template <class T>
+int run_fwd(const FfnShape& s, int act, const void* x, const void* wg, const void* wu, const void* wd, void* h, void* gate, void* up, void* y, hipStream_t st) {
+  GemmArgs a = one(product(x, s.ldx, wg, s.D, h, s.F, s.M, s.F, s.D), act);
+  a.p[0].b[1] = wu;
+  a.out0 = gate;
+  a.out1 = up;
+  int rc = gemm<T, true, true, EPI_GLU>(a, st);
+  if (rc == JZ_OK) rc = gemm<T, true, true, EPI_STORE>(one(product(h, s.F, wd, s.F, y, s.ldy, s.M, s.O, s.F), act), st);
+  return rc;
+}
+
+template <class T>
+int run_bwd(const FfnShape& s, int act, const void* x, const void* wg, const void* wu, const void* wd, const void* gate, const void* up, const void* h, const void* dy,
+            void* dx, void* dwg, void* dwu, void* dwd, void* dgate, void* dup, hipStream_t st) {
+  GemmArgs a = one(product(dy, s.lddy, wd, s.F, nullptr, 0, s.M, s.F, s.O), act);
+  a.gate = gate;
+  a.up = up;
+  a.out0 = dgate;
+  a.out1 = dup;
+  int rc = gemm<T, true, false, EPI_GLU_BWD>(a, st);
+  if (rc == JZ_OK && dx) {
+    a = one(product(dgate, s.F, wg, s.D, dx, s.lddx, s.M, s.D, s.F), act);
+    a.p[0].a[1] = dup;
+    a.p[0].b[1] = wu;
+    a.parts = 2;
+    rc = gemm<T, true, false, EPI_STORE>(a, st);
+  }
+  if (rc == JZ_OK && dwg) {
+    a = one(product(dgate, s.F, x, s.ldx, dwg, s.D, s.F, s.D, s.M), act);
+    a.p[1] = product(dup, s.F, x, s.ldx, dwu, s.D, s.F, s.D, s.M);
+    a.p[2] = product(dy, s.lddy, h, s.F, dwd, s.F, s.O, s.F, s.M);
+    a.products = 3;
+    rc = gemm<T, false, false, EPI_STORE>(a, st);
+  }
+  return rc;
+}
+
+size_t hidden_bytes(const FfnShape& s) { return ((size_t)s.M * s.F * 2 + 255) & ~size_t(255); }
+
+}  // namespace
+
+extern "C" int jz_ffn_fwd_workspace_bytes(const jz_ffn_desc* d, size_t* bytes) {
+  if (!bytes) return JZ_ERR_NULL;
+  FfnShape s;
+  const int rc = ffn_shape(d, &s);
+  if (rc == JZ_OK) *bytes = 0;
+  return rc;
+}
+
+extern "C" int jz_ffn_bwd_workspace_bytes(const jz_ffn_desc* d, size_t* bytes) {
+  if (!bytes) return JZ_ERR_NULL;
+  FfnShape s;
+  const int rc = ffn_shape(d, &s);
+  if (rc == JZ_OK) *bytes = 2 * hidden_bytes(s);
+  return rc;
+}
+
+extern "C" int jz_ffn_fwd(const jz_ffn_desc* d, const void* x, const void* w_gate, const void* w_up, const void* w_down, void* h, void* gate, void* up, void* y,
+                          void* ws, size_t ws_bytes, void* hip_stream) {
+  FfnShape s;
+  int rc = ffn_shape(d, &s);
+  if (rc != JZ_OK) return rc;
+  if (!w_gate || !w_up || !w_down || (s.M && (!x || !h || !y || !gate != !up))) return JZ_ERR_NULL;
+  if (s.M == 0) return JZ_OK;
+  const size_t hid = span(s.M, s.F, s.F), w = span(s.F, s.D, s.D);
+  const FfnTensor t[] = {{x, span(s.M, s.D, s.ldx), false}, {w_gate, w, false}, {w_up, w, false}, {w_down, span(s.O, s.F, s.F), false}, {h, hid, true},
+                         {gate, hid, true}, {up, hid, true}, {y, span(s.M, s.O, s.ldy), true}};
+  rc = ffn_look_over(t, 8, ws, ws_bytes);
+  if (rc != JZ_OK) return rc;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  return d->dtype == JZ_F16 ? run_fwd<_Float16>(s, d->act, x, w_gate, w_up, w_down, h, gate, up, y, st)
+                            : run_fwd<__bf16>(s, d->act, x, w_gate, w_up, w_down, h, gate, up, y, st);
+}
+
+extern "C" int jz_ffn_bwd(const jz_ffn_desc* d, const void* x, const void* w_gate, const void* w_up, const void* w_down, const void* gate, const void* up,
+                          const void* h, const void* dy, void* dx, void* dw_gate, void* dw_up, void* dw_down, void* ws, size_t ws_bytes, void* hip_stream) {
+  FfnShape s;
+  int rc = ffn_shape(d, &s);
+  if (rc != JZ_OK) return rc;
+  const bool weights = dw_gate || dw_up || dw_down;
+  if (!w_gate || !w_up || !w_down || (weights && (!dw_gate || !dw_up || !dw_down))) return JZ_ERR_NULL;
+  if (s.M && (!gate || !up || !dy || (weights && (!x || !h)) || (!dx && !weights))) return JZ_ERR_NULL;
+  const size_t need = 2 * hidden_bytes(s);
+  if (need && (!ws || ws_bytes < need)) return JZ_ERR_WORKSPACE;
+  if (need && !jz::aligned16(ws)) return JZ_ERR_ALIGN;
+  const size_t hid = span(s.M, s.F, s.F), w = span(s.F, s.D, s.D), w2 = span(s.O, s.F, s.F);
+  const FfnTensor t[] = {{weights ? x : nullptr, span(s.M, s.D, s.ldx), false}, {w_gate, w, false}, {w_up, w, false}, {w_down, w2, false}, {gate, hid, false}, {up, hid, false},
+                         {weights ? h : nullptr, hid, false}, {dy, span(s.M, s.O, s.lddy), false}, {dx, span(s.M, s.D, s.lddx), true}, {dw_gate, w, true}, {dw_up, w, true},
+                         {dw_down, w2, true}};
+  rc = ffn_look_over(t, 12, ws, need);
+  if (rc != JZ_OK) return rc;
+  char* b = static_cast<char*>(ws);
+  void *dgate = b, *dup = b + hidden_bytes(s);
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  return d->dtype == JZ_F16 ? run_bwd<_Float16>(s, d->act, x, w_gate, w_up, w_down, gate, up, h, dy, dx, dw_gate, dw_up, dw_down, dgate, dup, st)
+                            : run_bwd<__bf16>(s, d->act, x, w_gate, w_up, w_down, gate, up, h, dy, dx, dw_gate, dw_up, dw_down, dgate, dup, st);
+}

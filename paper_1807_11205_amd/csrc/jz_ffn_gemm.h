@@ -1,0 +1,294 @@
+// The matrix products of the gated feed-forward block: C[m][n] = sum over k of A(m, k) B(n, k), FP16 or BF16 operands, FP32 sums,
+// with the block's activation, product and their derivatives in the epilogue.  Included inside jz_ffn.hip's anonymous namespace.
+//
+// An operand is k-contiguous (KC, [row][k]) or row-contiguous (MC, [k][row]):
+//     forward   gate, up   A = x  KC     B = W_gate and W_up, interleaved 32 rows by 32 rows   KC
+//               down       A = h  KC     B = W_down KC
+//     backward  dh         A = dy KC     B = W_down MC
+//               dx         A = dgate, then dup KC     B = W_gate, then W_up MC         (one sum over 2 F)
+//               dW         A = dgate, dup, dy MC      B = x, x, h MC                    (three products in one launch)
+//
+// Tiles.  BM x BN x 64, four wavefronts in 2 x 2, each (BM / 2) x (BN / 2) in 32x32x16 matrix instructions with the operands exchanged, so
+// that a lane has four consecutive n of one m.  Two tiles of operands in LDS:
+//     KC  [row][8 chunks of 16 bytes], chunk c at position c ^ (row % 8); an operand is one 16-byte read
+//     MC  [k][ROWS / 8 chunks], chunk c at position c ^ 4 (k % 4); an operand is two 8-byte transposing reads
+// Both orders keep the reads of a wavefront on different banks.
+#pragma once
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+template <class T>
+using Op8 = typename Vec8<T>::V;
+
+__device__ __forceinline__ f32x16 mfma(Op8<_Float16> a, Op8<_Float16> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mfma(Op8<__bf16> a, Op8<__bf16> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+constexpr int BK = 64;
+
+// ---- activations ----------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
+constexpr float GELU_K = 0.7978845608028654f, GELU_C = 0.044715f;  // sqrt(2 / pi)
+
+__device__ __forceinline__ float act_fwd(int kind, float g) {
+  if (kind == JZ_ACT_SILU) return g * sigmoid(g);
+  if (kind == JZ_ACT_GELU_TANH) return g * sigmoid(2.f * GELU_K * (g + GELU_C * g * g * g));  // (1 + tanh z) / 2 = sigmoid(2 z)
+  if (kind == JZ_ACT_GELU) return 0.5f * g * erfcf(g * -0.7071067811865476f);
+  return !(g <= 0.f) ? g : 0.f;
+}
+// act and its derivative
+__device__ __forceinline__ float act_both(int kind, float g, float* slope) {
+  if (kind == JZ_ACT_SILU) {
+    const float s = sigmoid(g);
+    *slope = s * (1.f + g * (1.f - s));
+    return g * s;
+  }
+  if (kind == JZ_ACT_GELU_TANH) {
+    const float s = sigmoid(2.f * GELU_K * (g + GELU_C * g * g * g));
+    // beyond 30 the derivative is 0 or 1 to the last bit, and the cube below may overflow
+    *slope = fabsf(g) > 30.f ? (g > 0.f ? 1.f : 0.f) : s + g * s * (1.f - s) * (2.f * GELU_K) * (1.f + 3.f * GELU_C * g * g);
+    return g * s;
+  }
+  if (kind == JZ_ACT_GELU) {
+    const float phi = 0.5f * erfcf(g * -0.7071067811865476f);
+    *slope = phi + g * __expf(-0.5f * g * g) * 0.3989422804014327f;
+    return g * phi;
+  }
+  *slope = !(g <= 0.f) ? 1.f : 0.f;
+  return !(g <= 0.f) ? g : 0.f;
+}
+
+// ---- arguments ------------------------------------------------------------------------------------------------------------
+enum { EPI_STORE = 0, EPI_GLU = 1, EPI_GLU_BWD = 2 };
+
+struct Product {           // one product of a launch
+  const void *a[2], *b[2];  // [1]: the second part of the sum (dx), or the matrix interleaved with b[0] (gate and up)
+  void* c;
+  int64_t lda, ldb, ldc;    // elements
+  int64_t M, N, K;          // K of one part; N: columns of C (hidden units where gate and up are interleaved)
+  int tiles_m, tiles_n;
+};
+struct GemmArgs {
+  Product p[3];
+  int products, parts;      // parts of the sum: 1 or 2
+  int act;
+  int splits;               // of the k tiles, over blockIdx.y; above 1 the sums go to `partial`
+  int tiles_per_split;
+  float* partial;           // [splits][M][pitch], the products one behind the other
+  int64_t partial_pitch, partial_size;
+  const void *gate, *up;    // EPI_GLU_BWD: the saved projections, [M][N]
+  void *out0, *out1;        // EPI_GLU: gate and up, or NULL; EPI_GLU_BWD: dgate and dup
+};
+
+// ---- results --------------------------------------------------------------------------------------------------------------
+// What becomes of eight sums (or gate and up sums) that belong to columns n .. n + 7 of row m.
+template <class T, int EPI>
+__device__ __forceinline__ void finish8(const GemmArgs& a, const Product& p, int64_t m, int64_t n, f32x8 v, f32x8 w) {
+  const int left = p.N - n < 8 ? (int)(p.N - n) : 8;
+  if (m >= p.M || left <= 0) return;
+  if constexpr (EPI == EPI_STORE) {
+    store8(static_cast<T*>(p.c) + m * p.ldc + n, narrow8<T>(v), left);
+  } else if constexpr (EPI == EPI_GLU) {
+    f32x8 h;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = act_fwd(a.act, v[i]) * w[i];
+    store8(static_cast<T*>(p.c) + m * p.ldc + n, narrow8<T>(h), left);
+    if (a.out0) {
+      store8(static_cast<T*>(a.out0) + m * p.N + n, narrow8<T>(v), left);
+      store8(static_cast<T*>(a.out1) + m * p.N + n, narrow8<T>(w), left);
+    }
+  } else {
+    const f32x8 g = widen8<T>(load8(static_cast<const T*>(a.gate) + m * p.N + n, left)), u = widen8<T>(load8(static_cast<const T*>(a.up) + m * p.N + n, left));
+    f32x8 dg, du;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float slope;
+      du[i] = v[i] * act_both(a.act, g[i], &slope);
+      dg[i] = v[i] * u[i] * slope;
+    }
+    store8(static_cast<T*>(a.out0) + m * p.N + n, narrow8<T>(dg), left);
+    store8(static_cast<T*>(a.out1) + m * p.N + n, narrow8<T>(du), left);
+  }
+}
+
+// Lanes l and l + 32 hold columns 8 j .. 8 j + 3 and 8 j + 4 .. 8 j + 7 of one row in four registers a j.  For an even j: lane l gets all eight
+// columns of j, lane l + 32 those of j + 1.
+__device__ __forceinline__ f32x8 gather8(const f32x16& acc, int j) {
+  f32x8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float lo = acc[4 * j + i], hi = acc[4 * j + 4 + i];  // values of their own: a bit cast of a vector's element takes element 0
+    const auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, lo), __builtin_bit_cast(unsigned, hi), false, false);
+    const unsigned s0 = s[0], s1 = s[1];
+    r[i] = __builtin_bit_cast(float, s0);
+    r[4 + i] = __builtin_bit_cast(float, s1);
+  }
+  return r;
+}
+
+// ---- the tile kernel --------------------------------------------------------------------------------------------------------
+#define JZ_LDS __attribute__((address_space(3)))
+
+// One tile of one operand: where a thread's 16-byte chunks come from and go to.
+template <class T, bool KC, int ROWS>
+struct Staged {
+  static constexpr int BYTES = ROWS * BK * 2, CHUNKS = BYTES / 16, EACH = CHUNKS / 256;  // chunks a thread
+  // chunk i of thread t lies at LDS position (i * 256 + t) * 16, linear: what an LDS-direct load of a wavefront writes
+  static __device__ __forceinline__ void place(int i, int t, int* row, int* k) {
+    const int s = i * 256 + t;
+    if constexpr (KC) {
+      *row = s >> 3;
+      *k = ((s & 7) ^ (*row & 7)) * 8;
+    } else {
+      constexpr int PER = ROWS / 8;
+      *k = s / PER;
+      *row = ((s % PER) ^ (4 * (*k & 3))) * 8;
+    }
+  }
+  // operand of rows row0 .. row0 + 31, k 16 step .. 16 step + 15: lane l has row l % 32, k 8 (l / 32) .. + 7 of the step
+  static __device__ __forceinline__ Op8<T> read(const JZ_LDS unsigned char* lds, int row0, int step, int lane) {
+    if constexpr (KC) {
+      const int row = row0 + (lane & 31);
+      return *reinterpret_cast<const JZ_LDS Op8<T>*>(lds + row * 128 + (((step * 2 + (lane >> 5)) ^ (row & 7)) * 16));
+    } else {
+      // 16 lanes read four k of 16 rows, 8 bytes a lane, and get them transposed: lane i four k of row i
+      const int gi = lane >> 4, j = (lane >> 2) & 3, c4 = lane & 3;
+      const int k = step * 16 + 8 * (gi >> 1) + j, c = (row0 + 16 * (gi & 1) + 4 * c4) / 8;
+      const JZ_LDS unsigned char* at = lds + k * (ROWS * 2) + ((c ^ (4 * (k & 3))) * 16) + (c4 & 1) * 8;
+      struct { s16x4 lo, hi; } v;
+      v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((JZ_LDS s16x4*)at);
+      v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((JZ_LDS s16x4*)(at + 4 * (ROWS * 2)));
+      return __builtin_bit_cast(Op8<T>, v);
+    }
+  }
+};
+
+// Which tile of which product a workgroup has: consecutive workgroups land on different XCDs, each with an L2 of its own, so every XCD gets a
+// run of tiles, and within a run eight rows of tiles are taken column by column: what a run reads at a time is then a block.
+__device__ __forceinline__ int find_tile(const GemmArgs& a, unsigned* tm, unsigned* tn) {
+  unsigned t = xcd_remap(blockIdx.x, gridDim.x);
+  int q = 0;
+  while (q + 1 < a.products && t >= (unsigned)(a.p[q].tiles_m * a.p[q].tiles_n)) {
+    t -= a.p[q].tiles_m * a.p[q].tiles_n;
+    ++q;
+  }
+  const unsigned rows = a.p[q].tiles_m, cols = a.p[q].tiles_n, G = 8;
+  const unsigned band = t / (G * cols), in = t % (G * cols), high = rows - band * G < G ? rows - band * G : G;
+  *tm = band * G + in % high;
+  *tn = in / high;
+  return q;
+}
+
+// The sums of a wavefront's tile to their places: FP32 partial sums, or the epilogue.
+template <class T, int EPI, int TM, int TN>
+__device__ __forceinline__ void finish_tile(const GemmArgs& a, const Product& p, int q, f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, int lane) {
+  const int64_t m = m0 + (lane & 31);
+  if (a.splits > 1) {
+    float* out = a.partial + blockIdx.y * a.partial_size;
+    for (int i = 0; i < q; ++i) out += a.p[i].M * a.partial_pitch;
+#pragma unroll
+    for (int x = 0; x < TM; ++x)
+#pragma unroll
+      for (int y = 0; y < TN; ++y)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int64_t n = n0 + y * 32 + 8 * j + 4 * (lane >> 5);
+          if (m + x * 32 < p.M && n < a.partial_pitch)
+            *reinterpret_cast<f32x4*>(out + (m + x * 32) * a.partial_pitch + n) = f32x4{acc[x][y][4 * j], acc[x][y][4 * j + 1], acc[x][y][4 * j + 2], acc[x][y][4 * j + 3]};
+        }
+    return;
+  }
+#pragma unroll
+  for (int x = 0; x < TM; ++x)
+#pragma unroll
+    for (int y = 0; y < TN; y += EPI == EPI_GLU ? 2 : 1)
+#pragma unroll
+      for (int j = 0; j < 4; j += 2) {
+        const f32x8 v = gather8(acc[x][y], j), w = EPI == EPI_GLU ? gather8(acc[x][y + (EPI == EPI_GLU ? 1 : 0)], j) : v;
+        // gate and up alternate by 32 columns: a tile's column n is hidden unit n / 2 of its 64
+        const int64_t n = (EPI == EPI_GLU ? n0 / 2 + y * 16 : n0 + y * 32) + 8 * (j + (lane >> 5));
+        finish8<T, EPI>(a, p, m + x * 32, n, v, w);
+      }
+}
+
+// Any sizes, any alignment: the operands pass through registers on their way into LDS, element by element where a row ends.
+template <class T, bool KCA, bool KCB, int EPI, int BM, int BN>
+__global__ __launch_bounds__(256) void ffn_gemm_any(GemmArgs a) {
+  using SA = Staged<T, KCA, BM>;
+  using SB = Staged<T, KCB, BN>;
+  constexpr int TM = BM / 64, TN = BN / 64;
+  __shared__ __attribute__((aligned(16))) unsigned char sa[SA::BYTES], sb[SB::BYTES];
+  unsigned tm, tn;
+  const int q = find_tile(a, &tm, &tn);
+  const Product p = a.p[q];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, wm = wave >> 1, wn = wave & 1;
+  const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+  const int per_part = (int)((p.K + BK - 1) / BK), all = per_part * a.parts;
+  const int first = blockIdx.y * a.tiles_per_split, last = first + a.tiles_per_split < all ? first + a.tiles_per_split : all;
+
+  Op8<T> ra[SA::EACH], rb[SB::EACH];
+  auto fetch = [&](int kt) {
+    const int part = kt >= per_part;
+    const int64_t k0 = (int64_t)(kt - part * per_part) * BK;
+    const T* pa = static_cast<const T*>(p.a[part]);
+    const T* pb = static_cast<const T*>(p.b[part]);
+#pragma unroll
+    for (int i = 0; i < SA::EACH; ++i) {
+      int row, k;
+      SA::place(i, t, &row, &k);
+      const int64_t m = m0 + row, kk = k0 + k;
+      ra[i] = {};
+      if (m < p.M && kk < p.K) {
+        const int64_t left = KCA ? p.K - kk : p.M - m;
+        ra[i] = load8(KCA ? pa + m * p.lda + kk : pa + kk * p.lda + m, left < 8 ? (int)left : 8);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < SB::EACH; ++i) {
+      int row, k;
+      SB::place(i, t, &row, &k);
+      const T* pbb = pb;
+      int64_t n = n0 + row;
+      const int64_t kk = k0 + k;
+      if constexpr (EPI == EPI_GLU) {
+        pbb = static_cast<const T*>(p.b[(row >> 5) & 1]);
+        n = n0 / 2 + (row >> 6) * 32 + (row & 31);
+      }
+      rb[i] = {};
+      if (n < p.N && kk < p.K) {
+        const int64_t left = KCB ? p.K - kk : p.N - n;
+        rb[i] = load8(KCB ? pbb + n * p.ldb + kk : pbb + kk * p.ldb + n, left < 8 ? (int)left : 8);
+      }
+    }
+  };
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int x = 0; x < TM; ++x)
+#pragma unroll
+    for (int y = 0; y < TN; ++y) acc[x][y] = f32x16{};
+  if (first < last) fetch(first);
+  for (int kt = first; kt < last; ++kt) {
+#pragma unroll
+    for (int i = 0; i < SA::EACH; ++i) *reinterpret_cast<Op8<T>*>(sa + (i * 256 + t) * 16) = ra[i];
+#pragma unroll
+    for (int i = 0; i < SB::EACH; ++i) *reinterpret_cast<Op8<T>*>(sb + (i * 256 + t) * 16) = rb[i];
+    __syncthreads();
+    if (kt + 1 < last) fetch(kt + 1);
+#pragma unroll
+    for (int s = 0; s < BK / 16; ++s) {
+      Op8<T> fa[TM], fb[TN];
+#pragma unroll
+      for (int x = 0; x < TM; ++x) fa[x] = SA::read((const JZ_LDS unsigned char*)sa, wm * (BM / 2) + x * 32, s, lane);
+#pragma unroll
+      for (int y = 0; y < TN; ++y) fb[y] = SB::read((const JZ_LDS unsigned char*)sb, wn * (BN / 2) + y * 32, s, lane);
+#pragma unroll
+      for (int x = 0; x < TM; ++x)
+#pragma unroll
+        for (int y = 0; y < TN; ++y) acc[x][y] = mfma(fb[y], fa[x], acc[x][y]);
+    }
+    __syncthreads();
+  }
+  finish_tile<T, EPI>(a, p, q, acc, m0 + wm * (BM / 2), n0 + wn * (BN / 2), lane);
+}

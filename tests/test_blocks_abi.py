@@ -122,3 +122,49 @@ def test_norm_backward_arguments(jz):
     for bad in (dict(dr=A + (9 << 20) + 16), dict(dy=A + (1 << 20)), dict(dw_pre=A + (13 << 20)), dict(ws=A + (9 << 20)), dict(dgate=A + (16 << 20))):
         assert norm_call(jz, False, **bad) == jz.JZ_ERR_ALIAS, bad
     assert norm_call(jz, False, ws=None) == norm_call(jz, False, ws_bytes=16) == jz.JZ_ERR_WORKSPACE
+
+
+def ffn_call(jz, forward=True, ws_bytes=None, **over):
+    d = jz.ffn_desc(40, 64, 96, 80)
+    for k in list(over):
+        if hasattr(d, k):
+            setattr(d, k, over.pop(k))
+    at = {k: A + i * (1 << 20) for i, k in enumerate(["x", "w_gate", "w_up", "w_down", "h", "gate", "up", "y", "dy", "dx", "dw_gate", "dw_up", "dw_down", "ws"])}
+    at.update(over)
+    n = ctypes.c_size_t(0)
+    size = jz.lib().jz_ffn_fwd_workspace_bytes if forward else jz.lib().jz_ffn_bwd_workspace_bytes
+    size(ctypes.byref(d), ctypes.byref(n))
+    names = ["x", "w_gate", "w_up", "w_down", "h", "gate", "up", "y", "ws"] if forward else ["x", "w_gate", "w_up", "w_down", "gate", "up", "h", "dy", "dx", "dw_gate",
+                                                                                             "dw_up", "dw_down", "ws"]
+    fn = jz.lib().jz_ffn_fwd if forward else jz.lib().jz_ffn_bwd
+    return fn(ctypes.byref(d), *(at[k] for k in names), n.value if ws_bytes is None else ws_bytes, None)
+
+
+@pytest.mark.parametrize("forward", [True, False])
+def test_ffn_descriptors(jz, forward):
+    for bad in (dict(rows=-1), dict(in_features=0), dict(hidden=-3), dict(out_features=0), dict(act=4), dict(act=-1), dict(dtype=3), dict(x_stride=63), dict(y_stride=-1),
+                dict(dx_stride=5), dict(dy_stride=79)):
+        assert ffn_call(jz, forward, **bad) == jz.JZ_ERR_SHAPE, bad
+    for bad in (dict(dtype=2), dict(rows=(1 << 31) + 1), dict(hidden=(1 << 24) + 8), dict(x_stride=1 << 25)):
+        assert ffn_call(jz, forward, **bad) == jz.JZ_ERR_UNSUPPORTED, bad
+    n = ctypes.c_size_t(0)
+    for fn in (jz.lib().jz_ffn_fwd_workspace_bytes, jz.lib().jz_ffn_bwd_workspace_bytes):
+        assert fn(None, ctypes.byref(n)) == fn(ctypes.byref(jz.ffn_desc(1, 8, 8, 8)), None) == jz.JZ_ERR_NULL
+
+
+def test_ffn_arguments(jz):
+    for k in ("x", "w_gate", "w_up", "w_down", "h", "y", "gate", "up"):
+        assert ffn_call(jz, True, **{k: None}) == jz.JZ_ERR_NULL, k        # of gate and up both or neither
+    for k in ("x", "w_gate", "w_up", "w_down", "h", "y", "gate", "up"):
+        assert ffn_call(jz, True, **{k: A + (40 << 20) + 8}) == jz.JZ_ERR_ALIGN, k
+    for bad in (dict(h=A), dict(y=A + (4 << 20) + 64), dict(gate=A + (6 << 20)), dict(y=A + (3 << 20) + 16)):
+        assert ffn_call(jz, True, **bad) == jz.JZ_ERR_ALIAS, bad
+    assert ffn_call(jz, True, rows=0) == jz.JZ_OK
+    for bad in (dict(x=None), dict(w_up=None), dict(gate=None), dict(up=None), dict(h=None), dict(dy=None), dict(dw_gate=None), dict(dw_up=None, dw_down=None),
+                dict(dx=None, dw_gate=None, dw_up=None, dw_down=None)):
+        assert ffn_call(jz, False, **bad) == jz.JZ_ERR_NULL, bad
+    for k in ("x", "w_gate", "w_up", "w_down", "gate", "up", "h", "dy", "dx", "dw_gate", "dw_up", "dw_down", "ws"):
+        assert ffn_call(jz, False, **{k: A + (40 << 20) + 8}) == jz.JZ_ERR_ALIGN, k
+    for bad in (dict(dx=A + (8 << 20)), dict(dw_gate=A + (1 << 20) + 32), dict(dw_up=A + (12 << 20)), dict(ws=A + (9 << 20)), dict(dw_down=A + (13 << 20))):
+        assert ffn_call(jz, False, **bad) == jz.JZ_ERR_ALIAS, bad
+    assert ffn_call(jz, False, ws=None) == ffn_call(jz, False, ws_bytes=2 * 40 * 96 * 2 - 16) == jz.JZ_ERR_WORKSPACE
