@@ -65,13 +65,32 @@ int tile_count(const GemmArgs& a) {
   return n;
 }
 
+// LDS-direct loads move 16 bytes from multiples of 16 and reach 2^31 bytes behind a tile's first row.
+template <bool KCA, bool KCB>
+bool direct(const GemmArgs& a) {
+  for (int i = 0; i < a.products; ++i) {
+    const Product& p = a.p[i];
+    if (p.lda % 8 || p.ldb % 8 || p.lda >= (1 << 22) || p.ldb >= (1 << 22) || ((KCA || KCB) && p.K % 8)) return false;
+  }
+  return true;
+}
+
 template <class T, bool KCA, bool KCB, int EPI>
 int gemm(GemmArgs a, hipStream_t st) {
-  set_tiles<128, 128>(&a, EPI);
   a.splits = 1;
-  a.tiles_per_split = 0x7fffffff;
-  const int tiles = tile_count(a);
-  if (tiles > 0) ffn_gemm_any<T, KCA, KCB, EPI, 128, 128><<<tiles, 256, 0, st>>>(a);
+  a.tiles_per_split = 0x3fffffff;
+  if (direct<KCA, KCB>(a)) {
+    set_tiles<256, 256>(&a, EPI);
+    if (tile_count(a) >= 128) {
+      ffn_gemm<T, KCA, KCB, EPI, 256, 256, 2, 4><<<tile_count(a), 512, 0, st>>>(a);
+    } else {
+      set_tiles<128, 128>(&a, EPI);
+      if (tile_count(a) > 0) ffn_gemm<T, KCA, KCB, EPI, 128, 128, 2, 2><<<tile_count(a), 256, 0, st>>>(a);
+    }
+    return jz::launch_status();
+  }
+  set_tiles<128, 128>(&a, EPI);
+  if (tile_count(a) > 0) ffn_gemm_any<T, KCA, KCB, EPI, 128, 128><<<tile_count(a), 256, 0, st>>>(a);
   return jz::launch_status();
 }
 

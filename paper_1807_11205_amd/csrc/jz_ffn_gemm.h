@@ -113,31 +113,16 @@ __device__ __forceinline__ void finish8(const GemmArgs& a, const Product& p, int
   }
 }
 
-// Lanes l and l + 32 hold columns 8 j .. 8 j + 3 and 8 j + 4 .. 8 j + 7 of one row in four registers a j.  For an even j: lane l gets all eight
-// columns of j, lane l + 32 those of j + 1.
-__device__ __forceinline__ f32x8 gather8(const f32x16& acc, int j) {
-  f32x8 r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float lo = acc[4 * j + i], hi = acc[4 * j + 4 + i];  // values of their own: a bit cast of a vector's element takes element 0
-    const auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, lo), __builtin_bit_cast(unsigned, hi), false, false);
-    const unsigned s0 = s[0], s1 = s[1];
-    r[i] = __builtin_bit_cast(float, s0);
-    r[4 + i] = __builtin_bit_cast(float, s1);
-  }
-  return r;
-}
-
 // ---- the tile kernel --------------------------------------------------------------------------------------------------------
 #define JZ_LDS __attribute__((address_space(3)))
 
 // One tile of one operand: where a thread's 16-byte chunks come from and go to.
-template <class T, bool KC, int ROWS>
+template <class T, bool KC, int ROWS, int THREADS>
 struct Staged {
-  static constexpr int BYTES = ROWS * BK * 2, CHUNKS = BYTES / 16, EACH = CHUNKS / 256;  // chunks a thread
-  // chunk i of thread t lies at LDS position (i * 256 + t) * 16, linear: what an LDS-direct load of a wavefront writes
+  static constexpr int BYTES = ROWS * BK * 2, CHUNKS = BYTES / 16, EACH = CHUNKS / THREADS;  // chunks a thread
+  // chunk i of thread t lies at LDS position (i * THREADS + t) * 16, linear: what an LDS-direct load of a wavefront writes
   static __device__ __forceinline__ void place(int i, int t, int* row, int* k) {
-    const int s = i * 256 + t;
+    const int s = i * THREADS + t;
     if constexpr (KC) {
       *row = s >> 3;
       *k = ((s & 7) ^ (*row & 7)) * 8;
@@ -147,19 +132,27 @@ struct Staged {
       *row = ((s % PER) ^ (4 * (*k & 3))) * 8;
     }
   }
-  // operand of rows row0 .. row0 + 31, k 16 step .. 16 step + 15: lane l has row l % 32, k 8 (l / 32) .. + 7 of the step
-  static __device__ __forceinline__ Op8<T> read(const JZ_LDS unsigned char* lds, int row0, int step, int lane) {
+  // Operand x of step s: rows row0 + 32 x .. + 31, k 16 s .. 16 s + 15; lane l has row l % 32, k 8 (l / 32) .. + 7 of the step.  address() gives the four
+  // LDS offsets that a lane needs for all of them: KC one a step (an operand is 32 rows = 4 KB further), MC one an operand (a step is 16 k further).
+  static __device__ __forceinline__ void address(unsigned (&at)[4], int row0, int lane) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (KC) {
+        at[i] = (row0 + (lane & 31)) * 128 + (((i * 2 + (lane >> 5)) ^ (lane & 7)) * 16);
+      } else {
+        // 16 lanes read four k of 16 rows, 8 bytes a lane, and get them transposed: lane i four k of row i
+        const int gi = lane >> 4, j = (lane >> 2) & 3, c4 = lane & 3, c = (row0 + 32 * i + 16 * (gi & 1) + 4 * c4) / 8;
+        at[i] = (8 * (gi >> 1) + j) * (ROWS * 2) + ((c ^ (4 * j)) * 16) + (c4 & 1) * 8;
+      }
+    }
+  }
+  static __device__ __forceinline__ Op8<T> read(const JZ_LDS unsigned char* lds, const unsigned (&at)[4], int x, int s) {
     if constexpr (KC) {
-      const int row = row0 + (lane & 31);
-      return *reinterpret_cast<const JZ_LDS Op8<T>*>(lds + row * 128 + (((step * 2 + (lane >> 5)) ^ (row & 7)) * 16));
+      return *reinterpret_cast<const JZ_LDS Op8<T>*>(lds + at[s] + x * 4096);
     } else {
-      // 16 lanes read four k of 16 rows, 8 bytes a lane, and get them transposed: lane i four k of row i
-      const int gi = lane >> 4, j = (lane >> 2) & 3, c4 = lane & 3;
-      const int k = step * 16 + 8 * (gi >> 1) + j, c = (row0 + 16 * (gi & 1) + 4 * c4) / 8;
-      const JZ_LDS unsigned char* at = lds + k * (ROWS * 2) + ((c ^ (4 * (k & 3))) * 16) + (c4 & 1) * 8;
       struct { s16x4 lo, hi; } v;
-      v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((JZ_LDS s16x4*)at);
-      v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((JZ_LDS s16x4*)(at + 4 * (ROWS * 2)));
+      v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((JZ_LDS s16x4*)(lds + at[x] + s * (16 * ROWS * 2)));
+      v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((JZ_LDS s16x4*)(lds + at[x] + s * (16 * ROWS * 2) + 4 * (ROWS * 2)));
       return __builtin_bit_cast(Op8<T>, v);
     }
   }
@@ -181,45 +174,57 @@ __device__ __forceinline__ int find_tile(const GemmArgs& a, unsigned* tm, unsign
   return q;
 }
 
-// The sums of a wavefront's tile to their places: FP32 partial sums, or the epilogue.
+// The sums of a wavefront's tile to their places: FP32 partial sums, or the epilogue.  They pass through LDS 32 rows at a time, so that a lane has eight columns
+// of a row and neighbouring lanes its neighbours: whole lines are stored.  lds: 32 rows of TN * 32 floats of the wavefront's own, 16-byte chunk c of row r at
+// c ^ (r % 8).  Register 4 j + i of a lane holds row lane % 32, column 8 j + 4 (lane / 32) + i.
 template <class T, int EPI, int TM, int TN>
-__device__ __forceinline__ void finish_tile(const GemmArgs& a, const Product& p, int q, f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, int lane) {
-  const int64_t m = m0 + (lane & 31);
-  if (a.splits > 1) {
-    float* out = a.partial + blockIdx.y * a.partial_size;
-    for (int i = 0; i < q; ++i) out += a.p[i].M * a.partial_pitch;
-#pragma unroll
-    for (int x = 0; x < TM; ++x)
-#pragma unroll
-      for (int y = 0; y < TN; ++y)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int64_t n = n0 + y * 32 + 8 * j + 4 * (lane >> 5);
-          if (m + x * 32 < p.M && n < a.partial_pitch)
-            *reinterpret_cast<f32x4*>(out + (m + x * 32) * a.partial_pitch + n) = f32x4{acc[x][y][4 * j], acc[x][y][4 * j + 1], acc[x][y][4 * j + 2], acc[x][y][4 * j + 3]};
-        }
-    return;
-  }
-#pragma unroll
-  for (int x = 0; x < TM; ++x)
-#pragma unroll
-    for (int y = 0; y < TN; y += EPI == EPI_GLU ? 2 : 1)
-#pragma unroll
-      for (int j = 0; j < 4; j += 2) {
-        const f32x8 v = gather8(acc[x][y], j), w = EPI == EPI_GLU ? gather8(acc[x][y + (EPI == EPI_GLU ? 1 : 0)], j) : v;
-        // gate and up alternate by 32 columns: a tile's column n is hidden unit n / 2 of its 64
-        const int64_t n = (EPI == EPI_GLU ? n0 / 2 + y * 16 : n0 + y * 32) + 8 * (j + (lane >> 5));
-        finish8<T, EPI>(a, p, m + x * 32, n, v, w);
+__device__ __forceinline__ void finish_tile(const GemmArgs& a, const Product& p, int q, f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, JZ_LDS unsigned char* lds, int lane) {
+  constexpr int PITCH = TN * 128, PER = (EPI == EPI_GLU ? TN * 2 : TN * 4);  // bytes of a row; groups of eight results in one
+  auto chunk = [&](int row, int c) { return lds + row * PITCH + ((c ^ (row & 7)) * 16); };
+  auto eight = [&](int row, int c) {
+    const f32x4 lo = *reinterpret_cast<const JZ_LDS f32x4*>(chunk(row, c)), hi = *reinterpret_cast<const JZ_LDS f32x4*>(chunk(row, c + 1));
+    return f32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  };
+  static_for<0, TM>([&](auto X) {
+    constexpr int x = decltype(X)::value;
+    static_for<0, TN * 4>([&](auto I) {
+      constexpr int y = decltype(I)::value / 4, j = decltype(I)::value % 4;
+      *reinterpret_cast<JZ_LDS f32x4*>(chunk(lane & 31, y * 8 + j * 2 + (lane >> 5))) = f32x4{acc[x][y][4 * j], acc[x][y][4 * j + 1], acc[x][y][4 * j + 2], acc[x][y][4 * j + 3]};
+    });
+    if (a.splits > 1) {
+      float* out = a.partial + blockIdx.y * a.partial_size;
+      for (int i = 0; i < q; ++i) out += a.p[i].M * a.partial_pitch;
+#pragma unroll 1
+      for (int i = lane; i < 32 * TN * 4; i += 64) {
+        const int row = i / (TN * 4), c = i % (TN * 4);
+        const int64_t m = m0 + x * 32 + row, n = n0 + c * 8;
+        if (m < p.M && n < a.partial_pitch) *reinterpret_cast<f32x8*>(out + m * a.partial_pitch + n) = eight(row, c * 2);
       }
+    } else {
+#pragma unroll 1
+      for (int i = lane; i < 32 * PER; i += 64) {
+        const int row = i / PER, c = i % PER;
+        if constexpr (EPI == EPI_GLU) {  // gate and up alternate by 32 columns
+          const int g = (c >> 2) * 16 + (c & 3) * 2;
+          finish8<T, EPI>(a, p, m0 + x * 32 + row, n0 / 2 + c * 8, eight(row, g), eight(row, g + 8));
+        } else {
+          const f32x8 v = eight(row, c * 2);
+          finish8<T, EPI>(a, p, m0 + x * 32 + row, n0 + c * 8, v, v);
+        }
+      }
+    }
+  });
 }
 
 // Any sizes, any alignment: the operands pass through registers on their way into LDS, element by element where a row ends.
 template <class T, bool KCA, bool KCB, int EPI, int BM, int BN>
 __global__ __launch_bounds__(256) void ffn_gemm_any(GemmArgs a) {
-  using SA = Staged<T, KCA, BM>;
-  using SB = Staged<T, KCB, BN>;
+  using SA = Staged<T, KCA, BM, 256>;
+  using SB = Staged<T, KCB, BN, 256>;
   constexpr int TM = BM / 64, TN = BN / 64;
-  __shared__ __attribute__((aligned(16))) unsigned char sa[SA::BYTES], sb[SB::BYTES];
+  __shared__ __attribute__((aligned(1024))) unsigned char operands[SA::BYTES + SB::BYTES];
+  unsigned char *const sa = operands, *const sb = operands + SA::BYTES;
+  static_assert(SA::BYTES + SB::BYTES >= 4 * 32 * TN * 128, "the results pass through LDS");
   unsigned tm, tn;
   const int q = find_tile(a, &tm, &tn);
   const Product p = a.p[q];
@@ -263,6 +268,9 @@ __global__ __launch_bounds__(256) void ffn_gemm_any(GemmArgs a) {
       }
     }
   };
+  unsigned at_a[4], at_b[4];
+  SA::address(at_a, wm * (BM / 2), lane);
+  SB::address(at_b, wn * (BN / 2), lane);
   f32x16 acc[TM][TN];
 #pragma unroll
   for (int x = 0; x < TM; ++x)
@@ -280,9 +288,9 @@ __global__ __launch_bounds__(256) void ffn_gemm_any(GemmArgs a) {
     for (int s = 0; s < BK / 16; ++s) {
       Op8<T> fa[TM], fb[TN];
 #pragma unroll
-      for (int x = 0; x < TM; ++x) fa[x] = SA::read((const JZ_LDS unsigned char*)sa, wm * (BM / 2) + x * 32, s, lane);
+      for (int x = 0; x < TM; ++x) fa[x] = SA::read((const JZ_LDS unsigned char*)sa, at_a, x, s);
 #pragma unroll
-      for (int y = 0; y < TN; ++y) fb[y] = SB::read((const JZ_LDS unsigned char*)sb, wn * (BN / 2) + y * 32, s, lane);
+      for (int y = 0; y < TN; ++y) fb[y] = SB::read((const JZ_LDS unsigned char*)sb, at_b, y, s);
 #pragma unroll
       for (int x = 0; x < TM; ++x)
 #pragma unroll
@@ -290,5 +298,137 @@ __global__ __launch_bounds__(256) void ffn_gemm_any(GemmArgs a) {
     }
     __syncthreads();
   }
-  finish_tile<T, EPI>(a, p, q, acc, m0 + wm * (BM / 2), n0 + wn * (BN / 2), lane);
+  finish_tile<T, EPI>(a, p, q, acc, m0 + wm * (BM / 2), n0 + wn * (BN / 2), (JZ_LDS unsigned char*)operands + wave * (32 * TN * 128), lane);
+}
+
+// ---- LDS-direct ---------------------------------------------------------------------------------------------------------------
+// Everything has landed that this wavefront asked for, and every wavefront is past its reads: both sides are ordinary accesses, which the
+// fences keep in place.
+__device__ __forceinline__ void all_landed() {
+  __builtin_amdgcn_sched_barrier(0);
+  wait_vmcnt<0>();
+  lds_wait<0>();
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Where one operand's tile comes from.
+template <class T, bool KC, int ROWS, int THREADS, bool DUAL>
+struct Source {
+  using S = Staged<T, KC, ROWS, THREADS>;
+  const char* base[2];  // of the tile's rows: part 0 and 1 of the sum, or the two interleaved matrices
+  int64_t pitch, rows_left, K;
+  unsigned off, step;   // of the thread's first chunk, and from one to the next
+  int k;                // the chunk's place in a tile: k of KC, for the end of the sum
+
+  __device__ __forceinline__ void init(const void* const* p, int64_t ld, int64_t row0, int64_t rows, int64_t K_, int t) {
+    pitch = ld * 2;
+    rows_left = rows - row0;
+    K = K_;
+    base[0] = static_cast<const char*>(p[0]) + row0 * (KC ? pitch : 2);
+    base[1] = static_cast<const char*>(p[1]) + row0 * (KC ? pitch : 2);
+    int row;
+    S::place(0, t, &row, &k);
+    int row1, k1;
+    S::place(1, t, &row1, &k1);
+    step = KC ? (unsigned)((DUAL ? 32 : row1 - row) * pitch) : (unsigned)((k1 - k) * pitch);
+    if (DUAL) row &= 31;
+    off = KC ? (unsigned)(row * pitch + k * 2) : (unsigned)(k * pitch + row * 2);
+  }
+  // 16 bytes a lane into LDS; what lies outside the operand arrives as zeros
+  template <class L>
+  __device__ __forceinline__ void load(L* lds, int part, int64_t k0, int wave) const {
+    const int64_t skip = k0 * (KC ? 2 : pitch);
+    const int64_t span = KC ? (rows_left - 1) * pitch + (K - k0) * 2 : (K - k0 - 1) * pitch + rows_left * 2;
+    const int bytes = (int)(span < 0x7ffffff0 ? span : 0x7ffffff0);
+    const auto r0 = __builtin_amdgcn_make_buffer_rsrc((void*)(base[DUAL ? 0 : part] + skip), 0, bytes, 0x00020000);
+    const auto r1 = __builtin_amdgcn_make_buffer_rsrc((void*)(base[1] + skip), 0, bytes, 0x00020000);
+    const unsigned end = KC && k >= K - k0 ? 0x80000000u : 0u;  // a row's end inside the tile: the next row does not follow
+#pragma unroll
+    for (int i = 0; i < S::EACH; ++i) {
+      // interleaved by 32 rows: 256 threads bring 32 rows at a time, 512 threads 64
+      const bool second = DUAL && (THREADS == 256 ? i & 1 : wave >> 2);
+      const unsigned at = (off + (DUAL && THREADS == 256 ? i >> 1 : i) * step) | end;
+      jz_dma16(second ? r1 : r0, (lds_byte*)lds + (i * THREADS + wave * 64) * 16, at);
+    }
+  }
+};
+
+template <class T, bool KCA, bool KCB, int EPI, int BM, int BN, int WGM, int WGN>
+__global__ __launch_bounds__(64 * WGM * WGN, 2) void ffn_gemm(GemmArgs a) {
+  constexpr int THREADS = 64 * WGM * WGN, TM = BM / WGM / 32, TN = BN / WGN / 32, STEPS = BK / 16;
+  using SA = Staged<T, KCA, BM, THREADS>;
+  using SB = Staged<T, KCB, BN, THREADS>;
+  // four objects, not one: an LDS read then only waits for the loads into its own
+  __shared__ __attribute__((aligned(1024))) unsigned char a0[SA::BYTES], a1[SA::BYTES], b0[SB::BYTES], b1[SB::BYTES];
+  unsigned tm, tn;
+  const int q = find_tile(a, &tm, &tn);
+  const Product p = a.p[q];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), wm = wave / WGN, wn = wave % WGN;
+  const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+  const int per_part = (int)((p.K + BK - 1) / BK), all = per_part * a.parts;
+  const int first = blockIdx.y * a.tiles_per_split, last = first + a.tiles_per_split < all ? first + a.tiles_per_split : all;
+
+  Source<T, KCA, BM, THREADS, false> from_a;
+  Source<T, KCB, BN, THREADS, EPI == EPI_GLU> from_b;
+  from_a.init(p.a, p.lda, m0, p.M, p.K, t);
+  from_b.init(p.b, p.ldb, EPI == EPI_GLU ? n0 / 2 : n0, p.N, p.K, t);
+  auto fetch = [&](auto* la, auto* lb, int kt) {
+    if (kt >= last) return;
+    const int part = kt >= per_part;
+    const int64_t k0 = (int64_t)(kt - part * per_part) * BK;
+    from_a.load(la, part, k0, wave);
+    from_b.load(lb, part, k0, wave);
+  };
+  unsigned at_a[4], at_b[4];
+  SA::address(at_a, wm * TM * 32, lane);
+  SB::address(at_b, wn * TN * 32, lane);
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int x = 0; x < TM; ++x)
+#pragma unroll
+    for (int y = 0; y < TN; ++y) acc[x][y] = f32x16{};
+  Op8<T> fa[2][TM], fb[2][TN];
+  auto read = [&](auto* la, auto* lb, int s, int to) {
+#pragma unroll
+    for (int x = 0; x < TM; ++x) fa[to][x] = SA::read((const JZ_LDS unsigned char*)la, at_a, x, s);
+#pragma unroll
+    for (int y = 0; y < TN; ++y) fb[to][y] = SB::read((const JZ_LDS unsigned char*)lb, at_b, y, s);
+  };
+  auto multiply = [&](int from) {
+#pragma unroll
+    for (int x = 0; x < TM; ++x)
+#pragma unroll
+      for (int y = 0; y < TN; ++y) acc[x][y] = mfma(fb[from][y], fa[from][x], acc[x][y]);
+  };
+  // The tile in la, lb, whose first operands are in registers already.  Its last step's products run while the next tile's first operands are read and the
+  // tile after that is asked for, into the place that this one leaves.
+  auto tile = [&](auto* la, auto* lb, auto* na, auto* nb, int kt) {
+    static_for<0, STEPS - 1>([&](auto S) {
+      constexpr int s = decltype(S)::value;
+      read(la, lb, s + 1, (s + 1) & 1);
+      multiply(s & 1);
+    });
+    all_landed();
+    fetch(la, lb, kt + 2);
+    if (kt + 1 < last) read(na, nb, 0, 0);
+    multiply((STEPS - 1) & 1);
+  };
+  if (first < last) {
+    fetch(a0, b0, first);
+    all_landed();
+    fetch(a1, b1, first + 1);
+    read(a0, b0, 0, 0);
+    for (int kt = first; kt < last; kt += 2) {
+      tile(a0, b0, a1, b1, kt);
+      if (kt + 1 < last) tile(a1, b1, a0, b0, kt + 1);
+    }
+  }
+  // past the last barrier nobody reads operands any more
+  constexpr int STRIP = 32 * TN * 128, FIT = SA::BYTES / STRIP;
+  static_assert(2 * FIT >= WGM * WGN, "the results pass through the place of A");
+  unsigned char* const mine = (wave < FIT ? a0 + wave * STRIP : a1 + (wave - FIT) * STRIP);
+  finish_tile<T, EPI>(a, p, q, acc, m0 + wm * TM * 32, n0 + wn * TN * 32, (JZ_LDS unsigned char*)mine, lane);
 }
