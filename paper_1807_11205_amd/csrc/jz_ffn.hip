@@ -13,6 +13,7 @@ namespace {
 #include "jz_lds_dma.h"
 #include "jz_vec.h"
 #include "jz_ffn_gemm.h"
+#include "jz_ffn_few.h"
 
 struct FfnTensor {
   const void* p;
@@ -75,23 +76,79 @@ bool direct(const GemmArgs& a) {
   return true;
 }
 
+// What a launch does: a tile kernel (256 x 256 or 128 x 128), and how many workgroups share a tile's sum.
+struct FfnPlan {
+  int tile, splits;
+};
+struct Scratch {  // room for partial sums
+  void* p;
+  size_t bytes;
+};
+int64_t k_tiles(const GemmArgs& a) { return (a.p[0].K + BK - 1) / BK * a.parts; }  // the products of a launch have one K
+int64_t join_pitch(const GemmArgs& a, int epi) {
+  int64_t n = 0;
+  for (int i = 0; i < a.products; ++i) n = std::max(n, epi == EPI_GLU ? (a.p[i].N + 31) / 32 * 64 : (a.p[i].N + 7) / 8 * 8);
+  return n;
+}
+int64_t join_size(const GemmArgs& a, int epi) {  // floats of one split
+  int64_t n = 0;
+  for (int i = 0; i < a.products; ++i) n += a.p[i].M;
+  return n * join_pitch(a, epi);
+}
+int64_t count_tiles(const GemmArgs& a, int epi, int tile) {
+  int64_t n = 0;
+  for (int i = 0; i < a.products; ++i) n += ((a.p[i].M + tile - 1) / tile) * ((epi == EPI_GLU ? (a.p[i].N + 31) / 32 * 64 : a.p[i].N) + tile - 1) / tile;
+  return n;
+}
+
 template <class T, bool KCA, bool KCB, int EPI>
-int gemm(GemmArgs a, hipStream_t st) {
-  a.splits = 1;
-  a.tiles_per_split = 0x3fffffff;
-  if (direct<KCA, KCB>(a)) {
-    set_tiles<256, 256>(&a, EPI);
-    if (tile_count(a) >= 128) {
-      ffn_gemm<T, KCA, KCB, EPI, 256, 256, 2, 4><<<tile_count(a), 512, 0, st>>>(a);
-    } else {
-      set_tiles<128, 128>(&a, EPI);
-      if (tile_count(a) > 0) ffn_gemm<T, KCA, KCB, EPI, 128, 128, 2, 2><<<tile_count(a), 256, 0, st>>>(a);
-    }
-    return jz::launch_status();
+int launch(GemmArgs a, const FfnPlan& plan, const Scratch& ws, hipStream_t st) {
+  const bool lds_direct = direct<KCA, KCB>(a);
+  if (plan.tile == 256) set_tiles<256, 256>(&a, EPI);
+  else set_tiles<128, 128>(&a, EPI);
+  const int tiles = tile_count(a);
+  if (tiles <= 0) return JZ_OK;
+  a.splits = plan.splits;
+  a.tiles_per_split = (int)((k_tiles(a) + plan.splits - 1) / plan.splits);
+  a.partial = static_cast<float*>(ws.p);
+  a.partial_pitch = join_pitch(a, EPI);
+  a.partial_size = join_size(a, EPI);
+  const dim3 grid(tiles, plan.splits);
+  if (!lds_direct) ffn_gemm_any<T, KCA, KCB, EPI, 128, 128><<<grid, 256, 0, st>>>(a);
+  else if (plan.tile == 256) ffn_gemm<T, KCA, KCB, EPI, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
+  else ffn_gemm<T, KCA, KCB, EPI, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
+  if (jz::launch_status() != JZ_OK) return JZ_ERR_LAUNCH;
+  if (plan.splits > 1) {
+    int64_t n = 0;
+    for (int i = 0; i < a.products; ++i) n += a.p[i].M * ((a.p[i].N + 7) / 8);
+    ffn_join<T, EPI><<<(unsigned)((n + 255) / 256), 256, 0, st>>>(a);
   }
-  set_tiles<128, 128>(&a, EPI);
-  if (tile_count(a) > 0) ffn_gemm_any<T, KCA, KCB, EPI, 128, 128><<<tile_count(a), 256, 0, st>>>(a);
   return jz::launch_status();
+}
+
+FfnPlan choose(const GemmArgs& a, int epi, bool lds_direct, size_t ws_bytes) {
+  const int64_t t256 = count_tiles(a, epi, 256);
+  return FfnPlan{lds_direct && t256 >= 128 ? 256 : 128, 1};
+}
+
+template <class T, bool KCA, bool KCB, int EPI>
+int gemm(GemmArgs a, const Scratch& ws, hipStream_t st) {
+  return launch<T, KCA, KCB, EPI>(a, choose(a, EPI, direct<KCA, KCB>(a), ws.bytes), ws, st);
+}
+
+template <class T, bool GLU, int TT>
+int launch_few(const GemmArgs& a, hipStream_t st) {
+  const unsigned grid = (unsigned)((a.p[0].N + 15) / 16);
+  // a workgroup has one compute unit: with fewer of them, more wavefronts in each
+  if (grid >= 512) ffn_few<T, GLU, TT, 8><<<grid, 512, 0, st>>>(a);
+  else ffn_few<T, GLU, TT, 16><<<grid, 1024, 0, st>>>(a);
+  return jz::launch_status();
+}
+constexpr int64_t FEW_ROWS = 64;
+template <class T, bool GLU>
+int few(const GemmArgs& a, hipStream_t st) {
+  const int64_t M = a.p[0].M;
+  return M <= 16 ? launch_few<T, GLU, 1>(a, st) : M <= 32 ? launch_few<T, GLU, 2>(a, st) : launch_few<T, GLU, 4>(a, st);
 }
 
 Product product(const void* a, int64_t lda, const void* b, int64_t ldb, void* c, int64_t ldc, int64_t M, int64_t N, int64_t K) {
@@ -116,38 +173,43 @@ GemmArgs one(const Product& p, int act) {
 }
 
 template <class T>
-int run_fwd(const FfnShape& s, int act, const void* x, const void* wg, const void* wu, const void* wd, void* h, void* gate, void* up, void* y, hipStream_t st) {
+int run_fwd(const FfnShape& s, int act, const void* x, const void* wg, const void* wu, const void* wd, void* h, void* gate, void* up, void* y, const Scratch& ws,
+            hipStream_t st) {
   GemmArgs a = one(product(x, s.ldx, wg, s.D, h, s.F, s.M, s.F, s.D), act);
   a.p[0].b[1] = wu;
   a.out0 = gate;
   a.out1 = up;
-  int rc = gemm<T, true, true, EPI_GLU>(a, st);
-  if (rc == JZ_OK) rc = gemm<T, true, true, EPI_STORE>(one(product(h, s.F, wd, s.F, y, s.ldy, s.M, s.O, s.F), act), st);
-  return rc;
+  const GemmArgs b = one(product(h, s.F, wd, s.F, y, s.ldy, s.M, s.O, s.F), act);
+  if (s.M <= FEW_ROWS) {
+    const int rc = few<T, true>(a, st);
+    return rc == JZ_OK ? few<T, false>(b, st) : rc;
+  }
+  const int rc = gemm<T, true, true, EPI_GLU>(a, ws, st);
+  return rc == JZ_OK ? gemm<T, true, true, EPI_STORE>(b, ws, st) : rc;
 }
 
 template <class T>
 int run_bwd(const FfnShape& s, int act, const void* x, const void* wg, const void* wu, const void* wd, const void* gate, const void* up, const void* h, const void* dy,
-            void* dx, void* dwg, void* dwu, void* dwd, void* dgate, void* dup, hipStream_t st) {
+            void* dx, void* dwg, void* dwu, void* dwd, void* dgate, void* dup, const Scratch& ws, hipStream_t st) {
   GemmArgs a = one(product(dy, s.lddy, wd, s.F, nullptr, 0, s.M, s.F, s.O), act);
   a.gate = gate;
   a.up = up;
   a.out0 = dgate;
   a.out1 = dup;
-  int rc = gemm<T, true, false, EPI_GLU_BWD>(a, st);
+  int rc = gemm<T, true, false, EPI_GLU_BWD>(a, ws, st);
   if (rc == JZ_OK && dx) {
     a = one(product(dgate, s.F, wg, s.D, dx, s.lddx, s.M, s.D, s.F), act);
     a.p[0].a[1] = dup;
     a.p[0].b[1] = wu;
     a.parts = 2;
-    rc = gemm<T, true, false, EPI_STORE>(a, st);
+    rc = gemm<T, true, false, EPI_STORE>(a, ws, st);
   }
   if (rc == JZ_OK && dwg) {
     a = one(product(dgate, s.F, x, s.ldx, dwg, s.D, s.F, s.D, s.M), act);
     a.p[1] = product(dup, s.F, x, s.ldx, dwu, s.D, s.F, s.D, s.M);
     a.p[2] = product(dy, s.lddy, h, s.F, dwd, s.F, s.O, s.F, s.M);
     a.products = 3;
-    rc = gemm<T, false, false, EPI_STORE>(a, st);
+    rc = gemm<T, false, false, EPI_STORE>(a, ws, st);
   }
   return rc;
 }
@@ -185,8 +247,8 @@ extern "C" int jz_ffn_fwd(const jz_ffn_desc* d, const void* x, const void* w_gat
   rc = ffn_look_over(t, 8, ws, ws_bytes);
   if (rc != JZ_OK) return rc;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  return d->dtype == JZ_F16 ? run_fwd<_Float16>(s, d->act, x, w_gate, w_up, w_down, h, gate, up, y, st)
-                            : run_fwd<__bf16>(s, d->act, x, w_gate, w_up, w_down, h, gate, up, y, st);
+  return d->dtype == JZ_F16 ? run_fwd<_Float16>(s, d->act, x, w_gate, w_up, w_down, h, gate, up, y, Scratch{ws, ws_bytes}, st)
+                            : run_fwd<__bf16>(s, d->act, x, w_gate, w_up, w_down, h, gate, up, y, Scratch{ws, ws_bytes}, st);
 }
 
 extern "C" int jz_ffn_bwd(const jz_ffn_desc* d, const void* x, const void* w_gate, const void* w_up, const void* w_down, const void* gate, const void* up,
@@ -208,7 +270,8 @@ extern "C" int jz_ffn_bwd(const jz_ffn_desc* d, const void* x, const void* w_gat
   if (rc != JZ_OK) return rc;
   char* b = static_cast<char*>(ws);
   void *dgate = b, *dup = b + hidden_bytes(s);
+  const Scratch rest{b + need, ws_bytes - need};
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  return d->dtype == JZ_F16 ? run_bwd<_Float16>(s, d->act, x, w_gate, w_up, w_down, gate, up, h, dy, dx, dw_gate, dw_up, dw_down, dgate, dup, st)
-                            : run_bwd<__bf16>(s, d->act, x, w_gate, w_up, w_down, gate, up, h, dy, dx, dw_gate, dw_up, dw_down, dgate, dup, st);
+  return d->dtype == JZ_F16 ? run_bwd<_Float16>(s, d->act, x, w_gate, w_up, w_down, gate, up, h, dy, dx, dw_gate, dw_up, dw_down, dgate, dup, rest, st)
+                            : run_bwd<__bf16>(s, d->act, x, w_gate, w_up, w_down, gate, up, h, dy, dx, dw_gate, dw_up, dw_down, dgate, dup, rest, st);
 }

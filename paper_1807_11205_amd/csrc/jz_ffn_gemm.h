@@ -198,7 +198,7 @@ __device__ __forceinline__ void finish_tile(const GemmArgs& a, const Product& p,
       for (int i = lane; i < 32 * TN * 4; i += 64) {
         const int row = i / (TN * 4), c = i % (TN * 4);
         const int64_t m = m0 + x * 32 + row, n = n0 + c * 8;
-        if (m < p.M && n < a.partial_pitch) *reinterpret_cast<f32x8*>(out + m * a.partial_pitch + n) = eight(row, c * 2);
+        if (m < p.M && n < a.partial_pitch) store8(out + m * a.partial_pitch + n, eight(row, c * 2));
       }
     } else {
 #pragma unroll 1
@@ -431,4 +431,30 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void ffn_gemm(GemmArgs a) {
   static_assert(2 * FIT >= WGM * WGN, "the results pass through the place of A");
   unsigned char* const mine = (wave < FIT ? a0 + wave * STRIP : a1 + (wave - FIT) * STRIP);
   finish_tile<T, EPI>(a, p, q, acc, m0 + wm * TM * 32, n0 + wn * TN * 32, (JZ_LDS unsigned char*)mine, lane);
+}
+
+// The partial sums of a split reduction, added in the order of the splits, and the epilogue.  Eight columns a thread.
+template <class T, int EPI>
+__global__ __launch_bounds__(256) void ffn_join(GemmArgs a) {
+  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const float* at = a.partial;
+  for (int q = 0; q < a.products; ++q) {
+    const Product& p = a.p[q];
+    const int64_t per = (p.N + 7) / 8, n = p.M * per;
+    if (i < n) {
+      const int64_t m = i / per, c = (i % per) * 8;
+      const int64_t g = EPI == EPI_GLU ? (c >> 5) * 64 + (c & 31) : c;
+      auto total = [&](int64_t col) {
+        const float* f = at + m * a.partial_pitch + col;
+        f32x8 v = load8(f);
+        for (int s = 1; s < a.splits; ++s) v += load8(f + s * a.partial_size);
+        return v;
+      };
+      const f32x8 v = total(g), w = EPI == EPI_GLU ? total(g + 32) : v;
+      finish8<T, EPI>(a, p, m, c, v, w);
+      return;
+    }
+    i -= n;
+    at += p.M * a.partial_pitch;
+  }
 }
