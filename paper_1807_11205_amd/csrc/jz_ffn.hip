@@ -76,64 +76,99 @@ bool direct(const GemmArgs& a) {
   return true;
 }
 
-// What a launch does: a tile kernel (256 x 256 or 128 x 128), and how many workgroups share a tile's sum.
+// What a launch does: a tile kernel (256 x 256 or 128 x 128), how many tiles have a workgroup of their own, and how many workgroups share the sum of each of
+// the others.
 struct FfnPlan {
-  int tile, splits;
+  int tile, full, splits;
 };
 struct Scratch {  // room for partial sums
   void* p;
   size_t bytes;
 };
 int64_t k_tiles(const GemmArgs& a) { return (a.p[0].K + BK - 1) / BK * a.parts; }  // the products of a launch have one K
-int64_t join_pitch(const GemmArgs& a, int epi) {
-  int64_t n = 0;
-  for (int i = 0; i < a.products; ++i) n = std::max(n, epi == EPI_GLU ? (a.p[i].N + 31) / 32 * 64 : (a.p[i].N + 7) / 8 * 8);
-  return n;
-}
-int64_t join_size(const GemmArgs& a, int epi) {  // floats of one split
-  int64_t n = 0;
-  for (int i = 0; i < a.products; ++i) n += a.p[i].M;
-  return n * join_pitch(a, epi);
-}
 int64_t count_tiles(const GemmArgs& a, int epi, int tile) {
   int64_t n = 0;
-  for (int i = 0; i < a.products; ++i) n += ((a.p[i].M + tile - 1) / tile) * ((epi == EPI_GLU ? (a.p[i].N + 31) / 32 * 64 : a.p[i].N) + tile - 1) / tile;
+  for (int i = 0; i < a.products; ++i) n += ((a.p[i].M + tile - 1) / tile) * (((epi == EPI_GLU ? (a.p[i].N + 31) / 32 * 64 : a.p[i].N) + tile - 1) / tile);
   return n;
+}
+size_t partial_bytes(const FfnPlan& p, int64_t tiles) { return p.splits > 1 ? (size_t)(tiles - p.full) * p.splits * p.tile * p.tile * 4 : 0; }
+
+template <class T, bool KCA, bool KCB, int EPI, int ACT>
+void launch_direct(const GemmArgs& a, int tile, unsigned grid, hipStream_t st) {
+  if (tile == 256) ffn_gemm<T, KCA, KCB, EPI, ACT, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
+  else ffn_gemm<T, KCA, KCB, EPI, ACT, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
 }
 
 template <class T, bool KCA, bool KCB, int EPI>
 int launch(GemmArgs a, const FfnPlan& plan, const Scratch& ws, hipStream_t st) {
-  const bool lds_direct = direct<KCA, KCB>(a);
   if (plan.tile == 256) set_tiles<256, 256>(&a, EPI);
   else set_tiles<128, 128>(&a, EPI);
-  const int tiles = tile_count(a);
+  const int tiles = tile_count(a), full = plan.splits > 1 ? plan.full : tiles, split = tiles - full;
   if (tiles <= 0) return JZ_OK;
+  a.full = full;
   a.splits = plan.splits;
   a.tiles_per_split = (int)((k_tiles(a) + plan.splits - 1) / plan.splits);
   a.partial = static_cast<float*>(ws.p);
-  a.partial_pitch = join_pitch(a, EPI);
-  a.partial_size = join_size(a, EPI);
-  const dim3 grid(tiles, plan.splits);
-  if (!lds_direct) ffn_gemm_any<T, KCA, KCB, EPI, 128, 128><<<grid, 256, 0, st>>>(a);
-  else if (plan.tile == 256) ffn_gemm<T, KCA, KCB, EPI, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
-  else ffn_gemm<T, KCA, KCB, EPI, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
+  const unsigned grid = full + split * plan.splits;
+  if (!direct<KCA, KCB>(a)) ffn_gemm_any<T, KCA, KCB, EPI, 128, 128><<<grid, 256, 0, st>>>(a);
+  else if (EPI != EPI_GLU_BWD || a.act == 0) launch_direct<T, KCA, KCB, EPI, 0>(a, plan.tile, grid, st);
+  else if constexpr (EPI == EPI_GLU_BWD) {
+    if (a.act == 1) launch_direct<T, KCA, KCB, EPI, 1>(a, plan.tile, grid, st);
+    else if (a.act == 2) launch_direct<T, KCA, KCB, EPI, 2>(a, plan.tile, grid, st);
+    else launch_direct<T, KCA, KCB, EPI, 3>(a, plan.tile, grid, st);
+  }
   if (jz::launch_status() != JZ_OK) return JZ_ERR_LAUNCH;
-  if (plan.splits > 1) {
-    int64_t n = 0;
-    for (int i = 0; i < a.products; ++i) n += a.p[i].M * ((a.p[i].N + 7) / 8);
-    ffn_join<T, EPI><<<(unsigned)((n + 255) / 256), 256, 0, st>>>(a);
+  if (split > 0) {
+    const dim3 join(plan.tile * plan.tile / (EPI == EPI_GLU ? 16 : 8) / 256, split);
+    if (plan.tile == 256) ffn_join<T, EPI, 256><<<join, 256, 0, st>>>(a);
+    else ffn_join<T, EPI, 128><<<join, 256, 0, st>>>(a);
   }
   return jz::launch_status();
 }
 
+// The plan with the least expected time.  Microseconds, fitted to FP16 and BF16 products of 128 to 16384 rows and 1024 to 12288 features: a k tile of a
+// 256 x 256 tile takes 1.22 alone on the chip and 1.75 with all 256 compute units busy (0.62 and, two workgroups a unit, 1.08 for 128 x 128), what comes before
+// and after the k tiles 10 (3); joining moves the partial sums twice and is a launch.
 FfnPlan choose(const GemmArgs& a, int epi, bool lds_direct, size_t ws_bytes) {
-  const int64_t t256 = count_tiles(a, epi, 256);
-  return FfnPlan{lds_direct && t256 >= 128 ? 256 : 128, 1};
+  FfnPlan best = {128, 0, 1};  // one workgroup a tile: always among the plans below
+  double least = 1e30;
+  const double kt = (double)k_tiles(a);
+  for (int tile : {256, 128}) {
+    if (tile == 256 && !lds_direct) continue;
+    const int64_t tiles = count_tiles(a, epi, tile), slots = tile == 256 ? 256 : 512;
+    auto tile_time = [&](double workgroups, double k) {
+      const double fill = std::min(1., workgroups / slots);
+      return tile == 256 ? k * (1.22 + 0.53 * fill) + 10. : k * (0.62 + 0.46 * fill) + 3.;
+    };
+    for (int rounds = 0; rounds < 2; ++rounds) {  // all tiles are split, or those of the last round, which does not fill the chip
+      const int64_t full = rounds ? tiles / slots * slots : 0, rest = tiles - full;
+      if (rounds && full == 0) continue;
+      for (int s = 1; s <= 32 && (s == 1 || s <= kt); s += s < 4 ? 1 : s < 8 ? 2 : s < 16 ? 4 : 8) {
+        const FfnPlan p = {tile, (int)(s == 1 ? tiles : full), s};
+        if (partial_bytes(p, tiles) > ws_bytes) continue;
+        const double each = std::ceil(kt / s);
+        const int64_t wg = rest * s, turns = (wg + slots - 1) / slots;
+        double t = full / slots * tile_time(slots, kt) + (turns ? (turns - 1) * tile_time(slots, each) + tile_time(turns > 1 ? slots : wg, each) : 0);
+        if (s > 1 && rest > 0) t += 5. + (double)partial_bytes(p, tiles) * 2. / 5e6;
+        if (t < least) {
+          least = t;
+          best = p;
+        }
+      }
+    }
+  }
+  return best;
+}
+// room for partial sums that a plan may use
+constexpr size_t PARTIAL_LIMIT = size_t(128) << 20;
+size_t wanted(const GemmArgs& a, int epi, bool lds_direct) {
+  const FfnPlan p = choose(a, epi, lds_direct, PARTIAL_LIMIT);
+  return partial_bytes(p, count_tiles(a, epi, p.tile));
 }
 
 template <class T, bool KCA, bool KCB, int EPI>
 int gemm(GemmArgs a, const Scratch& ws, hipStream_t st) {
-  return launch<T, KCA, KCB, EPI>(a, choose(a, EPI, direct<KCA, KCB>(a), ws.bytes), ws, st);
+  return launch<T, KCA, KCB, EPI>(a, choose(a, EPI, direct<KCA, KCB>(a), std::min(ws.bytes, PARTIAL_LIMIT)), ws, st);
 }
 
 template <class T, bool GLU, int TT>
@@ -172,14 +207,42 @@ GemmArgs one(const Product& p, int act) {
   return a;
 }
 
-template <class T>
-int run_fwd(const FfnShape& s, int act, const void* x, const void* wg, const void* wu, const void* wd, void* h, void* gate, void* up, void* y, const Scratch& ws,
-            hipStream_t st) {
+// the products of the block, in the order of the calls
+GemmArgs glu_args(const FfnShape& s, int act, const void* x, const void* wg, const void* wu, void* h, void* gate, void* up) {
   GemmArgs a = one(product(x, s.ldx, wg, s.D, h, s.F, s.M, s.F, s.D), act);
   a.p[0].b[1] = wu;
   a.out0 = gate;
   a.out1 = up;
-  const GemmArgs b = one(product(h, s.F, wd, s.F, y, s.ldy, s.M, s.O, s.F), act);
+  return a;
+}
+GemmArgs down_args(const FfnShape& s, const void* h, const void* wd, void* y) { return one(product(h, s.F, wd, s.F, y, s.ldy, s.M, s.O, s.F), 0); }
+GemmArgs dh_args(const FfnShape& s, int act, const void* dy, const void* wd, const void* gate, const void* up, void* dgate, void* dup) {
+  GemmArgs a = one(product(dy, s.lddy, wd, s.F, nullptr, 0, s.M, s.F, s.O), act);
+  a.gate = gate;
+  a.up = up;
+  a.out0 = dgate;
+  a.out1 = dup;
+  return a;
+}
+GemmArgs dx_args(const FfnShape& s, const void* dgate, const void* dup, const void* wg, const void* wu, void* dx) {
+  GemmArgs a = one(product(dgate, s.F, wg, s.D, dx, s.lddx, s.M, s.D, s.F), 0);
+  a.p[0].a[1] = dup;
+  a.p[0].b[1] = wu;
+  a.parts = 2;
+  return a;
+}
+GemmArgs dw_args(const FfnShape& s, const void* dgate, const void* dup, const void* dy, const void* x, const void* h, void* dwg, void* dwu, void* dwd) {
+  GemmArgs a = one(product(dgate, s.F, x, s.ldx, dwg, s.D, s.F, s.D, s.M), 0);
+  a.p[1] = product(dup, s.F, x, s.ldx, dwu, s.D, s.F, s.D, s.M);
+  a.p[2] = product(dy, s.lddy, h, s.F, dwd, s.F, s.O, s.F, s.M);
+  a.products = 3;
+  return a;
+}
+
+template <class T>
+int run_fwd(const FfnShape& s, int act, const void* x, const void* wg, const void* wu, const void* wd, void* h, void* gate, void* up, void* y, const Scratch& ws,
+            hipStream_t st) {
+  const GemmArgs a = glu_args(s, act, x, wg, wu, h, gate, up), b = down_args(s, h, wd, y);
   if (s.M <= FEW_ROWS) {
     const int rc = few<T, true>(a, st);
     return rc == JZ_OK ? few<T, false>(b, st) : rc;
@@ -191,26 +254,9 @@ int run_fwd(const FfnShape& s, int act, const void* x, const void* wg, const voi
 template <class T>
 int run_bwd(const FfnShape& s, int act, const void* x, const void* wg, const void* wu, const void* wd, const void* gate, const void* up, const void* h, const void* dy,
             void* dx, void* dwg, void* dwu, void* dwd, void* dgate, void* dup, const Scratch& ws, hipStream_t st) {
-  GemmArgs a = one(product(dy, s.lddy, wd, s.F, nullptr, 0, s.M, s.F, s.O), act);
-  a.gate = gate;
-  a.up = up;
-  a.out0 = dgate;
-  a.out1 = dup;
-  int rc = gemm<T, true, false, EPI_GLU_BWD>(a, ws, st);
-  if (rc == JZ_OK && dx) {
-    a = one(product(dgate, s.F, wg, s.D, dx, s.lddx, s.M, s.D, s.F), act);
-    a.p[0].a[1] = dup;
-    a.p[0].b[1] = wu;
-    a.parts = 2;
-    rc = gemm<T, true, false, EPI_STORE>(a, ws, st);
-  }
-  if (rc == JZ_OK && dwg) {
-    a = one(product(dgate, s.F, x, s.ldx, dwg, s.D, s.F, s.D, s.M), act);
-    a.p[1] = product(dup, s.F, x, s.ldx, dwu, s.D, s.F, s.D, s.M);
-    a.p[2] = product(dy, s.lddy, h, s.F, dwd, s.F, s.O, s.F, s.M);
-    a.products = 3;
-    rc = gemm<T, false, false, EPI_STORE>(a, ws, st);
-  }
+  int rc = gemm<T, true, false, EPI_GLU_BWD>(dh_args(s, act, dy, wd, gate, up, dgate, dup), ws, st);
+  if (rc == JZ_OK && dx) rc = gemm<T, true, false, EPI_STORE>(dx_args(s, dgate, dup, wg, wu, dx), ws, st);
+  if (rc == JZ_OK && dwg) rc = gemm<T, false, false, EPI_STORE>(dw_args(s, dgate, dup, dy, x, h, dwg, dwu, dwd), ws, st);
   return rc;
 }
 
@@ -222,7 +268,9 @@ extern "C" int jz_ffn_fwd_workspace_bytes(const jz_ffn_desc* d, size_t* bytes) {
   if (!bytes) return JZ_ERR_NULL;
   FfnShape s;
   const int rc = ffn_shape(d, &s);
-  if (rc == JZ_OK) *bytes = 0;
+  if (rc != JZ_OK) return rc;
+  const GemmArgs a = glu_args(s, 0, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr), b = down_args(s, nullptr, nullptr, nullptr);
+  *bytes = s.M <= FEW_ROWS ? 0 : std::max(wanted(a, EPI_GLU, direct<true, true>(a)), wanted(b, EPI_STORE, direct<true, true>(b)));
   return rc;
 }
 
@@ -230,7 +278,11 @@ extern "C" int jz_ffn_bwd_workspace_bytes(const jz_ffn_desc* d, size_t* bytes) {
   if (!bytes) return JZ_ERR_NULL;
   FfnShape s;
   const int rc = ffn_shape(d, &s);
-  if (rc == JZ_OK) *bytes = 2 * hidden_bytes(s);
+  if (rc != JZ_OK) return rc;
+  const GemmArgs a = dh_args(s, 0, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr), b = dx_args(s, nullptr, nullptr, nullptr, nullptr, nullptr),
+                 c = dw_args(s, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr);
+  *bytes = 2 * hidden_bytes(s) + std::max(wanted(a, EPI_GLU_BWD, direct<true, false>(a)),
+                                          std::max(wanted(b, EPI_STORE, direct<true, false>(b)), wanted(c, EPI_STORE, direct<false, false>(c))));
   return rc;
 }
 
@@ -244,6 +296,8 @@ extern "C" int jz_ffn_fwd(const jz_ffn_desc* d, const void* x, const void* w_gat
   const size_t hid = span(s.M, s.F, s.F), w = span(s.F, s.D, s.D);
   const FfnTensor t[] = {{x, span(s.M, s.D, s.ldx), false}, {w_gate, w, false}, {w_up, w, false}, {w_down, span(s.O, s.F, s.F), false}, {h, hid, true},
                          {gate, hid, true}, {up, hid, true}, {y, span(s.M, s.O, s.ldy), true}};
+  if (ws_bytes && !ws) return JZ_ERR_WORKSPACE;
+  if (ws && !jz::aligned16(ws)) return JZ_ERR_ALIGN;
   rc = ffn_look_over(t, 8, ws, ws_bytes);
   if (rc != JZ_OK) return rc;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
@@ -266,7 +320,7 @@ extern "C" int jz_ffn_bwd(const jz_ffn_desc* d, const void* x, const void* w_gat
   const FfnTensor t[] = {{weights ? x : nullptr, span(s.M, s.D, s.ldx), false}, {w_gate, w, false}, {w_up, w, false}, {w_down, w2, false}, {gate, hid, false}, {up, hid, false},
                          {weights ? h : nullptr, hid, false}, {dy, span(s.M, s.O, s.lddy), false}, {dx, span(s.M, s.D, s.lddx), true}, {dw_gate, w, true}, {dw_up, w, true},
                          {dw_down, w2, true}};
-  rc = ffn_look_over(t, 12, ws, need);
+  rc = ffn_look_over(t, 12, ws, ws_bytes);
   if (rc != JZ_OK) return rc;
   char* b = static_cast<char*>(ws);
   void *dgate = b, *dup = b + hidden_bytes(s);

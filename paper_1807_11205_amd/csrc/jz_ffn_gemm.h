@@ -74,13 +74,22 @@ struct GemmArgs {
   Product p[3];
   int products, parts;      // parts of the sum: 1 or 2
   int act;
-  int splits;               // of the k tiles, over blockIdx.y; above 1 the sums go to `partial`
-  int tiles_per_split;
-  float* partial;           // [splits][M][pitch], the products one behind the other
-  int64_t partial_pitch, partial_size;
+  int full;                 // tiles that one workgroup computes; of each further one `splits` workgroups take tiles_per_split k tiles
+  int splits, tiles_per_split;
+  float* partial;           // [tiles behind `full`][splits][BM][BN]
   const void *gate, *up;    // EPI_GLU_BWD: the saved projections, [M][N]
   void *out0, *out1;        // EPI_GLU: gate and up, or NULL; EPI_GLU_BWD: dgate and dup
 };
+
+// dgate and dup of eight elements from dh = v
+__device__ __forceinline__ void glu_bwd8(int act, f32x8 v, f32x8 g, f32x8 u, f32x8* dg, f32x8* du) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float slope;
+    (*du)[i] = v[i] * act_both(act, g[i], &slope);
+    (*dg)[i] = v[i] * u[i] * slope;
+  }
+}
 
 // ---- results --------------------------------------------------------------------------------------------------------------
 // What becomes of eight sums (or gate and up sums) that belong to columns n .. n + 7 of row m.
@@ -100,14 +109,8 @@ __device__ __forceinline__ void finish8(const GemmArgs& a, const Product& p, int
       store8(static_cast<T*>(a.out1) + m * p.N + n, narrow8<T>(w), left);
     }
   } else {
-    const f32x8 g = widen8<T>(load8(static_cast<const T*>(a.gate) + m * p.N + n, left)), u = widen8<T>(load8(static_cast<const T*>(a.up) + m * p.N + n, left));
     f32x8 dg, du;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float slope;
-      du[i] = v[i] * act_both(a.act, g[i], &slope);
-      dg[i] = v[i] * u[i] * slope;
-    }
+    glu_bwd8(a.act, v, widen8<T>(load8(static_cast<const T*>(a.gate) + m * p.N + n, left)), widen8<T>(load8(static_cast<const T*>(a.up) + m * p.N + n, left)), &dg, &du);
     store8(static_cast<T*>(a.out0) + m * p.N + n, narrow8<T>(dg), left);
     store8(static_cast<T*>(a.out1) + m * p.N + n, narrow8<T>(du), left);
   }
@@ -158,27 +161,46 @@ struct Staged {
   }
 };
 
-// Which tile of which product a workgroup has: consecutive workgroups land on different XCDs, each with an L2 of its own, so every XCD gets a
-// run of tiles, and within a run eight rows of tiles are taken column by column: what a run reads at a time is then a block.
-__device__ __forceinline__ int find_tile(const GemmArgs& a, unsigned* tm, unsigned* tn) {
-  unsigned t = xcd_remap(blockIdx.x, gridDim.x);
-  int q = 0;
-  while (q + 1 < a.products && t >= (unsigned)(a.p[q].tiles_m * a.p[q].tiles_n)) {
-    t -= a.p[q].tiles_m * a.p[q].tiles_n;
-    ++q;
+// Which tile of which product a workgroup has.  Consecutive workgroups land on different XCDs, each with an L2 of its own, so every XCD gets a run of
+// tiles, and within a run eight rows of tiles are taken column by column: what a run reads at a time is then a block.
+struct Tile {
+  int product, split;  // split < 0: the whole sum
+  unsigned m, n, behind;  // behind: number among the tiles that are split
+};
+__device__ __forceinline__ void place_tile(const GemmArgs& a, unsigned t, Tile* w) {
+  w->product = 0;
+  while (w->product + 1 < a.products && t >= (unsigned)(a.p[w->product].tiles_m * a.p[w->product].tiles_n)) {
+    t -= a.p[w->product].tiles_m * a.p[w->product].tiles_n;
+    ++w->product;
   }
-  const unsigned rows = a.p[q].tiles_m, cols = a.p[q].tiles_n, G = 8;
+  const unsigned rows = a.p[w->product].tiles_m, cols = a.p[w->product].tiles_n, G = 8;
   const unsigned band = t / (G * cols), in = t % (G * cols), high = rows - band * G < G ? rows - band * G : G;
-  *tm = band * G + in % high;
-  *tn = in / high;
-  return q;
+  w->m = band * G + in % high;
+  w->n = in / high;
+}
+__device__ __forceinline__ Tile find_tile(const GemmArgs& a) {
+  Tile w;
+  const unsigned full = a.full;
+  if (blockIdx.x < full) {
+    w.split = -1;
+    w.behind = 0;
+    place_tile(a, xcd_remap(blockIdx.x, full), &w);
+  } else {
+    const unsigned i = blockIdx.x - full, rest = (gridDim.x - full) / a.splits;
+    w.split = i / rest;
+    w.behind = i % rest;
+    place_tile(a, full + w.behind, &w);
+  }
+  return w;
 }
 
 // The sums of a wavefront's tile to their places: FP32 partial sums, or the epilogue.  They pass through LDS 32 rows at a time, so that a lane has eight columns
 // of a row and neighbouring lanes its neighbours: whole lines are stored.  lds: 32 rows of TN * 32 floats of the wavefront's own, 16-byte chunk c of row r at
 // c ^ (r % 8).  Register 4 j + i of a lane holds row lane % 32, column 8 j + 4 (lane / 32) + i.
+// partial: where the sums of the wavefront's first row and column go instead, rows `pitch` apart; or NULL.
 template <class T, int EPI, int TM, int TN>
-__device__ __forceinline__ void finish_tile(const GemmArgs& a, const Product& p, int q, f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, JZ_LDS unsigned char* lds, int lane) {
+__device__ __forceinline__ void finish_tile(const GemmArgs& a, const Product& p, f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, float* partial, int pitch,
+                                            JZ_LDS unsigned char* lds, int lane) {
   constexpr int PITCH = TN * 128, PER = (EPI == EPI_GLU ? TN * 2 : TN * 4);  // bytes of a row; groups of eight results in one
   auto chunk = [&](int row, int c) { return lds + row * PITCH + ((c ^ (row & 7)) * 16); };
   auto eight = [&](int row, int c) {
@@ -191,14 +213,11 @@ __device__ __forceinline__ void finish_tile(const GemmArgs& a, const Product& p,
       constexpr int y = decltype(I)::value / 4, j = decltype(I)::value % 4;
       *reinterpret_cast<JZ_LDS f32x4*>(chunk(lane & 31, y * 8 + j * 2 + (lane >> 5))) = f32x4{acc[x][y][4 * j], acc[x][y][4 * j + 1], acc[x][y][4 * j + 2], acc[x][y][4 * j + 3]};
     });
-    if (a.splits > 1) {
-      float* out = a.partial + blockIdx.y * a.partial_size;
-      for (int i = 0; i < q; ++i) out += a.p[i].M * a.partial_pitch;
+    if (partial) {
 #pragma unroll 1
       for (int i = lane; i < 32 * TN * 4; i += 64) {
         const int row = i / (TN * 4), c = i % (TN * 4);
-        const int64_t m = m0 + x * 32 + row, n = n0 + c * 8;
-        if (m < p.M && n < a.partial_pitch) store8(out + m * a.partial_pitch + n, eight(row, c * 2));
+        store8(partial + (x * 32 + row) * pitch + c * 8, eight(row, c * 2));
       }
     } else {
 #pragma unroll 1
@@ -216,6 +235,51 @@ __device__ __forceinline__ void finish_tile(const GemmArgs& a, const Product& p,
   });
 }
 
+// The same for EPI_GLU_BWD, whose results need gate and up from memory: those of a strip are asked for a strip ahead.  Columns are a multiple of 8.
+template <class T, int ACT, int TM, int TN>
+__device__ __forceinline__ void finish_bwd(const GemmArgs& a, const Product& p, f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, JZ_LDS unsigned char* lds, int lane) {
+  constexpr int PITCH = TN * 128, PER = TN * 4, EACH = 32 * PER / 64;
+  typename Vec8<T>::V g[EACH], u[EACH];
+  auto place = [&](int x, int i, int64_t* m, int64_t* n) {
+    const int s = i * 64 + lane;
+    *m = m0 + x * 32 + s / PER;
+    *n = n0 + s % PER * 8;
+    return *m < p.M && *n < p.N;
+  };
+  auto ask = [&](int x, int i) {
+    int64_t m, n;
+    if (!place(x, i, &m, &n)) return;
+    g[i] = load8(static_cast<const T*>(a.gate) + m * p.N + n);
+    u[i] = load8(static_cast<const T*>(a.up) + m * p.N + n);
+  };
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    g[i] = u[i] = {};
+    ask(0, i);
+  }
+  auto chunk = [&](int row, int c) { return lds + row * PITCH + ((c ^ (row & 7)) * 16); };
+  static_for<0, TM>([&](auto X) {
+    constexpr int x = decltype(X)::value;
+    static_for<0, TN * 4>([&](auto I) {
+      constexpr int y = decltype(I)::value / 4, j = decltype(I)::value % 4;
+      *reinterpret_cast<JZ_LDS f32x4*>(chunk(lane & 31, y * 8 + j * 2 + (lane >> 5))) = f32x4{acc[x][y][4 * j], acc[x][y][4 * j + 1], acc[x][y][4 * j + 2], acc[x][y][4 * j + 3]};
+    });
+    static_for<0, EACH>([&](auto I) {
+      constexpr int i = decltype(I)::value;
+      const int s = i * 64 + lane, row = s / PER, c = s % PER * 2;
+      const f32x4 lo = *reinterpret_cast<const JZ_LDS f32x4*>(chunk(row, c)), hi = *reinterpret_cast<const JZ_LDS f32x4*>(chunk(row, c + 1));
+      f32x8 dg, du;
+      glu_bwd8(ACT, f32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, widen8<T>(g[i]), widen8<T>(u[i]), &dg, &du);
+      if constexpr (x + 1 < TM) ask(x + 1, i);
+      int64_t m, n;
+      if (place(x, i, &m, &n)) {
+        store8(static_cast<T*>(a.out0) + m * p.N + n, narrow8<T>(dg));
+        store8(static_cast<T*>(a.out1) + m * p.N + n, narrow8<T>(du));
+      }
+    });
+  });
+}
+
 // Any sizes, any alignment: the operands pass through registers on their way into LDS, element by element where a row ends.
 template <class T, bool KCA, bool KCB, int EPI, int BM, int BN>
 __global__ __launch_bounds__(256) void ffn_gemm_any(GemmArgs a) {
@@ -225,13 +289,13 @@ __global__ __launch_bounds__(256) void ffn_gemm_any(GemmArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char operands[SA::BYTES + SB::BYTES];
   unsigned char *const sa = operands, *const sb = operands + SA::BYTES;
   static_assert(SA::BYTES + SB::BYTES >= 4 * 32 * TN * 128, "the results pass through LDS");
-  unsigned tm, tn;
-  const int q = find_tile(a, &tm, &tn);
-  const Product p = a.p[q];
+  const Tile w = find_tile(a);
+  const Product p = a.p[w.product];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, wm = wave >> 1, wn = wave & 1;
-  const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+  const int64_t m0 = (int64_t)w.m * BM, n0 = (int64_t)w.n * BN;
   const int per_part = (int)((p.K + BK - 1) / BK), all = per_part * a.parts;
-  const int first = blockIdx.y * a.tiles_per_split, last = first + a.tiles_per_split < all ? first + a.tiles_per_split : all;
+  const int first = w.split < 0 ? 0 : w.split * a.tiles_per_split, last = w.split < 0 || first + a.tiles_per_split > all ? all : first + a.tiles_per_split;
+  float* const partial = w.split < 0 ? nullptr : a.partial + ((size_t)w.behind * a.splits + w.split) * (BM * BN);
 
   Op8<T> ra[SA::EACH], rb[SB::EACH];
   auto fetch = [&](int kt) {
@@ -298,7 +362,7 @@ __global__ __launch_bounds__(256) void ffn_gemm_any(GemmArgs a) {
     }
     __syncthreads();
   }
-  finish_tile<T, EPI>(a, p, q, acc, m0 + wm * (BM / 2), n0 + wn * (BN / 2), (JZ_LDS unsigned char*)operands + wave * (32 * TN * 128), lane);
+  finish_tile<T, EPI>(a, p, acc, m0 + wm * (BM / 2), n0 + wn * (BN / 2), partial ? partial + wm * (BM / 2) * BN + wn * (BN / 2) : nullptr, BN, (JZ_LDS unsigned char*)operands + wave * (32 * TN * 128), lane);
 }
 
 // ---- LDS-direct ---------------------------------------------------------------------------------------------------------------
@@ -339,10 +403,10 @@ struct Source {
   }
   // 16 bytes a lane into LDS; what lies outside the operand arrives as zeros
   template <class L>
-  __device__ __forceinline__ void load(L* lds, int part, int64_t k0, int wave) const {
-    const int64_t skip = k0 * (KC ? 2 : pitch);
+  __device__ __forceinline__ void load(L* lds, int part, int64_t k0, int wave, bool wanted) const {
+    const int64_t skip = wanted ? k0 * (KC ? 2 : pitch) : 0;
     const int64_t span = KC ? (rows_left - 1) * pitch + (K - k0) * 2 : (K - k0 - 1) * pitch + rows_left * 2;
-    const int bytes = (int)(span < 0x7ffffff0 ? span : 0x7ffffff0);
+    const int bytes = !wanted ? 0 : (int)(span < 0x7ffffff0 ? span : 0x7ffffff0);
     const auto r0 = __builtin_amdgcn_make_buffer_rsrc((void*)(base[DUAL ? 0 : part] + skip), 0, bytes, 0x00020000);
     const auto r1 = __builtin_amdgcn_make_buffer_rsrc((void*)(base[1] + skip), 0, bytes, 0x00020000);
     const unsigned end = KC && k >= K - k0 ? 0x80000000u : 0u;  // a row's end inside the tile: the next row does not follow
@@ -356,31 +420,44 @@ struct Source {
   }
 };
 
-template <class T, bool KCA, bool KCB, int EPI, int BM, int BN, int WGM, int WGN>
+// The order of a step's instructions: between one matrix instruction and the next a read of LDS or a load.
+template <int MULTIPLY, int READ, int LOAD>
+__device__ __forceinline__ void spread_out() {
+  constexpr int OTHER = READ + LOAD;
+  static_for<0, MULTIPLY>([&](auto I) {
+    constexpr int i = decltype(I)::value, from = i * OTHER / MULTIPLY, to = (i + 1) * OTHER / MULTIPLY;
+    constexpr int reads = (to < READ ? to : READ) - (from < READ ? from : READ), loads = to - from - reads;
+    if constexpr (reads > 0) __builtin_amdgcn_sched_group_barrier(0x100, reads, 0);
+    if constexpr (loads > 0) __builtin_amdgcn_sched_group_barrier(0x10, loads, 0);
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+  });
+}
+
+// ACT: the activation where EPI is EPI_GLU_BWD, else 0
+template <class T, bool KCA, bool KCB, int EPI, int ACT, int BM, int BN, int WGM, int WGN>
 __global__ __launch_bounds__(64 * WGM * WGN, 2) void ffn_gemm(GemmArgs a) {
-  constexpr int THREADS = 64 * WGM * WGN, TM = BM / WGM / 32, TN = BN / WGN / 32, STEPS = BK / 16;
+  constexpr int THREADS = 64 * WGM * WGN, TM = BM / WGM / 32, TN = BN / WGN / 32, STEPS = BK / 16, READS = TM * (KCA ? 1 : 2) + TN * (KCB ? 1 : 2);
   using SA = Staged<T, KCA, BM, THREADS>;
   using SB = Staged<T, KCB, BN, THREADS>;
   // four objects, not one: an LDS read then only waits for the loads into its own
   __shared__ __attribute__((aligned(1024))) unsigned char a0[SA::BYTES], a1[SA::BYTES], b0[SB::BYTES], b1[SB::BYTES];
-  unsigned tm, tn;
-  const int q = find_tile(a, &tm, &tn);
-  const Product p = a.p[q];
+  const Tile w = find_tile(a);
+  const Product p = a.p[w.product];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), wm = wave / WGN, wn = wave % WGN;
-  const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+  const int64_t m0 = (int64_t)w.m * BM, n0 = (int64_t)w.n * BN;
   const int per_part = (int)((p.K + BK - 1) / BK), all = per_part * a.parts;
-  const int first = blockIdx.y * a.tiles_per_split, last = first + a.tiles_per_split < all ? first + a.tiles_per_split : all;
+  const int first = w.split < 0 ? 0 : w.split * a.tiles_per_split, last = w.split < 0 || first + a.tiles_per_split > all ? all : first + a.tiles_per_split;
+  float* const partial = w.split < 0 ? nullptr : a.partial + ((size_t)w.behind * a.splits + w.split) * (BM * BN);
 
   Source<T, KCA, BM, THREADS, false> from_a;
   Source<T, KCB, BN, THREADS, EPI == EPI_GLU> from_b;
   from_a.init(p.a, p.lda, m0, p.M, p.K, t);
   from_b.init(p.b, p.ldb, EPI == EPI_GLU ? n0 / 2 : n0, p.N, p.K, t);
   auto fetch = [&](auto* la, auto* lb, int kt) {
-    if (kt >= last) return;
-    const int part = kt >= per_part;
+    const int part = kt >= per_part && a.parts > 1;  // behind the last tile: zeros, so that there is no branch among the products
     const int64_t k0 = (int64_t)(kt - part * per_part) * BK;
-    from_a.load(la, part, k0, wave);
-    from_b.load(lb, part, k0, wave);
+    from_a.load(la, part, k0, wave, kt < last);
+    from_b.load(lb, part, k0, wave, kt < last);
   };
   unsigned at_a[4], at_b[4];
   SA::address(at_a, wm * TM * 32, lane);
@@ -403,58 +480,64 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void ffn_gemm(GemmArgs a) {
 #pragma unroll
       for (int y = 0; y < TN; ++y) acc[x][y] = mfma(fb[from][y], fa[from][x], acc[x][y]);
   };
-  // The tile in la, lb, whose first operands are in registers already.  Its last step's products run while the next tile's first operands are read and the
-  // tile after that is asked for, into the place that this one leaves.
+  // The tile in la, lb.  The products of its predecessor's last step run while its first operands are read and the next tile is asked for, into the place
+  // that the predecessor leaves.  The loop turns at the barrier: loads that are in flight across its turn would be waited for.
   auto tile = [&](auto* la, auto* lb, auto* na, auto* nb, int kt) {
+    all_landed();
+    read(la, lb, 0, 0);
+    fetch(na, nb, kt + 1);
+    multiply((STEPS - 1) & 1);
+    spread_out<TM * TN, READS, SA::EACH + SB::EACH>();
     static_for<0, STEPS - 1>([&](auto S) {
       constexpr int s = decltype(S)::value;
       read(la, lb, s + 1, (s + 1) & 1);
       multiply(s & 1);
+      spread_out<TM * TN, READS, 0>();
     });
-    all_landed();
-    fetch(la, lb, kt + 2);
-    if (kt + 1 < last) read(na, nb, 0, 0);
-    multiply((STEPS - 1) & 1);
   };
   if (first < last) {
+#pragma unroll
+    for (int x = 0; x < TM; ++x) fa[1][x] = Op8<T>{};  // the first tile has no predecessor
+#pragma unroll
+    for (int y = 0; y < TN; ++y) fb[1][y] = Op8<T>{};
     fetch(a0, b0, first);
-    all_landed();
-    fetch(a1, b1, first + 1);
-    read(a0, b0, 0, 0);
     for (int kt = first; kt < last; kt += 2) {
       tile(a0, b0, a1, b1, kt);
       if (kt + 1 < last) tile(a1, b1, a0, b0, kt + 1);
     }
+    multiply((STEPS - 1) & 1);
   }
-  // past the last barrier nobody reads operands any more
+  all_landed();  // zeros too: the results take the operands' place
   constexpr int STRIP = 32 * TN * 128, FIT = SA::BYTES / STRIP;
   static_assert(2 * FIT >= WGM * WGN, "the results pass through the place of A");
   unsigned char* const mine = (wave < FIT ? a0 + wave * STRIP : a1 + (wave - FIT) * STRIP);
-  finish_tile<T, EPI>(a, p, q, acc, m0 + wm * TM * 32, n0 + wn * TN * 32, (JZ_LDS unsigned char*)mine, lane);
+  const int64_t m = m0 + wm * TM * 32, n = n0 + wn * TN * 32;
+  float* const mine_partial = partial ? partial + wm * TM * 32 * BN + wn * TN * 32 : nullptr;
+  if constexpr (EPI == EPI_GLU_BWD) {
+    if (partial) finish_tile<T, EPI_STORE>(a, p, acc, m, n, mine_partial, BN, (JZ_LDS unsigned char*)mine, lane);
+    else finish_bwd<T, ACT>(a, p, acc, m, n, (JZ_LDS unsigned char*)mine, lane);
+  } else {
+    finish_tile<T, EPI>(a, p, acc, m, n, mine_partial, BN, (JZ_LDS unsigned char*)mine, lane);
+  }
 }
 
-// The partial sums of a split reduction, added in the order of the splits, and the epilogue.  Eight columns a thread.
-template <class T, int EPI>
+// The partial sums of the tiles that are split, added in the order of the splits, and the epilogue.  Eight columns a thread, blockIdx.y a tile.
+template <class T, int EPI, int TILE>
 __global__ __launch_bounds__(256) void ffn_join(GemmArgs a) {
-  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const float* at = a.partial;
-  for (int q = 0; q < a.products; ++q) {
-    const Product& p = a.p[q];
-    const int64_t per = (p.N + 7) / 8, n = p.M * per;
-    if (i < n) {
-      const int64_t m = i / per, c = (i % per) * 8;
-      const int64_t g = EPI == EPI_GLU ? (c >> 5) * 64 + (c & 31) : c;
-      auto total = [&](int64_t col) {
-        const float* f = at + m * a.partial_pitch + col;
-        f32x8 v = load8(f);
-        for (int s = 1; s < a.splits; ++s) v += load8(f + s * a.partial_size);
-        return v;
-      };
-      const f32x8 v = total(g), w = EPI == EPI_GLU ? total(g + 32) : v;
-      finish8<T, EPI>(a, p, m, c, v, w);
-      return;
-    }
-    i -= n;
-    at += p.M * a.partial_pitch;
-  }
+  constexpr int PER = EPI == EPI_GLU ? TILE / 16 : TILE / 8;  // groups of eight results in a row of a tile
+  Tile w;
+  place_tile(a, a.full + blockIdx.y, &w);
+  const Product& p = a.p[w.product];
+  const int i = blockIdx.x * 256 + threadIdx.x, row = i / PER, c = i % PER;
+  const int64_t m = (int64_t)w.m * TILE + row, n = (int64_t)w.n * (EPI == EPI_GLU ? TILE / 2 : TILE) + c * 8;
+  if (m >= p.M || n >= p.N) return;
+  auto total = [&](int col) {
+    const float* f = a.partial + (size_t)blockIdx.y * a.splits * (TILE * TILE) + row * TILE + col;
+    f32x8 v = load8(f);
+    for (int s = 1; s < a.splits; ++s) v += load8(f + (size_t)s * (TILE * TILE));
+    return v;
+  };
+  const int col = EPI == EPI_GLU ? (c >> 2) * 64 + (c & 3) * 8 : c * 8;
+  const f32x8 v = total(col), u = EPI == EPI_GLU ? total(col + 32) : v;
+  finish8<T, EPI>(a, p, m, n, v, u);
 }
