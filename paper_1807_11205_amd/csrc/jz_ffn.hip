@@ -174,9 +174,10 @@ int gemm(GemmArgs a, const Scratch& ws, hipStream_t st) {
 template <class T, bool GLU, int TT>
 int launch_few(const GemmArgs& a, hipStream_t st) {
   const unsigned grid = (unsigned)((a.p[0].N + 15) / 16);
-  // a workgroup has one compute unit: with fewer of them, more wavefronts in each
-  if (grid >= 512) ffn_few<T, GLU, TT, 8><<<grid, 512, 0, st>>>(a);
-  else ffn_few<T, GLU, TT, 16><<<grid, 1024, 0, st>>>(a);
+  // sixteen wavefronts fit a compute unit: as many to a workgroup as keep all workgroups on the chip at once
+  if (grid <= 256) ffn_few<T, GLU, TT, 16><<<grid, 1024, 0, st>>>(a);
+  else if (grid <= 512) ffn_few<T, GLU, TT, 8><<<grid, 512, 0, st>>>(a);
+  else ffn_few<T, GLU, TT, 4><<<grid, 256, 0, st>>>(a);
   return jz::launch_status();
 }
 constexpr int64_t FEW_ROWS = 64;

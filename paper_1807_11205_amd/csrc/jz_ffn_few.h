@@ -13,7 +13,7 @@ __device__ __forceinline__ f32x4 mfma16(Op8<__bf16> a, Op8<__bf16> b, f32x4 c) {
 
 template <class T, bool GLU, int TT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void ffn_few(GemmArgs a) {
-  constexpr int MATS = GLU ? 2 : 1, UNROLL = TT == 1 ? 8 / MATS : 4 / MATS;
+  constexpr int MATS = GLU ? 2 : 1, UNROLL = TT == 1 && WAVES < 16 ? 4 : (TT == 4 ? 2 : 4) / MATS;  // as registers allow
   __shared__ f32x4 sums[WAVES][MATS][TT][64];
   const Product& p = a.p[0];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r16 = lane & 15, k8 = (lane >> 4) * 8;
@@ -30,38 +30,38 @@ __global__ __launch_bounds__(64 * WAVES) void ffn_few(GemmArgs a) {
 #pragma unroll
     for (int j = 0; j < TT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  struct Step {
-    Op8<T> w[UNROLL][MATS], x[UNROLL][TT];
-  };
-  auto load = [&](Step& s, int64_t k0) {  // whole steps only
+  // Weights are asked for a turn ahead; the rows of A, which all workgroups share and the caches hold, in their own turn.
+  constexpr int64_t DEPTH = UNROLL * 32, TURN = DEPTH * WAVES;
+  const int64_t whole = p.K / DEPTH * DEPTH;
+  Op8<T> cur[UNROLL][MATS], next[UNROLL][MATS];
+  auto weights = [&](Op8<T>(&to)[UNROLL][MATS], int64_t k0) {  // whole steps only
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u)
 #pragma unroll
-      for (int i = 0; i < MATS; ++i) s.w[u][i] = __builtin_nontemporal_load(reinterpret_cast<const typename Vec8<T>::U*>(w[i] + k0 + u * 32 + k8));
+      for (int i = 0; i < MATS; ++i) to[u][i] = load8(w[i] + k0 + u * 32 + k8);
+  };
+  auto turn = [&](Op8<T>(&have)[UNROLL][MATS], Op8<T>(&ask)[UNROLL][MATS], int64_t k0) {
+    Op8<T> xs[UNROLL][TT];
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u)
 #pragma unroll
-      for (int j = 0; j < TT; ++j) s.x[u][j] = load8(x[j] + k0 + u * 32 + k8);
-  };
-  auto multiply = [&](const Step& s) {
+      for (int j = 0; j < TT; ++j) xs[u][j] = load8(x[j] + k0 + u * 32 + k8);
+    if (k0 + TURN < whole) weights(ask, k0 + TURN);
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u)
 #pragma unroll
       for (int i = 0; i < MATS; ++i)
 #pragma unroll
-        for (int j = 0; j < TT; ++j) acc[i][j] = mfma16(s.w[u][i], s.x[u][j], acc[i][j]);
+        for (int j = 0; j < TT; ++j) acc[i][j] = mfma16(have[u][i], xs[u][j], acc[i][j]);
   };
-  constexpr int64_t DEPTH = UNROLL * 32, TURN = DEPTH * WAVES;
-  const int64_t whole = p.K / DEPTH * DEPTH;
   int64_t k0 = wave * DEPTH;
-  Step cur, next;
-  if (k0 < whole) load(cur, k0);
+  if (k0 < whole) weights(cur, k0);
   while (k0 < whole) {
-    const int64_t k1 = k0 + TURN;
-    if (k1 < whole) load(next, k1);
-    multiply(cur);
-    cur = next;
-    k0 = k1;
+    turn(cur, next, k0);
+    k0 += TURN;
+    if (k0 >= whole) break;
+    turn(next, cur, k0);
+    k0 += TURN;
   }
   // what is left, 32 k at a time, one wavefront each
   for (int64_t k = whole + wave * 32; k < p.K; k += WAVES * 32) {

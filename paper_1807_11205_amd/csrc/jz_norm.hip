@@ -51,160 +51,253 @@ __device__ __forceinline__ float row_sum(float s, float* lds) {
 __device__ __forceinline__ float sum8(f32x8 v) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
 __device__ __forceinline__ f32x8 splat8(float v) { return f32x8{v, v, v, v, v, v, v, v}; }
 
-// element index of a lane's vector i, and how many of its eight elements the row has
-#define JZ_AT(i) (((i) * THREADS + lane) * 8)
+// Which elements of a row a lane has: NV vectors of eight, vector i from element 8 (i THREADS + lane) on.  Loads are not predicated, so that all of a row's are on
+// their way at once: a vector that would pass the row's end is the row's last eight elements instead, and what of it lies outside the lane's own part is left
+// out of the sums.  (What a lane then stores a second time are the bits that their owner stores.)
+//   EVEN   channels are a multiple of 8: a vector is a lane's own or nobody's        RAGGED   others from 8 on: the last vector overlaps its neighbour
+//   TINY   less than 8: one vector, element by element
+enum { EVEN = 0, RAGGED = 1, TINY = 2 };
+template <int MODE, int THREADS>
+struct Lane {
+  int C, lane;
+  __device__ __forceinline__ int own(int i) const { return (i * THREADS + lane) * 8; }
+  __device__ __forceinline__ int at(int i) const { return MODE == TINY || own(i) + 8 <= C ? own(i) : C - 8; }
+  __device__ __forceinline__ bool on(int i) const { return own(i) < C; }
+  template <class T>
+  __device__ __forceinline__ typename Vec8<T>::V load(const T* row, int i) const {
+    if constexpr (MODE == TINY) {
+      typename Vec8<T>::V v = {};
+      if (on(i)) v = load8(row + own(i), C - own(i));
+      return v;
+    } else {
+      return load8(row + at(i));
+    }
+  }
+  template <class T>
+  __device__ __forceinline__ void store(T* row, int i, f32x8 v) const {
+    if (!on(i)) return;
+    if constexpr (MODE == TINY) store8(row + own(i), narrow8<T>(v), C - own(i));
+    else store8(row + at(i), narrow8<T>(v));
+  }
+  __device__ __forceinline__ float sum(f32x8 v, int i) const {
+    if constexpr (MODE == RAGGED) {
+      const int skip = on(i) ? own(i) - at(i) : 8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = e < skip ? 0.f : v[e];
+    }
+    const float s = sum8(v);
+    return MODE == EVEN && !on(i) ? 0.f : s;
+  }
+};
 
 // ROWS rows at a time in a workgroup of ROWS * THREADS lanes (ROWS > 1 only where a wavefront has a row alone)
-template <class T, class R, int THREADS, int NV>
+template <class T, class R, int MODE, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS >= 256 ? THREADS : 256) void norm_fwd(NormArgs a) {
   constexpr int ROWS = THREADS >= 256 ? 1 : 256 / THREADS;
   __shared__ float lds[2][THREADS >= 256 ? THREADS / 64 : 1];
   const bool branch = a.y, post = a.w_post, with_gate = a.gate, pre = a.n;
-  const int lane = threadIdx.x % THREADS;
+  const Lane<MODE, THREADS> l = {a.C, (int)threadIdx.x % THREADS};
   const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
   if (row >= a.rows) return;  // whole wavefronts; with one row a workgroup the grid ends with the rows
-  const T* y = static_cast<const T*>(a.y) + row * a.C;
-  const R* r = static_cast<const R*>(a.r) + row * a.C;
   typename Vec8<R>::V rv[NV];
   typename Vec8<T>::V yv[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int left = a.C - JZ_AT(i);
-    rv[i] = {};
-    if (left > 0) rv[i] = load8(r + JZ_AT(i), left);
-    if (branch) {
-      yv[i] = {};
-      if (left > 0) yv[i] = load8(y + JZ_AT(i), left);
-    }
+    rv[i] = l.load(static_cast<const R*>(a.r) + row * a.C, i);
+    yv[i] = {};
+    if (branch) yv[i] = l.load(static_cast<const T*>(a.y) + row * a.C, i);
   }
   f32x8 o[NV];
   if (branch) {
     float k1 = 1.f;
+    f32x8 w[NV];  // what y is multiplied by besides rstd
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      w[i] = splat8(a.branch_scale);
+      if (post) w[i] *= l.load(a.w_post, i);
+      if (with_gate) w[i] *= l.load(a.gate + row / a.rows_per_group * a.C, i);
+    }
     if (post) {
       float s = 0.f;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const f32x8 v = widen8<T>(yv[i]);
-        s += sum8(v * v);
+        s += l.sum(v * v, i);
       }
       k1 = 1.f / sqrtf(row_sum<THREADS>(s, lds[0]) * a.inv_c + a.eps);
-      if (lane == 0) a.rstd_post[row] = k1;
+      if (l.lane == 0) a.rstd_post[row] = k1;
     }
-    const float* gate = with_gate ? a.gate + row / a.rows_per_group * a.C : nullptr;
-    k1 *= a.branch_scale;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int left = a.C - JZ_AT(i);
-      f32x8 p = widen8<T>(yv[i]) * k1;
-      if (left > 0) {
-        if (post) p *= load8(a.w_post + JZ_AT(i), left);
-        if (with_gate) p *= load8(gate + JZ_AT(i), left);
-      }
-      o[i] = widen8<R>(rv[i]) * a.res_scale + p;
-      if (left > 0) store8(static_cast<R*>(a.r_out) + row * a.C + JZ_AT(i), narrow8<R>(o[i]), left);
+      o[i] = widen8<R>(rv[i]) * a.res_scale + widen8<T>(yv[i]) * k1 * w[i];
+      l.store(static_cast<R*>(a.r_out) + row * a.C, i, o[i]);
     }
   } else {
 #pragma unroll
     for (int i = 0; i < NV; ++i) o[i] = widen8<R>(rv[i]);
   }
   if (pre) {
+    f32x8 w[NV];
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) s += sum8(o[i] * o[i]);
-    const float k2 = 1.f / sqrtf(row_sum<THREADS>(s, lds[1]) * a.inv_c + a.eps);
-    if (lane == 0) a.rstd_pre[row] = k2;
-#pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int left = a.C - JZ_AT(i);
-      if (left > 0) store8(static_cast<T*>(a.n) + row * a.C + JZ_AT(i), narrow8<T>(o[i] * k2 * load8(a.w_pre + JZ_AT(i), left)), left);
+      w[i] = l.load(a.w_pre, i);
+      s += l.sum(o[i] * o[i], i);
     }
+    const float k2 = 1.f / sqrtf(row_sum<THREADS>(s, lds[1]) * a.inv_c + a.eps);
+    if (l.lane == 0) a.rstd_pre[row] = k2;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) l.store(static_cast<T*>(a.n) + row * a.C, i, o[i] * k2 * w[i]);
   }
 }
 
-// One workgroup of THREADS lanes takes the rows of a slab one after the other.
-template <class T, class R, int THREADS, int NV>
-__global__ __launch_bounds__(THREADS) void norm_bwd(NormArgs a) {
-  __shared__ float lds[4][THREADS / 64];
-  const bool branch = a.dy, post = a.w_post, with_gate = a.gate, pre = a.dn;
-  const int lane = threadIdx.x;
+// One workgroup of THREADS lanes takes the rows of a slab one after the other, the next row's loads ahead of a row's arithmetic; parameters and the sums over
+// rows stay in registers.  A row's two means need one meeting of its lanes, not two: with q = branch_scale gate w_post y^ and t = w_pre dn,
+//   c2 = mean(t r^),   c1 = mean(q R) = mean(q (dr_out + rstd_pre t)) - c2 mean(q rstd_pre r^)
+template <class T, class R, int MODE, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void norm_bwd(NormArgs a) {
+  constexpr int W = THREADS / 64;
+  // 1024 lanes have 128 registers each: no row is asked for ahead, the parameters are read for every row, and two of the three sums lie in LDS, every
+  // lane's in its own place
+  constexpr bool WIDE = THREADS == 1024;
+  __shared__ float lds[2][3][W];
+  __shared__ f32x4 wide[WIDE ? 2 * NV * 2 * THREADS : 1];
+  const bool branch = a.dy, post = a.w_post, with_gate = a.gate, pre = a.dn, arrives = a.dr_out;
+  const Lane<MODE, THREADS> l = {a.C, (int)threadIdx.x};
   const int64_t first = (int64_t)blockIdx.x * a.slab, last = first + a.slab < a.rows ? first + a.slab : a.rows;
-  f32x8 sum_pre[NV], sum_post[NV], sum_gate[NV];
+  f32x8 sum_pre[NV], sum_post[WIDE ? 1 : NV], sum_gate[WIDE ? 1 : NV];
+  auto sum = [&](bool gate, int i) -> f32x8 {
+    if constexpr (WIDE) {
+      const f32x4* at = wide + ((gate * NV + i) * 2) * THREADS + l.lane;
+      const f32x4 lo = at[0], hi = at[THREADS];
+      return f32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    } else {
+      return gate ? sum_gate[i] : sum_post[i];
+    }
+  };
+  auto put = [&](bool gate, int i, f32x8 v) {
+    if constexpr (WIDE) {
+      f32x4* at = wide + ((gate * NV + i) * 2) * THREADS + l.lane;
+      at[0] = f32x4{v[0], v[1], v[2], v[3]};
+      at[THREADS] = f32x4{v[4], v[5], v[6], v[7]};
+    } else if (gate) {
+      sum_gate[i] = v;
+    } else {
+      sum_post[i] = v;
+    }
+  };
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    sum_pre[i] = sum_post[i] = sum_gate[i] = splat8(0.f);
+    sum_pre[i] = splat8(0.f);
+    put(false, i, splat8(0.f));
+    put(true, i, splat8(0.f));
   }
   float* const part = a.part + (size_t)blockIdx.x * 4 * a.C;
   int64_t group = with_gate ? first / a.rows_per_group : 0;
-  for (int64_t row = first; row < last; ++row) {
-    const int turn = (int)(row - first) & 1;  // two sets of LDS cells: a row's sums are read while the next one's are written
-    const float k1 = post ? a.rstd_post[row] : 1.f, k2 = pre ? a.rstd_pre[row] : 0.f;
-    typename Vec8<R>::V tv[NV], ov[NV];
-    typename Vec8<T>::V dv[NV], yv[NV];
+
+  struct Row {
+    typename Vec8<R>::V t[NV], o[NV];
+    typename Vec8<T>::V d[NV], y[NV];
+    float k1, k2;
+  } next, now;
+  auto ask = [&](Row& v, int64_t row) {
+    v.k1 = post ? a.rstd_post[row] : 1.f;
+    v.k2 = pre ? a.rstd_pre[row] : 0.f;
+    const int64_t at = row * a.C;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int left = a.C - JZ_AT(i);
-      tv[i] = {};
-      ov[i] = {};
-      dv[i] = {};
-      yv[i] = {};
-      if (left > 0) {
-        const int64_t at = row * a.C + JZ_AT(i);
-        if (a.dr_out) tv[i] = load8(static_cast<const R*>(a.dr_out) + at, left);
-        if (pre) {
-          ov[i] = load8(static_cast<const R*>(a.r_out) + at, left);
-          dv[i] = load8(static_cast<const T*>(a.dn) + at, left);
-        }
-        if (post || with_gate) yv[i] = load8(static_cast<const T*>(a.y) + at, left);
-      }
-    }
-    float c2 = 0.f;
-    if (pre) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int left = a.C - JZ_AT(i);
-        const f32x8 t = widen8<T>(dv[i]) * (widen8<R>(ov[i]) * k2);  // dn rhat
-        sum_pre[i] += t;
-        if (left > 0) c2 += sum8(t * load8(a.w_pre + JZ_AT(i), left));
-      }
-      c2 = row_sum<THREADS>(c2, lds[turn]) * a.inv_c;
-    }
-    f32x8 e[NV];
-    float c1 = 0.f;
-    const float* gate = with_gate ? a.gate + group * a.C : nullptr;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int left = a.C - JZ_AT(i);
-      f32x8 total = widen8<R>(tv[i]);
+      v.t[i] = v.o[i] = {};
+      v.d[i] = v.y[i] = {};
+      if (arrives) v.t[i] = l.load(static_cast<const R*>(a.dr_out) + at, i);
       if (pre) {
-        const f32x8 w = left > 0 ? f32x8(load8(a.w_pre + JZ_AT(i), left)) : splat8(0.f);
-        total += (widen8<T>(dv[i]) * w - widen8<R>(ov[i]) * (k2 * c2)) * k2;
+        v.o[i] = l.load(static_cast<const R*>(a.r_out) + at, i);
+        v.d[i] = l.load(static_cast<const T*>(a.dn) + at, i);
       }
-      if (left > 0) store8(static_cast<R*>(a.dr) + row * a.C + JZ_AT(i), narrow8<R>(total * a.res_scale), left);
-      if (branch) {
-        f32x8 b = total * a.branch_scale, yh = widen8<T>(yv[i]) * k1;
-        if (with_gate) {
-          f32x8 q = yh * b;
-          if (post)
-            if (left > 0) q *= load8(a.w_post + JZ_AT(i), left);
-          sum_gate[i] += q;
-          if (left > 0) b *= load8(gate + JZ_AT(i), left);
-        }
-        if (post) {
-          sum_post[i] += b * yh;
-          if (left > 0) b *= load8(a.w_post + JZ_AT(i), left);
-          c1 += sum8(b * yh);
-        }
-        e[i] = b;
+      if (post || with_gate) v.y[i] = l.load(static_cast<const T*>(a.y) + at, i);
+    }
+  };
+  f32x8 w_pre[WIDE ? 1 : NV], w_post[WIDE ? 1 : NV], w_gate[WIDE ? 1 : NV];
+  auto parameter = [&](const float* from, int i) -> f32x8 { return from ? f32x8(l.load(from, i)) : splat8(1.f); };
+  auto gate_row = [&]() { return with_gate ? a.gate + group * a.C : nullptr; };
+  auto pre_of = [&](int i) -> f32x8 { return WIDE ? parameter(pre ? a.w_pre : nullptr, i) : w_pre[WIDE ? 0 : i]; };
+  auto post_of = [&](int i) -> f32x8 { return WIDE ? parameter(a.w_post, i) : w_post[WIDE ? 0 : i]; };
+  auto gate_of = [&](int i) -> f32x8 { return WIDE ? parameter(gate_row(), i) * a.branch_scale : w_gate[WIDE ? 0 : i]; };
+  if (!WIDE && first < last) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      w_pre[WIDE ? 0 : i] = parameter(pre ? a.w_pre : nullptr, i);
+      w_post[WIDE ? 0 : i] = parameter(a.w_post, i);
+      w_gate[WIDE ? 0 : i] = parameter(gate_row(), i) * a.branch_scale;
+    }
+    ask(next, first);
+  }
+  for (int64_t row = first; row < last; ++row) {
+    if constexpr (WIDE) {
+      ask(now, row);
+    } else {
+      now = next;
+      ask(next, row + 1 < last ? row + 1 : row);
+    }
+    const float k1 = now.k1, k2 = now.k2;
+    float s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const f32x8 hat = widen8<R>(now.o[i]) * k2, d = widen8<T>(now.d[i]);
+      f32x8 t = splat8(0.f);
+      if (pre) {
+        sum_pre[i] += d * hat;
+        t = d * pre_of(i);
+        s1 += l.sum(t * hat, i);
+      }
+      if (post) {
+        const f32x8 u = gate_of(i) * post_of(i) * (widen8<T>(now.y[i]) * k1);
+        s2 += l.sum(u * (widen8<R>(now.t[i]) + t * k2), i);
+        s3 += l.sum(u * hat, i);
       }
     }
-    if (branch) {
-      if (post) c1 = row_sum<THREADS>(c1, lds[2 + turn]) * a.inv_c;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int left = a.C - JZ_AT(i);
-        f32x8 d = e[i];
-        if (post) d = (d - widen8<T>(yv[i]) * (k1 * c1)) * k1;
-        if (left > 0) store8(static_cast<T*>(a.dy) + row * a.C + JZ_AT(i), narrow8<T>(d), left);
+    for (int m = 32; m > 0; m >>= 1) {
+      s1 += __shfl_xor(s1, m);
+      s2 += __shfl_xor(s2, m);
+      s3 += __shfl_xor(s3, m);
+    }
+    if constexpr (W > 1) {
+      float(*cell)[W] = lds[(int)(row - first) & 1];  // two sets: a row's sums are read while the next one's are written
+      if ((l.lane & 63) == 0) {
+        cell[0][l.lane >> 6] = s1;
+        cell[1][l.lane >> 6] = s2;
+        cell[2][l.lane >> 6] = s3;
+      }
+      // the wavefronts meet over LDS alone: the next row's loads stay on their way
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+      s1 = cell[0][0];
+      s2 = cell[1][0];
+      s3 = cell[2][0];
+#pragma unroll
+      for (int i = 1; i < W; ++i) {
+        s1 += cell[0][i];
+        s2 += cell[1][i];
+        s3 += cell[2][i];
+      }
+    }
+    const float c2 = s1 * a.inv_c, c1 = (s2 - c2 * (s3 * k2)) * a.inv_c;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int64_t at = row * a.C;
+      const f32x8 hat = widen8<R>(now.o[i]) * k2, yh = widen8<T>(now.y[i]) * k1;
+      f32x8 total = widen8<R>(now.t[i]);
+      if (pre) total += (widen8<T>(now.d[i]) * pre_of(i) - hat * c2) * k2;
+      l.store(static_cast<R*>(a.dr) + at, i, total * a.res_scale);
+      if (branch) {
+        if (with_gate) put(true, i, sum(true, i) + yh * post_of(i) * (total * a.branch_scale));
+        f32x8 e = gate_of(i) * total;
+        if (post) {
+          put(false, i, sum(false, i) + e * yh);
+          e = (e * post_of(i) - yh * c1) * k1;
+        }
+        l.store(static_cast<T*>(a.dy) + at, i, e);
       }
     }
     if (with_gate) {
@@ -212,29 +305,31 @@ __global__ __launch_bounds__(THREADS) void norm_bwd(NormArgs a) {
       if (row + 1 == end || row + 1 == last) {  // the group or the slab ends: whole groups are done, others go to the workspace
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-          const int left = a.C - JZ_AT(i);
-          if (left > 0) {
-            if (begin >= first && end <= last) store8(static_cast<T*>(a.dgate) + group * a.C + JZ_AT(i), narrow8<T>(sum_gate[i]), left);
-            else store8(part + (begin < first ? 2 : 3) * a.C + JZ_AT(i), typename Vec8<float>::V(sum_gate[i]), left);
-          }
-          sum_gate[i] = splat8(0.f);
+          if (begin >= first && end <= last) l.store(static_cast<T*>(a.dgate) + group * a.C, i, sum(true, i));
+          else l.store(part + (begin < first ? 2 : 3) * a.C, i, sum(true, i));
+          put(true, i, splat8(0.f));
         }
-        if (row + 1 == end) ++group;
+        if (row + 1 == end && row + 1 < last) {
+          ++group;
+          if constexpr (!WIDE) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) w_gate[i] = parameter(gate_row(), i) * a.branch_scale;
+          }
+        }
       }
     }
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int left = a.C - JZ_AT(i);
-    if (left <= 0) continue;
-    if (pre) store8(part + JZ_AT(i), sum_pre[i], left);
-    if (post) store8(part + a.C + JZ_AT(i), sum_post[i], left);
+    if (pre) l.store(part, i, sum_pre[i]);
+    if (post) l.store(part + a.C, i, sum(false, i));
   }
 }
 
-// Adds the slabs' sums up in the order of the rows: 64 columns a workgroup, its four wavefronts take a quarter of the slabs each.
+// Adds the slabs' sums up in the order of the rows: 64 columns a workgroup, its sixteen wavefronts take a sixteenth of the slabs each, eight
+// loads at a time.
 // blockIdx.y: 0 dw_pre, 1 dw_post, from 2 on the gate's groups that cross a slab's end, by group or, where those are more, by slab.
-constexpr int JOIN_WAVES = 4;
+constexpr int JOIN_WAVES = 16;
 template <class T>
 __global__ __launch_bounds__(64 * JOIN_WAVES) void norm_join(NormArgs a, int64_t groups, int by_slab) {
   __shared__ float lds[JOIN_WAVES][64];
@@ -266,11 +361,27 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void norm_join(NormArgs a, int64_t
   float s = 0.f;
   if (col < a.C) {
     const int64_t each = (to - from + JOIN_WAVES - 1) / JOIN_WAVES, lo = from + wave * each, hi = lo + each < to ? lo + each : to;
-    for (int64_t k = lo; k < hi; ++k) s += a.part[((size_t)k * 4 + (what < 2 ? what : k == from ? 3 : 2)) * a.C + col];
+    const float* at = a.part + (what < 2 ? what : 2) * a.C + col;
+    const size_t pitch = (size_t)4 * a.C;
+    int64_t k = lo;
+    if (what >= 2 && k == from && k < hi) s = at[k++ * pitch + a.C];
+    for (; k + 8 <= hi; k += 8) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = at[(k + i) * pitch];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += v[i];
+    }
+    for (; k < hi; ++k) s += at[k * pitch];
   }
   lds[wave][lane] = s;
   __syncthreads();
-  if (wave == 0 && col < a.C) static_cast<T*>(out)[col] = (T)((lds[0][lane] + lds[1][lane]) + (lds[2][lane] + lds[3][lane]));
+  if (wave == 0 && col < a.C) {
+    s = lds[0][lane];
+#pragma unroll
+    for (int i = 1; i < JOIN_WAVES; ++i) s += lds[i][lane];
+    static_cast<T*>(out)[col] = (T)s;
+  }
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------
@@ -330,16 +441,29 @@ void with_types(const jz_norm_residual_desc* d, F&& f) {
 }
 template <int N>
 using Int = std::integral_constant<int, N>;
-// Lanes that share a row, and vectors of eight elements a lane: a wavefront alone up to 1024 channels (no barrier), more lanes
-// above, so that a lane keeps at most 16 elements of every tensor in registers.
-template <class F>
+// f(mode, lanes that share a row, vectors of eight elements a lane).  Forward a wavefront alone up to 1024 channels (no barrier), more lanes above, so that a lane
+// keeps at most 16 elements of every tensor in registers.  Backward, where a lane also keeps parameters, their gradients and the next row, eight (up to 8192).
+template <bool FORWARD, class F>
 void with_lanes(int channels, F&& f) {
-  if (channels <= 512) f(Int<64>(), Int<1>());
-  else if (channels <= 1024) f(Int<64>(), Int<2>());
-  else if (channels <= 2048) f(Int<256>(), Int<1>());
-  else if (channels <= 4096) f(Int<256>(), Int<2>());
-  else if (channels <= 8192) f(Int<512>(), Int<2>());
-  else f(Int<1024>(), Int<2>());
+  auto sized = [&](auto mode) {
+    if (channels <= 512) f(mode, Int<64>(), Int<1>());
+    else if constexpr (FORWARD) {
+      if (channels <= 1024) f(mode, Int<64>(), Int<2>());
+      else if (channels <= 2048) f(mode, Int<256>(), Int<1>());
+      else if (channels <= 4096) f(mode, Int<256>(), Int<2>());
+      else if (channels <= 8192) f(mode, Int<512>(), Int<2>());
+      else f(mode, Int<1024>(), Int<2>());
+    } else {
+      if (channels <= 1024) f(mode, Int<128>(), Int<1>());
+      else if (channels <= 2048) f(mode, Int<256>(), Int<1>());
+      else if (channels <= 4096) f(mode, Int<512>(), Int<1>());
+      else if (channels <= 8192) f(mode, Int<1024>(), Int<1>());
+      else f(mode, Int<1024>(), Int<2>());
+    }
+  };
+  if (channels < 8) f(Int<TINY>(), Int<64>(), Int<1>());
+  else if (channels % 8) sized(Int<RAGGED>());
+  else sized(Int<EVEN>());
 }
 
 }  // namespace
@@ -363,9 +487,9 @@ extern "C" int jz_norm_residual_fwd(const jz_norm_residual_desc* d, const void* 
   a.r_out = r_out; a.n = n; a.rstd_post = rstd_post; a.rstd_pre = rstd_pre;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   with_types(d, [&](auto te, auto re) {
-    with_lanes(d->channels, [&](auto th, auto nv) {
+    with_lanes<true>(d->channels, [&](auto mode, auto th, auto nv) {
       constexpr int TH = decltype(th)::value, ROWS = TH >= 256 ? 1 : 256 / TH;
-      norm_fwd<decltype(te), decltype(re), TH, decltype(nv)::value><<<(unsigned)((a.rows + ROWS - 1) / ROWS), TH >= 256 ? TH : 256, 0, st>>>(a);
+      norm_fwd<decltype(te), decltype(re), decltype(mode)::value, TH, decltype(nv)::value><<<(unsigned)((a.rows + ROWS - 1) / ROWS), TH >= 256 ? TH : 256, 0, st>>>(a);
     });
   });
   return jz::launch_status();
@@ -411,8 +535,8 @@ extern "C" int jz_norm_residual_bwd(const jz_norm_residual_desc* d, const void* 
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (rows) {
     with_types(d, [&](auto te, auto re) {
-      with_lanes(d->channels, [&](auto th, auto nv) {
-        norm_bwd<decltype(te), decltype(re), decltype(th)::value, decltype(nv)::value><<<(unsigned)a.slabs, decltype(th)::value, 0, st>>>(a);
+      with_lanes<false>(d->channels, [&](auto mode, auto th, auto nv) {
+        norm_bwd<decltype(te), decltype(re), decltype(mode)::value, decltype(th)::value, decltype(nv)::value><<<(unsigned)a.slabs, decltype(th)::value, 0, st>>>(a);
       });
     });
     if (jz::launch_status() != JZ_OK) return JZ_ERR_LAUNCH;
