@@ -20,6 +20,7 @@ namespace {
 
 struct NormArgs {
   int64_t rows, rows_per_group, slab;
+  int64_t step;  // backward: from one of a slab's rows to the next
   int C;
   float eps, res_scale, branch_scale, inv_c;
   const void *r, *y;
@@ -56,6 +57,7 @@ __device__ __forceinline__ f32x8 splat8(float v) { return f32x8{v, v, v, v, v, v
 // out of the sums.  (What a lane then stores a second time are the bits that their owner stores.)
 //   EVEN   channels are a multiple of 8: a vector is a lane's own or nobody's        RAGGED   others from 8 on: the last vector overlaps its neighbour
 //   TINY   less than 8: one vector, element by element
+#define JZ_GLOBAL __attribute__((address_space(1)))
 enum { EVEN = 0, RAGGED = 1, TINY = 2 };
 template <int MODE, int THREADS>
 struct Lane {
@@ -70,14 +72,20 @@ struct Lane {
       if (on(i)) v = load8(row + own(i), C - own(i));
       return v;
     } else {
-      return load8(row + at(i));
+      // one address a wavefront and 32-bit offsets a lane: registers are short backward
+      const JZ_GLOBAL char* base = (const JZ_GLOBAL char*)row;
+      return *reinterpret_cast<const JZ_GLOBAL typename Vec8<T>::U*>(base + (unsigned)at(i) * (unsigned)sizeof(T));
     }
   }
   template <class T>
   __device__ __forceinline__ void store(T* row, int i, f32x8 v) const {
     if (!on(i)) return;
-    if constexpr (MODE == TINY) store8(row + own(i), narrow8<T>(v), C - own(i));
-    else store8(row + at(i), narrow8<T>(v));
+    if constexpr (MODE == TINY) {
+      store8(row + own(i), narrow8<T>(v), C - own(i));
+    } else {
+      JZ_GLOBAL char* base = (JZ_GLOBAL char*)row;
+      *reinterpret_cast<JZ_GLOBAL typename Vec8<T>::U*>(base + (unsigned)at(i) * (unsigned)sizeof(T)) = narrow8<T>(v);
+    }
   }
   __device__ __forceinline__ float sum(f32x8 v, int i) const {
     if constexpr (MODE == RAGGED) {
@@ -154,37 +162,41 @@ __global__ __launch_bounds__(THREADS >= 256 ? THREADS : 256) void norm_fwd(NormA
 // One workgroup of THREADS lanes takes the rows of a slab one after the other, the next row's loads ahead of a row's arithmetic; parameters and the sums over
 // rows stay in registers.  A row's two means need one meeting of its lanes, not two: with q = branch_scale gate w_post y^ and t = w_pre dn,
 //   c2 = mean(t r^),   c1 = mean(q R) = mean(q (dr_out + rstd_pre t)) - c2 mean(q rstd_pre r^)
-template <class T, class R, int MODE, int THREADS, int NV>
+// HAS: which tensors the call has, where that is usual.  A load in a branch keeps the compiler from counting the loads on their way, and a row would wait for the next one's.
+enum { ANY = 0, BLOCK = 1, SUM = 2 };  // BLOCK: dn, dr_out and y (a post-norm or a gate); SUM: dn and dr_out, y is not needed
+template <class T, class R, int MODE, int THREADS, int NV, int HAS>
 __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void norm_bwd(NormArgs a) {
   constexpr int W = THREADS / 64;
-  // 1024 lanes have 128 registers each: no row is asked for ahead, the parameters are read for every row, and two of the three sums lie in LDS, every
-  // lane's in its own place
-  constexpr bool WIDE = THREADS == 1024;
+  // 1024 lanes have 128 registers each: two of the three sums and of the three parameters lie in LDS, every lane's in its own place, and no row is asked for
+  // ahead; above 8192 channels, where LDS is full, the parameters are read for every row.
+  constexpr bool WIDE = THREADS == 1024, REREAD = WIDE && NV > 1, KEPT = WIDE && !REREAD;
   __shared__ float lds[2][3][W];
-  __shared__ f32x4 wide[WIDE ? 2 * NV * 2 * THREADS : 1];
-  const bool branch = a.dy, post = a.w_post, with_gate = a.gate, pre = a.dn, arrives = a.dr_out;
+  __shared__ f32x4 wide[WIDE ? (KEPT ? 4 : 2) * NV * 2 * THREADS : 1];
+  const bool branch = HAS != ANY || a.dy, post = HAS != SUM && a.w_post, with_gate = HAS != SUM && a.gate, pre = HAS != ANY || a.dn, arrives = HAS != ANY || a.dr_out;
+  const bool needs_y = HAS == BLOCK || (HAS == ANY && (post || with_gate));
   const Lane<MODE, THREADS> l = {a.C, (int)threadIdx.x};
-  const int64_t first = (int64_t)blockIdx.x * a.slab, last = first + a.slab < a.rows ? first + a.slab : a.rows;
+  // Rows first, first + step, ...: with one gate for all the slabs are interleaved, since slabs of consecutive rows lie so far apart that workgroups side by side would
+  // read the same few memory channels; with more, consecutive.
+  const int64_t first = a.step == 1 ? blockIdx.x * a.slab : blockIdx.x, end_of_slab = a.step == 1 && first + a.slab < a.rows ? first + a.slab : a.rows;
   f32x8 sum_pre[NV], sum_post[WIDE ? 1 : NV], sum_gate[WIDE ? 1 : NV];
+  auto from_lds = [&](int what, int i) {
+    const f32x4* at = wide + ((what * NV + i) * 2) * THREADS + l.lane;
+    const f32x4 lo = at[0], hi = at[THREADS];
+    return f32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  };
+  auto to_lds = [&](int what, int i, f32x8 v) {
+    f32x4* at = wide + ((what * NV + i) * 2) * THREADS + l.lane;
+    at[0] = f32x4{v[0], v[1], v[2], v[3]};
+    at[THREADS] = f32x4{v[4], v[5], v[6], v[7]};
+  };
   auto sum = [&](bool gate, int i) -> f32x8 {
-    if constexpr (WIDE) {
-      const f32x4* at = wide + ((gate * NV + i) * 2) * THREADS + l.lane;
-      const f32x4 lo = at[0], hi = at[THREADS];
-      return f32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    } else {
-      return gate ? sum_gate[i] : sum_post[i];
-    }
+    if constexpr (WIDE) return from_lds(gate, i);
+    else return gate ? sum_gate[i] : sum_post[i];
   };
   auto put = [&](bool gate, int i, f32x8 v) {
-    if constexpr (WIDE) {
-      f32x4* at = wide + ((gate * NV + i) * 2) * THREADS + l.lane;
-      at[0] = f32x4{v[0], v[1], v[2], v[3]};
-      at[THREADS] = f32x4{v[4], v[5], v[6], v[7]};
-    } else if (gate) {
-      sum_gate[i] = v;
-    } else {
-      sum_post[i] = v;
-    }
+    if constexpr (WIDE) to_lds(gate, i, v);
+    else if (gate) sum_gate[i] = v;
+    else sum_post[i] = v;
   };
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -201,7 +213,8 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void norm_bwd(Nor
     float k1, k2;
   } next, now;
   auto ask = [&](Row& v, int64_t row) {
-    v.k1 = post ? a.rstd_post[row] : 1.f;
+    if constexpr (HAS == ANY) v.k1 = post ? a.rstd_post[row] : 1.f;
+    else v.k1 = *(post ? a.rstd_post + row : a.rstd_pre + row);  // read and put away without a post-norm
     v.k2 = pre ? a.rstd_pre[row] : 0.f;
     const int64_t at = row * a.C;
 #pragma unroll
@@ -213,32 +226,39 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void norm_bwd(Nor
         v.o[i] = l.load(static_cast<const R*>(a.r_out) + at, i);
         v.d[i] = l.load(static_cast<const T*>(a.dn) + at, i);
       }
-      if (post || with_gate) v.y[i] = l.load(static_cast<const T*>(a.y) + at, i);
+      if (needs_y) v.y[i] = l.load(static_cast<const T*>(a.y) + at, i);
     }
   };
-  f32x8 w_pre[WIDE ? 1 : NV], w_post[WIDE ? 1 : NV], w_gate[WIDE ? 1 : NV];
+  f32x8 w_pre[REREAD ? 1 : NV], w_post[WIDE ? 1 : NV], w_gate[WIDE ? 1 : NV];
   auto parameter = [&](const float* from, int i) -> f32x8 { return from ? f32x8(l.load(from, i)) : splat8(1.f); };
-  auto gate_row = [&]() { return with_gate ? a.gate + group * a.C : nullptr; };
-  auto pre_of = [&](int i) -> f32x8 { return WIDE ? parameter(pre ? a.w_pre : nullptr, i) : w_pre[WIDE ? 0 : i]; };
-  auto post_of = [&](int i) -> f32x8 { return WIDE ? parameter(a.w_post, i) : w_post[WIDE ? 0 : i]; };
-  auto gate_of = [&](int i) -> f32x8 { return WIDE ? parameter(gate_row(), i) * a.branch_scale : w_gate[WIDE ? 0 : i]; };
-  if (!WIDE && first < last) {
+  auto gate_row = [&](int i) -> f32x8 { return parameter(with_gate ? a.gate + group * a.C : nullptr, i) * a.branch_scale; };
+  auto pre_of = [&](int i) -> f32x8 { return REREAD ? parameter(pre ? a.w_pre : nullptr, i) : w_pre[REREAD ? 0 : i]; };
+  auto post_of = [&](int i) -> f32x8 { return REREAD ? parameter(a.w_post, i) : KEPT ? from_lds(2, i) : w_post[WIDE ? 0 : i]; };
+  auto gate_of = [&](int i) -> f32x8 { return REREAD ? gate_row(i) : KEPT ? from_lds(3, i) : w_gate[WIDE ? 0 : i]; };
+  auto keep_gate = [&](int i) {
+    if constexpr (KEPT) to_lds(3, i, gate_row(i));
+    else if constexpr (!REREAD) w_gate[i] = gate_row(i);
+  };
+  if (!REREAD && first < end_of_slab) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      w_pre[WIDE ? 0 : i] = parameter(pre ? a.w_pre : nullptr, i);
-      w_post[WIDE ? 0 : i] = parameter(a.w_post, i);
-      w_gate[WIDE ? 0 : i] = parameter(gate_row(), i) * a.branch_scale;
+      w_pre[REREAD ? 0 : i] = parameter(pre ? a.w_pre : nullptr, i);
+      if constexpr (KEPT) to_lds(2, i, parameter(a.w_post, i));
+      else w_post[WIDE ? 0 : i] = parameter(a.w_post, i);
+      keep_gate(i);
     }
-    ask(next, first);
   }
-  for (int64_t row = first; row < last; ++row) {
+  if (!WIDE && first < end_of_slab) ask(next, first);
+  int turn = 0;
+  for (int64_t row = first; row < end_of_slab; row += a.step, turn ^= 1) {
+    const bool last = row + a.step >= end_of_slab;
     if constexpr (WIDE) {
       ask(now, row);
     } else {
       now = next;
-      ask(next, row + 1 < last ? row + 1 : row);
+      ask(next, last ? row : row + a.step);
     }
-    const float k1 = now.k1, k2 = now.k2;
+    const float k1 = post ? now.k1 : 1.f, k2 = now.k2;
     float s1 = 0.f, s2 = 0.f, s3 = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -262,7 +282,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void norm_bwd(Nor
       s3 += __shfl_xor(s3, m);
     }
     if constexpr (W > 1) {
-      float(*cell)[W] = lds[(int)(row - first) & 1];  // two sets: a row's sums are read while the next one's are written
+      float(*cell)[W] = lds[turn];  // two sets: a row's sums are read while the next one's are written
       if ((l.lane & 63) == 0) {
         cell[0][l.lane >> 6] = s1;
         cell[1][l.lane >> 6] = s2;
@@ -302,19 +322,18 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void norm_bwd(Nor
     }
     if (with_gate) {
       const int64_t begin = group * a.rows_per_group, end = begin + a.rows_per_group;
-      if (row + 1 == end || row + 1 == last) {  // the group or the slab ends: whole groups are done, others go to the workspace
+      if (row + 1 == end || last) {  // the group or the slab ends: whole groups are done, others go to the workspace
+        const bool whole = a.step == 1 ? begin >= first && end <= end_of_slab : gridDim.x == 1, began = a.step == 1 ? begin < first : blockIdx.x > 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-          if (begin >= first && end <= last) l.store(static_cast<T*>(a.dgate) + group * a.C, i, sum(true, i));
-          else l.store(part + (begin < first ? 2 : 3) * a.C, i, sum(true, i));
+          if (whole) l.store(static_cast<T*>(a.dgate) + group * a.C, i, sum(true, i));
+          else l.store(part + (began ? 2 : 3) * a.C, i, sum(true, i));
           put(true, i, splat8(0.f));
         }
-        if (row + 1 == end && row + 1 < last) {
+        if (!last) {
           ++group;
-          if constexpr (!WIDE) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) w_gate[i] = parameter(gate_row(), i) * a.branch_scale;
-          }
+          for (int i = 0; i < NV; ++i) keep_gate(i);
         }
       }
     }
@@ -386,7 +405,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void norm_join(NormArgs a, int64_t
 
 // ---- host ---------------------------------------------------------------------------------------------------------------
 constexpr int NORM_MAX_C = 16384;
-constexpr int NORM_SLABS = 512;  // at most
+constexpr int NORM_SLABS = 512;  // at most; half as many where a workgroup of the backward pass fills a compute unit
 
 struct Tensor {
   const void* p;
@@ -416,8 +435,11 @@ int norm_shape(const jz_norm_residual_desc* d, int64_t* groups, int64_t* per) {
   return JZ_OK;
 }
 // A slab's sums are 16 bytes a channel; slabs of at least 8 rows, so that they are a small part of what moves.
-int64_t slab_rows(int64_t rows) { return std::max<int64_t>(8, (rows + NORM_SLABS - 1) / NORM_SLABS); }
-int slab_count(int64_t rows) { return (int)((rows + slab_rows(rows) - 1) / slab_rows(rows)); }
+int64_t slab_rows(int64_t rows, int channels) {
+  const int most = channels > 2048 ? NORM_SLABS / 2 : NORM_SLABS;
+  return std::max<int64_t>(8, (rows + most - 1) / most);
+}
+int slab_count(int64_t rows, int channels) { return (int)((rows + slab_rows(rows, channels) - 1) / slab_rows(rows, channels)); }
 
 NormArgs norm_args(const jz_norm_residual_desc* d, int64_t per) {
   NormArgs a = {};
@@ -499,7 +521,7 @@ extern "C" int jz_norm_residual_bwd_workspace_bytes(const jz_norm_residual_desc*
   if (!bytes) return JZ_ERR_NULL;
   int64_t groups, per;
   const int rc = norm_shape(d, &groups, &per);
-  if (rc == JZ_OK) *bytes = (size_t)slab_count(d->rows) * 4 * d->channels * sizeof(float);
+  if (rc == JZ_OK) *bytes = (size_t)slab_count(d->rows, d->channels) * 4 * d->channels * sizeof(float);
   return rc;
 }
 
@@ -513,7 +535,7 @@ extern "C" int jz_norm_residual_bwd(const jz_norm_residual_desc* d, const void* 
   if ((post && !dw_post) || (gate && !dgate) || (pre && (!dw_pre || !w_pre))) return JZ_ERR_NULL;
   if (rows && (!dr || (!pre && !dr_out) || ((post || gate) && !branch) || (branch && (post || gate) && !y) || (!branch && !pre) || (post && !rstd_post) || (pre && (!r_out || !rstd_pre))))
     return JZ_ERR_NULL;
-  const size_t need = (size_t)slab_count(d->rows) * 4 * d->channels * sizeof(float);
+  const size_t need = (size_t)slab_count(d->rows, d->channels) * 4 * d->channels * sizeof(float);
   if (need && (!ws || ws_bytes < need)) return JZ_ERR_WORKSPACE;
   if (need && !jz::aligned16(ws)) return JZ_ERR_ALIGN;
   const size_t e = (size_t)d->rows * d->channels, tb = d->dtype == JZ_F32 ? 4 : 2, rb = d->res_dtype == JZ_F32 ? 4 : 2, c4 = (size_t)d->channels * 4;
@@ -530,13 +552,19 @@ extern "C" int jz_norm_residual_bwd(const jz_norm_residual_desc* d, const void* 
   a.dr_out = dr_out; a.dn = dn; a.dr = dr; a.dy = dy;
   a.dw_post = post ? dw_post : nullptr; a.dgate = gate ? dgate : nullptr; a.dw_pre = pre ? dw_pre : nullptr;
   a.part = static_cast<float*>(ws);
-  a.slab = slab_rows(d->rows);
-  a.slabs = slab_count(d->rows);
+  a.slab = slab_rows(d->rows, d->channels);
+  a.slabs = slab_count(d->rows, d->channels);
+  a.step = groups == 1 ? std::max(a.slabs, 1) : 1;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (rows) {
     with_types(d, [&](auto te, auto re) {
       with_lanes<false>(d->channels, [&](auto mode, auto th, auto nv) {
-        norm_bwd<decltype(te), decltype(re), decltype(mode)::value, decltype(th)::value, decltype(nv)::value><<<(unsigned)a.slabs, decltype(th)::value, 0, st>>>(a);
+        constexpr int M = decltype(mode)::value, TH = decltype(th)::value, NV = decltype(nv)::value;
+        auto launch = [&](auto has) { norm_bwd<decltype(te), decltype(re), M, TH, NV, decltype(has)::value><<<(unsigned)a.slabs, TH, 0, st>>>(a); };
+        if constexpr (M != TINY && TH < 1024) {  // those that ask ahead
+          if (pre && dr_out && branch) return post || gate ? launch(Int<BLOCK>()) : launch(Int<SUM>());
+        }
+        launch(Int<ANY>());
       });
     });
     if (jz::launch_status() != JZ_OK) return JZ_ERR_LAUNCH;
