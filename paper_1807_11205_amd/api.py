@@ -898,6 +898,13 @@ def jz_conv2d_bwd_data_block_end_bwd(desc, dy16, w16, dyb16, bn_x16, y_out16, ga
 # ---------------------------------------------------------------------------------------------
 # residual blocks: clipping by the global norm, norms around a block, gated feed-forward block
 # ---------------------------------------------------------------------------------------------
+def _invoke(name: str, words, stream):
+    """An entry point called with integers and addresses (None: NULL) by the binding's native part."""
+    st = _host.invoke(_address(name), tuple(w or 0 for w in words), _stream(stream))
+    if st:      # JZ_OK is 0
+        raise JzError(st, name)
+
+
 _DTYPES = {torch.float16: JZ_F16, torch.bfloat16: JZ_BF16, torch.float32: JZ_F32}
 _TORCH_TYPES = (torch.float16, torch.bfloat16, torch.float32)
 
@@ -973,10 +980,10 @@ def jz_norm_residual_fwd(desc, r, y, w_post, gate, w_pre, r_out, n, rstd_post=No
     the sum alone; w_post None: y as it is; gate None: 1."""
     t, rt, e, groups = _norm_types(desc)
     C, f = desc.channels, torch.float32
-    _check(lib().jz_norm_residual_fwd(ctypes.byref(desc), _dev_ptr(r, rt, e, "r"), _dev_ptr(y, t, e, "y"), _dev_ptr(w_post, f, C, "w_post"),
+    _invoke("jz_norm_residual_fwd", (ctypes.addressof(desc), _dev_ptr(r, rt, e, "r"), _dev_ptr(y, t, e, "y"), _dev_ptr(w_post, f, C, "w_post"),
                                       _dev_ptr(gate, f, groups * C, "gate"), _dev_ptr(w_pre, f, C, "w_pre"), _dev_ptr(r_out, rt, e, "r_out"),
                                       _dev_ptr(n, t, e, "n"), _dev_ptr(rstd_post, f, desc.rows, "rstd_post"),
-                                      _dev_ptr(rstd_pre, f, desc.rows, "rstd_pre"), _stream(stream)), "jz_norm_residual_fwd")
+                                      _dev_ptr(rstd_pre, f, desc.rows, "rstd_pre")), stream)
 
 
 def jz_norm_residual_bwd_workspace_bytes(desc) -> int:
@@ -990,12 +997,12 @@ def jz_norm_residual_bwd(desc, y, r_out, w_post, gate, w_pre, rstd_post, rstd_pr
     t, rt, e, groups = _norm_types(desc)
     C, f = desc.channels, torch.float32
     wp, wn = _ws(ws)
-    _check(lib().jz_norm_residual_bwd(ctypes.byref(desc), _dev_ptr(y, t, e, "y"), _dev_ptr(r_out, rt, e, "r_out"), _dev_ptr(w_post, f, C, "w_post"),
+    _invoke("jz_norm_residual_bwd", (ctypes.addressof(desc), _dev_ptr(y, t, e, "y"), _dev_ptr(r_out, rt, e, "r_out"), _dev_ptr(w_post, f, C, "w_post"),
                                       _dev_ptr(gate, f, groups * C, "gate"), _dev_ptr(w_pre, f, C, "w_pre"),
                                       _dev_ptr(rstd_post, f, desc.rows, "rstd_post"), _dev_ptr(rstd_pre, f, desc.rows, "rstd_pre"),
                                       _dev_ptr(dr_out, rt, e, "dr_out"), _dev_ptr(dn, t, e, "dn"), _dev_ptr(dr, rt, e, "dr"), _dev_ptr(dy, t, e, "dy"),
                                       _dev_ptr(dw_post, t, C, "dw_post"), _dev_ptr(dgate, t, groups * C, "dgate"), _dev_ptr(dw_pre, t, C, "dw_pre"),
-                                      wp, wn, _stream(stream)), "jz_norm_residual_bwd")
+                                      wp, wn), stream)
 
 
 def ffn_desc(rows: int, in_features: int, hidden: int, out_features: int, act: int = JZ_ACT_SILU, dtype: int = JZ_F16, x_stride: int = 0,
@@ -1036,9 +1043,9 @@ def jz_ffn_fwd(desc, x, w_gate, w_up, w_down, h, y, gate=None, up=None, ws=None,
     d, t = desc, _ffn_type(desc)
     M, D, F, O = d.rows, d.in_features, d.hidden, d.out_features
     wp, wn = _ws(ws)
-    _check(lib().jz_ffn_fwd(ctypes.byref(d), _rows_ptr(x, t, M, D, d.x_stride, "x"), _dev_ptr(w_gate, t, F * D, "w_gate"), _dev_ptr(w_up, t, F * D, "w_up"),
+    _invoke("jz_ffn_fwd", (ctypes.addressof(d), _rows_ptr(x, t, M, D, d.x_stride, "x"), _dev_ptr(w_gate, t, F * D, "w_gate"), _dev_ptr(w_up, t, F * D, "w_up"),
                             _dev_ptr(w_down, t, O * F, "w_down"), _dev_ptr(h, t, M * F, "h"), _dev_ptr(gate, t, M * F, "gate"), _dev_ptr(up, t, M * F, "up"),
-                            _rows_ptr(y, t, M, O, d.y_stride, "y"), wp, wn, _stream(stream)), "jz_ffn_fwd")
+                            _rows_ptr(y, t, M, O, d.y_stride, "y"), wp, wn), stream)
 
 
 def jz_ffn_bwd(desc, x, w_gate, w_up, w_down, gate, up, h, dy, dx, dw_gate, dw_up, dw_down, ws=None, stream=None):
@@ -1046,7 +1053,7 @@ def jz_ffn_bwd(desc, x, w_gate, w_up, w_down, gate, up, h, dy, dx, dw_gate, dw_u
     d, t = desc, _ffn_type(desc)
     M, D, F, O = d.rows, d.in_features, d.hidden, d.out_features
     wp, wn = _ws(ws)
-    _check(lib().jz_ffn_bwd(ctypes.byref(d), _rows_ptr(x, t, M, D, d.x_stride, "x"), _dev_ptr(w_gate, t, F * D, "w_gate"), _dev_ptr(w_up, t, F * D, "w_up"),
+    _invoke("jz_ffn_bwd", (ctypes.addressof(d), _rows_ptr(x, t, M, D, d.x_stride, "x"), _dev_ptr(w_gate, t, F * D, "w_gate"), _dev_ptr(w_up, t, F * D, "w_up"),
                             _dev_ptr(w_down, t, O * F, "w_down"), _dev_ptr(gate, t, M * F, "gate"), _dev_ptr(up, t, M * F, "up"), _dev_ptr(h, t, M * F, "h"),
                             _rows_ptr(dy, t, M, O, d.dy_stride, "dy"), _rows_ptr(dx, t, M, D, d.dx_stride, "dx"), _dev_ptr(dw_gate, t, F * D, "dw_gate"),
-                            _dev_ptr(dw_up, t, F * D, "dw_up"), _dev_ptr(dw_down, t, O * F, "dw_down"), wp, wn, _stream(stream)), "jz_ffn_bwd")
+                            _dev_ptr(dw_up, t, F * D, "dw_up"), _dev_ptr(dw_down, t, O * F, "dw_down"), wp, wn), stream)

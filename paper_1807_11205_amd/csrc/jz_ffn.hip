@@ -94,8 +94,9 @@ int64_t count_tiles(const GemmArgs& a, int epi, int tile) {
 size_t partial_bytes(const FfnPlan& p, int64_t tiles) { return p.splits > 1 ? (size_t)(tiles - p.full) * p.splits * p.tile * p.tile * 4 : 0; }
 
 template <class T, bool KCA, bool KCB, int EPI, int ACT>
-void launch_direct(const GemmArgs& a, int tile, unsigned grid, hipStream_t st) {
-  if (tile == 256) ffn_gemm<T, KCA, KCB, EPI, ACT, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
+void launch_tiles(const GemmArgs& a, int tile, unsigned grid, hipStream_t st) {
+  if (!direct<KCA, KCB>(a)) ffn_gemm_any<T, KCA, KCB, EPI, ACT, 128, 128><<<grid, 256, 0, st>>>(a);
+  else if (tile == 256) ffn_gemm<T, KCA, KCB, EPI, ACT, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
   else ffn_gemm<T, KCA, KCB, EPI, ACT, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
 }
 
@@ -110,12 +111,11 @@ int launch(GemmArgs a, const FfnPlan& plan, const Scratch& ws, hipStream_t st) {
   a.tiles_per_split = (int)((k_tiles(a) + plan.splits - 1) / plan.splits);
   a.partial = static_cast<float*>(ws.p);
   const unsigned grid = full + split * plan.splits;
-  if (!direct<KCA, KCB>(a)) ffn_gemm_any<T, KCA, KCB, EPI, 128, 128><<<grid, 256, 0, st>>>(a);
-  else if (EPI != EPI_GLU_BWD || a.act == 0) launch_direct<T, KCA, KCB, EPI, 0>(a, plan.tile, grid, st);
+  if (EPI != EPI_GLU_BWD || a.act == 0) launch_tiles<T, KCA, KCB, EPI, 0>(a, plan.tile, grid, st);
   else if constexpr (EPI == EPI_GLU_BWD) {
-    if (a.act == 1) launch_direct<T, KCA, KCB, EPI, 1>(a, plan.tile, grid, st);
-    else if (a.act == 2) launch_direct<T, KCA, KCB, EPI, 2>(a, plan.tile, grid, st);
-    else launch_direct<T, KCA, KCB, EPI, 3>(a, plan.tile, grid, st);
+    if (a.act == 1) launch_tiles<T, KCA, KCB, EPI, 1>(a, plan.tile, grid, st);
+    else if (a.act == 2) launch_tiles<T, KCA, KCB, EPI, 2>(a, plan.tile, grid, st);
+    else launch_tiles<T, KCA, KCB, EPI, 3>(a, plan.tile, grid, st);
   }
   if (jz::launch_status() != JZ_OK) return JZ_ERR_LAUNCH;
   if (split > 0) {

@@ -235,7 +235,7 @@ __device__ __forceinline__ void finish_tile(const GemmArgs& a, const Product& p,
   });
 }
 
-// The same for EPI_GLU_BWD, whose results need gate and up from memory: those of a strip are asked for a strip ahead.  Columns are a multiple of 8.
+// The same for EPI_GLU_BWD, whose results need gate and up from memory: those of a strip are asked for a strip ahead.
 template <class T, int ACT, int TM, int TN>
 __device__ __forceinline__ void finish_bwd(const GemmArgs& a, const Product& p, f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, JZ_LDS unsigned char* lds, int lane) {
   constexpr int PITCH = TN * 128, PER = TN * 4, EACH = 32 * PER / 64;
@@ -249,8 +249,10 @@ __device__ __forceinline__ void finish_bwd(const GemmArgs& a, const Product& p, 
   auto ask = [&](int x, int i) {
     int64_t m, n;
     if (!place(x, i, &m, &n)) return;
-    g[i] = load8(static_cast<const T*>(a.gate) + m * p.N + n);
-    u[i] = load8(static_cast<const T*>(a.up) + m * p.N + n);
+    const int64_t at = m * p.N + n;
+    const int left = at + 8 > p.M * p.N ? (int)(p.N - n) : 8;  // what follows a row's end is read and not stored; behind the last row there is nothing
+    g[i] = load8(static_cast<const T*>(a.gate) + at, left);
+    u[i] = load8(static_cast<const T*>(a.up) + at, left);
   };
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {
@@ -273,21 +275,51 @@ __device__ __forceinline__ void finish_bwd(const GemmArgs& a, const Product& p, 
       if constexpr (x + 1 < TM) ask(x + 1, i);
       int64_t m, n;
       if (place(x, i, &m, &n)) {
-        store8(static_cast<T*>(a.out0) + m * p.N + n, narrow8<T>(dg));
-        store8(static_cast<T*>(a.out1) + m * p.N + n, narrow8<T>(du));
+        const int left = p.N - n < 8 ? (int)(p.N - n) : 8;
+        store8(static_cast<T*>(a.out0) + m * p.N + n, narrow8<T>(dg), left);
+        store8(static_cast<T*>(a.out1) + m * p.N + n, narrow8<T>(du), left);
       }
     });
   });
 }
 
-// Any sizes, any alignment: the operands pass through registers on their way into LDS, element by element where a row ends.
-template <class T, bool KCA, bool KCB, int EPI, int BM, int BN>
-__global__ __launch_bounds__(256) void ffn_gemm_any(GemmArgs a) {
+template <class T, int EPI, int ACT, int TM, int TN>
+__device__ __forceinline__ void finish(const GemmArgs& a, const Product& p, f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, float* partial, int pitch,
+                                       JZ_LDS unsigned char* lds, int lane) {
+  if constexpr (EPI == EPI_GLU_BWD) {
+    if (partial) finish_tile<T, EPI_STORE>(a, p, acc, m0, n0, partial, pitch, lds, lane);
+    else finish_bwd<T, ACT>(a, p, acc, m0, n0, lds, lane);
+  } else {
+    finish_tile<T, EPI>(a, p, acc, m0, n0, partial, pitch, lds, lane);
+  }
+}
+
+// Any sizes, any alignment: the operands pass through registers on their way into LDS, the next tile's while a tile is multiplied.  Loads are full vectors without
+// branches (global memory takes them at any alignment), from where the element is or would be: rows outside are the last row, and what follows a row's end belongs to
+// no result, or to the end of the sum, where it is cleared.  Only the vectors that would pass the tensor's last element are loaded one by one.
+template <class T, bool KC>
+struct AnySource {
+  int64_t ld, rows, K;
+  __device__ __forceinline__ Op8<T> load(const T* p, int64_t row, int64_t k) const {
+    const int64_t r = row < rows ? row : rows - 1, kk = k < K ? k : K - 1, at = KC ? r * ld + kk : kk * ld + r;
+    const int64_t all = KC ? (rows - 1) * ld + K : (K - 1) * ld + rows;
+    if (at + 8 > all) return load8(p + at, (int)(KC ? K - kk : rows - r));  // less than eight to the row's end then
+    return load8(p + at);
+  }
+  __device__ __forceinline__ Op8<T> cleared(Op8<T> v, int64_t k) const {  // behind the end of the sum
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (KC ? k + e : k) < K ? v[e] : T(0.f);
+    return v;
+  }
+};
+
+// ACT: the activation where EPI is EPI_GLU_BWD, else 0
+template <class T, bool KCA, bool KCB, int EPI, int ACT, int BM, int BN>
+__global__ __launch_bounds__(256, 2) void ffn_gemm_any(GemmArgs a) {
   using SA = Staged<T, KCA, BM, 256>;
   using SB = Staged<T, KCB, BN, 256>;
   constexpr int TM = BM / 64, TN = BN / 64;
-  __shared__ __attribute__((aligned(1024))) unsigned char operands[SA::BYTES + SB::BYTES];
-  unsigned char *const sa = operands, *const sb = operands + SA::BYTES;
+  __shared__ __attribute__((aligned(1024))) unsigned char operands[2][SA::BYTES + SB::BYTES];
   static_assert(SA::BYTES + SB::BYTES >= 4 * 32 * TN * 128, "the results pass through LDS");
   const Tile w = find_tile(a);
   const Product p = a.p[w.product];
@@ -296,41 +328,46 @@ __global__ __launch_bounds__(256) void ffn_gemm_any(GemmArgs a) {
   const int per_part = (int)((p.K + BK - 1) / BK), all = per_part * a.parts;
   const int first = w.split < 0 ? 0 : w.split * a.tiles_per_split, last = w.split < 0 || first + a.tiles_per_split > all ? all : first + a.tiles_per_split;
   float* const partial = w.split < 0 ? nullptr : a.partial + ((size_t)w.behind * a.splits + w.split) * (BM * BN);
+  const AnySource<T, KCA> from_a = {p.lda, p.M, p.K};
+  const AnySource<T, KCB> from_b = {p.ldb, p.N, p.K};
 
   Op8<T> ra[SA::EACH], rb[SB::EACH];
   auto fetch = [&](int kt) {
     const int part = kt >= per_part;
     const int64_t k0 = (int64_t)(kt - part * per_part) * BK;
-    const T* pa = static_cast<const T*>(p.a[part]);
-    const T* pb = static_cast<const T*>(p.b[part]);
 #pragma unroll
     for (int i = 0; i < SA::EACH; ++i) {
       int row, k;
       SA::place(i, t, &row, &k);
-      const int64_t m = m0 + row, kk = k0 + k;
-      ra[i] = {};
-      if (m < p.M && kk < p.K) {
-        const int64_t left = KCA ? p.K - kk : p.M - m;
-        ra[i] = load8(KCA ? pa + m * p.lda + kk : pa + kk * p.lda + m, left < 8 ? (int)left : 8);
-      }
+      ra[i] = from_a.load(static_cast<const T*>(p.a[part]), m0 + row, k0 + k);
     }
 #pragma unroll
     for (int i = 0; i < SB::EACH; ++i) {
       int row, k;
       SB::place(i, t, &row, &k);
-      const T* pbb = pb;
-      int64_t n = n0 + row;
-      const int64_t kk = k0 + k;
-      if constexpr (EPI == EPI_GLU) {
-        pbb = static_cast<const T*>(p.b[(row >> 5) & 1]);
-        n = n0 / 2 + (row >> 6) * 32 + (row & 31);
+      if constexpr (EPI == EPI_GLU) rb[i] = from_b.load(static_cast<const T*>((row >> 5) & 1 ? p.b[1] : p.b[0]), n0 / 2 + (row >> 6) * 32 + (row & 31), k0 + k);
+      else rb[i] = from_b.load(static_cast<const T*>(p.b[part]), n0 + row, k0 + k);
+    }
+    if (k0 + BK > p.K) {
+#pragma unroll
+      for (int i = 0; i < SA::EACH; ++i) {
+        int row, k;
+        SA::place(i, t, &row, &k);
+        ra[i] = from_a.cleared(ra[i], k0 + k);
       }
-      rb[i] = {};
-      if (n < p.N && kk < p.K) {
-        const int64_t left = KCB ? p.K - kk : p.N - n;
-        rb[i] = load8(KCB ? pbb + n * p.ldb + kk : pbb + kk * p.ldb + n, left < 8 ? (int)left : 8);
+#pragma unroll
+      for (int i = 0; i < SB::EACH; ++i) {
+        int row, k;
+        SB::place(i, t, &row, &k);
+        rb[i] = from_b.cleared(rb[i], k0 + k);
       }
     }
+  };
+  auto put = [&](unsigned char* lds) {
+#pragma unroll
+    for (int i = 0; i < SA::EACH; ++i) *reinterpret_cast<Op8<T>*>(lds + (i * 256 + t) * 16) = ra[i];
+#pragma unroll
+    for (int i = 0; i < SB::EACH; ++i) *reinterpret_cast<Op8<T>*>(lds + SA::BYTES + (i * 256 + t) * 16) = rb[i];
   };
   unsigned at_a[4], at_b[4];
   SA::address(at_a, wm * (BM / 2), lane);
@@ -340,29 +377,31 @@ __global__ __launch_bounds__(256) void ffn_gemm_any(GemmArgs a) {
   for (int x = 0; x < TM; ++x)
 #pragma unroll
     for (int y = 0; y < TN; ++y) acc[x][y] = f32x16{};
-  if (first < last) fetch(first);
+  if (first < last) {
+    fetch(first);
+    put(operands[0]);
+  }
+  __syncthreads();
   for (int kt = first; kt < last; ++kt) {
-#pragma unroll
-    for (int i = 0; i < SA::EACH; ++i) *reinterpret_cast<Op8<T>*>(sa + (i * 256 + t) * 16) = ra[i];
-#pragma unroll
-    for (int i = 0; i < SB::EACH; ++i) *reinterpret_cast<Op8<T>*>(sb + (i * 256 + t) * 16) = rb[i];
-    __syncthreads();
+    const JZ_LDS unsigned char* const lds = (const JZ_LDS unsigned char*)operands[(kt - first) & 1];
     if (kt + 1 < last) fetch(kt + 1);
 #pragma unroll
     for (int s = 0; s < BK / 16; ++s) {
       Op8<T> fa[TM], fb[TN];
 #pragma unroll
-      for (int x = 0; x < TM; ++x) fa[x] = SA::read((const JZ_LDS unsigned char*)sa, at_a, x, s);
+      for (int x = 0; x < TM; ++x) fa[x] = SA::read(lds, at_a, x, s);
 #pragma unroll
-      for (int y = 0; y < TN; ++y) fb[y] = SB::read((const JZ_LDS unsigned char*)sb, at_b, y, s);
+      for (int y = 0; y < TN; ++y) fb[y] = SB::read(lds + SA::BYTES, at_b, y, s);
 #pragma unroll
       for (int x = 0; x < TM; ++x)
 #pragma unroll
         for (int y = 0; y < TN; ++y) acc[x][y] = mfma(fb[y], fa[x], acc[x][y]);
     }
+    if (kt + 1 < last) put(operands[(kt + 1 - first) & 1]);
     __syncthreads();
   }
-  finish_tile<T, EPI>(a, p, acc, m0 + wm * (BM / 2), n0 + wn * (BN / 2), partial ? partial + wm * (BM / 2) * BN + wn * (BN / 2) : nullptr, BN, (JZ_LDS unsigned char*)operands + wave * (32 * TN * 128), lane);
+  finish<T, EPI, ACT>(a, p, acc, m0 + wm * (BM / 2), n0 + wn * (BN / 2), partial ? partial + wm * (BM / 2) * BN + wn * (BN / 2) : nullptr, BN,
+                      (JZ_LDS unsigned char*)operands[0] + wave * (32 * TN * 128), lane);
 }
 
 // ---- LDS-direct ---------------------------------------------------------------------------------------------------------------
@@ -433,7 +472,6 @@ __device__ __forceinline__ void spread_out() {
   });
 }
 
-// ACT: the activation where EPI is EPI_GLU_BWD, else 0
 template <class T, bool KCA, bool KCB, int EPI, int ACT, int BM, int BN, int WGM, int WGN>
 __global__ __launch_bounds__(64 * WGM * WGN, 2) void ffn_gemm(GemmArgs a) {
   constexpr int THREADS = 64 * WGM * WGN, TM = BM / WGM / 32, TN = BN / WGN / 32, STEPS = BK / 16, READS = TM * (KCA ? 1 : 2) + TN * (KCB ? 1 : 2);
@@ -511,14 +549,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void ffn_gemm(GemmArgs a) {
   constexpr int STRIP = 32 * TN * 128, FIT = SA::BYTES / STRIP;
   static_assert(2 * FIT >= WGM * WGN, "the results pass through the place of A");
   unsigned char* const mine = (wave < FIT ? a0 + wave * STRIP : a1 + (wave - FIT) * STRIP);
-  const int64_t m = m0 + wm * TM * 32, n = n0 + wn * TN * 32;
-  float* const mine_partial = partial ? partial + wm * TM * 32 * BN + wn * TN * 32 : nullptr;
-  if constexpr (EPI == EPI_GLU_BWD) {
-    if (partial) finish_tile<T, EPI_STORE>(a, p, acc, m, n, mine_partial, BN, (JZ_LDS unsigned char*)mine, lane);
-    else finish_bwd<T, ACT>(a, p, acc, m, n, (JZ_LDS unsigned char*)mine, lane);
-  } else {
-    finish_tile<T, EPI>(a, p, acc, m, n, mine_partial, BN, (JZ_LDS unsigned char*)mine, lane);
-  }
+  finish<T, EPI, ACT>(a, p, acc, m0 + wm * TM * 32, n0 + wn * TN * 32, partial ? partial + wm * TM * 32 * BN + wn * TN * 32 : nullptr, BN, (JZ_LDS unsigned char*)mine, lane);
 }
 
 // The partial sums of the tiles that are split, added in the order of the splits, and the epilogue.  Eight columns a thread, blockIdx.y a tile.
