@@ -174,10 +174,18 @@ int gemm(GemmArgs a, const Scratch& ws, hipStream_t st) {
 template <class T, bool GLU, int TT>
 int launch_few(const GemmArgs& a, hipStream_t st) {
   const unsigned grid = (unsigned)((a.p[0].N + 15) / 16);
-  // sixteen wavefronts fit a compute unit: as many to a workgroup as keep all workgroups on the chip at once
-  if (grid <= 256) ffn_few<T, GLU, TT, 16><<<grid, 1024, 0, st>>>(a);
-  else if (grid <= 512) ffn_few<T, GLU, TT, 8><<<grid, 512, 0, st>>>(a);
-  else ffn_few<T, GLU, TT, 4><<<grid, 256, 0, st>>>(a);
+  if (direct<true, true>(a)) {
+    // stages of a wavefront's own: as many wavefronts as LDS holds, in one workgroup a compute unit or, where there are more of them, two
+    constexpr int W = GLU && TT == 4 ? 4 : 8, CH = TT == 1 && !GLU ? 2 : 1;
+    if (grid <= 256 || W == 4) ffn_few<T, GLU, TT, W, CH><<<grid, 64 * W, 0, st>>>(a);
+    else ffn_few<T, GLU, TT, 4, CH><<<grid, 256, 0, st>>>(a);
+  } else if (grid <= 256) {  // sixteen wavefronts fit a compute unit: as many to a workgroup as keep all workgroups on the chip at once
+    ffn_few_any<T, GLU, TT, 16><<<grid, 1024, 0, st>>>(a);
+  } else if (grid <= 512) {
+    ffn_few_any<T, GLU, TT, 8><<<grid, 512, 0, st>>>(a);
+  } else {
+    ffn_few_any<T, GLU, TT, 4><<<grid, 256, 0, st>>>(a);
+  }
   return jz::launch_status();
 }
 constexpr int64_t FEW_ROWS = 64;
