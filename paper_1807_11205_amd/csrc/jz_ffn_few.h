@@ -126,7 +126,7 @@ __global__ __launch_bounds__(64 * WAVES) void ffn_few_any(GemmArgs a) {
 
 // Rows that are multiples of 8: LDS-direct loads of 8 rows x 128 bytes, whole lines, into places of the wavefront's own, so that it waits for nobody.  (Loads in
 // the matrix instruction's layout, 16 rows x 64 bytes, bring a compute unit 17 bytes a clock: 5632 -> 2048 features, 24 tokens, BF16, 17.0 us; these
-// 7.2.)  A stage is 64 CH k of the weights' and the tokens' rows, chunk c of a row at c ^ (row % 8); two stages.
+// 7.2.)  A stage is 64 CH k of the weights' and the tokens' rows, chunk c of a row at c ^ (row / 2 % 8); two stages.
 template <class T, bool GLU, int TT, int WAVES, int CH>
 __global__ __launch_bounds__(64 * WAVES) void ffn_few(GemmArgs a) {
   constexpr int MATS = GLU ? 2 : 1, ROWS = 16 * (MATS + TT), CHUNK = ROWS * 128, STAGE = CHUNK * CH;
@@ -134,15 +134,17 @@ __global__ __launch_bounds__(64 * WAVES) void ffn_few(GemmArgs a) {
   const Product& p = a.p[0];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r16 = lane & 15;
   const int64_t n0 = (int64_t)blockIdx.x * 16;
-  const int row = lane >> 3, k8 = ((lane & 7) ^ row) * 8;  // of 8 rows, and elements of 64, that an LDS-direct load brings to position lane % 8
-  const unsigned off_w = (unsigned)(row * p.ldb + k8) * 2, off_x = (unsigned)(row * p.lda + k8) * 2;
+  // the first and the second 8 of 16 rows: which elements of 64 an LDS-direct load brings to position lane % 8 of row lane / 8
+  const int row = lane >> 3;
+  const unsigned k8[2] = {((lane & 7u) ^ (row >> 1)) * 8u, ((lane & 7u) ^ (4 + (row >> 1))) * 8u};
+  const unsigned off_w = (unsigned)(row * p.ldb) * 2, off_x = (unsigned)(row * p.lda) * 2;
   const int stages = (int)((p.K + 64 * CH - 1) / (64 * CH));
   auto fetch = [&](unsigned char* s, int j) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int64_t k0 = ((int64_t)j * CH + c) * 64;
       const bool wanted = k0 < p.K;
-      const unsigned end = k8 >= p.K - k0 ? 0x80000000u : 0u;
+      auto at = [&](int h, int64_t ld, unsigned off) { return (off + (unsigned)(h * 8 * ld * 2) + k8[h & 1] * 2) | (k8[h & 1] >= p.K - k0 ? 0x80000000u : 0u); };
       auto span = [&](int64_t rows, int64_t ld) {  // bytes from the place on; nothing behind the end
         const int64_t n = ((rows - 1) * ld + p.K - k0) * 2;
         return wanted ? (int)(n < 0x7ffffff0 ? n : 0x7ffffff0) : 0;
@@ -152,11 +154,11 @@ __global__ __launch_bounds__(64 * WAVES) void ffn_few(GemmArgs a) {
       for (int i = 0; i < MATS; ++i) {
         const auto r = __builtin_amdgcn_make_buffer_rsrc((void*)(static_cast<const T*>(p.b[i]) + n0 * p.ldb + (wanted ? k0 : 0)), 0, span(p.N - n0, p.ldb), 0x00020000);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) jz_dma16(r, (lds_byte*)to + (i * 2 + h) * 1024, (off_w + (unsigned)(h * 8 * p.ldb * 2)) | end);
+        for (int h = 0; h < 2; ++h) jz_dma16(r, (lds_byte*)to + (i * 2 + h) * 1024, at(h, p.ldb, off_w));
       }
       const auto r = __builtin_amdgcn_make_buffer_rsrc((void*)(static_cast<const T*>(p.a[0]) + (wanted ? k0 : 0)), 0, span(p.M, p.lda), 0x00020000);
 #pragma unroll
-      for (int h = 0; h < 2 * TT; ++h) jz_dma16(r, (lds_byte*)to + (MATS * 2 + h) * 1024, (off_x + (unsigned)(h * 8 * p.lda * 2)) | end);
+      for (int h = 0; h < 2 * TT; ++h) jz_dma16(r, (lds_byte*)to + (MATS * 2 + h) * 1024, at(h, p.lda, off_x));
     }
   };
   f32x4 acc[MATS][TT];
@@ -171,7 +173,7 @@ __global__ __launch_bounds__(64 * WAVES) void ffn_few(GemmArgs a) {
     for (int c = 0; c < CH; ++c)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int at = c * CHUNK + (((u * 4 + (lane >> 4)) ^ (lane & 7)) * 16);
+        const int at = c * CHUNK + (((u * 4 + (lane >> 4)) ^ ((lane >> 1) & 7)) * 16);
 #pragma unroll
         for (int i = 0; i < MATS; ++i) w[c][u][i] = *reinterpret_cast<const JZ_LDS Op8<T>*>(from + at + i * 2048);
 #pragma unroll

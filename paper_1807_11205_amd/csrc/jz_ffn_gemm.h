@@ -10,7 +10,8 @@
 //
 // Tiles.  BM x BN x 64, four wavefronts in 2 x 2, each (BM / 2) x (BN / 2) in 32x32x16 matrix instructions with the operands exchanged, so
 // that a lane has four consecutive n of one m.  Two tiles of operands in LDS:
-//     KC  [row][8 chunks of 16 bytes], chunk c at position c ^ (row % 8); an operand is one 16-byte read
+//     KC  [row][8 chunks of 16 bytes], chunk c at position c ^ (row / 2 % 8); an operand is one 16-byte read (16 lanes at a time reach 256 bytes of
+//         banks, two rows: c ^ (row % 8) left every read with a conflict)
 //     MC  [k][ROWS / 8 chunks], chunk c at position c ^ 4 (k % 4); an operand is two 8-byte transposing reads
 // Both orders keep the reads of a wavefront on different banks.
 #pragma once
@@ -128,7 +129,7 @@ struct Staged {
     const int s = i * THREADS + t;
     if constexpr (KC) {
       *row = s >> 3;
-      *k = ((s & 7) ^ (*row & 7)) * 8;
+      *k = ((s & 7) ^ ((*row >> 1) & 7)) * 8;
     } else {
       constexpr int PER = ROWS / 8;
       *k = s / PER;
@@ -141,7 +142,7 @@ struct Staged {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (KC) {
-        at[i] = (row0 + (lane & 31)) * 128 + (((i * 2 + (lane >> 5)) ^ (lane & 7)) * 16);
+        at[i] = (row0 + (lane & 31)) * 128 + (((i * 2 + (lane >> 5)) ^ ((lane >> 1) & 7)) * 16);
       } else {
         // 16 lanes read four k of 16 rows, 8 bytes a lane, and get them transposed: lane i four k of row i
         const int gi = lane >> 4, j = (lane >> 2) & 3, c4 = lane & 3, c = (row0 + 32 * i + 16 * (gi & 1) + 4 * c4) / 8;
@@ -162,7 +163,7 @@ struct Staged {
 };
 
 // Which tile of which product a workgroup has.  Consecutive workgroups land on different XCDs, each with an L2 of its own, so every XCD gets a run of
-// tiles, and within a run eight rows of tiles are taken column by column: what a run reads at a time is then a block.
+// tiles, and within a run four rows of tiles are taken column by column: what a run reads at a time is then a block.
 struct Tile {
   int product, split;  // split < 0: the whole sum
   unsigned m, n, behind;  // behind: number among the tiles that are split
@@ -173,7 +174,7 @@ __device__ __forceinline__ void place_tile(const GemmArgs& a, unsigned t, Tile* 
     t -= a.p[w->product].tiles_m * a.p[w->product].tiles_n;
     ++w->product;
   }
-  const unsigned rows = a.p[w->product].tiles_m, cols = a.p[w->product].tiles_n, G = 8;
+  const unsigned rows = a.p[w->product].tiles_m, cols = a.p[w->product].tiles_n, G = 4;
   const unsigned band = t / (G * cols), in = t % (G * cols), high = rows - band * G < G ? rows - band * G : G;
   w->m = band * G + in % high;
   w->n = in / high;
@@ -196,13 +197,14 @@ __device__ __forceinline__ Tile find_tile(const GemmArgs& a) {
 
 // The sums of a wavefront's tile to their places: FP32 partial sums, or the epilogue.  They pass through LDS 32 rows at a time, so that a lane has eight columns
 // of a row and neighbouring lanes its neighbours: whole lines are stored.  lds: 32 rows of TN * 32 floats of the wavefront's own, 16-byte chunk c of row r at
-// c ^ (r % 8).  Register 4 j + i of a lane holds row lane % 32, column 8 j + 4 (lane / 32) + i.
+// c ^ (r % 16).  Register 4 j + i of a lane holds row lane % 32, column 8 j + 4 (lane / 32) + i.
 // partial: where the sums of the wavefront's first row and column go instead, rows `pitch` apart; or NULL.
 template <class T, int EPI, int TM, int TN>
 __device__ __forceinline__ void finish_tile(const GemmArgs& a, const Product& p, f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, float* partial, int pitch,
                                             JZ_LDS unsigned char* lds, int lane) {
+  static_assert(TN % 2 == 0, "16 chunks or more a row");
   constexpr int PITCH = TN * 128, PER = (EPI == EPI_GLU ? TN * 2 : TN * 4);  // bytes of a row; groups of eight results in one
-  auto chunk = [&](int row, int c) { return lds + row * PITCH + ((c ^ (row & 7)) * 16); };
+  auto chunk = [&](int row, int c) { return lds + row * PITCH + ((c ^ (row & 15)) * 16); };
   auto eight = [&](int row, int c) {
     const f32x4 lo = *reinterpret_cast<const JZ_LDS f32x4*>(chunk(row, c)), hi = *reinterpret_cast<const JZ_LDS f32x4*>(chunk(row, c + 1));
     return f32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
@@ -259,7 +261,7 @@ __device__ __forceinline__ void finish_bwd(const GemmArgs& a, const Product& p, 
     g[i] = u[i] = {};
     ask(0, i);
   }
-  auto chunk = [&](int row, int c) { return lds + row * PITCH + ((c ^ (row & 7)) * 16); };
+  auto chunk = [&](int row, int c) { return lds + row * PITCH + ((c ^ (row & 15)) * 16); };
   static_for<0, TM>([&](auto X) {
     constexpr int x = decltype(X)::value;
     static_for<0, TN * 4>([&](auto I) {
