@@ -4,4 +4,4 @@
 Importing the package loads nothing; `paper_1807_11205_amd.api` opens the built library
 and raises if it is missing.
 """
-__all__ = ["api", "inputs", "shapes"]
+__all__ = ["api", "gated_mlp", "inputs", "shapes"]
