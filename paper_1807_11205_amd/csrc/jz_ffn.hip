@@ -72,6 +72,7 @@ bool direct(const GemmArgs& a) {
   for (int i = 0; i < a.products; ++i) {
     const Product& p = a.p[i];
     if (p.lda % 8 || p.ldb % 8 || p.lda >= (1 << 22) || p.ldb >= (1 << 22) || ((KCA || KCB) && p.K % 8)) return false;
+    if (!p.eights && ((!KCA && p.M % 8) || (!KCB && p.N % 8))) return false;
   }
   return true;
 }
@@ -205,7 +206,7 @@ Product product(const void* a, int64_t lda, const void* b, int64_t ldb, void* c,
   p.ldc = ldc;
   p.M = M;
   p.N = N;
-  p.K = K;
+  p.K = p.k_rows = K;
   return p;
 }
 GemmArgs one(const Product& p, int act) {
@@ -216,60 +217,151 @@ GemmArgs one(const Product& p, int act) {
   return a;
 }
 
-// the products of the block, in the order of the calls
-GemmArgs glu_args(const FfnShape& s, int act, const void* x, const void* wg, const void* wu, void* h, void* gate, void* up) {
-  GemmArgs a = one(product(x, s.ldx, wg, s.D, h, s.F, s.M, s.F, s.D), act);
-  a.p[0].b[1] = wu;
+// ---- operands ---------------------------------------------------------------------------------------------------------------
+int64_t round8(int64_t n) { return (n + 7) & ~int64_t(7); }
+struct Matrix {
+  const void* p;
+  int64_t rows, cols, ld;
+};
+// The LDS-direct kernels want rows that start on 16 bytes, and as operands along k rows that are a multiple of 8 long: others are copied into the workspace first,
+// where it has room, since the kernel that takes any sizes runs at half their rate (8192 rows, 2047 -> 5631 features, FP16: 543 to 659 TFLOP/s against 940 to 1160;
+// the copies are 230 MB each way at most).
+class Aligner {
+ public:
+  explicit Aligner(Scratch* room) : room_(room) {}
+  static size_t bytes(const Matrix& m) { return m.ld % 8 || m.cols % 8 ? (size_t)m.rows * round8(m.cols) * 2 + 255 & ~size_t(255) : 0; }
+  Matrix operator()(const Matrix& m) {
+    const size_t n = bytes(m);
+    if (!n || m.rows == 0) return m;
+    const Matrix to = {room_->p, m.rows, m.cols, round8(m.cols)};
+    c_.m[c_.count++] = {m.p, room_->p, m.rows, m.cols, m.ld, to.ld, blocks_};
+    blocks_ += (m.rows * (to.ld / 8) + 255) / 256;
+    room_->p = static_cast<char*>(room_->p) + n;
+    room_->bytes -= n;
+    return to;
+  }
+  template <class T>
+  int run(hipStream_t st) {
+    if (c_.count) ffn_copy<T><<<(unsigned)blocks_, 256, 0, st>>>(c_);
+    return jz::launch_status();
+  }
+
+ private:
+  Scratch* room_;
+  Copies c_ = {};
+  int64_t blocks_ = 0;
+};
+// A copied row ends in zeros, which a sum may count; another's may be followed by anything.
+struct Operands {
+  Matrix x, wg, wu, wd, h, dy;
+  bool copied;
+};
+Operands operands(const FfnShape& s, const void* x, const void* wg, const void* wu, const void* wd, const void* h, const void* dy) {
+  return {{x, s.M, s.D, s.ldx}, {wg, s.F, s.D, s.D}, {wu, s.F, s.D, s.D}, {wd, s.O, s.F, s.F}, {h, s.M, s.F, s.F}, {dy, s.M, s.O, s.lddy}, false};
+}
+size_t copies_fwd(const Operands& o) { return Aligner::bytes(o.x) + Aligner::bytes(o.wg) + Aligner::bytes(o.wu) + Aligner::bytes(o.wd) + Aligner::bytes(o.h); }
+size_t copies_bwd(const Operands& o) { return copies_fwd(o) + Aligner::bytes(o.dy); }
+
+// ---- the products of the block, in the order of the calls ---------------------------------------------------------------------
+GemmArgs glu_args(const FfnShape& s, int act, const Operands& o, void* h, void* gate, void* up) {
+  GemmArgs a = one(product(o.x.p, o.x.ld, o.wg.p, o.wg.ld, h, s.F, s.M, s.F, s.D), act);
+  if (o.copied) a.p[0].K = round8(s.D);
+  a.p[0].b[1] = o.wu.p;
   a.out0 = gate;
   a.out1 = up;
   return a;
 }
-GemmArgs down_args(const FfnShape& s, const void* h, const void* wd, void* y) { return one(product(h, s.F, wd, s.F, y, s.ldy, s.M, s.O, s.F), 0); }
-GemmArgs dh_args(const FfnShape& s, int act, const void* dy, const void* wd, const void* gate, const void* up, void* dgate, void* dup) {
-  GemmArgs a = one(product(dy, s.lddy, wd, s.F, nullptr, 0, s.M, s.F, s.O), act);
+GemmArgs down_args(const FfnShape& s, const Operands& o, void* y) {
+  GemmArgs a = one(product(o.h.p, o.h.ld, o.wd.p, o.wd.ld, y, s.ldy, s.M, s.O, s.F), 0);
+  if (o.copied) a.p[0].K = round8(s.F);
+  return a;
+}
+GemmArgs dh_args(const FfnShape& s, int act, const Operands& o, const void* gate, const void* up, void* dgate, void* dup) {
+  GemmArgs a = one(product(o.dy.p, o.dy.ld, o.wd.p, o.wd.ld, nullptr, round8(s.F), s.M, s.F, s.O), act);
+  if (o.copied) a.p[0].K = round8(s.O);
+  a.p[0].eights = o.copied;
   a.gate = gate;
   a.up = up;
   a.out0 = dgate;
   a.out1 = dup;
   return a;
 }
-GemmArgs dx_args(const FfnShape& s, const void* dgate, const void* dup, const void* wg, const void* wu, void* dx) {
-  GemmArgs a = one(product(dgate, s.F, wg, s.D, dx, s.lddx, s.M, s.D, s.F), 0);
+GemmArgs dx_args(const FfnShape& s, const Operands& o, const void* dgate, const void* dup, void* dx) {
+  GemmArgs a = one(product(dgate, round8(s.F), o.wg.p, o.wg.ld, dx, s.lddx, s.M, s.D, s.F), 0);
+  a.p[0].K = round8(s.F);  // dgate and dup always end in zeros
+  a.p[0].eights = o.copied;
   a.p[0].a[1] = dup;
-  a.p[0].b[1] = wu;
+  a.p[0].b[1] = o.wu.p;
   a.parts = 2;
   return a;
 }
-GemmArgs dw_args(const FfnShape& s, const void* dgate, const void* dup, const void* dy, const void* x, const void* h, void* dwg, void* dwu, void* dwd) {
-  GemmArgs a = one(product(dgate, s.F, x, s.ldx, dwg, s.D, s.F, s.D, s.M), 0);
-  a.p[1] = product(dup, s.F, x, s.ldx, dwu, s.D, s.F, s.D, s.M);
-  a.p[2] = product(dy, s.lddy, h, s.F, dwd, s.F, s.O, s.F, s.M);
+GemmArgs dw_args(const FfnShape& s, const Operands& o, const void* dgate, const void* dup, void* dwg, void* dwu, void* dwd) {
+  GemmArgs a = one(product(dgate, round8(s.F), o.x.p, o.x.ld, dwg, s.D, s.F, s.D, s.M), 0);
+  a.p[1] = product(dup, round8(s.F), o.x.p, o.x.ld, dwu, s.D, s.F, s.D, s.M);
+  a.p[2] = product(o.dy.p, o.dy.ld, o.h.p, o.h.ld, dwd, s.F, s.O, s.F, s.M);
   a.products = 3;
+  for (Product& p : a.p) p.eights = o.copied;
   return a;
 }
-
-template <class T>
-int run_fwd(const FfnShape& s, int act, const void* x, const void* wg, const void* wu, const void* wd, void* h, void* gate, void* up, void* y, const Scratch& ws,
-            hipStream_t st) {
-  const GemmArgs a = glu_args(s, act, x, wg, wu, h, gate, up), b = down_args(s, h, wd, y);
-  if (s.M <= FEW_ROWS) {
-    const int rc = few<T, true>(a, st);
-    return rc == JZ_OK ? few<T, false>(b, st) : rc;
-  }
-  const int rc = gemm<T, true, true, EPI_GLU>(a, ws, st);
-  return rc == JZ_OK ? gemm<T, true, true, EPI_STORE>(b, ws, st) : rc;
+// the same with every operand that would be copied as its copy will be, for planning
+Operands aligned_shapes(Operands o) {
+  for (Matrix* m : {&o.x, &o.wg, &o.wu, &o.wd, &o.h, &o.dy})
+    if (Aligner::bytes(*m)) m->ld = round8(m->cols);
+  o.copied = true;
+  return o;
 }
 
 template <class T>
-int run_bwd(const FfnShape& s, int act, const void* x, const void* wg, const void* wu, const void* wd, const void* gate, const void* up, const void* h, const void* dy,
-            void* dx, void* dwg, void* dwu, void* dwd, void* dgate, void* dup, const Scratch& ws, hipStream_t st) {
-  int rc = gemm<T, true, false, EPI_GLU_BWD>(dh_args(s, act, dy, wd, gate, up, dgate, dup), ws, st);
-  if (rc == JZ_OK && dx) rc = gemm<T, true, false, EPI_STORE>(dx_args(s, dgate, dup, wg, wu, dx), ws, st);
-  if (rc == JZ_OK && dwg) rc = gemm<T, false, false, EPI_STORE>(dw_args(s, dgate, dup, dy, x, h, dwg, dwu, dwd), ws, st);
+int run_fwd(const FfnShape& s, int act, Operands o, void* h, void* gate, void* up, void* y, Scratch ws, hipStream_t st) {
+  if (s.M <= FEW_ROWS) {
+    const int rc = few<T, true>(glu_args(s, act, o, h, gate, up), st);
+    return rc == JZ_OK ? few<T, false>(down_args(s, o, y), st) : rc;
+  }
+  o.copied = copies_fwd(o) <= ws.bytes;
+  if (o.copied) {
+    Aligner align(&ws);
+    o.x = align(o.x);
+    o.wg = align(o.wg);
+    o.wu = align(o.wu);
+    o.wd = align(o.wd);
+    const int rc = align.run<T>(st);
+    if (rc != JZ_OK) return rc;
+  }
+  Scratch rest = ws;
+  Aligner align(&rest);
+  const Matrix h_copy = o.copied ? align(o.h) : o.h;  // made behind the first product
+  int rc = gemm<T, true, true, EPI_GLU>(glu_args(s, act, o, h, gate, up), rest, st);
+  if (rc == JZ_OK && o.copied) rc = align.run<T>(st);
+  o.h = h_copy;
+  return rc == JZ_OK ? gemm<T, true, true, EPI_STORE>(down_args(s, o, y), rest, st) : rc;
+}
+
+template <class T>
+int run_bwd(const FfnShape& s, int act, Operands o, const void* gate, const void* up, void* dx, void* dwg, void* dwu, void* dwd, void* dgate, void* dup, Scratch ws,
+            hipStream_t st) {
+  o.copied = copies_bwd(o) <= ws.bytes;
+  if (o.copied) {
+    Aligner align(&ws);
+    if (dwg) {
+      o.x = align(o.x);
+      o.h = align(o.h);
+    }
+    if (dx) {
+      o.wg = align(o.wg);
+      o.wu = align(o.wu);
+    }
+    o.wd = align(o.wd);
+    o.dy = align(o.dy);
+    const int rc = align.run<T>(st);
+    if (rc != JZ_OK) return rc;
+  }
+  int rc = gemm<T, true, false, EPI_GLU_BWD>(dh_args(s, act, o, gate, up, dgate, dup), ws, st);
+  if (rc == JZ_OK && dx) rc = gemm<T, true, false, EPI_STORE>(dx_args(s, o, dgate, dup, dx), ws, st);
+  if (rc == JZ_OK && dwg) rc = gemm<T, false, false, EPI_STORE>(dw_args(s, o, dgate, dup, dwg, dwu, dwd), ws, st);
   return rc;
 }
 
-size_t hidden_bytes(const FfnShape& s) { return ((size_t)s.M * s.F * 2 + 255) & ~size_t(255); }
+size_t hidden_bytes(const FfnShape& s) { return ((size_t)s.M * round8(s.F) * 2 + 255) & ~size_t(255); }
 
 }  // namespace
 
@@ -278,9 +370,10 @@ extern "C" int jz_ffn_fwd_workspace_bytes(const jz_ffn_desc* d, size_t* bytes) {
   FfnShape s;
   const int rc = ffn_shape(d, &s);
   if (rc != JZ_OK) return rc;
-  const GemmArgs a = glu_args(s, 0, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr), b = down_args(s, nullptr, nullptr, nullptr);
-  *bytes = s.M <= FEW_ROWS ? 0 : std::max(wanted(a, EPI_GLU, direct<true, true>(a)), wanted(b, EPI_STORE, direct<true, true>(b)));
-  return rc;
+  const Operands o = operands(s, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr), al = aligned_shapes(o);
+  const GemmArgs a = glu_args(s, 0, al, nullptr, nullptr, nullptr), b = down_args(s, al, nullptr);
+  *bytes = s.M <= FEW_ROWS ? 0 : copies_fwd(o) + std::max(wanted(a, EPI_GLU, direct<true, true>(a)), wanted(b, EPI_STORE, direct<true, true>(b)));
+  return JZ_OK;
 }
 
 extern "C" int jz_ffn_bwd_workspace_bytes(const jz_ffn_desc* d, size_t* bytes) {
@@ -288,11 +381,12 @@ extern "C" int jz_ffn_bwd_workspace_bytes(const jz_ffn_desc* d, size_t* bytes) {
   FfnShape s;
   const int rc = ffn_shape(d, &s);
   if (rc != JZ_OK) return rc;
-  const GemmArgs a = dh_args(s, 0, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr), b = dx_args(s, nullptr, nullptr, nullptr, nullptr, nullptr),
-                 c = dw_args(s, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr);
-  *bytes = 2 * hidden_bytes(s) + std::max(wanted(a, EPI_GLU_BWD, direct<true, false>(a)),
-                                          std::max(wanted(b, EPI_STORE, direct<true, false>(b)), wanted(c, EPI_STORE, direct<false, false>(c))));
-  return rc;
+  const Operands o = operands(s, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr), al = aligned_shapes(o);
+  const GemmArgs a = dh_args(s, 0, al, nullptr, nullptr, nullptr, nullptr), b = dx_args(s, al, nullptr, nullptr, nullptr),
+                 c = dw_args(s, al, nullptr, nullptr, nullptr, nullptr, nullptr);
+  *bytes = 2 * hidden_bytes(s) + copies_bwd(o) + std::max(wanted(a, EPI_GLU_BWD, direct<true, false>(a)),
+                                                          std::max(wanted(b, EPI_STORE, direct<true, false>(b)), wanted(c, EPI_STORE, direct<false, false>(c))));
+  return JZ_OK;
 }
 
 extern "C" int jz_ffn_fwd(const jz_ffn_desc* d, const void* x, const void* w_gate, const void* w_up, const void* w_down, void* h, void* gate, void* up, void* y,
@@ -310,8 +404,9 @@ extern "C" int jz_ffn_fwd(const jz_ffn_desc* d, const void* x, const void* w_gat
   rc = ffn_look_over(t, 8, ws, ws_bytes);
   if (rc != JZ_OK) return rc;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  return d->dtype == JZ_F16 ? run_fwd<_Float16>(s, d->act, x, w_gate, w_up, w_down, h, gate, up, y, Scratch{ws, ws_bytes}, st)
-                            : run_fwd<__bf16>(s, d->act, x, w_gate, w_up, w_down, h, gate, up, y, Scratch{ws, ws_bytes}, st);
+  const Operands o = operands(s, x, w_gate, w_up, w_down, h, nullptr);
+  const Scratch room = {ws, ws_bytes};
+  return d->dtype == JZ_F16 ? run_fwd<_Float16>(s, d->act, o, h, gate, up, y, room, st) : run_fwd<__bf16>(s, d->act, o, h, gate, up, y, room, st);
 }
 
 extern "C" int jz_ffn_bwd(const jz_ffn_desc* d, const void* x, const void* w_gate, const void* w_up, const void* w_down, const void* gate, const void* up,
@@ -335,6 +430,7 @@ extern "C" int jz_ffn_bwd(const jz_ffn_desc* d, const void* x, const void* w_gat
   void *dgate = b, *dup = b + hidden_bytes(s);
   const Scratch rest{b + need, ws_bytes - need};
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  return d->dtype == JZ_F16 ? run_bwd<_Float16>(s, d->act, x, w_gate, w_up, w_down, gate, up, h, dy, dx, dw_gate, dw_up, dw_down, dgate, dup, rest, st)
-                            : run_bwd<__bf16>(s, d->act, x, w_gate, w_up, w_down, gate, up, h, dy, dx, dw_gate, dw_up, dw_down, dgate, dup, rest, st);
+  const Operands o = operands(s, x, w_gate, w_up, w_down, h, dy);
+  return d->dtype == JZ_F16 ? run_bwd<_Float16>(s, d->act, o, gate, up, dx, dw_gate, dw_up, dw_down, dgate, dup, rest, st)
+                            : run_bwd<__bf16>(s, d->act, o, gate, up, dx, dw_gate, dw_up, dw_down, dgate, dup, rest, st);
 }

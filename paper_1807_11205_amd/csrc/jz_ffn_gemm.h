@@ -69,6 +69,8 @@ struct Product {           // one product of a launch
   void* c;
   int64_t lda, ldb, ldc;    // elements
   int64_t M, N, K;          // K of one part; N: columns of C (hidden units where gate and up are interleaved)
+  int64_t k_rows;           // the rows of an MC operand: K, or less where a KC operand's rows end in zeros that K counts
+  bool eights;              // MC operands' rows can be read to a multiple of 8 elements, whatever M and N are
   int tiles_m, tiles_n;
 };
 struct GemmArgs {
@@ -93,6 +95,14 @@ __device__ __forceinline__ void glu_bwd8(int act, f32x8 v, f32x8 g, f32x8 u, f32
 }
 
 // ---- results --------------------------------------------------------------------------------------------------------------
+// dgate and dup lie in the workspace, rows a multiple of 8 long and zero behind their end: they are operands of the next products
+template <class T>
+__device__ __forceinline__ void store_padded(T* p, f32x8 v, int left) {
+#pragma unroll
+  for (int i = 1; i < 8; ++i) v[i] = i < left ? v[i] : 0.f;
+  store8(p, narrow8<T>(v));
+}
+
 // What becomes of eight sums (or gate and up sums) that belong to columns n .. n + 7 of row m.
 template <class T, int EPI>
 __device__ __forceinline__ void finish8(const GemmArgs& a, const Product& p, int64_t m, int64_t n, f32x8 v, f32x8 w) {
@@ -112,8 +122,8 @@ __device__ __forceinline__ void finish8(const GemmArgs& a, const Product& p, int
   } else {
     f32x8 dg, du;
     glu_bwd8(a.act, v, widen8<T>(load8(static_cast<const T*>(a.gate) + m * p.N + n, left)), widen8<T>(load8(static_cast<const T*>(a.up) + m * p.N + n, left)), &dg, &du);
-    store8(static_cast<T*>(a.out0) + m * p.N + n, narrow8<T>(dg), left);
-    store8(static_cast<T*>(a.out1) + m * p.N + n, narrow8<T>(du), left);
+    store_padded<T>(static_cast<T*>(a.out0) + m * p.ldc + n, dg, left);
+    store_padded<T>(static_cast<T*>(a.out1) + m * p.ldc + n, du, left);
   }
 }
 
@@ -278,8 +288,8 @@ __device__ __forceinline__ void finish_bwd(const GemmArgs& a, const Product& p, 
       int64_t m, n;
       if (place(x, i, &m, &n)) {
         const int left = p.N - n < 8 ? (int)(p.N - n) : 8;
-        store8(static_cast<T*>(a.out0) + m * p.N + n, narrow8<T>(dg), left);
-        store8(static_cast<T*>(a.out1) + m * p.N + n, narrow8<T>(du), left);
+        store_padded<T>(static_cast<T*>(a.out0) + m * p.ldc + n, dg, left);
+        store_padded<T>(static_cast<T*>(a.out1) + m * p.ldc + n, du, left);
       }
     });
   });
@@ -330,8 +340,8 @@ __global__ __launch_bounds__(256, 2) void ffn_gemm_any(GemmArgs a) {
   const int per_part = (int)((p.K + BK - 1) / BK), all = per_part * a.parts;
   const int first = w.split < 0 ? 0 : w.split * a.tiles_per_split, last = w.split < 0 || first + a.tiles_per_split > all ? all : first + a.tiles_per_split;
   float* const partial = w.split < 0 ? nullptr : a.partial + ((size_t)w.behind * a.splits + w.split) * (BM * BN);
-  const AnySource<T, KCA> from_a = {p.lda, p.M, p.K};
-  const AnySource<T, KCB> from_b = {p.ldb, p.N, p.K};
+  const AnySource<T, KCA> from_a = {p.lda, p.M, p.k_rows};
+  const AnySource<T, KCB> from_b = {p.ldb, p.N, p.k_rows};
 
   Op8<T> ra[SA::EACH], rb[SB::EACH];
   auto fetch = [&](int kt) {
@@ -350,7 +360,7 @@ __global__ __launch_bounds__(256, 2) void ffn_gemm_any(GemmArgs a) {
       if constexpr (EPI == EPI_GLU) rb[i] = from_b.load(static_cast<const T*>((row >> 5) & 1 ? p.b[1] : p.b[0]), n0 / 2 + (row >> 6) * 32 + (row & 31), k0 + k);
       else rb[i] = from_b.load(static_cast<const T*>(p.b[part]), n0 + row, k0 + k);
     }
-    if (k0 + BK > p.K) {
+    if (k0 + BK > p.k_rows) {
 #pragma unroll
       for (int i = 0; i < SA::EACH; ++i) {
         int row, k;
@@ -430,7 +440,7 @@ struct Source {
 
   __device__ __forceinline__ void init(const void* const* p, int64_t ld, int64_t row0, int64_t rows, int64_t K_, int t) {
     pitch = ld * 2;
-    rows_left = rows - row0;
+    rows_left = (KC ? rows : (rows + 7) & ~int64_t(7)) - row0;  // an MC operand's rows can be read in eights
     K = K_;
     base[0] = static_cast<const char*>(p[0]) + row0 * (KC ? pitch : 2);
     base[1] = static_cast<const char*>(p[1]) + row0 * (KC ? pitch : 2);
@@ -447,7 +457,7 @@ struct Source {
   __device__ __forceinline__ void load(L* lds, int part, int64_t k0, int wave, bool wanted) const {
     const int64_t skip = wanted ? k0 * (KC ? 2 : pitch) : 0;
     const int64_t span = KC ? (rows_left - 1) * pitch + (K - k0) * 2 : (K - k0 - 1) * pitch + rows_left * 2;
-    const int bytes = !wanted ? 0 : (int)(span < 0x7ffffff0 ? span : 0x7ffffff0);
+    const int bytes = !wanted || span < 0 ? 0 : (int)(span < 0x7ffffff0 ? span : 0x7ffffff0);
     const auto r0 = __builtin_amdgcn_make_buffer_rsrc((void*)(base[DUAL ? 0 : part] + skip), 0, bytes, 0x00020000);
     const auto r1 = __builtin_amdgcn_make_buffer_rsrc((void*)(base[1] + skip), 0, bytes, 0x00020000);
     const unsigned end = KC && k >= K - k0 ? 0x80000000u : 0u;  // a row's end inside the tile: the next row does not follow
@@ -491,8 +501,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void ffn_gemm(GemmArgs a) {
 
   Source<T, KCA, BM, THREADS, false> from_a;
   Source<T, KCB, BN, THREADS, EPI == EPI_GLU> from_b;
-  from_a.init(p.a, p.lda, m0, p.M, p.K, t);
-  from_b.init(p.b, p.ldb, EPI == EPI_GLU ? n0 / 2 : n0, p.N, p.K, t);
+  from_a.init(p.a, p.lda, m0, p.M, KCA ? p.K : p.k_rows, t);
+  from_b.init(p.b, p.ldb, EPI == EPI_GLU ? n0 / 2 : n0, p.N, KCB ? p.K : p.k_rows, t);
   auto fetch = [&](auto* la, auto* lb, int kt) {
     const int part = kt >= per_part && a.parts > 1;  // behind the last tile: zeros, so that there is no branch among the products
     const int64_t k0 = (int64_t)(kt - part * per_part) * BK;
@@ -573,4 +583,24 @@ __global__ __launch_bounds__(256) void ffn_join(GemmArgs a) {
   const int col = EPI == EPI_GLU ? (c >> 2) * 64 + (c & 3) * 8 : c * 8;
   const f32x8 v = total(col), u = EPI == EPI_GLU ? total(col + 32) : v;
   finish8<T, EPI>(a, p, m, n, v, u);
+}
+
+// Copies of matrices with rows on 16 bytes, zeros behind a row's end, for operands whose rows are not.  Eight elements a thread.
+struct Copies {
+  struct One {
+    const void* from;
+    void* to;
+    int64_t rows, cols, ld, pitch, first;  // first: its first block
+  } m[6];
+  int count;
+};
+template <class T>
+__global__ __launch_bounds__(256) void ffn_copy(Copies c) {
+  int q = 0;
+  while (q + 1 < c.count && blockIdx.x >= c.m[q + 1].first) ++q;
+  const Copies::One& o = c.m[q];
+  const int64_t i = ((int64_t)blockIdx.x - o.first) * 256 + threadIdx.x, per = o.pitch / 8, row = i / per, col = (i - row * per) * 8;
+  if (row >= o.rows) return;
+  const int64_t left = o.cols - col;
+  store8(static_cast<T*>(o.to) + row * o.pitch + col, load8(static_cast<const T*>(o.from) + row * o.ld + col, left < 8 ? (int)left : 8));
 }

@@ -269,6 +269,18 @@ def test_less_workspace_than_reported(jz, M, D, F, O):
         c.check_backward()
 
 
+@pytest.mark.parametrize("M, D, F, O", [(70, 101, 203, 99), (300, 250, 333, 250), (300, 256, 333, 256), (300, 255, 512, 256), (300, 256, 512, 255), (777, 1001, 2731, 1001)])
+@pytest.mark.parametrize("strides", [(0, 0, 0, 0), (1037, 1041, 1029, 1055)])
+def test_rows_that_are_not_on_16_bytes(jz, M, D, F, O, strides):
+    """With copies of the operands in the workspace, and where it has no room for them."""
+    c = Case(jz, M, D, F, O, "bf16", "silu", strides)
+    c.check()
+    c.forward(ws=None)
+    c.check_forward()
+    c.backward(ws=torch.full((2 * ((M * ((F + 7) // 8 * 8) * 2 + 255) // 256 * 256),), 0xff, dtype=torch.uint8, device=DEV))
+    c.check_backward()
+
+
 def test_gradient_is_the_difference(jz):
     """The loss sum(dy y) of the 64-bit formula at the same inputs, by differences, against the kernels' gradients along one direction of each input:
     the gradients are within 2 u of the formula's (the bound of every whole result), the difference within 1e-6 of it."""
