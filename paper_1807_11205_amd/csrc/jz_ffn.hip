@@ -418,8 +418,8 @@ extern "C" int jz_ffn_bwd(const jz_ffn_desc* d, const void* x, const void* w_gat
   if (!w_gate || !w_up || !w_down || (weights && (!dw_gate || !dw_up || !dw_down))) return JZ_ERR_NULL;
   if (s.M && (!gate || !up || !dy || (weights && (!x || !h)) || (!dx && !weights))) return JZ_ERR_NULL;
   const size_t need = 2 * hidden_bytes(s);
-  if (need && (!ws || ws_bytes < need)) return JZ_ERR_WORKSPACE;
-  if (need && !jz::aligned16(ws)) return JZ_ERR_ALIGN;
+  if (ws_bytes < need || (ws_bytes && !ws)) return JZ_ERR_WORKSPACE;
+  if (ws && !jz::aligned16(ws)) return JZ_ERR_ALIGN;
   const size_t hid = span(s.M, s.F, s.F), w = span(s.F, s.D, s.D), w2 = span(s.O, s.F, s.F);
   const FfnTensor t[] = {{weights ? x : nullptr, span(s.M, s.D, s.ldx), false}, {w_gate, w, false}, {w_up, w, false}, {w_down, w2, false}, {gate, hid, false}, {up, hid, false},
                          {weights ? h : nullptr, hid, false}, {dy, span(s.M, s.O, s.lddy), false}, {dx, span(s.M, s.D, s.lddx), true}, {dw_gate, w, true}, {dw_up, w, true},

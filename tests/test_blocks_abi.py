@@ -168,3 +168,11 @@ def test_ffn_arguments(jz):
     for bad in (dict(dx=A + (8 << 20)), dict(dw_gate=A + (1 << 20) + 32), dict(dw_up=A + (12 << 20)), dict(ws=A + (9 << 20)), dict(dw_down=A + (13 << 20))):
         assert ffn_call(jz, False, **bad) == jz.JZ_ERR_ALIAS, bad
     assert ffn_call(jz, False, ws=None) == ffn_call(jz, False, ws_bytes=2 * 40 * 96 * 2 - 16) == jz.JZ_ERR_WORKSPACE
+
+
+def test_ffn_workspace_without_rows(jz):
+    """Without rows the backward call needs no workspace, but one that it is told of has to be there: odd feature counts are copied into it."""
+    for k in (dict(ws=None), dict(ws=None, in_features=63)):
+        assert ffn_call(jz, False, rows=0, ws_bytes=1 << 20, **k) == jz.JZ_ERR_WORKSPACE, k
+    assert ffn_call(jz, False, rows=0, ws=A + (40 << 20) + 8, ws_bytes=1 << 20) == jz.JZ_ERR_ALIGN
+    assert ffn_call(jz, True, rows=40, ws=None, ws_bytes=1 << 20) == jz.JZ_ERR_WORKSPACE
