@@ -54,7 +54,8 @@ __device__ __forceinline__ f32x8 splat8(float v) { return f32x8{v, v, v, v, v, v
 
 // Which elements of a row a lane has: NV vectors of eight, vector i from element 8 (i THREADS + lane) on.  Loads are not predicated, so that all of a row's are on
 // their way at once: a vector that would pass the row's end is the row's last eight elements instead, and what of it lies outside the lane's own part is left
-// out of the sums.  (What a lane then stores a second time are the bits that their owner stores.)
+// out of the sums.  What a lane then stores a second time are the bits that their owner stores, except in place, where the owner, in another wavefront, may not have
+// loaded them yet: there a lane stores its own elements alone.
 //   EVEN   channels are a multiple of 8: a vector is a lane's own or nobody's        RAGGED   others from 8 on: the last vector overlaps its neighbour
 //   TINY   less than 8: one vector, element by element
 #define JZ_GLOBAL __attribute__((address_space(1)))
@@ -78,10 +79,16 @@ struct Lane {
     }
   }
   template <class T>
-  __device__ __forceinline__ void store(T* row, int i, f32x8 v) const {
+  __device__ __forceinline__ void store(T* row, int i, f32x8 v, bool in_place = false) const {
     if (!on(i)) return;
     if constexpr (MODE == TINY) {
       store8(row + own(i), narrow8<T>(v), C - own(i));
+    } else if (MODE == RAGGED && in_place && own(i) + 8 > C) {
+      const typename Vec8<T>::V o = narrow8<T>(v);
+      const int skip = own(i) - at(i);
+#pragma unroll
+      for (int e = 1; e < 8; ++e)
+        if (e >= skip) row[at(i) + e] = o[e];
     } else {
       JZ_GLOBAL char* base = (JZ_GLOBAL char*)row;
       *reinterpret_cast<JZ_GLOBAL typename Vec8<T>::U*>(base + (unsigned)at(i) * (unsigned)sizeof(T)) = narrow8<T>(v);
@@ -138,7 +145,7 @@ __global__ __launch_bounds__(THREADS >= 256 ? THREADS : 256) void norm_fwd(NormA
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       o[i] = widen8<R>(rv[i]) * a.res_scale + widen8<T>(yv[i]) * k1 * w[i];
-      l.store(static_cast<R*>(a.r_out) + row * a.C, i, o[i]);
+      l.store(static_cast<R*>(a.r_out) + row * a.C, i, o[i], a.r_out == a.r);
     }
   } else {
 #pragma unroll
@@ -309,7 +316,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void norm_bwd(Nor
       const f32x8 hat = widen8<R>(now.o[i]) * k2, yh = widen8<T>(now.y[i]) * k1;
       f32x8 total = widen8<R>(now.t[i]);
       if (pre) total += (widen8<T>(now.d[i]) * pre_of(i) - hat * c2) * k2;
-      l.store(static_cast<R*>(a.dr) + at, i, total * a.res_scale);
+      l.store(static_cast<R*>(a.dr) + at, i, total * a.res_scale, a.dr == a.dr_out);
       if (branch) {
         if (with_gate) put(true, i, sum(true, i) + yh * post_of(i) * (total * a.branch_scale));
         f32x8 e = gate_of(i) * total;

@@ -241,3 +241,21 @@ def test_gradient_is_the_difference_of_what_the_forward_call_computes(jz):
         setattr(c, name, base)
         size = float((getattr(c, grad).double() ** 2).sum() ** 0.5)
         assert abs((loss[0] - loss[1]) / 2e-2 - slope) <= 0.02 * size + 0.02, (name, loss, slope)
+
+
+@pytest.mark.parametrize("C", [513, 1027, 2049, 4103, 8193])
+@pytest.mark.parametrize("post, pre", [(False, False), (True, False), (False, True), (True, True)])
+def test_in_place_where_a_row_ends_in_a_wavefront_of_its_own(jz, C, post, pre):
+    """The last vector of a row then begins among the elements of another wavefront, which may load them later: the same bits in place as out of place."""
+    c = Case(jz, 600, C, per=8, post=post, pre=pre, seed=3)
+    c.forward()
+    r = c.r.clone()
+    n = nans((c.rows, C), c.t) if pre else None
+    jz.jz_norm_residual_fwd(c.desc, r, c.y, c.w_post, c.gate, c.w_pre, r, n, c.k1, c.k2)
+    torch.cuda.synchronize()
+    assert torch.equal(r, c.r_out) and (not pre or torch.equal(n, c.n))
+    c.backward()
+    dr, dy, dgate = c.dr_out.clone(), torch.empty_like(c.dy), torch.empty_like(c.dgate)
+    jz.jz_norm_residual_bwd(c.desc, c.y, c.r_out, c.w_post, c.gate, c.w_pre, c.k1, c.k2, dr, c.dn, dr, dy, c.dw_post, dgate, c.dw_pre, c.ws)
+    torch.cuda.synchronize()
+    assert torch.equal(dr, c.dr) and torch.equal(dy, c.dy) and torch.equal(dgate, c.dgate)
