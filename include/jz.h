@@ -379,17 +379,20 @@ int jz_norm_residual_bwd(const jz_norm_residual_desc* desc, const void* y, const
  * DEVICE, dtype JZ_F16 or JZ_BF16 (JZ_F32: JZ_ERR_UNSUPPORTED).  The two projections, the activation and the product are one
  * kernel; the product is formed from the FP32 sums and rounded once.
  *   h         [rows][hidden] out: what the second product reads, and the backward pass
- *   gate, up  [rows][hidden] out, both or neither: the projections, rounded, for the backward pass; NULL when none follows
+ *   gate, up  [rows][hidden] out, both or neither: the projections, rounded to the storage type as every forward tensor, for the backward
+ *             pass; NULL when none follows
  * jz_ffn_bwd, with dh = dy W_down and act evaluated at the rounded gate:
  *   dup = RNE(dh act(gate)),  dgate = RNE(dh up act'(gate)),  dx = RNE(dgate W_gate + dup W_up)  (one FP32 sum),
  *   dW_gate = RNE(dgate^T x),  dW_up = RNE(dup^T x),  dW_down = RNE(dy^T h)
  *   dx may be NULL (the first block); dw_gate, dw_up, dw_down all or none (frozen weights; x and h may then be NULL).
  * Activations: SILU v sigmoid(v); GELU v Phi(v) by the error function; GELU_TANH its tanh form; RELU with derivative 0 at 0.
- * Sizes: any positive feature counts (multiples of 8 with strides that are multiples of 8 take the LDS-direct kernels), rows >= 0
+ * Sizes: any positive feature counts (operands whose rows are not on 16 bytes are copied into the workspace first), rows >= 0
  * (without rows the weight gradients are zeros).  *_stride: elements from one row to the next of x, y, dx, dy; 0 is dense, below the feature
  * count is JZ_ERR_SHAPE; h, gate, up and the weights are dense.  Feature counts and strides up to 2^24, rows up to 2^31.
- * Workspace: dgate and dup, and partial sums (FP32) of reductions that are split where there are few rows or few features; with less
- * than the backward call's dgate and dup need: JZ_ERR_WORKSPACE, with less than reported otherwise fewer splits. */
+ * Workspace: dgate and dup (backward), copies of operands whose feature count or stride is not a multiple of 8, and partial sums (FP32) of
+ * reductions that are split where there are few rows or few features.  With less than dgate and dup need: JZ_ERR_WORKSPACE.  With less than
+ * reported otherwise: fewer splits, and without room for the copies a kernel that needs none, at about half the rate.  Results then differ by the order of FP32
+ * sums.  A workspace that is announced has to be there: JZ_ERR_WORKSPACE for NULL with ws_bytes > 0.  A forward call of at most 64 rows needs none. */
 enum { JZ_ACT_SILU = 0, JZ_ACT_GELU = 1, JZ_ACT_GELU_TANH = 2, JZ_ACT_RELU = 3 };
 typedef struct {
   int64_t rows;

@@ -8,8 +8,18 @@
 //               dx         A = dgate, then dup KC     B = W_gate, then W_up MC         (one sum over 2 F)
 //               dW         A = dgate, dup, dy MC      B = x, x, h MC                    (three products in one launch)
 //
-// Tiles.  BM x BN x 64, four wavefronts in 2 x 2, each (BM / 2) x (BN / 2) in 32x32x16 matrix instructions with the operands exchanged, so
-// that a lane has four consecutive n of one m.  Two tiles of operands in LDS:
+// Bound: the matrix instructions, that is the clock the card keeps under them (1.5 to 1.8 GHz; they are busy 54 to 70 % of it), with enough rows; with few
+// rows or features the tiles that the chip has at a time, and the memory where those are few.  Measured, FP16, silu: 16384 rows, 4096 -> 12288 -> 4096 forward
+// 1.24 PFLOP/s in BF16; 8192 rows, 2048 -> 5632 -> 2048 forward and backward 1.05 PFLOP/s.
+//
+// Roundings.  Sums are FP32; h is made from the unrounded gate and up.  What one call leaves for another is in the storage type, as every forward and
+// backward tensor is: gate and up, and dgate and dup, which the matrix instructions take in 16 bits anyway.  A weight gradient has three such roundings behind it
+// (relative 2^-12 each in FP16) instead of the one of its own store.  Saving gate and up in FP32 would double what the forward pass leaves;
+// making them again backward would add two products to the nine of a training step.
+//
+// Tiles.  256 x 256 x 64 by eight wavefronts in 2 x 4, each 128 x 64, one workgroup a compute unit; 128 x 128 x 64 by four in 2 x 2, each 64 x 64, two a compute
+// unit, where there are too few of the others (jz_ffn.hip: choose).  (256 x 256 by four wavefronts of 128 x 128: 8 % slower, no registers left for reads ahead.)
+// 32x32x16 matrix instructions with the operands exchanged, so that a lane has four consecutive n of one m.  Two tiles of operands in LDS:
 //     KC  [row][8 chunks of 16 bytes], chunk c at position c ^ (row / 2 % 8); an operand is one 16-byte read (16 lanes at a time reach 256 bytes of
 //         banks, two rows: c ^ (row % 8) left every read with a conflict)
 //     MC  [k][ROWS / 8 chunks], chunk c at position c ^ 4 (k % 4); an operand is two 8-byte transposing reads
@@ -18,8 +28,6 @@
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 template <class T>
 using Op8 = typename Vec8<T>::V;
@@ -173,7 +181,7 @@ struct Staged {
 };
 
 // Which tile of which product a workgroup has.  Consecutive workgroups land on different XCDs, each with an L2 of its own, so every XCD gets a run of
-// tiles, and within a run four rows of tiles are taken column by column: what a run reads at a time is then a block.
+// tiles, and within a run four rows of tiles are taken column by column: what a run reads at a time is then a block.  (Eight and sixteen rows: within 2 %.)
 struct Tile {
   int product, split;  // split < 0: the whole sum
   unsigned m, n, behind;  // behind: number among the tiles that are split
@@ -306,7 +314,7 @@ __device__ __forceinline__ void finish(const GemmArgs& a, const Product& p, f32x
   }
 }
 
-// Any sizes, any alignment: the operands pass through registers on their way into LDS, the next tile's while a tile is multiplied.  Loads are full vectors without
+// Any sizes, any alignment, at about half the rate of the LDS-direct kernels: the operands pass through registers on their way into LDS, the next tile's while a tile is multiplied.  Loads are full vectors without
 // branches (global memory takes them at any alignment), from where the element is or would be: rows outside are the last row, and what follows a row's end belongs to
 // no result, or to the end of the sum, where it is cleared.  Only the vectors that would pass the tensor's last element are loaded one by one.
 template <class T, bool KC>
@@ -471,7 +479,8 @@ struct Source {
   }
 };
 
-// The order of a step's instructions: between one matrix instruction and the next a read of LDS or a load.
+// The order of a step's instructions: between one matrix instruction and the next a read of LDS or a load.  (In the compiler's order, all reads first, 8192 rows, 2048 ->
+// 5632 features take 10 % longer.)
 template <int MULTIPLY, int READ, int LOAD>
 __device__ __forceinline__ void spread_out() {
   constexpr int OTHER = READ + LOAD;
