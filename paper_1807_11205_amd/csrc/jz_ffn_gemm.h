@@ -41,10 +41,27 @@ constexpr int BK = 64;
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
 constexpr float GELU_K = 0.7978845608028654f, GELU_C = 0.044715f;  // sqrt(2 / pi)
 
+// Phi, the normal distribution function, and bell(v) = exp(-v^2 / 2).  Phi(-|v|) = bell(v) t P(t) with t = 1 / (1 + 0.35 |v|): the factor of the bell is smooth and falls like
+// 1 / |v|, and P, of degree 8, was fitted to it for the least largest relative error, 3.2e-8 up to |v| = 14; with the exponent's rounding the result is within
+// 10 (1 + |v|) 2^-24 of itself.  One exponential serves the slope too.  (By erfcf a training pass over 8192 rows, 2048 -> 5632 features took 6 % longer.)
+__device__ __forceinline__ float normal(float v, float* bell) {
+  constexpr float P[9] = {0.139621407f, 0.139861897f, 0.119832709f, 0.105508648f, -0.0231113750f, 0.159176439f, -0.255716264f, 0.143972680f, -0.0291461349f};
+  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(v), 0.35f, 1.f));
+  float p = P[8];
+#pragma unroll
+  for (int i = 7; i >= 0; --i) p = fmaf(p, t, P[i]);
+  *bell = __builtin_amdgcn_exp2f(v * v * -0.72134752f);  // log2(e) / 2
+  const float tail = t * p * *bell;
+  return v < 0.f ? tail : 1.f - tail;
+}
+
 __device__ __forceinline__ float act_fwd(int kind, float g) {
   if (kind == JZ_ACT_SILU) return g * sigmoid(g);
   if (kind == JZ_ACT_GELU_TANH) return g * sigmoid(2.f * GELU_K * (g + GELU_C * g * g * g));  // (1 + tanh z) / 2 = sigmoid(2 z)
-  if (kind == JZ_ACT_GELU) return 0.5f * g * erfcf(g * -0.7071067811865476f);
+  if (kind == JZ_ACT_GELU) {
+    float bell;
+    return g * normal(g, &bell);
+  }
   return !(g <= 0.f) ? g : 0.f;
 }
 // act and its derivative
@@ -61,8 +78,9 @@ __device__ __forceinline__ float act_both(int kind, float g, float* slope) {
     return g * s;
   }
   if (kind == JZ_ACT_GELU) {
-    const float phi = 0.5f * erfcf(g * -0.7071067811865476f);
-    *slope = phi + g * __expf(-0.5f * g * g) * 0.3989422804014327f;
+    float bell;
+    const float phi = normal(g, &bell);
+    *slope = phi + g * bell * 0.3989422804014327f;  // 1 / sqrt(2 pi)
     return g * phi;
   }
   *slope = !(g <= 0.f) ? 1.f : 0.f;
