@@ -230,14 +230,19 @@ class Aligner {
  public:
   explicit Aligner(Scratch* room) : room_(room) {}
   static size_t bytes(const Matrix& m) { return m.ld % 8 || m.cols % 8 ? (size_t)m.rows * round8(m.cols) * 2 + 255 & ~size_t(255) : 0; }
-  Matrix operator()(const Matrix& m) {
+  Matrix room(const Matrix& m) {  // where the copy will lie
     const size_t n = bytes(m);
     if (!n || m.rows == 0) return m;
     const Matrix to = {room_->p, m.rows, m.cols, round8(m.cols)};
-    c_.m[c_.count++] = {m.p, room_->p, m.rows, m.cols, m.ld, to.ld, blocks_};
-    blocks_ += (m.rows * (to.ld / 8) + 255) / 256;
     room_->p = static_cast<char*>(room_->p) + n;
     room_->bytes -= n;
+    return to;
+  }
+  Matrix operator()(const Matrix& m) {
+    const Matrix to = room(m);
+    if (to.p == m.p) return m;
+    c_.m[c_.count++] = {m.p, const_cast<void*>(to.p), m.rows, m.cols, m.ld, to.ld, blocks_};
+    blocks_ += (m.rows * (to.ld / 8) + 255) / 256;
     return to;
   }
   template <class T>
@@ -324,16 +329,17 @@ int run_fwd(const FfnShape& s, int act, Operands o, void* h, void* gate, void* u
     o.wg = align(o.wg);
     o.wu = align(o.wu);
     o.wd = align(o.wd);
+    o.h = align.room(o.h);
     const int rc = align.run<T>(st);
     if (rc != JZ_OK) return rc;
   }
-  Scratch rest = ws;
-  Aligner align(&rest);
-  const Matrix h_copy = o.copied ? align(o.h) : o.h;  // made behind the first product
-  int rc = gemm<T, true, true, EPI_GLU>(glu_args(s, act, o, h, gate, up), rest, st);
-  if (rc == JZ_OK && o.copied) rc = align.run<T>(st);
-  o.h = h_copy;
-  return rc == JZ_OK ? gemm<T, true, true, EPI_STORE>(down_args(s, o, y), rest, st) : rc;
+  GemmArgs first = glu_args(s, act, o, h, gate, up);
+  if (o.h.p != h) {  // the first product writes both
+    first.padded = const_cast<void*>(o.h.p);
+    first.ld_padded = o.h.ld;
+  }
+  const int rc = gemm<T, true, true, EPI_GLU>(first, ws, st);
+  return rc == JZ_OK ? gemm<T, true, true, EPI_STORE>(down_args(s, o, y), ws, st) : rc;
 }
 
 template <class T>

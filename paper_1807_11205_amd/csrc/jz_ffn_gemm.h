@@ -108,6 +108,8 @@ struct GemmArgs {
   float* partial;           // [tiles behind `full`][splits][BM][BN]
   const void *gate, *up;    // EPI_GLU_BWD: the saved projections, [M][N]
   void *out0, *out1;        // EPI_GLU: gate and up, or NULL; EPI_GLU_BWD: dgate and dup
+  void* padded;             // EPI_GLU: h once more, rows of ld_padded elements that end in zeros, or NULL
+  int64_t ld_padded;
 };
 
 // dgate and dup of eight elements from dh = v
@@ -121,7 +123,8 @@ __device__ __forceinline__ void glu_bwd8(int act, f32x8 v, f32x8 g, f32x8 u, f32
 }
 
 // ---- results --------------------------------------------------------------------------------------------------------------
-// dgate and dup lie in the workspace, rows a multiple of 8 long and zero behind their end: they are operands of the next products
+// dgate and dup, and where its own rows are not on 16 bytes a second h, lie in the workspace, rows a multiple of 8 long and zero behind their end: they are
+// operands of the next products
 template <class T>
 __device__ __forceinline__ void store_padded(T* p, f32x8 v, int left) {
 #pragma unroll
@@ -141,6 +144,7 @@ __device__ __forceinline__ void finish8(const GemmArgs& a, const Product& p, int
 #pragma unroll
     for (int i = 0; i < 8; ++i) h[i] = act_fwd(a.act, v[i]) * w[i];
     store8(static_cast<T*>(p.c) + m * p.ldc + n, narrow8<T>(h), left);
+    if (a.padded) store_padded<T>(static_cast<T*>(a.padded) + m * a.ld_padded + n, h, left);
     if (a.out0) {
       store8(static_cast<T*>(a.out0) + m * p.N + n, narrow8<T>(v), left);
       store8(static_cast<T*>(a.out1) + m * p.N + n, narrow8<T>(w), left);
