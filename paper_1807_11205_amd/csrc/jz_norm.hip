@@ -395,7 +395,14 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void norm_join(NormArgs a, int64_t
     const size_t pitch = (size_t)4 * a.C;
     int64_t k = lo;
     if (what >= 2 && k == from && k < hi) s = at[k++ * pitch + a.C];
-    for (; k < hi; k += 8) {
+    for (; k + 8 <= hi; k += 8) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = at[(k + i) * pitch];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += v[i];
+    }
+    if (k < hi) {
       float v[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = at[(k + i < hi ? k + i : hi - 1) * pitch];
@@ -417,7 +424,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void norm_join(NormArgs a, int64_t
 
 // ---- host ---------------------------------------------------------------------------------------------------------------
 constexpr int NORM_MAX_C = 16384;
-constexpr int NORM_SLABS = 512;  // at most; half as many where a workgroup of the backward pass fills a compute unit
+constexpr int NORM_SLABS = 512;  // half as many where a workgroup of the backward pass fills a compute unit
 
 struct Tensor {
   const void* p;
@@ -446,10 +453,12 @@ int norm_shape(const jz_norm_residual_desc* d, int64_t* groups, int64_t* per) {
   *groups = d->rows_per_group ? d->rows / *per : 1;
   return JZ_OK;
 }
-// A slab's sums are 16 bytes a channel; slabs of at least 8 rows, so that they are a small part of what moves.
+// A slab's sums are 16 bytes a channel, so slabs should be long, but a slab's rows follow one another, so they should be many.  At least four rows (BF16, both directions, at least
+// eight: 1000 rows of 768 channels 20.8 us, four: 17.4; 333 rows of 4096: 30.1 and 20.3).  Up to 1024 channels, where a workgroup is one or two wavefronts, twice as many from
+// 32 rows each on (65536 rows of 512 channels: 190 us with 512, 147 with 1024; 4096 rows of 1024 channels 30 and 34, which is why not below).
 int64_t slab_rows(int64_t rows, int channels) {
-  const int most = channels > 2048 ? NORM_SLABS / 2 : NORM_SLABS;
-  return std::max<int64_t>(8, (rows + most - 1) / most);
+  const int most = channels > 2048 ? NORM_SLABS / 2 : channels <= 1024 && rows >= 32 * NORM_SLABS ? 2 * NORM_SLABS : NORM_SLABS;
+  return std::max<int64_t>(4, (rows + most - 1) / most);
 }
 int slab_count(int64_t rows, int channels) { return (int)((rows + slab_rows(rows, channels) - 1) / slab_rows(rows, channels)); }
 

@@ -259,3 +259,12 @@ def test_in_place_where_a_row_ends_in_a_wavefront_of_its_own(jz, C, post, pre):
     jz.jz_norm_residual_bwd(c.desc, c.y, c.r_out, c.w_post, c.gate, c.w_pre, c.k1, c.k2, dr, c.dn, dr, dy, c.dw_post, dgate, c.dw_pre, c.ws)
     torch.cuda.synchronize()
     assert torch.equal(dr, c.dr) and torch.equal(dy, c.dy) and torch.equal(dgate, c.dgate)
+
+
+@pytest.mark.parametrize("rows, per", [(16383, 0), (16384, 0), (16385, 0), (20480, 40), (16384, 128), (2047, 23), (1999, 0), (203, 7)])
+def test_slabs_of_many_and_of_few_rows(jz, rows, per):
+    c = Case(jz, rows, 72, "bf16", per=per, seed=5)
+    c.forward()
+    c.backward()
+    c.check_forward()
+    c.check_backward()
