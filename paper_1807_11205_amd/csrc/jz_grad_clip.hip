@@ -23,7 +23,6 @@ namespace {
 
 constexpr uint64_t CLIP_MAGIC = 0x70696c6367726164ull;
 constexpr int CLIP_THREADS = 256;
-constexpr int64_t CLIP_CHUNK = 16384;  // elements; 8 vectors of 8 a lane
 constexpr int CLIP_GRID = 2048;        // workgroups at most: 8 a compute unit
 
 struct ClipChunk {
@@ -32,8 +31,12 @@ struct ClipChunk {
   int count, dtype;
 };
 
+// Elements of a chunk: eight vectors of eight a lane, or one where a list is so short that its chunks would not fill the chip (FP16: 400 000 elements in 24 tensors
+// 8.5 us with the longer, 7.6 with the shorter; 1 million 9.2 and 7.6, 2 million 9.2 and 9.3, 4.1 million 10.9 and 12.3).
+int64_t chunk_of(int64_t elements) { return elements <= int64_t(3) << 19 ? 2048 : 16384; }
+
 struct ClipLayout {
-  int64_t n_chunks = 0;
+  int64_t chunk = 0, n_chunks = 0;
   size_t off_chunks = 0, static_bytes = 0, off_psum = 0, total = 0;
   int grid = 0;
 };
@@ -46,7 +49,7 @@ int clip_layout(const jz_grad_list* gl, ClipLayout* L) {
   if (gl->num_tensors < 0) return JZ_ERR_SHAPE;
   if (gl->num_tensors > 0 && (!gl->grads || !gl->numel || !gl->dtypes)) return JZ_ERR_NULL;
   if (gl->num_tensors >= (int64_t(1) << 24)) return JZ_ERR_UNSUPPORTED;
-  int64_t chunks = 0;
+  int64_t elements = 0, chunks = 0;
   for (int64_t t = 0; t < gl->num_tensors; ++t) {
     const int64_t n = gl->numel[t];
     if (n < 0 || gl->dtypes[t] < JZ_F16 || gl->dtypes[t] > JZ_F32) return JZ_ERR_SHAPE;
@@ -55,9 +58,12 @@ int clip_layout(const jz_grad_list* gl, ClipLayout* L) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(gl->grads[t]), o = gl->out ? reinterpret_cast<uintptr_t>(gl->out[t]) : a;
     if (!a || !o) return JZ_ERR_NULL;
     if (((a | o) & (elem_bytes(gl->dtypes[t]) - 1)) != 0) return JZ_ERR_ALIGN;
-    chunks += (n + CLIP_CHUNK - 1) / CLIP_CHUNK;
-    if (chunks >= (int64_t(1) << 30)) return JZ_ERR_UNSUPPORTED;
+    elements += n;
+    if (elements >= (int64_t(1) << 44)) return JZ_ERR_UNSUPPORTED;
   }
+  L->chunk = chunk_of(elements);
+  for (int64_t t = 0; t < gl->num_tensors; ++t) chunks += (gl->numel[t] + L->chunk - 1) / L->chunk;
+  if (chunks >= (int64_t(1) << 30)) return JZ_ERR_UNSUPPORTED;
   L->n_chunks = chunks;
   L->grid = (int)std::min<int64_t>(chunks, CLIP_GRID);
   size_t o = up256(64);
@@ -290,8 +296,8 @@ int prepare(const jz_grad_list* gl, const ClipLayout& L, void* ws, size_t ws_byt
     const int b = elem_bytes(gl->dtypes[t]);
     const char* in = static_cast<const char*>(gl->grads[t]);
     char* out = gl->out ? static_cast<char*>(gl->out[t]) : const_cast<char*>(in);
-    for (int64_t at = 0; at < gl->numel[t]; at += CLIP_CHUNK)
-      *c++ = ClipChunk{in + at * b, out + at * b, (int)std::min(CLIP_CHUNK, gl->numel[t] - at), gl->dtypes[t]};
+    for (int64_t at = 0; at < gl->numel[t]; at += L.chunk)
+      *c++ = ClipChunk{in + at * b, out + at * b, (int)std::min(L.chunk, gl->numel[t] - at), gl->dtypes[t]};
   }
   if (hipMemcpyAsync(ws, host.data(), L.static_bytes, hipMemcpyHostToDevice, st) != hipSuccess) return JZ_ERR_LAUNCH;
   return hipStreamSynchronize(st) == hipSuccess ? JZ_OK : JZ_ERR_LAUNCH;

@@ -242,3 +242,19 @@ def test_overlaps_are_refused_before_anything_runs(jz):
     assert status([ws[:64].view(torch.float32)]) == jz.JZ_ERR_ALIAS
     assert status([a], None, ws[:64]) == jz.JZ_ERR_WORKSPACE
     assert torch.all(v == 1)
+
+
+@pytest.mark.parametrize("sizes", [(1572864,), (1572865,), (1572864 - 2049, 2048, 1), (16384 * 90, 16385, 1, 100001, 0, 16383, 8197)])
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_lists_of_short_and_of_long_chunks(jz, dtype, sizes):
+    g = np.random.default_rng((7, len(sizes), sizes[0]))
+    _, grads = views(g, sizes, TYPES[dtype], 0.5)
+    before = [wide(v) for v in grads]
+    r = Run(jz, grads, None)
+    exact, _, _ = blocks.grad_clip(before, math.inf, 4.0)
+    _, _, c = blocks.grad_clip(before, exact * 0.125, 4.0)
+    norm, flag = r.clip(exact * 0.125, loss_scale=4.0)
+    check_norm(norm, exact)
+    assert flag == 0
+    for o, b in zip(grads, before):
+        check_out(o, b, c)
