@@ -10,6 +10,7 @@ this package.  It shares nothing with the HIP library and never imports it.
 * the dynamic loss-scale controller around that update (``loss_scale.py``).
 * batch normalization + ReLU (Section 4.2's formulas) and its gradient, fp64 numpy (``bn.py``).
 * the small layers between the convolutions (residual add, pooling, bias, softmax loss), fp64 numpy (``layers.py``).
+* the gated feed-forward block, the norms around it, clipping by the global norm, fp64 numpy (``blocks.py``).
 """
 import ctypes
 import os

@@ -5,7 +5,7 @@
 // Two launches over a table of chunks.  The first leaves one partial sum of squares a workgroup; the second adds those up in every
 // workgroup (in one order, so all of them have the same bits), forms c and scales.  What bounds it: memory.  A gradient is read
 // twice and written once, and the second pass takes the chunks in the reverse order, so that it begins with what the first
-// read last and the 256 MiB last-level cache still holds.
+// read last and the 256 MiB last-level cache still holds.  25.6 M FP16 elements 33 us, 600 M of BF16 729 us (4.9 TB/s of the three passes), 400 000 8 us (launches).
 //
 // Numbers: eight squares are added in FP32, which holds the square of an FP16 value exactly; everything above that is FP64.  BF16 and FP32
 // values whose squares leave the FP32 range are squared again in FP64, so the sum is not finite exactly if a gradient is not.
