@@ -9,8 +9,8 @@
 //               dW         A = dgate, dup, dy MC      B = x, x, h MC                    (three products in one launch)
 //
 // Bound: the matrix instructions, that is the clock the card keeps under them (1.5 to 1.8 GHz; they are busy 54 to 70 % of it), with enough rows; with few
-// rows or features the tiles that the chip has at a time, and the memory where those are few.  Measured, FP16, silu: 16384 rows, 4096 -> 12288 -> 4096 forward
-// 1.24 PFLOP/s in BF16; 8192 rows, 2048 -> 5632 -> 2048 forward and backward 1.05 PFLOP/s.
+// rows or features the tiles that the chip has at a time, and the memory where those are few.  Measured, silu: 16384 rows, 4096 -> 12288 -> 4096 forward
+// 1.16 to 1.24 PFLOP/s in BF16 (cards differ); FP16, 8192 rows, 2048 -> 5632 -> 2048 forward and backward, 1.02 to 1.05.
 //
 // Roundings.  Sums are FP32; h is made from the unrounded gate and up.  What one call leaves for another is in the storage type, as every forward and
 // backward tensor is: gate and up, and dgate and dup, which the matrix instructions take in 16 bits anyway.  A weight gradient has three such roundings behind it
