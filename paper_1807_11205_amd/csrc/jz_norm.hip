@@ -55,8 +55,9 @@ __device__ __forceinline__ f32x8 splat8(float v) { return f32x8{v, v, v, v, v, v
 
 // Which elements of a row a lane has: NV vectors of eight, vector i from element 8 (i THREADS + lane) on.  Loads are not predicated, so that all of a row's are on
 // their way at once: a vector that would pass the row's end is the row's last eight elements instead, and what of it lies outside the lane's own part is left
-// out of the sums.  What a lane then stores a second time are the bits that their owner stores, except in place, where the owner, in another wavefront, may not have
-// loaded them yet: there a lane stores its own elements alone.
+// out of the sums.  What a lane then stores a second time are the bits that their owner stores, except where the call works in place and the owner is in another
+// wavefront: the owner may not have loaded yet, or, where no barrier lies between a row's loads and its stores (forward without a post-norm), have stored already, so that
+// all that this lane makes of those elements is wrong.  There a lane stores its own elements alone, of every result.  (Backward a barrier lies between: dr alone needs it.)
 //   EVEN   channels are a multiple of 8: a vector is a lane's own or nobody's        RAGGED   others from 8 on: the last vector overlaps its neighbour
 //   TINY   less than 8: one vector, element by element
 #define JZ_GLOBAL __attribute__((address_space(1)))
@@ -163,7 +164,7 @@ __global__ __launch_bounds__(THREADS >= 256 ? THREADS : 256) void norm_fwd(NormA
     const float k2 = 1.f / sqrtf(row_sum<THREADS>(s, lds[1]) * a.inv_c + a.eps);
     if (l.lane == 0) a.rstd_pre[row] = k2;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) l.store(static_cast<T*>(a.n) + row * a.C, i, o[i] * k2 * w[i]);
+    for (int i = 0; i < NV; ++i) l.store(static_cast<T*>(a.n) + row * a.C, i, o[i] * k2 * w[i], a.r_out == a.r);
   }
 }
 
