@@ -145,16 +145,31 @@ class GatedMLP:
 
     # ---- answers -------------------------------------------------------------------------------------------------------
     def answer(self, x: torch.Tensor, stream=None) -> torch.Tensor:
-        """Logits (float16) of the rows of x (float32 [any number of rows, width]), nothing kept for a backward pass."""
+        """Logits (float16) of the rows of x (float32 [any number of rows, width]), nothing kept for a backward pass.  x is as the current stream
+        leaves it; the logits are ready once `stream` is (None: the current one)."""
+        current = torch.cuda.current_stream(self.device)
+        if stream is None or api._stream(stream) == api._stream(current):
+            return self._answer(x)
+        if not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream), self.device) if int(stream) else torch.cuda.default_stream(self.device)
+        stream.wait_stream(current)
+        with torch.cuda.stream(stream):         # copies, temporaries and launches all belong to it
+            logits = self._answer(x)
+        x.record_stream(stream)
+        logits.record_stream(current)
+        return logits
+
+    def _answer(self, x):
+        """On the current stream."""
         rows, D, F = x.shape[0], self.width, self.hidden
         m = lambda n: self._param(self.master, n)
         ffn, around = api.ffn_desc(rows, D, F, D, api.JZ_ACT_SILU, api.JZ_F16), self._around(rows)
         r, n, y, h, k1, k2 = x.to(torch.float32).clone(), self._buf((rows, D)), self._buf((rows, D)), self._buf((rows, F)), self._buf(rows, torch.float32), self._buf(rows, torch.float32)
         logits = self._buf((rows, self.classes))
         ws = self._buf(max(16, api.jz_ffn_fwd_workspace_bytes(ffn), api.jz_gemm_fc_workspace_bytes(api.JZ_FWD, rows, D, self.classes)), torch.uint8)
-        api.jz_norm_residual_fwd(around, r, None, None, None, m("w_pre_0"), None, n, None, k2, stream)
+        api.jz_norm_residual_fwd(around, r, None, None, None, m("w_pre_0"), None, n, None, k2)
         for i in range(self.blocks):
-            api.jz_ffn_fwd(ffn, n, *self._ffn_weights(i), h, y, ws=ws, stream=stream)
-            api.jz_norm_residual_fwd(around, r, y, m("w_post_%d" % i), m("gate_%d" % i), m("w_pre_%d" % (i + 1)), r, n, k1, k2, stream)
-        api.jz_gemm_fc(api.JZ_FWD, rows, D, self.classes, n, self._param(self.w16, "w_fc"), logits, ws, stream)
+            api.jz_ffn_fwd(ffn, n, *self._ffn_weights(i), h, y, ws=ws)
+            api.jz_norm_residual_fwd(around, r, y, m("w_post_%d" % i), m("gate_%d" % i), m("w_pre_%d" % (i + 1)), r, n, k1, k2)
+        api.jz_gemm_fc(api.JZ_FWD, rows, D, self.classes, n, self._param(self.w16, "w_fc"), logits, ws)
         return logits

@@ -1,0 +1,38 @@
+"""The stack of gated blocks on a stream that is not torch's current one, with other work in front of both."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+CYCLES = 50_000_000         # some tens of milliseconds
+
+
+def make(**kw):
+    from paper_1807_11205_amd.gated_mlp import GatedMLP
+    return GatedMLP(96, 128, 352, 40, 2, **kw)
+
+
+def rows(n):
+    return torch.from_numpy(np.random.default_rng(n).standard_normal((n, 128)) * 2).float().cuda()
+
+
+@pytest.mark.parametrize("n", [1, 70])
+@pytest.mark.parametrize("how", ["stream", "handle"])
+@pytest.mark.parametrize("late", ["current", "other"])
+def test_answers_on_another_stream(n, how, late):
+    m, s = make(), torch.cuda.Stream()
+    x = rows(n)
+    want = m.answer(x)
+    torch.cuda.synchronize()
+    source, late_x = x.clone(), torch.zeros_like(x)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.current_stream() if late == "current" else s):
+        torch.cuda._sleep(CYCLES)
+    late_x.copy_(source)                        # on the current stream, behind what it is busy with
+    got = m.answer(late_x, s if how == "stream" else s.cuda_stream)
+    # memory that was given back too early would be handed out here, and written before the answer is made
+    others = [torch.full((n, c), float("nan"), dtype=t, device="cuda") for c in (128, 352, 40) for t in (torch.float16, torch.float32) for _ in range(4)]
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(got, want)
+    torch.cuda.synchronize()
+    assert all(torch.isnan(o).all() for o in others)
