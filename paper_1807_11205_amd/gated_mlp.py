@@ -140,7 +140,8 @@ class GatedMLP:
         self.update(stream)
 
     def mean_loss(self) -> float:
-        """Of the last forward pass (synchronizes)."""
+        """Of the last forward pass, on whatever stream it ran (synchronizes)."""
+        torch.cuda.synchronize(self.device)
         return float(self.loss.double().mean().item())
 
     # ---- answers -------------------------------------------------------------------------------------------------------

@@ -36,3 +36,16 @@ def test_answers_on_another_stream(n, how, late):
     assert torch.equal(got, want)
     torch.cuda.synchronize()
     assert all(torch.isnan(o).all() for o in others)
+
+
+def test_the_mean_loss_of_a_step_on_another_stream():
+    a, b, s = make(), make(), torch.cuda.Stream()
+    x, labels = rows(96), torch.arange(96, dtype=torch.int32, device="cuda") % 40
+    for m in (a, b):
+        m.set_batch(x, labels)
+    a.step()
+    want = a.mean_loss()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(CYCLES)
+    b.step(s)
+    assert b.mean_loss() == want and want > 0
