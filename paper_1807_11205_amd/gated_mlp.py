@@ -85,6 +85,7 @@ class GatedMLP:
         need = [api.jz_ffn_fwd_workspace_bytes(self.ffn), api.jz_ffn_bwd_workspace_bytes(self.ffn), api.jz_norm_residual_bwd_workspace_bytes(self.around)]
         need += [api.jz_gemm_fc_workspace_bytes(mode, rows, D, classes) for mode in (api.JZ_FWD, api.JZ_BWD_DATA, api.JZ_BWD_WEIGHT)]
         self.ws = torch.zeros(max(16, *need), dtype=torch.uint8, device=self.device)
+        torch.cuda.current_stream(self.device).synchronize()    # whatever stream a step runs on, the buffers' fills are behind it
 
     # ---- buffers and parameter views --------------------------------------------------------------------------------
     def _buf(self, shape, dtype=torch.float16):
@@ -101,10 +102,11 @@ class GatedMLP:
         return tuple(self._param(self.w16, "%s_%d" % (n, i)) for n in ("w_gate", "w_up", "w_down"))
 
     # ---- the step ------------------------------------------------------------------------------------------------------
-    def set_batch(self, x: torch.Tensor, labels: torch.Tensor):
-        """r_0 (float32 [rows, width]) and the classes of the rows."""
-        self.r[0].copy_(x)
-        self.labels.copy_(labels)
+    def set_batch(self, x: torch.Tensor, labels: torch.Tensor, stream=None):
+        """r_0 (float32 [rows, width]) and the classes of the rows, copied on the stream of the step that takes them."""
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+            self.r[0].copy_(x)
+            self.labels.copy_(labels)
 
     def forward(self, stream=None):
         m = lambda n: self._param(self.master, n)

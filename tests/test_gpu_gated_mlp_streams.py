@@ -49,3 +49,18 @@ def test_the_mean_loss_of_a_step_on_another_stream():
         torch.cuda._sleep(CYCLES)
     b.step(s)
     assert b.mean_loss() == want and want > 0
+
+
+def test_buffers_are_filled_and_batches_come_before_a_step_on_any_stream():
+    a, s = make(), torch.cuda.Stream()
+    x, labels = rows(96), torch.arange(96, dtype=torch.int32, device="cuda") % 40
+    a.set_batch(x, labels)
+    a.step()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(CYCLES)
+    b = make()
+    assert torch.cuda.current_stream().query()
+    torch.cuda._sleep(CYCLES)                   # a copy on the current stream would come too late
+    b.set_batch(x, labels, stream=s)
+    b.step(s)
+    assert b.mean_loss() == a.mean_loss() and torch.equal(a.master, b.master) and torch.equal(a.grad, b.grad)
