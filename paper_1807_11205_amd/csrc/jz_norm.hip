@@ -21,7 +21,8 @@ namespace {
 
 struct NormArgs {
   int64_t rows, rows_per_group, slab;
-  int64_t step;  // backward: from one of a slab's rows to the next
+  int64_t step;   // backward: from one of a slab's rows to the next
+  int64_t first;  // forward: the launch's first row
   int C;
   float eps, res_scale, branch_scale, inv_c;
   const void *r, *y;
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(THREADS >= 256 ? THREADS : 256) void norm_fwd(NormA
   __shared__ float lds[2][THREADS >= 256 ? THREADS / 64 : 1];
   const bool branch = a.y, post = a.w_post, with_gate = a.gate, pre = a.n;
   const Lane<MODE, THREADS> l = {a.C, (int)threadIdx.x % THREADS};
-  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
+  const int64_t row = a.first + (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
   if (row >= a.rows) return;  // whole wavefronts; with one row a workgroup the grid ends with the rows
   typename Vec8<R>::V rv[NV];
   typename Vec8<T>::V yv[NV];
@@ -534,7 +535,11 @@ extern "C" int jz_norm_residual_fwd(const jz_norm_residual_desc* d, const void* 
   with_types(d, [&](auto te, auto re) {
     with_lanes<true>(d->channels, [&](auto mode, auto th, auto nv) {
       constexpr int TH = decltype(th)::value, ROWS = TH >= 256 ? 1 : 256 / TH;
-      norm_fwd<decltype(te), decltype(re), decltype(mode)::value, TH, decltype(nv)::value><<<(unsigned)((a.rows + ROWS - 1) / ROWS), TH >= 256 ? TH : 256, 0, st>>>(a);
+      constexpr int64_t LANES = TH >= 256 ? TH : 256, MOST = (int64_t(1) << 32) / LANES - 1;  // a launch has fewer than 2^32 lanes
+      for (int64_t all = (a.rows + ROWS - 1) / ROWS, done = 0; done < all; done += MOST) {
+        a.first = done * ROWS;
+        norm_fwd<decltype(te), decltype(re), decltype(mode)::value, TH, decltype(nv)::value><<<(unsigned)std::min(all - done, MOST), (unsigned)LANES, 0, st>>>(a);
+      }
     });
   });
   return jz::launch_status();

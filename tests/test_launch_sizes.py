@@ -1,0 +1,104 @@
+"""Grids of the residual-block operators over the whole range of what their descriptors accept (no GPU: launches are recorded by a library in front of the HIP
+runtime, in a process of its own).  A launch has fewer than 2^32 lanes along x and at most 65535 workgroups along y, else the runtime refuses it."""
+import ctypes
+import json
+import os
+import subprocess
+import sys
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROOT = os.path.dirname(HERE)
+A = 1 << 50             # tensors' addresses, far apart; never followed
+
+
+class Recorded:
+    """In the child process: the library behind the recorder."""
+
+    def __init__(self, recorder):
+        self.rec = ctypes.CDLL(recorder, mode=ctypes.RTLD_GLOBAL)
+        self.lib = ctypes.CDLL(os.path.join(ROOT, "paper_1807_11205_amd", "libjz.so"))
+
+    def call(self, name, *args):
+        self.rec.forget()
+        conv = [a if not isinstance(a, int) or isinstance(a, bool) else ctypes.c_void_p(a) for a in args]
+        status = getattr(self.lib, name)(*conv)
+        out = (ctypes.c_uint * 6)()
+        grids = []
+        for i in range(min(self.rec.launches(), 4096)):
+            self.rec.launch(i, out)
+            grids.append(list(out))
+        return dict(status=status, launches=self.rec.launches(), grids=grids)
+
+
+def tensors(n):
+    return [A * (i + 1) for i in range(n)]
+
+
+def norm_desc(rows, channels, dtype=0):
+    class D(ctypes.Structure):
+        _fields_ = [("rows", ctypes.c_int64), ("channels", ctypes.c_int), ("rows_per_group", ctypes.c_int64), ("dtype", ctypes.c_int), ("res_dtype", ctypes.c_int),
+                    ("eps", ctypes.c_float), ("res_scale", ctypes.c_float), ("branch_scale", ctypes.c_float)]
+    return D(rows, channels, 0, dtype, dtype, 1e-5, 1.0, 1.0)
+
+
+def child(recorder, job):
+    r = Recorded(recorder)
+    print(json.dumps([JOBS[job["job"]](r, *c) for c in job["cases"]]))
+
+
+def norm_forward(r, rows, channels):
+    d = norm_desc(rows, channels)
+    return r.call("jz_norm_residual_fwd", ctypes.byref(d), *tensors(9), None)
+
+
+def norm_backward(r, rows, channels):
+    d, n = norm_desc(rows, channels), ctypes.c_size_t(0)
+    r.lib.jz_norm_residual_bwd_workspace_bytes(ctypes.byref(d), ctypes.byref(n))
+    return r.call("jz_norm_residual_bwd", ctypes.byref(d), *tensors(15), ctypes.c_size_t(n.value), None)
+
+
+JOBS = dict(norm_forward=norm_forward, norm_backward=norm_backward)
+
+
+@pytest.fixture(scope="module")
+def recorder(tmp_path_factory):
+    from paper_1807_11205_amd import api
+    if not os.path.exists(api.LIB_PATH):
+        from paper_1807_11205_amd import build
+        build.build()
+    out = tmp_path_factory.mktemp("recorder") / "librecorder.so"
+    subprocess.run([os.environ.get("CC", "gcc"), "-O1", "-shared", "-fPIC", "-o", str(out), os.path.join(HERE, "launch_recorder.c")], check=True)
+    return str(out)
+
+
+def run(recorder, job, cases):
+    r = subprocess.run([sys.executable, os.path.abspath(__file__), recorder, json.dumps(dict(job=job, cases=cases))], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr
+    return list(zip(cases, json.loads(r.stdout.splitlines()[-1])))
+
+
+def fits(g):
+    return all(v > 0 for v in g) and g[0] * g[3] < 1 << 32 and g[1] <= 65535 and g[2] <= 65535
+
+
+ROWS = [1, 5, 1 << 20, (1 << 24) - 1, 1 << 24, (1 << 24) + 1, (1 << 26) - 4, 1 << 26, (1 << 26) + 3, (1 << 30) + 7, (1 << 31) - 256]
+
+
+def test_norms_forward(recorder):
+    for (rows, channels), got in run(recorder, "norm_forward", [(m, c) for m in ROWS for c in (1, 8, 64, 512, 1000, 1024, 1025, 4096, 8192, 16384)]):
+        assert got["status"] == 0 and got["launches"] >= 1, (rows, channels, got)
+        assert all(fits(g) for g in got["grids"]), (rows, channels, got)
+        each = 4 if channels <= 1024 else 1
+        assert sum(g[0] for g in got["grids"]) == -(-rows // each), (rows, channels, got)
+
+
+def test_norms_backward(recorder):
+    for (rows, channels), got in run(recorder, "norm_backward", [(m, c) for m in ROWS for c in (1, 8, 64, 512, 1000, 1024, 1025, 4096, 8192, 16384)]):
+        assert got["status"] == 0 and got["launches"] == 2, (rows, channels, got)
+        assert all(fits(g) for g in got["grids"]), (rows, channels, got)
+
+
+if __name__ == "__main__":
+    child(sys.argv[1], json.loads(sys.argv[2]))
