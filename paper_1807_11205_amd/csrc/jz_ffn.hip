@@ -43,10 +43,10 @@ int ffn_shape(const jz_ffn_desc* d, FfnShape* s) {
   *s = {d->rows, in, d->hidden, out, d->x_stride ? d->x_stride : in, d->y_stride ? d->y_stride : out, d->dx_stride ? d->dx_stride : in,
         d->dy_stride ? d->dy_stride : out};
   if (s->ldx < in || s->ldy < out || s->lddx < in || s->lddy < out) return JZ_ERR_SHAPE;
-  // a tensor's bytes stay far inside 64 bits, tile counts inside a grid
-  const int64_t most = int64_t(1) << 24;
-  if (d->dtype == JZ_F32 || d->rows > (int64_t(1) << 31) || in > most || d->hidden > most || out > most || std::max(std::max(s->ldx, s->ldy), std::max(s->lddx, s->lddy)) > most)
-    return JZ_ERR_UNSUPPORTED;
+  const int64_t most = int64_t(1) << 24, wide = std::max(std::max(s->ldx, s->ldy), std::max(s->lddx, s->lddy));
+  if (d->dtype == JZ_F32 || d->rows > (int64_t(1) << 31) || in > most || d->hidden > most || out > most || wide > most) return JZ_ERR_UNSUPPORTED;
+  // tensors larger than any card's memory; below, tiles are counted in 32 bits (at most 2^27 in a launch)
+  if (std::max(std::max(d->rows * std::max<int64_t>(wide, d->hidden), d->hidden * in), d->hidden * out) > int64_t(1) << 38) return JZ_ERR_UNSUPPORTED;
   return JZ_OK;
 }
 // bytes from the first to the last element of rows x cols with a row pitch
@@ -94,11 +94,18 @@ int64_t count_tiles(const GemmArgs& a, int epi, int tile) {
 }
 size_t partial_bytes(const FfnPlan& p, int64_t tiles) { return p.splits > 1 ? (size_t)(tiles - p.full) * p.splits * p.tile * p.tile * 4 : 0; }
 
+constexpr int64_t LANES = int64_t(1) << 32;  // a launch has fewer
+
 template <class T, bool KCA, bool KCB, int EPI, int ACT>
-void launch_tiles(const GemmArgs& a, int tile, unsigned grid, hipStream_t st) {
-  if (!direct<KCA, KCB>(a)) ffn_gemm_any<T, KCA, KCB, EPI, ACT, 128, 128><<<grid, 256, 0, st>>>(a);
-  else if (tile == 256) ffn_gemm<T, KCA, KCB, EPI, ACT, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
-  else ffn_gemm<T, KCA, KCB, EPI, ACT, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
+void launch_tiles(GemmArgs a, int tile, hipStream_t st) {
+  const bool lds_direct = direct<KCA, KCB>(a);
+  const unsigned threads = lds_direct && tile == 256 ? 512 : 256, most = (unsigned)(LANES / threads - 1);
+  for (a.first = 0; a.first < a.workgroups; a.first += most) {
+    const unsigned grid = std::min(a.workgroups - a.first, most);
+    if (!lds_direct) ffn_gemm_any<T, KCA, KCB, EPI, ACT, 128, 128><<<grid, threads, 0, st>>>(a);
+    else if (tile == 256) ffn_gemm<T, KCA, KCB, EPI, ACT, 256, 256, 2, 4><<<grid, threads, 0, st>>>(a);
+    else ffn_gemm<T, KCA, KCB, EPI, ACT, 128, 128, 2, 2><<<grid, threads, 0, st>>>(a);
+  }
 }
 
 template <class T, bool KCA, bool KCB, int EPI>
@@ -111,12 +118,12 @@ int launch(GemmArgs a, const FfnPlan& plan, const Scratch& ws, hipStream_t st) {
   a.splits = plan.splits;
   a.tiles_per_split = (int)((k_tiles(a) + plan.splits - 1) / plan.splits);
   a.partial = static_cast<float*>(ws.p);
-  const unsigned grid = full + split * plan.splits;
-  if (EPI != EPI_GLU_BWD || a.act == 0) launch_tiles<T, KCA, KCB, EPI, 0>(a, plan.tile, grid, st);
+  a.workgroups = (unsigned)(full + split * plan.splits);
+  if (EPI != EPI_GLU_BWD || a.act == 0) launch_tiles<T, KCA, KCB, EPI, 0>(a, plan.tile, st);
   else if constexpr (EPI == EPI_GLU_BWD) {
-    if (a.act == 1) launch_tiles<T, KCA, KCB, EPI, 1>(a, plan.tile, grid, st);
-    else if (a.act == 2) launch_tiles<T, KCA, KCB, EPI, 2>(a, plan.tile, grid, st);
-    else launch_tiles<T, KCA, KCB, EPI, 3>(a, plan.tile, grid, st);
+    if (a.act == 1) launch_tiles<T, KCA, KCB, EPI, 1>(a, plan.tile, st);
+    else if (a.act == 2) launch_tiles<T, KCA, KCB, EPI, 2>(a, plan.tile, st);
+    else launch_tiles<T, KCA, KCB, EPI, 3>(a, plan.tile, st);
   }
   if (jz::launch_status() != JZ_OK) return JZ_ERR_LAUNCH;
   if (split > 0) {
@@ -247,7 +254,7 @@ class Aligner {
   }
   template <class T>
   int run(hipStream_t st) {
-    if (c_.count) ffn_copy<T><<<(unsigned)blocks_, 256, 0, st>>>(c_);
+    for (c_.first = 0; c_.first < blocks_; c_.first += LANES / 256 - 1) ffn_copy<T><<<(unsigned)std::min(blocks_ - c_.first, LANES / 256 - 1), 256, 0, st>>>(c_);
     return jz::launch_status();
   }
 

@@ -105,6 +105,7 @@ struct GemmArgs {
   int act;
   int full;                 // tiles that one workgroup computes; of each further one `splits` workgroups take tiles_per_split k tiles
   int splits, tiles_per_split;
+  unsigned workgroups, first;  // of the product; the first of this launch's
   float* partial;           // [tiles behind `full`][splits][BM][BN]
   const void *gate, *up;    // EPI_GLU_BWD: the saved projections, [M][N]
   void *out0, *out1;        // EPI_GLU: gate and up, or NULL; EPI_GLU_BWD: dgate and dup
@@ -221,13 +222,13 @@ __device__ __forceinline__ void place_tile(const GemmArgs& a, unsigned t, Tile* 
 }
 __device__ __forceinline__ Tile find_tile(const GemmArgs& a) {
   Tile w;
-  const unsigned full = a.full;
-  if (blockIdx.x < full) {
+  const unsigned full = a.full, number = a.first + blockIdx.x;
+  if (number < full) {
     w.split = -1;
     w.behind = 0;
-    place_tile(a, xcd_remap(blockIdx.x, full), &w);
+    place_tile(a, xcd_remap(number, full), &w);
   } else {
-    const unsigned i = blockIdx.x - full, rest = (gridDim.x - full) / a.splits;
+    const unsigned i = number - full, rest = (a.workgroups - full) / a.splits;
     w.split = i / rest;
     w.behind = i % rest;
     place_tile(a, full + w.behind, &w);
@@ -624,13 +625,15 @@ struct Copies {
     int64_t rows, cols, ld, pitch, first;  // first: its first block
   } m[6];
   int count;
+  int64_t first;  // the launch's first block
 };
 template <class T>
 __global__ __launch_bounds__(256) void ffn_copy(Copies c) {
+  const int64_t block = c.first + blockIdx.x;
   int q = 0;
-  while (q + 1 < c.count && blockIdx.x >= c.m[q + 1].first) ++q;
+  while (q + 1 < c.count && block >= c.m[q + 1].first) ++q;
   const Copies::One& o = c.m[q];
-  const int64_t i = ((int64_t)blockIdx.x - o.first) * 256 + threadIdx.x, per = o.pitch / 8, row = i / per, col = (i - row * per) * 8;
+  const int64_t i = (block - o.first) * 256 + threadIdx.x, per = o.pitch / 8, row = i / per, col = (i - row * per) * 8;
   if (row >= o.rows) return;
   const int64_t left = o.cols - col;
   store8(static_cast<T*>(o.to) + row * o.pitch + col, load8(static_cast<const T*>(o.from) + row * o.ld + col, left < 8 ? (int)left : 8));

@@ -10,7 +10,7 @@ import pytest
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-A = 1 << 50             # tensors' addresses, far apart; never followed
+A = 1 << 58             # tensors' addresses, far apart; never followed
 
 
 class Recorded:
@@ -59,7 +59,32 @@ def norm_backward(r, rows, channels):
     return r.call("jz_norm_residual_bwd", ctypes.byref(d), *tensors(15), ctypes.c_size_t(n.value), None)
 
 
-JOBS = dict(norm_forward=norm_forward, norm_backward=norm_backward)
+def ffn_desc(rows, D, F, O):
+    class D_(ctypes.Structure):
+        _fields_ = [("rows", ctypes.c_int64), ("in_features", ctypes.c_int), ("hidden", ctypes.c_int), ("out_features", ctypes.c_int), ("act", ctypes.c_int),
+                    ("dtype", ctypes.c_int), ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64), ("dy_stride", ctypes.c_int64)]
+    return D_(rows, D, F, O, 0, 0, 0, 0, 0, 0)
+
+
+def ffn_forward(r, rows, D, F, O, all_of_it):
+    d, n = ffn_desc(rows, D, F, O), ctypes.c_size_t(0)
+    status = r.lib.jz_ffn_fwd_workspace_bytes(ctypes.byref(d), ctypes.byref(n))
+    if not all_of_it:
+        n.value = 0
+    got = r.call("jz_ffn_fwd", ctypes.byref(d), *tensors(9), n, None)
+    return dict(got, asked=status)
+
+
+def ffn_backward(r, rows, D, F, O, all_of_it):
+    d, n = ffn_desc(rows, D, F, O), ctypes.c_size_t(0)
+    status = r.lib.jz_ffn_bwd_workspace_bytes(ctypes.byref(d), ctypes.byref(n))
+    if not all_of_it:
+        n.value = 2 * ((rows * ((F + 7) // 8 * 8) * 2 + 255) // 256 * 256)
+    got = r.call("jz_ffn_bwd", ctypes.byref(d), *tensors(13), n, None)
+    return dict(got, asked=status)
+
+
+JOBS = dict(ffn_forward=ffn_forward, ffn_backward=ffn_backward, norm_forward=norm_forward, norm_backward=norm_backward)
 
 
 @pytest.fixture(scope="module")
@@ -98,6 +123,31 @@ def test_norms_backward(recorder):
     for (rows, channels), got in run(recorder, "norm_backward", [(m, c) for m in ROWS for c in (1, 8, 64, 512, 1000, 1024, 1025, 4096, 8192, 16384)]):
         assert got["status"] == 0 and got["launches"] == 2, (rows, channels, got)
         assert all(fits(g) for g in got["grids"]), (rows, channels, got)
+
+
+# rows and features whose tensors have up to 2^38 elements each
+BLOCKS = [(m, d, f, o) for m in (1, 64, 65, 1 << 20, (1 << 30) + 1, (1 << 31) - 1, 1 << 31)
+          for d, f, o in ((1, 1, 1), (8, 8, 8), (9, 8, 1), (64, 64, 64), (64, 65, 64), (127, 128, 120), (1000, 2730, 1000), (1 << 14, 1 << 14, 1 << 14), (1 << 24, 8, 8),
+                          (8, 1 << 24, 8), (1, (1 << 24) - 1, 1), (1, 1, 1 << 24), ((1 << 24) - 3, 9, 1 << 24))
+          if m * max(d, f, o) <= 1 << 38]
+
+
+@pytest.mark.parametrize("job", ["ffn_forward", "ffn_backward"])
+@pytest.mark.parametrize("all_of_it", [True, False])
+def test_feed_forward_block(recorder, job, all_of_it):
+    for (m, d, f, o, _), got in run(recorder, job, [(*b, all_of_it) for b in BLOCKS]):
+        assert got["status"] == got["asked"] == 0 and got["launches"] >= 2, (m, d, f, o, got)
+        assert all(fits(g) for g in got["grids"]), (m, d, f, o, got)
+        if m > 64:              # every product of the rows' has a workgroup for each of its tiles, which are 256 x 256 at most
+            cols = (2 * ((f + 31) // 32 * 32), o) if job == "ffn_forward" else (f, d)
+            assert sum(g[0] * g[1] for g in got["grids"]) >= sum(-(-m // 256) * -(-c // 256) for c in cols), (m, d, f, o, got)
+
+
+def test_blocks_larger_than_any_memory_are_refused(recorder):
+    sizes = [(1 << 31, 129, 8, 8), (1 << 31, 8, 129, 8), (1 << 31, 8, 8, 129), (1, 1 << 24, (1 << 14) + 1, 8), (1, 8, 1 << 24, (1 << 14) + 1), (1 << 31, 1 << 24, 1 << 24, 1 << 24)]
+    for job in ("ffn_forward", "ffn_backward"):
+        for c, got in run(recorder, job, [(*z, False) for z in sizes]):
+            assert got["status"] == got["asked"] == -3 and got["launches"] == 0, (c, got)
 
 
 if __name__ == "__main__":
