@@ -138,17 +138,24 @@ __device__ __forceinline__ double chunk_sumsq(const T* __restrict__ p, int n, in
   return s;
 }
 
-template <class T>
-__device__ __forceinline__ void chunk_scale(const T* in, T* out, int n, float c, int lane) {
+// c g in FP32, from a factor in FP32 or, where that would be below FP32's smallest normal number (exploded gradients of FP32 or BF16), in FP64
+__device__ __forceinline__ f32x8 scaled8(f32x8 v, float c) { return v * c; }
+__device__ __forceinline__ f32x8 scaled8(f32x8 v, double c) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (float)((double)v[i] * c);
+  return v;
+}
+template <class T, class F>
+__device__ __forceinline__ void chunk_scale(const T* in, T* out, int n, F c, int lane) {
   int i = lane * 8;
   for (; i + 3 * CLIP_THREADS * 8 + 8 <= n; i += 4 * CLIP_THREADS * 8) {
     typename Vec8<T>::V v[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = load8(in + i + k * CLIP_THREADS * 8);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) store8(out + i + k * CLIP_THREADS * 8, narrow8<T>(widen8<T>(v[k]) * c));
+    for (int k = 0; k < 4; ++k) store8(out + i + k * CLIP_THREADS * 8, narrow8<T>(scaled8(widen8<T>(v[k]), c)));
   }
-  for (; i < n; i += CLIP_THREADS * 8) store8(out + i, narrow8<T>(widen8<T>(load8(in + i, n - i)) * c), n - i);
+  for (; i < n; i += CLIP_THREADS * 8) store8(out + i, narrow8<T>(scaled8(widen8<T>(load8(in + i, n - i)), c)), n - i);
 }
 template <class T>
 __device__ __forceinline__ void chunk_copy(const T* in, T* out, int n, int lane) {  // bit for bit: a NaN keeps its payload
@@ -179,7 +186,7 @@ __global__ __launch_bounds__(CLIP_THREADS) void grad_sumsq(ClipArgs a) {
 }
 
 // The norm from the partial sums, the same bits in every workgroup; workgroup 0 writes it and the flag.  Returns the factor.
-__device__ __forceinline__ float join_norm(const ClipArgs& a, double* lds) {
+__device__ __forceinline__ double join_norm(const ClipArgs& a, double* lds) {
   double s = 0.;
 #pragma unroll
   for (int k = 0; k < CLIP_GRID / CLIP_THREADS; ++k) {
@@ -194,7 +201,7 @@ __device__ __forceinline__ float join_norm(const ClipArgs& a, double* lds) {
     *a.norm = (float)norm;
     *a.found_inf = bad ? 1 : 0;
   }
-  return !bad && norm > (double)a.max_norm ? (float)((double)a.max_norm / norm) : 1.f;
+  return !bad && norm > (double)a.max_norm ? (double)a.max_norm / norm : 1.;
 }
 
 __global__ __launch_bounds__(CLIP_THREADS) void grad_norm_final(ClipArgs a) {
@@ -209,7 +216,8 @@ __global__ __launch_bounds__(CLIP_THREADS) void grad_norm_final(ClipArgs a) {
   join_norm(a, lds);
 }
 
-__global__ __launch_bounds__(CLIP_THREADS) void grad_scale(ClipArgs a) {
+// 64 registers a lane, so that all of the workgroups are on the chip at once (the FP64 form would take 70)
+__global__ __launch_bounds__(CLIP_THREADS, 8) void grad_scale(ClipArgs a) {
   __shared__ double lds[CLIP_THREADS / 64];
   if (!list_ok(a)) {
     if (blockIdx.x == 0 && threadIdx.x == 0) {
@@ -218,17 +226,22 @@ __global__ __launch_bounds__(CLIP_THREADS) void grad_scale(ClipArgs a) {
     }
     return;
   }
-  const float f = join_norm(a, lds);
+  const double exact = join_norm(a, lds);
+  const float f = (float)exact;
+  const bool tiny = exact < 0x1p-126 && exact > 0.;
   for (int c = a.n_chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
     const ClipChunk r = a.chunks[c];
     if (f == 1.f && r.in == r.out) continue;
     if (r.dtype == JZ_F32) {
       if (f == 1.f) chunk_copy(static_cast<const float*>(r.in), static_cast<float*>(r.out), r.count, threadIdx.x);
+      else if (tiny) chunk_scale(static_cast<const float*>(r.in), static_cast<float*>(r.out), r.count, exact, threadIdx.x);
       else chunk_scale(static_cast<const float*>(r.in), static_cast<float*>(r.out), r.count, f, threadIdx.x);
     } else if (f == 1.f) {
       chunk_copy(static_cast<const _Float16*>(r.in), static_cast<_Float16*>(r.out), r.count, threadIdx.x);
     } else if (r.dtype == JZ_F16) {
-      chunk_scale(static_cast<const _Float16*>(r.in), static_cast<_Float16*>(r.out), r.count, f, threadIdx.x);
+      chunk_scale(static_cast<const _Float16*>(r.in), static_cast<_Float16*>(r.out), r.count, f, threadIdx.x);  // of a tiny factor zeros, in FP16 as in FP32
+    } else if (tiny) {
+      chunk_scale(static_cast<const __bf16*>(r.in), static_cast<__bf16*>(r.out), r.count, exact, threadIdx.x);
     } else {
       chunk_scale(static_cast<const __bf16*>(r.in), static_cast<__bf16*>(r.out), r.count, f, threadIdx.x);
     }
