@@ -42,8 +42,9 @@ __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf
 constexpr float GELU_K = 0.7978845608028654f, GELU_C = 0.044715f;  // sqrt(2 / pi)
 
 // Phi, the normal distribution function, and bell(v) = exp(-v^2 / 2).  Phi(-|v|) = bell(v) t P(t) with t = 1 / (1 + 0.35 |v|): the factor of the bell is smooth and falls like
-// 1 / |v|, and P, of degree 8, was fitted to it for the least largest relative error, 3.2e-8 up to |v| = 14; with the exponent's rounding the result is within
-// 10 (1 + |v|) 2^-24 of itself.  One exponential serves the slope too.  (By erfcf a training pass over 8192 rows, 2048 -> 5632 features took 6 % longer.)
+// 1 / |v|, and P, of degree 8, was fitted to it for the least
+// largest relative error, 7.7e-8 with the coefficients rounded to FP32, up to |v| = 14; with the exponent's rounding the result is within 10 (1 + |v|) 2^-24 of
+// itself.  One exponential serves the slope too.  (By erfcf a training pass over 8192 rows, 2048 -> 5632 features took 6 % longer.)
 __device__ __forceinline__ float normal(float v, float* bell) {
   constexpr float P[9] = {0.139621407f, 0.139861897f, 0.119832709f, 0.105508648f, -0.0231113750f, 0.159176439f, -0.255716264f, 0.143972680f, -0.0291461349f};
   const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(v), 0.35f, 1.f));
