@@ -143,6 +143,34 @@ def test_feed_forward_block(recorder, job, all_of_it):
             assert sum(g[0] * g[1] for g in got["grids"]) >= sum(-(-m // 256) * -(-c // 256) for c in cols), (m, d, f, o, got)
 
 
+# (product, tile, are sums shared) by sizes; test_gpu_block_variants.py compares the results of these
+PLANS = [((7536, 8, 1928, 648), "dh", 256, False), ((7048, 56, 2464, 2552), "dh", 256, True), ((136, 8, 8, 696), "dh", 128, True), ((2240, 2120, 3664, 16), "glu", 256, True),
+         ((968, 120, 7032, 4192), "down", 256, True), ((8136, 136, 5944, 152), "dw", 256, True), ((8272, 416, 3640, 40), "dx", 256, True), ((136, 672, 8, 8), "glu", 128, True),
+         ((80, 8, 696, 8), "down", 128, True), ((672, 8, 8, 8), "dw", 128, True), ((152, 8, 360, 8), "dx", 128, True)]
+
+
+def readings(grids, products):
+    """What the launches of a call may be: a product's tiles (512 or 256 lanes) each, and one that joins, which has tile^2 / 8 / 256 workgroups along x (half as many
+    for gate and up)."""
+    if not products:
+        return [] if grids else [{}]
+    if not grids:
+        return []
+    tile = 256 if grids[0][3] == 512 else 128
+    res = [{products[0]: (tile, False), **r} for r in readings(grids[1:], products[1:])]
+    if len(grids) > 1 and grids[1][0] == tile * tile // (4096 if products[0] == "glu" else 2048) and grids[1][3] == 256:
+        res += [{products[0]: (tile, True), **r} for r in readings(grids[2:], products[1:])]
+    return res
+
+
+def test_sizes_that_stand_for_a_plan_have_it(recorder):
+    got = {job: dict((tuple(c[:4]), g["grids"]) for c, g in run(recorder, job, [(*p[0], True) for p in PLANS])) for job in ("ffn_forward", "ffn_backward")}
+    for size, product, tile, shared in PLANS:
+        forward = product in ("glu", "down")
+        found = {r[product] for r in readings(got["ffn_forward" if forward else "ffn_backward"][size], ["glu", "down"] if forward else ["dh", "dx", "dw"])}
+        assert (tile, shared) in found and (tile == 128 or len(found) == 1), (size, product, found)
+
+
 def test_blocks_larger_than_any_memory_are_refused(recorder):
     sizes = [(1 << 31, 129, 8, 8), (1 << 31, 8, 129, 8), (1 << 31, 8, 8, 129), (1, 1 << 24, (1 << 14) + 1, 8), (1, 8, 1 << 24, (1 << 14) + 1), (1 << 31, 1 << 24, 1 << 24, 1 << 24)]
     for job in ("ffn_forward", "ffn_backward"):
