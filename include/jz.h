@@ -311,7 +311,8 @@ enum { JZ_F16 = 0, JZ_BF16 = 1, JZ_F32 = 2 };
 /* Global norm of the gradients of many tensors, and clipping by it, on gradients that carry a loss scale S:
  *   norm = sqrt( sum over all tensors and elements of g^2 ) / S       (squares of eight elements added in FP32, or in FP64 where they leave
  *                                                                      its range; everything above in FP64; fixed order)
- *   out  = RNE( c * g ),  c = max_norm / norm where norm > max_norm, else 1: the loss scale stays in the gradients
+ *   out  = RNE( c * g ),  c = max_norm / norm where norm > max_norm, else 1: the loss scale stays in the gradients  (c in FP32, in FP64
+ *                                                                      where FP32 has no normal number for it; one further rounding in FP32)
  * found_inf_dev (DEVICE int): 1 if an element is +-Inf or NaN, else 0; with 1 (the norm is then Inf or NaN) and whenever
  * c = 1 the gradients are not scaled: out receives a copy, in place nothing is written.  norm_dev: DEVICE float.  S is state_dev->scale when
  * state_dev (DEVICE, as in jz_lars_mp_update_dyn) is not NULL, else loss_scale (> 0).  Clip before the optimiser sees the
@@ -343,7 +344,8 @@ int jz_grad_clip(const jz_grad_list* list, float max_norm, float loss_scale, con
  *   p     = y * rstd(y) * w_post               (the norm after the block; p = y where w_post is NULL)
  *   r_out = res_scale * r + branch_scale * gate * p          (gate: one row of channels for each group of rows; 1 where NULL)
  *   n     = r_out * rstd(r_out) * w_pre        (the norm before the next block)
- * FP32 arithmetic and sums, one rounding to the type of each output; n is formed from the unrounded r_out.
+ * FP32 arithmetic and sums, one rounding to the type of each output; n is formed from the unrounded r_out.  (Squares too are FP32: values
+ * beyond 1.8e19 overflow them, and the row's rstd is 0.)
  *   r, r_out: DEVICE [rows][channels] res_dtype, the residual stream.  r_out may be r.  y, n: DEVICE [rows][channels] dtype.
  *   w_post, w_pre: DEVICE FP32 [channels], gate: DEVICE FP32 [groups][channels] (master precision)
  *   rstd_post, rstd_pre: DEVICE FP32 [rows], written forward, read backward; each may be NULL where its norm is not asked for
@@ -354,10 +356,10 @@ int jz_grad_clip(const jz_grad_list* list, float max_norm, float loss_scale, con
  *     R  = dr_out + rstd_pre * (w_pre dn - r^ mean(w_pre dn r^)),  r^ = r_out rstd_pre          dw_pre = sum over rows of dn r^
  *     dr = res_scale * R                                              dgate = sum over the group's rows of branch_scale p R
  *     dp = branch_scale gate R,   dw_post = sum over rows of dp y^,   dy = rstd_post * (w_post dp - y^ mean(w_post dp y^)),  y^ = y rstd_post
- *   (dy = dp without a post-norm).  r_out is the tensor that the forward call wrote (r itself for the norm alone, with dy == NULL).
+ *   (dy = dp without a post-norm).  r_out is the tensor that the forward call wrote, rounded to its type (r itself for the norm alone, with dy == NULL).
  *   dr: res_dtype, may be dr_out.  dy: dtype.  dw_post, dgate, dw_pre: dtype, as an optimiser's gradient buffer takes them (they carry whatever
  *   loss scale dr_out and dn carry); required where w_post, gate, dn are given.  The sums over rows are FP32 in a fixed order.
- * Shapes: rows >= 0 (no rows: parameter gradients are zeros), channels from 1 to 16384, any number (odd ones too); res_dtype is dtype
+ * Shapes: rows from 0 (parameter gradients are zeros then) to 2^31 - 256, channels from 1 to 16384, any number (odd ones too); res_dtype is dtype
  * or JZ_F32.  rows_per_group divides rows; 0 is one group.  JZ_ERR_SHAPE / JZ_ERR_UNSUPPORTED otherwise. */
 typedef struct {
   int64_t rows;
@@ -378,7 +380,8 @@ int jz_norm_residual_bwd(const jz_norm_residual_desc* desc, const void* y, const
  * x [rows][in_features], W_gate and W_up [hidden][in_features], W_down [out_features][hidden], y [rows][out_features], all
  * DEVICE, dtype JZ_F16 or JZ_BF16 (JZ_F32: JZ_ERR_UNSUPPORTED).  The two projections, the activation and the product are one
  * kernel; the product is formed from the FP32 sums and rounded once.
- *   h         [rows][hidden] out: what the second product reads, and the backward pass
+ *   h         [rows][hidden] out: what the second product reads, and the backward pass; rounded to the storage type, so in FP16 a product beyond
+ *             65504 is Inf in h, and y then Inf or NaN
  *   gate, up  [rows][hidden] out, both or neither: the projections, rounded to the storage type as every forward tensor, for the backward
  *             pass; NULL when none follows
  * jz_ffn_bwd, with dh = dy W_down and act evaluated at the rounded gate:
@@ -388,7 +391,9 @@ int jz_norm_residual_bwd(const jz_norm_residual_desc* desc, const void* y, const
  * Activations: SILU v sigmoid(v); GELU v Phi(v) by the error function; GELU_TANH its tanh form; RELU with derivative 0 at 0.
  * Sizes: any positive feature counts (operands whose rows are not on 16 bytes are copied into the workspace first), rows >= 0
  * (without rows the weight gradients are zeros).  *_stride: elements from one row to the next of x, y, dx, dy; 0 is dense, below the feature
- * count is JZ_ERR_SHAPE; h, gate, up and the weights are dense.  Feature counts and strides up to 2^24, rows up to 2^31.
+ * count is JZ_ERR_SHAPE; h, gate, up and the weights are dense.  Feature counts and strides up to 2^24, rows up to 2^31, a tensor
+ * (strided: with what lies between its rows) up to 2^38 elements; JZ_ERR_UNSUPPORTED beyond.  Outputs overlap nothing, where a strided tensor reaches from its first
+ * element to its last: column slices of one buffer overlap (JZ_ERR_ALIAS).
  * Workspace: dgate and dup (backward), copies of operands whose feature count or stride is not a multiple of 8, and partial sums (FP32) of
  * reductions that are split where there are few rows or few features.  With less than dgate and dup need: JZ_ERR_WORKSPACE.  With less than
  * reported otherwise: fewer splits, and without room for the copies a kernel that needs none, at about half the rate.  Results then differ by the order of FP32

@@ -42,7 +42,9 @@ __device__ __forceinline__ void few_finish(const GemmArgs& a, const Product& p, 
   }
 }
 
-// Any sizes, any alignment (BF16, 24 rows, 5632 -> 2048 features in this kernel 17.0 us, in the next 7.2): weights go straight into the registers that the matrix instruction takes them from, UNROLL steps of 32 k ahead.
+// Any sizes, any alignment: weights go straight into the registers that the matrix instruction takes them from, UNROLL steps of 32 k ahead.  Slower than the next kernel at
+// aligned sizes (BF16, 24 rows, 5632 -> 2048 features 17.0 us and 7.2), and slower still where rows are not: both products of 24 rows, 2048 -> 5632 -> 2048 features, take 20 us
+// there, 38 at 2046 -> 5630 -> 2046 (rows on 4 bytes) and 105 at 2047 -> 5631 -> 2047 (on 2).
 template <class T, bool GLU, int TT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void ffn_few_any(GemmArgs a) {
   constexpr int MATS = GLU ? 2 : 1, UNROLL = TT == 1 && WAVES < 16 ? 4 : (TT == 4 ? 2 : 4) / MATS;  // as registers allow
@@ -126,7 +128,7 @@ __global__ __launch_bounds__(64 * WAVES) void ffn_few_any(GemmArgs a) {
 
 // Rows that are multiples of 8: LDS-direct loads of 8 rows x 128 bytes, whole lines, into places of the wavefront's own, so that it waits for nobody.  (Loads in
 // the matrix instruction's layout, 16 rows x 64 bytes, bring a compute unit 17 bytes a clock.)  FP16, one row, 4096 -> 12288 -> 4096 forward in both products:
-// 53 us, the weights at 5.7 TB/s; BF16, 24 rows, 2048 -> 5632 -> 2048: 21 us.  A stage is 64 CH k of the weights' and the tokens' rows, chunk c of a row at c ^ (row / 2 % 8); two stages.
+// 53 us, the weights at 5.7 TB/s (other weights every time: 56 us); BF16, 2048 -> 5632 -> 2048 features: 21 us for 24 rows, 26 for 40, 32 for 64.  A stage is 64 CH k of the weights' and the tokens' rows, chunk c of a row at c ^ (row / 2 % 8); two stages.
 template <class T, bool GLU, int TT, int WAVES, int CH>
 __global__ __launch_bounds__(64 * WAVES) void ffn_few(GemmArgs a) {
   constexpr int MATS = GLU ? 2 : 1, ROWS = 16 * (MATS + TT), CHUNK = ROWS * 128, STAGE = CHUNK * CH;

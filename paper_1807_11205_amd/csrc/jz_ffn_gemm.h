@@ -13,9 +13,10 @@
 // 1.16 to 1.24 PFLOP/s in BF16 (cards differ); FP16, 8192 rows, 2048 -> 5632 -> 2048 forward and backward, 1.02 to 1.05.
 //
 // Roundings.  Sums are FP32; h is made from the unrounded gate and up.  What one call leaves for another is in the storage type, as every forward and
-// backward tensor is: gate and up, and dgate and dup, which the matrix instructions take in 16 bits anyway.  A weight gradient has three such roundings behind it
-// (relative 2^-12 each in FP16) instead of the one of its own store.  Saving gate and up in FP32 would double what the forward pass leaves;
-// making them again backward would add two products to the nine of a training step.
+// backward tensor is: gate and up, and dgate and dup, which the matrix instructions take in 16 bits anyway.  A weight gradient and
+// dx have four such roundings behind them (up, gate through the slope, dgate or dup, their own store; relative 2^-12 each in FP16) instead of the last alone: against 64 bits
+// 1.8 to 1.9 times the error of one.  y has two (h and its own), 1.4 times.  In 16 bits h, dgate and dup are what the matrix instructions take; gate and up are a choice: in FP32
+// they would double what the forward pass leaves, and making them again backward would add two products to the nine of a training step.
 //
 // Tiles.  256 x 256 x 64 by eight wavefronts in 2 x 4, each 128 x 64, one workgroup a compute unit; 128 x 128 x 64 by four in 2 x 2, each 64 x 64, two a compute
 // unit, where there are too few of the others (jz_ffn.hip: choose).  (256 x 256 by four wavefronts of 128 x 128: 8 % slower, no registers left for reads ahead.)

@@ -5,7 +5,7 @@
 // Two launches over a table of chunks.  The first leaves one partial sum of squares a workgroup; the second adds those up in every
 // workgroup (in one order, so all of them have the same bits), forms c and scales.  What bounds it: memory.  A gradient is read
 // twice and written once, and the second pass takes the chunks in the reverse order, so that it begins with what the first
-// read last and the 256 MiB last-level cache still holds.  25.6 M FP16 elements 33 us, 600 M of BF16 729 us (4.9 TB/s of the three passes), 400 000 8 us (launches).
+// read last and the 256 MiB last-level cache still holds.  25.6 M FP16 elements 33 us, 600 M of BF16 728 us (4.9 TB/s of the three passes), 400 000 7 to 9 us (launches).
 //
 // Numbers: eight squares are added in FP32, which holds the square of an FP16 value exactly; everything above that is FP64.  BF16 and FP32
 // values whose squares leave the FP32 range are squared again in FP64, so the sum is not finite exactly if a gradient is not.
@@ -31,8 +31,9 @@ struct ClipChunk {
   int count, dtype;
 };
 
-// Elements of a chunk: eight vectors of eight a lane, or one where a list is so short that its chunks would not fill the chip (FP16: 400 000 elements in 24 tensors
-// 8.5 us with the longer, 7.6 with the shorter; 1 million 9.2 and 7.6, 2 million 9.2 and 9.3, 4.1 million 10.9 and 12.3).
+// Elements of a chunk: eight vectors of eight a lane, or one where a list is so short that its chunks would not fill the chip (FP16, 24 tensors, calls on the same gradients
+// one behind the other: 400 000 elements 8.4 us with the longer, 7.2 with the shorter; 1 million 9.3 and 7.4, 1.5 million 8.8 and 8.4; waited for after every call 21.3 and 19.4, 21.9 and
+// 19.9, 21.3 and 20.8.  2 million: 9.2 with either, 4.1 million 10.9 and 12.3).
 int64_t chunk_of(int64_t elements) { return elements <= int64_t(3) << 19 ? 2048 : 16384; }
 
 struct ClipLayout {
