@@ -413,6 +413,90 @@ int jz_ffn_bwd(const jz_ffn_desc* desc, const void* x, const void* w_gate, const
                const void* up, const void* h, const void* dy, void* dx, void* dw_gate, void* dw_up, void* dw_down, void* ws, size_t ws_bytes,
                void* hip_stream);
 
+/* ---- tokens, orthogonalised updates, 8-bit answers ---------------------------------------------------------------------
+ * Embedding lookup and the gradient of its table, for networks whose rows are tokens:
+ *   jz_embed_fwd   out[t] = RNE( scale * table[ids[t]] )                           table [vocab][channels], out [tokens][channels]
+ *   jz_embed_bwd   dtable[v] = RNE( scale * sum over t with ids[t] == v of dout[t]  [+ dtable[v]] )
+ * ids: DEVICE int32 [tokens], 4-byte aligned.  A token outside [0, vocab) (a masked place) gets a row of zeros, and its row of dout is not
+ * read.  The sum of a row is FP32, in an order that tokens and their positions alone decide (positions are sorted by token on the
+ * device, stably): bit-identical from run to run.  accumulate == 0: every row of dtable is written, zeros where no token stands.  accumulate != 0:
+ * only rows with tokens are, each read, added to in FP32 and rounded once more: for a table that is also the classifier's matrix, whose gradient is
+ * there already.
+ * dtype: of table and dtable (JZ_F16, JZ_BF16, JZ_F32); out_dtype: of out and dout, dtype or JZ_F32 (JZ_ERR_UNSUPPORTED otherwise): an FP32 residual stream.
+ * Any positive channel count; out_stride: elements from one row of out (dout) to the next, 0 is dense.  tokens below 2^31, channels and strides up to 2^24, a tensor up
+ * to 2^38 elements (JZ_ERR_UNSUPPORTED beyond).  The gradient's workspace holds the sorted positions, a byte for each token of the vocabulary and partial sums of frequent
+ * tokens; JZ_ERR_WORKSPACE with less than reported.  scale finite, else JZ_ERR_SHAPE.  tokens == 0: nothing, or zeros in dtable. */
+typedef struct {
+  int64_t tokens;
+  int vocab, channels;
+  int dtype, out_dtype;
+  float scale;
+  int64_t out_stride;
+} jz_embed_desc;
+int jz_embed_fwd(const jz_embed_desc* desc, const int* ids_dev, const void* table, void* out, void* hip_stream);
+int jz_embed_bwd_workspace_bytes(const jz_embed_desc* desc, size_t* bytes);
+int jz_embed_bwd(const jz_embed_desc* desc, const int* ids_dev, const void* dout, int accumulate, void* dtable, void* ws, size_t ws_bytes,
+                 void* hip_stream);
+
+/* Orthogonalised updates of weight matrices, beside LARS for those that are no matrices.  For each of `count` matrices [rows][cols], `stride` elements apart (0: dense):
+ *   X = G / (||G||_F + eps),  then `steps` times   X <- a X + (b A + c A^2) X,  A = X X^T       (X^T in X's place where rows > cols)
+ * a Newton-Schulz iteration: every singular value s of X goes to a s + b s^3 + c s^5 each time, the singular vectors stay.  With a, b, c = 3.4445, -4.7750, 2.0315 and
+ * five steps the values that are not tiny end near 1 (0.7 to 1.2).  a, b, c finite, and such that every element of X, A and b A + c A^2 + a I stays below 31 in magnitude
+ * (results are Inf or NaN otherwise: the products take 22 bits of every element, as two FP16 parts).  Sums are FP32, ||G|| is added up in FP64.
+ *   jz_orthogonalize   x (dtype) -> y (out_dtype), each JZ_F16, JZ_BF16 or JZ_F32, one rounding.  A matrix of zeros gives zeros; one with Inf or NaN NaNs.
+ *   jz_muon_mp_update  one optimiser step in mixed precision; grad16 and weight16 have dtype == out_dtype == JZ_F16 or JZ_BF16:
+ *       g = float(grad16) / S,  v <- momentum v + g,  u = g + momentum v where nesterov, else v,  O = the iteration's result for u (FP32)
+ *       w <- w - lr (update_scale O + weight_decay w),   weight16 = RNE(w)
+ *     S is state_dev->scale when state_dev (DEVICE, as in jz_lars_mp_update_dyn) is not NULL, else hp->loss_scale.  update_scale is the caller's choice, usually
+ *     sqrt(max(1, rows / cols)).  *found_inf_dev (DEVICE int): 1 if a gradient is Inf or NaN, or if skip_dev (DEVICE int, may be NULL: another
+ *     call's flag, as of jz_grad_clip) is not 0, else 0; with 1 nothing else is written.  Call it before jz_lars_mp_update_dyn, which adjusts the scale.  found_inf_dev may be the
+ *     `nonfinite` of a LARS sink (jz_lars_sumsq_sink, after jz_lars_begin_step) of a tensor that no kernel fills, so that the presummed LARS update of the other
+ *     parameters is skipped, and the scale lowered, together with this one.
+ * Sides up to 2^17, count up to 65535, count * stride and the padded matrices up to 2^35 elements, steps 1 to 64 (JZ_ERR_UNSUPPORTED beyond).  Outputs overlap
+ * nothing (a batch reaches from its first element to its last).  The workspace holds the matrices in parts: 20 bytes an element and more; JZ_ERR_WORKSPACE with
+ * less than reported. */
+typedef struct {
+  int64_t count;
+  int rows, cols;
+  int64_t stride;
+  int dtype, out_dtype;
+  int steps;
+  float a, b, c, eps;
+} jz_ortho_desc;
+typedef struct {
+  float lr, momentum, weight_decay, update_scale, loss_scale;
+  int nesterov;
+} jz_muon_hparams;
+int jz_orthogonalize_workspace_bytes(const jz_ortho_desc* desc, size_t* bytes);
+int jz_orthogonalize(const jz_ortho_desc* desc, const void* x, void* y, void* ws, size_t ws_bytes, void* hip_stream);
+int jz_muon_mp_update_workspace_bytes(const jz_ortho_desc* desc, size_t* bytes);
+int jz_muon_mp_update(const jz_ortho_desc* desc, const jz_muon_hparams* hp, const jz_loss_scale_state* state_dev, const int* skip_dev, float* master_w,
+                      float* momentum, const void* grad16, void* weight16, int* found_inf_dev, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Products in 8-bit integers with a scale for each token (row of x) and each channel (row of W), for answers: weights take half the bytes, and the matrix instructions twice
+ * the rate, of FP16.  A row's scale s is max |x| / 127 (FP32 division), its codes q are x / s (FP32 division) rounded to the nearest whole number, ties to
+ * even, and held to +-127; a row of zeros, or one whose s is no positive number, has zeros.  A row with Inf or NaN has codes 0 and scale NaN: every result that it enters is NaN.
+ *   jz_quantize_i8   x [rows][cols] (x_stride elements apart, 0: dense; JZ_F16, JZ_BF16, JZ_F32) -> q, scale [rows] (FP32).  Codes lie in rows of
+ *                    round16(cols) bytes, the multiple of 16 from cols on, zeros behind the last: the layout that the products want of weights.
+ *   jz_linear_i8     y[m][n] = RNE( sum over k of q_x[m][k] q_w[n][k] * (s_x[m] s_w[n]) ): x is quantised row by row in the workspace; the sum is
+ *                    int32 and exact.  x, y: dtype (all three).  in_features up to 131072 (what int32 holds).
+ *   jz_ffn_i8_fwd    the gated block of jz_ffn_fwd with all three matrices in codes: h = act(x W_gate^T) * (x W_up^T) in FP32 from the two products as above,
+ *                    unrounded, then quantised row by row, y = RNE of the third.  dtype JZ_F16 or JZ_BF16; desc as for jz_ffn_fwd (dx_stride, dy_stride not used).
+ * Any positive feature counts, rows >= 0 up to 2^31, other features and strides up to 2^24, a tensor up to 2^38 elements (JZ_ERR_UNSUPPORTED beyond).  Outputs overlap
+ * nothing.  The workspace holds codes and scales of the rows, and h; JZ_ERR_WORKSPACE with less than reported. */
+typedef struct {
+  int64_t rows;
+  int in_features, out_features;
+  int dtype;
+  int64_t x_stride, y_stride;
+} jz_linear_i8_desc;
+int jz_quantize_i8(int64_t rows, int cols, int dtype, const void* x, int64_t x_stride, void* q, float* scale, void* hip_stream);
+int jz_linear_i8_workspace_bytes(const jz_linear_i8_desc* desc, size_t* bytes);
+int jz_linear_i8(const jz_linear_i8_desc* desc, const void* x, const void* wq, const float* w_scale, void* y, void* ws, size_t ws_bytes, void* hip_stream);
+int jz_ffn_i8_workspace_bytes(const jz_ffn_desc* desc, size_t* bytes);
+int jz_ffn_i8_fwd(const jz_ffn_desc* desc, const void* x, const void* wq_gate, const float* s_gate, const void* wq_up, const float* s_up, const void* wq_down,
+                  const float* s_down, void* y, void* ws, size_t ws_bytes, void* hip_stream);
+
 /* Backward-data of a convolution together with the backward pass of the batch normalization + ReLU that produced the
  * convolution's input (Section 4.2's layer; the counterpart of jz_conv2d_bn_relu_fwd):  y = relu(bn(c)) was the input of
  * this convolution in the forward pass.  One call computes

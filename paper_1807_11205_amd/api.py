@@ -50,6 +50,9 @@ EXPORTS = [
     "jz_grad_clip_workspace_bytes", "jz_grad_clip_prepare", "jz_grad_norm", "jz_grad_clip",
     "jz_norm_residual_fwd", "jz_norm_residual_bwd_workspace_bytes", "jz_norm_residual_bwd",
     "jz_ffn_fwd_workspace_bytes", "jz_ffn_fwd", "jz_ffn_bwd_workspace_bytes", "jz_ffn_bwd",
+    "jz_embed_fwd", "jz_embed_bwd_workspace_bytes", "jz_embed_bwd",
+    "jz_orthogonalize_workspace_bytes", "jz_orthogonalize", "jz_muon_mp_update_workspace_bytes", "jz_muon_mp_update",
+    "jz_quantize_i8", "jz_linear_i8_workspace_bytes", "jz_linear_i8", "jz_ffn_i8_workspace_bytes", "jz_ffn_i8_fwd",
     "jz_status_string", "jz_version",
 ]
 
@@ -114,6 +117,25 @@ class jz_ffn_desc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("in_features", ctypes.c_int), ("hidden", ctypes.c_int), ("out_features", ctypes.c_int),
                 ("act", ctypes.c_int), ("dtype", ctypes.c_int), ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64),
                 ("dx_stride", ctypes.c_int64), ("dy_stride", ctypes.c_int64)]
+
+
+class jz_embed_desc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("vocab", ctypes.c_int), ("channels", ctypes.c_int), ("dtype", ctypes.c_int), ("out_dtype", ctypes.c_int),
+                ("scale", ctypes.c_float), ("out_stride", ctypes.c_int64)]
+
+
+class jz_ortho_desc(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int64), ("rows", ctypes.c_int), ("cols", ctypes.c_int), ("stride", ctypes.c_int64), ("dtype", ctypes.c_int), ("out_dtype", ctypes.c_int),
+                ("steps", ctypes.c_int), ("a", ctypes.c_float), ("b", ctypes.c_float), ("c", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class jz_muon_hparams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_float) for n in ("lr", "momentum", "weight_decay", "update_scale", "loss_scale")] + [("nesterov", ctypes.c_int)]
+
+
+class jz_linear_i8_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("in_features", ctypes.c_int), ("out_features", ctypes.c_int), ("dtype", ctypes.c_int), ("x_stride", ctypes.c_int64),
+                ("y_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -197,6 +219,18 @@ def lib() -> ctypes.CDLL:
         L.jz_ffn_fwd_workspace_bytes.argtypes = L.jz_ffn_bwd_workspace_bytes.argtypes = [fp, ctypes.POINTER(sz)]
         L.jz_ffn_fwd.argtypes = [fp] + [vp] * 9 + [sz, vp]
         L.jz_ffn_bwd.argtypes = [fp] + [vp] * 13 + [sz, vp]
+        ep, op, lp = ctypes.POINTER(jz_embed_desc), ctypes.POINTER(jz_ortho_desc), ctypes.POINTER(jz_linear_i8_desc)
+        L.jz_embed_fwd.argtypes = [ep, vp, vp, vp, vp]
+        L.jz_embed_bwd_workspace_bytes.argtypes = [ep, ctypes.POINTER(sz)]
+        L.jz_embed_bwd.argtypes = [ep, vp, vp, ci, vp, vp, sz, vp]
+        L.jz_orthogonalize_workspace_bytes.argtypes = L.jz_muon_mp_update_workspace_bytes.argtypes = [op, ctypes.POINTER(sz)]
+        L.jz_orthogonalize.argtypes = [op, vp, vp, vp, sz, vp]
+        L.jz_muon_mp_update.argtypes = [op, ctypes.POINTER(jz_muon_hparams)] + [vp] * 8 + [sz, vp]
+        L.jz_quantize_i8.argtypes = [i64, ci, ci, vp, i64, vp, vp, vp]
+        L.jz_linear_i8_workspace_bytes.argtypes = [lp, ctypes.POINTER(sz)]
+        L.jz_linear_i8.argtypes = [lp, vp, vp, vp, vp, vp, sz, vp]
+        L.jz_ffn_i8_workspace_bytes.argtypes = [fp, ctypes.POINTER(sz)]
+        L.jz_ffn_i8_fwd.argtypes = [fp] + [vp] * 9 + [sz, vp]
         L.jz_status_string.argtypes = [ci]
         L.jz_status_string.restype = ctypes.c_char_p
         L.jz_version.argtypes = []
@@ -1057,3 +1091,148 @@ def jz_ffn_bwd(desc, x, w_gate, w_up, w_down, gate, up, h, dy, dx, dw_gate, dw_u
                             _dev_ptr(w_down, t, O * F, "w_down"), _dev_ptr(gate, t, M * F, "gate"), _dev_ptr(up, t, M * F, "up"), _dev_ptr(h, t, M * F, "h"),
                             _rows_ptr(dy, t, M, O, d.dy_stride, "dy"), _rows_ptr(dx, t, M, D, d.dx_stride, "dx"), _dev_ptr(dw_gate, t, F * D, "dw_gate"),
                             _dev_ptr(dw_up, t, F * D, "dw_up"), _dev_ptr(dw_down, t, O * F, "dw_down"), wp, wn), stream)
+
+
+# ---- tokens, orthogonalised updates, 8-bit answers ---------------------------------------------------------------------------
+def _ids(t, tokens):
+    return _dev_ptr(t, torch.int32, tokens, "ids")
+
+
+def _type(dtype):
+    """The torch type of JZ_F16, JZ_BF16 or JZ_F32; another is the library's to refuse."""
+    return _TORCH_TYPES[dtype] if 0 <= dtype <= 2 else None
+
+
+def _workspace_bytes(name, desc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(getattr(lib(), name)(ctypes.byref(desc), ctypes.byref(n)), name)
+    return n.value
+
+
+def _here(*tensors):
+    """Launches go to the current device: tensors that lie on another are refused."""
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != torch.cuda.current_device():
+            raise ValueError("a tensor is on device %d, the current one is %d" % (t.get_device(), torch.cuda.current_device()))
+
+
+def embed_desc(tokens: int, vocab: int, channels: int, dtype: int = JZ_F16, out_dtype: Optional[int] = None, scale: float = 1.0, out_stride: int = 0) -> jz_embed_desc:
+    """dtype: of the table and its gradient; out_dtype: of the looked-up rows and their gradient (None: dtype)."""
+    return jz_embed_desc(tokens, vocab, channels, dtype, dtype if out_dtype is None else out_dtype, scale, out_stride)
+
+
+def jz_embed_fwd(desc: jz_embed_desc, ids, table, out, stream=None):
+    """out[t] = scale * table[ids[t]]; zeros where ids[t] is outside the table."""
+    d = desc
+    _here(table, out)
+    _invoke("jz_embed_fwd", (ctypes.addressof(d), _ids(ids, d.tokens), _dev_ptr(table, _type(d.dtype), d.vocab * d.channels, "table"),
+                              _rows_ptr(out, _type(d.out_dtype), d.tokens, d.channels, d.out_stride, "out")), stream)
+
+
+def jz_embed_bwd_workspace_bytes(desc: jz_embed_desc) -> int:
+    return _workspace_bytes("jz_embed_bwd_workspace_bytes", desc)
+
+
+def jz_embed_bwd(desc: jz_embed_desc, ids, dout, dtable, ws, accumulate: bool = False, stream=None):
+    """dtable[v] = scale * sum of dout[t] over the places t of token v; accumulate: added to what is there, rows without a token left as they are."""
+    d = desc
+    _here(dout, dtable, ws)
+    wp, wn = _ws(ws)
+    _invoke("jz_embed_bwd", (ctypes.addressof(d), _ids(ids, d.tokens), _rows_ptr(dout, _type(d.out_dtype), d.tokens, d.channels, d.out_stride, "dout"), int(bool(accumulate)),
+                              _dev_ptr(dtable, _type(d.dtype), d.vocab * d.channels, "dtable"), wp, wn), stream)
+
+
+def ortho_desc(count: int, rows: int, cols: int, dtype: int = JZ_F16, out_dtype: Optional[int] = None, steps: int = 5, coefs: Sequence[float] = (3.4445, -4.7750, 2.0315),
+               eps: float = 1e-7, stride: int = 0) -> jz_ortho_desc:
+    """`count` matrices, `stride` elements apart (0: dense); coefs are a, b, c of X <- a X + (b A + c A^2) X."""
+    return jz_ortho_desc(count, rows, cols, stride, dtype, dtype if out_dtype is None else out_dtype, steps, *coefs, eps)
+
+
+def _matrices_ptr(t, dtype, d, what):
+    """[count, rows, cols] with dense matrices, `stride` elements apart."""
+    each = d.rows * d.cols
+    if t is None or d.stride in (0, each):
+        return _dev_ptr(t, dtype, d.count * each, what)
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 3:
+        raise TypeError("%s must be a three-dimensional %s tensor on the GPU" % (what, dtype))
+    if t.shape != (d.count, d.rows, d.cols) or (d.cols > 1 and t.stride(2) != 1) or (d.rows > 1 and t.stride(1) != d.cols) or (d.count > 1 and t.stride(0) != d.stride):
+        raise ValueError("%s must be [%d, %d, %d] with dense matrices %d elements apart" % (what, d.count, d.rows, d.cols, d.stride))
+    return t.data_ptr() if t.numel() else None
+
+
+def jz_orthogonalize_workspace_bytes(desc: jz_ortho_desc) -> int:
+    return _workspace_bytes("jz_orthogonalize_workspace_bytes", desc)
+
+
+def jz_orthogonalize(desc: jz_ortho_desc, x, y, ws, stream=None):
+    """y: every matrix of x with its singular values brought near 1 by `steps` Newton-Schulz steps."""
+    _here(x, y, ws)
+    wp, wn = _ws(ws)
+    _invoke("jz_orthogonalize", (ctypes.addressof(desc), _matrices_ptr(x, _type(desc.dtype), desc, "x"), _matrices_ptr(y, _type(desc.out_dtype), desc, "y"), wp, wn), stream)
+
+
+def muon_hparams(lr: float = 0.02, momentum: float = 0.95, weight_decay: float = 0.0, update_scale: float = 1.0, nesterov: bool = True, loss_scale: float = 1.0) -> jz_muon_hparams:
+    return jz_muon_hparams(lr, momentum, weight_decay, update_scale, loss_scale, int(bool(nesterov)))
+
+
+def jz_muon_mp_update_workspace_bytes(desc: jz_ortho_desc) -> int:
+    return _workspace_bytes("jz_muon_mp_update_workspace_bytes", desc)
+
+
+def jz_muon_mp_update(desc: jz_ortho_desc, hp: jz_muon_hparams, master, momentum, grad16, weight16, found_inf, ws, state: Optional[torch.Tensor] = None, skip=None, stream=None):
+    """The momentum, the orthogonalised update of the FP32 master weights and their 16-bit copy.  state: the device-resident loss scale (else hp.loss_scale); skip: another
+    call's overflow flag (int32[1]); found_inf: int32[1], or the address of a flag (as jz_lars_sumsq_sink gives them)."""
+    t, f = _type(desc.dtype), torch.float32
+    _here(master, grad16, ws)
+    wp, wn = _ws(ws)
+    _invoke("jz_muon_mp_update", (ctypes.addressof(desc), ctypes.addressof(hp), _ls_state(state) if state is not None else 0, _flag(skip) if skip is not None else 0,
+                                   _matrices_ptr(master, f, desc, "master"), _matrices_ptr(momentum, f, desc, "momentum"), _matrices_ptr(grad16, t, desc, "grad16"),
+                                   _matrices_ptr(weight16, t, desc, "weight16"), found_inf if isinstance(found_inf, int) else _flag(found_inf), wp, wn), stream)
+
+
+def i8_pitch(cols: int) -> int:
+    """Bytes from one row of codes to the next."""
+    return (cols + 15) // 16 * 16
+
+
+def _codes_ptr(t, rows, cols, what):
+    return _dev_ptr(t, torch.int8, rows * i8_pitch(cols), what)
+
+
+def jz_quantize_i8(rows: int, cols: int, x, q, scale, x_stride: int = 0, stream=None):
+    """Codes (int8 [rows, i8_pitch(cols)], zeros behind column cols) and scales (float32 [rows]) of the rows of x."""
+    _here(x, q)
+    _invoke("jz_quantize_i8", (rows, cols, dtype_of(x.dtype), _rows_ptr(x, x.dtype, rows, cols, x_stride, "x"), x_stride, _codes_ptr(q, rows, cols, "q"),
+                                _dev_ptr(scale, torch.float32, rows, "scale")), stream)
+
+
+def linear_i8_desc(rows: int, in_features: int, out_features: int, dtype: int = JZ_F16, x_stride: int = 0, y_stride: int = 0) -> jz_linear_i8_desc:
+    return jz_linear_i8_desc(rows, in_features, out_features, dtype, x_stride, y_stride)
+
+
+def jz_linear_i8_workspace_bytes(desc: jz_linear_i8_desc) -> int:
+    return _workspace_bytes("jz_linear_i8_workspace_bytes", desc)
+
+
+def jz_linear_i8(desc: jz_linear_i8_desc, x, wq, w_scale, y, ws=None, stream=None):
+    """y = x w^T with x quantised row by row and w in codes [out_features, i8_pitch(in_features)] with a scale for each row."""
+    d, t = desc, _type(desc.dtype)
+    _here(x, wq, y, ws)
+    wp, wn = _ws(ws)
+    _invoke("jz_linear_i8", (ctypes.addressof(d), _rows_ptr(x, t, d.rows, d.in_features, d.x_stride, "x"), _codes_ptr(wq, d.out_features, d.in_features, "wq"),
+                              _dev_ptr(w_scale, torch.float32, d.out_features, "w_scale"), _rows_ptr(y, t, d.rows, d.out_features, d.y_stride, "y"), wp, wn), stream)
+
+
+def jz_ffn_i8_workspace_bytes(desc: jz_ffn_desc) -> int:
+    return _workspace_bytes("jz_ffn_i8_workspace_bytes", desc)
+
+
+def jz_ffn_i8_fwd(desc: jz_ffn_desc, x, wq_gate, s_gate, wq_up, s_up, wq_down, s_down, y, ws=None, stream=None):
+    """The gated block with its three matrices in codes, each with a scale for each row."""
+    d, t, f = desc, _type(desc.dtype), torch.float32
+    M, D, F, O = d.rows, d.in_features, d.hidden, d.out_features
+    _here(x, wq_gate, y, ws)
+    wp, wn = _ws(ws)
+    _invoke("jz_ffn_i8_fwd", (ctypes.addressof(d), _rows_ptr(x, t, M, D, d.x_stride, "x"), _codes_ptr(wq_gate, F, D, "wq_gate"), _dev_ptr(s_gate, f, F, "s_gate"),
+                               _codes_ptr(wq_up, F, D, "wq_up"), _dev_ptr(s_up, f, F, "s_up"), _codes_ptr(wq_down, O, F, "wq_down"), _dev_ptr(s_down, f, O, "s_down"),
+                               _rows_ptr(y, t, M, O, d.y_stride, "y"), wp, wn), stream)

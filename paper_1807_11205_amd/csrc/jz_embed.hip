@@ -1,0 +1,370 @@
+// Embedding lookup and the gradient of its table (include/jz.h: jz_embed_fwd, jz_embed_bwd).
+//
+//   out[t] = RNE(scale * table[id_t]),      dtable[v] = RNE(scale * sum over t with id_t = v of dout[t]  [+ dtable[v]])
+//
+// What bounds both: memory.  Forward a table row is read where its token stands and a row is written; backward every row of dout is read once
+// and every row of dtable written once.  For that the positions are first sorted by token, stably, so that every sum has one order: first by position.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "jz_internal.h"
+
+namespace {
+
+#include "jz_vec.h"
+#include "jz_sort.h"
+
+constexpr int EMBED_GRID = 1 << 16;  // workgroups at most: each takes further turns
+
+// ---- lookup -----------------------------------------------------------------------------------------------------------------
+struct LookupArgs {
+  const int* ids;
+  const void* table;
+  void* out;
+  int64_t tokens, ld;
+  int vocab, channels;
+  float scale;
+};
+
+// Groups of eight channels; a row's last group ends with the row, so that it overlaps its neighbour where channels are no multiple of 8 (both store the
+// same values).  FEW: less than eight channels.
+template <class T, class O, bool FEW>
+__global__ __launch_bounds__(256) void embed_lookup(LookupArgs a) {
+  constexpr int U = 4;  // loads in flight
+  const int64_t per = (a.channels + 7) / 8, all = a.tokens * per;
+  for (int64_t base = (int64_t)blockIdx.x * (256 * U); base < all; base += (int64_t)gridDim.x * (256 * U)) {
+    typename Vec8<T>::V v[U];
+    int64_t to[U];
+    bool there[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = base + u * 256 + threadIdx.x;
+      to[u] = -1;
+      there[u] = false;
+      v[u] = {};
+      if (i < all) {
+        const int64_t t = i / per;
+        int64_t c = (i - t * per) * 8;
+        if (!FEW && c + 8 > a.channels) c = a.channels - 8;
+        const int id = a.ids[t];
+        there[u] = (unsigned)id < (unsigned)a.vocab;
+        to[u] = t * a.ld + c;
+        if (there[u]) {
+          const T* p = static_cast<const T*>(a.table) + (int64_t)id * a.channels + c;
+          v[u] = FEW ? load8(p, a.channels) : load8(p);
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (to[u] < 0) continue;
+      // a token outside the table: zeros, also with a scale that is not finite
+      const typename Vec8<O>::V r = there[u] ? narrow8<O>(widen8<T>(v[u]) * a.scale) : typename Vec8<O>::V{};
+      O* p = static_cast<O*>(a.out) + to[u];
+      if (FEW) store8(p, r, a.channels);
+      else store8(p, r);
+    }
+  }
+}
+
+// ---- gradient ---------------------------------------------------------------------------------------------------------------
+// The sorted positions are cut into pieces of `piece`.  Where a token's places begin, its piece adds them up, to the end of the next piece at most; if there are more
+// of them (a frequent token), every further piece leaves a partial sum of its own, and embed_join adds those up in order.  A thread has eight channels; `lanes`
+// threads (a power of two) have a row, or `span` = 8 lanes of its channels.
+struct SumArgs {
+  const unsigned *keys, *pos;   // sorted
+  const void* dout;
+  void* dtable;
+  const unsigned char* used;    // rows of the table that have a token
+  float* partial;               // [piece][2][channels]: of a token that began two pieces ago or earlier; of one that goes on behind the next piece
+  unsigned *n_long, *long_list; // pieces where such a token begins
+  int64_t tokens, ld, pieces;
+  int vocab, channels, piece, lanes, slices, accumulate;
+  int64_t sum_blocks, zero_blocks, zero_rows;
+  float scale;
+};
+
+// eight channels from c on of a row, or what there is of them
+template <class T>
+__device__ __forceinline__ f32x8 row8(const T* p, int left) {
+  return widen8<T>(left >= 8 ? load8(p) : load8(p, left));
+}
+
+template <class G>
+__device__ __forceinline__ void finish_row(const SumArgs& a, unsigned key, int c, int left, f32x8 sum) {
+  G* p = static_cast<G*>(a.dtable) + (int64_t)key * a.channels + c;
+  f32x8 v = sum * a.scale;
+  if (a.accumulate) v += row8(p, left);
+  store8(p, narrow8<G>(v), left);
+}
+
+template <class O, class G>
+__device__ void sum_piece(const SumArgs& a, int64_t piece, int c) {
+  const int64_t s = piece * a.piece, T = a.tokens;
+  const int64_t own_end = s + a.piece < T ? s + a.piece : T, far_end = own_end + a.piece < T ? own_end + a.piece : T;
+  const int left = a.channels - c < 8 ? a.channels - c : 8;
+  int64_t i = s;
+  const unsigned first = a.keys[s];
+  if (first >= (unsigned)a.vocab) return;  // tokens outside the table come last
+  bool head = false;                       // a token's further part
+  if (s > 0 && a.keys[s - 1] == first) {
+    head = s > a.piece && a.keys[s - a.piece - 1] == first;
+    if (!head)  // it began in the piece before, which adds this piece's places too
+      while (i < own_end && a.keys[i] == first) ++i;
+  }
+  const O* const dout = static_cast<const O*>(a.dout) + c;
+  while (i < own_end) {
+    const unsigned key = a.keys[i];
+    if (key >= (unsigned)a.vocab) return;
+    const int64_t end = head ? own_end : far_end;
+    f32x8 sum = {};
+    for (;;) {  // four places at a time
+      int n = 1;
+      unsigned at[4];
+      at[0] = a.pos[i];
+#pragma unroll
+      for (int u = 1; u < 4; ++u) {
+        const bool more = n == u && i + u < end && a.keys[i + u] == key;
+        at[u] = more ? a.pos[i + u] : at[0];
+        n += more;
+      }
+      f32x8 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = row8(dout + (int64_t)at[u] * a.ld, left);
+      sum += v[0];
+      if (n > 1) sum += v[1];
+      if (n > 2) sum += v[2];
+      if (n > 3) sum += v[3];
+      i += n;
+      if (n < 4 || i >= end || a.keys[i] != key) break;
+    }
+    const bool goes_on = i == end && i < T && a.keys[i] == key;
+    if (head || goes_on) {
+      store8(a.partial + (piece * 2 + !head) * a.channels + c, sum, left);
+      if (!head && c == 0) a.long_list[atomicAdd(a.n_long, 1u)] = (unsigned)piece;  // their order is of no consequence: each has a row of its own
+    } else {
+      finish_row<G>(a, key, c, left, sum);
+    }
+    head = false;
+  }
+}
+
+template <class O, class G>
+__global__ __launch_bounds__(256) void embed_sum(SumArgs a) {
+  const int per = 256 / a.lanes, mine = threadIdx.x / a.lanes, lane = threadIdx.x % a.lanes;
+  for (int64_t b = blockIdx.x; b < a.sum_blocks + a.zero_blocks; b += gridDim.x) {
+    if (b < a.sum_blocks) {
+      const int64_t w = b * per + mine, piece = w / a.slices;
+      const int c = ((int)(w - piece * a.slices) * a.lanes + lane) * 8;
+      if (piece < a.pieces && c < a.channels) sum_piece<O, G>(a, piece, c);
+    } else {  // rows of the table without a token
+      const int64_t row0 = (b - a.sum_blocks) * a.zero_rows, vecs = (a.channels + 7) / 8;
+      const int64_t rows = a.vocab - row0 < a.zero_rows ? a.vocab - row0 : a.zero_rows;
+      for (int64_t i = threadIdx.x; i < rows * vecs; i += 256) {
+        const int64_t r = i / vecs, c = (i - r * vecs) * 8;
+        if (a.used[row0 + r]) continue;
+        store8(static_cast<G*>(a.dtable) + (row0 + r) * a.channels + c, typename Vec8<G>::V{}, (int)(a.channels - c < 8 ? a.channels - c : 8));
+      }
+    }
+  }
+}
+
+// The partial sums of a frequent token, added in order: eight wavefronts take an eighth of them each, four channels a lane.
+template <class G>
+__global__ __launch_bounds__(512) void embed_join(SumArgs a) {
+  __shared__ f32x4 sums[8][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const unsigned n = *a.n_long;
+  for (int64_t c0 = (int64_t)blockIdx.y * 256; c0 < a.channels; c0 += (int64_t)gridDim.y * 256) {
+    const int64_t c = c0 + lane * 4;
+    const int left = (int)(a.channels - c < 4 ? a.channels - c : 4);
+    for (unsigned i = blockIdx.x; i < n; i += gridDim.x) {
+      const int64_t from = a.long_list[i];
+      const unsigned key = a.keys[(from + 1) * a.piece];  // the next piece's places are all the token's
+      int64_t lo = from + 2, hi = a.pieces;               // first piece that does not begin with it
+      while (lo < hi) {
+        const int64_t mid = (lo + hi) / 2;
+        if (a.keys[mid * a.piece] == key) lo = mid + 1;
+        else hi = mid;
+      }
+      const int64_t parts = lo - (from + 2), each = (parts + 7) / 8, b = wave * each, e = b + each < parts ? b + each : parts;
+      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+      auto add = [&](const float* p) {
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (k < left) v[k] = p[k];
+        sum += v;
+      };
+      if (left > 0) {
+        if (wave == 0) add(a.partial + (from * 2 + 1) * a.channels + c);
+#pragma unroll 4
+        for (int64_t x = b; x < e; ++x) add(a.partial + (from + 2 + x) * 2 * a.channels + c);
+      }
+      sums[wave][lane] = sum;
+      __syncthreads();
+      if (wave == 0 && left > 0) {
+#pragma unroll
+        for (int k = 1; k < 8; ++k) sum += sums[k][lane];
+        G* p = static_cast<G*>(a.dtable) + (int64_t)key * a.channels + c;
+        for (int k = 0; k < left; ++k) {
+          float v = sum[k] * a.scale;
+          if (a.accumulate) v += (float)p[k];
+          p[k] = (G)v;
+        }
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// ---- host -------------------------------------------------------------------------------------------------------------------
+struct EmbedShape {
+  int64_t T, ld;
+  int V, D;
+};
+int embed_shape(const jz_embed_desc* d, EmbedShape* s) {
+  if (!d) return JZ_ERR_NULL;
+  if (d->tokens < 0 || d->vocab <= 0 || d->channels <= 0 || d->dtype < JZ_F16 || d->dtype > JZ_F32 || d->out_dtype < JZ_F16 || d->out_dtype > JZ_F32 ||
+      !(fabsf(d->scale) < INFINITY))
+    return JZ_ERR_SHAPE;
+  *s = {d->tokens, d->out_stride ? d->out_stride : d->channels, d->vocab, d->channels};
+  if (s->ld < s->D) return JZ_ERR_SHAPE;
+  if ((d->out_dtype != d->dtype && d->out_dtype != JZ_F32) || s->D > (1 << 24) || s->ld > (1 << 24) || s->T >= int64_t(1) << 31) return JZ_ERR_UNSUPPORTED;
+  // tensors larger than any card's memory
+  if (std::max(s->T * s->ld, (int64_t)s->V * s->D) > int64_t(1) << 38) return JZ_ERR_UNSUPPORTED;
+  return JZ_OK;
+}
+size_t bytes_of(int dtype) { return dtype == JZ_F32 ? 4 : 2; }
+size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
+size_t stream_bytes(const EmbedShape& s, int dtype) { return s.T ? ((size_t)(s.T - 1) * s.ld + s.D) * bytes_of(dtype) : 0; }
+
+struct SumPlan {
+  int piece, lanes, slices;
+  int64_t pieces;
+};
+SumPlan sum_plan(const EmbedShape& s) {
+  SumPlan p;
+  p.piece = s.T >= 32768 ? 32 : s.T >= 4096 ? 16 : 8;
+  p.pieces = (s.T + p.piece - 1) / p.piece;
+  const int64_t vecs = (s.D + 7) / 8;
+  p.lanes = 8;
+  while (p.lanes < vecs && p.lanes < 256) p.lanes *= 2;
+  p.slices = (int)((vecs + p.lanes - 1) / p.lanes);
+  return p;
+}
+
+struct EmbedLayout {
+  SortLayout sort;
+  size_t used, counter, list, partial, total;
+};
+EmbedLayout embed_layout(const EmbedShape& s) {
+  EmbedLayout L;
+  L.sort = sort_layout(s.T, s.V);
+  const SumPlan p = sum_plan(s);
+  size_t o = L.sort.total;
+  L.used = o;
+  o = up256(o + (size_t)s.V);
+  L.counter = o;
+  o += 256;
+  L.list = o;
+  o = up256(o + (size_t)p.pieces * 4);
+  L.partial = o;
+  if (s.T > 2 * p.piece) o = up256(o + (size_t)p.pieces * 2 * s.D * 4);
+  L.total = o;
+  return L;
+}
+
+template <class T, class O>
+void lookup(const LookupArgs& a, hipStream_t st) {
+  const int64_t vecs = a.tokens * ((a.channels + 7) / 8);
+  const unsigned grid = (unsigned)std::min<int64_t>((vecs + 1023) / 1024, EMBED_GRID);
+  if (a.channels < 8) embed_lookup<T, O, true><<<grid, 256, 0, st>>>(a);
+  else embed_lookup<T, O, false><<<grid, 256, 0, st>>>(a);
+}
+
+template <class O, class G>
+int sums(const SumArgs& a, hipStream_t st) {
+  const int64_t blocks = a.sum_blocks + a.zero_blocks;
+  if (blocks > 0) embed_sum<O, G><<<(unsigned)std::min<int64_t>(blocks, int64_t(1) << 23), 256, 0, st>>>(a);
+  if (jz::launch_status() != JZ_OK) return JZ_ERR_LAUNCH;
+  if (a.tokens > 2 * a.piece) {
+    const dim3 grid((unsigned)std::min<int64_t>(a.pieces, 64), (unsigned)std::min<int64_t>((a.channels + 255) / 256, 64));
+    embed_join<G><<<grid, 512, 0, st>>>(a);
+  }
+  return jz::launch_status();
+}
+
+}  // namespace
+
+extern "C" int jz_embed_fwd(const jz_embed_desc* d, const int* ids, const void* table, void* out, void* hip_stream) {
+  EmbedShape s;
+  const int rc = embed_shape(d, &s);
+  if (rc != JZ_OK) return rc;
+  if (!table || (s.T && (!ids || !out))) return JZ_ERR_NULL;
+  if (s.T == 0) return JZ_OK;
+  if ((reinterpret_cast<uintptr_t>(ids) & 3) || !jz::aligned16(table) || !jz::aligned16(out)) return JZ_ERR_ALIGN;
+  const size_t n = stream_bytes(s, d->out_dtype);
+  if (jz::overlaps(out, n, table, (size_t)s.V * s.D * bytes_of(d->dtype)) || jz::overlaps(out, n, ids, (size_t)s.T * 4)) return JZ_ERR_ALIAS;
+  const LookupArgs a = {ids, table, out, s.T, s.ld, s.V, s.D, d->scale};
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (d->dtype == JZ_F32) lookup<float, float>(a, st);
+  else if (d->dtype == JZ_F16) d->out_dtype == JZ_F32 ? lookup<_Float16, float>(a, st) : lookup<_Float16, _Float16>(a, st);
+  else d->out_dtype == JZ_F32 ? lookup<__bf16, float>(a, st) : lookup<__bf16, __bf16>(a, st);
+  return jz::launch_status();
+}
+
+extern "C" int jz_embed_bwd_workspace_bytes(const jz_embed_desc* d, size_t* bytes) {
+  if (!bytes) return JZ_ERR_NULL;
+  EmbedShape s;
+  const int rc = embed_shape(d, &s);
+  if (rc != JZ_OK) return rc;
+  *bytes = embed_layout(s).total;
+  return JZ_OK;
+}
+
+extern "C" int jz_embed_bwd(const jz_embed_desc* d, const int* ids, const void* dout, int accumulate, void* dtable, void* ws, size_t ws_bytes, void* hip_stream) {
+  EmbedShape s;
+  int rc = embed_shape(d, &s);
+  if (rc != JZ_OK) return rc;
+  if (!dtable || (s.T && (!ids || !dout))) return JZ_ERR_NULL;
+  const EmbedLayout L = embed_layout(s);
+  if (!ws || ws_bytes < L.total) return JZ_ERR_WORKSPACE;
+  if ((reinterpret_cast<uintptr_t>(ids) & 3) || !jz::aligned16(dout) || !jz::aligned16(dtable) || !jz::aligned16(ws)) return JZ_ERR_ALIGN;
+  const size_t n = stream_bytes(s, d->out_dtype), t = (size_t)s.V * s.D * bytes_of(d->dtype);
+  if (jz::overlaps(dtable, t, dout, n) || jz::overlaps(dtable, t, ids, (size_t)s.T * 4) || jz::overlaps(dtable, t, ws, ws_bytes) || jz::overlaps(ws, ws_bytes, dout, n) ||
+      jz::overlaps(ws, ws_bytes, ids, (size_t)s.T * 4))
+    return JZ_ERR_ALIAS;
+  if (s.T == 0 && accumulate) return JZ_OK;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  char* const b = static_cast<char*>(ws);
+  SumArgs a = {};
+  a.used = reinterpret_cast<unsigned char*>(b + L.used);
+  a.n_long = reinterpret_cast<unsigned*>(b + L.counter);
+  a.long_list = reinterpret_cast<unsigned*>(b + L.list);
+  a.partial = reinterpret_cast<float*>(b + L.partial);
+  rc = sort_tokens(L.sort, ids, s.T, s.V, accumulate ? nullptr : reinterpret_cast<unsigned char*>(b + L.used), a.n_long, b, &a.keys, &a.pos, st);
+  if (rc != JZ_OK) return rc;
+  const SumPlan p = sum_plan(s);
+  a.dout = dout;
+  a.dtable = dtable;
+  a.tokens = s.T;
+  a.ld = s.ld;
+  a.pieces = p.pieces;
+  a.vocab = s.V;
+  a.channels = s.D;
+  a.piece = p.piece;
+  a.lanes = p.lanes;
+  a.slices = p.slices;
+  a.accumulate = accumulate != 0;
+  a.scale = d->scale;
+  const int64_t per = 256 / p.lanes;
+  a.sum_blocks = (p.pieces * p.slices + per - 1) / per;
+  a.zero_rows = std::max<int64_t>(1, 16384 / s.D);
+  a.zero_blocks = accumulate ? 0 : (s.V + a.zero_rows - 1) / a.zero_rows;
+  if (d->dtype == JZ_F32) return sums<float, float>(a, st);
+  if (d->dtype == JZ_F16) return d->out_dtype == JZ_F32 ? sums<float, _Float16>(a, st) : sums<_Float16, _Float16>(a, st);
+  return d->out_dtype == JZ_F32 ? sums<float, __bf16>(a, st) : sums<__bf16, __bf16>(a, st);
+}

@@ -27,6 +27,8 @@
 // Both orders keep the reads of a wavefront on different banks.
 #pragma once
 
+#include "jz_tile_schedule.h"
+
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
@@ -161,8 +163,6 @@ __device__ __forceinline__ void finish8(const GemmArgs& a, const Product& p, int
 }
 
 // ---- the tile kernel --------------------------------------------------------------------------------------------------------
-#define JZ_LDS __attribute__((address_space(3)))
-
 // One tile of one operand: where a thread's 16-byte chunks come from and go to.
 template <class T, bool KC, int ROWS, int THREADS>
 struct Staged {
@@ -450,18 +450,6 @@ __global__ __launch_bounds__(256, 2) void ffn_gemm_any(GemmArgs a) {
 }
 
 // ---- LDS-direct ---------------------------------------------------------------------------------------------------------------
-// Everything has landed that this wavefront asked for, and every wavefront is past its reads: both sides are ordinary accesses, which the
-// fences keep in place.
-__device__ __forceinline__ void all_landed() {
-  __builtin_amdgcn_sched_barrier(0);
-  wait_vmcnt<0>();
-  lds_wait<0>();
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-  __builtin_amdgcn_sched_barrier(0);
-}
-
 // Where one operand's tile comes from.
 template <class T, bool KC, int ROWS, int THREADS, bool DUAL>
 struct Source {
@@ -503,20 +491,6 @@ struct Source {
     }
   }
 };
-
-// The order of a step's instructions: between one matrix instruction and the next a read of LDS or a load.  (In the compiler's order, all reads first, 8192 rows, 2048 ->
-// 5632 features take 10 % longer.)
-template <int MULTIPLY, int READ, int LOAD>
-__device__ __forceinline__ void spread_out() {
-  constexpr int OTHER = READ + LOAD;
-  static_for<0, MULTIPLY>([&](auto I) {
-    constexpr int i = decltype(I)::value, from = i * OTHER / MULTIPLY, to = (i + 1) * OTHER / MULTIPLY;
-    constexpr int reads = (to < READ ? to : READ) - (from < READ ? from : READ), loads = to - from - reads;
-    if constexpr (reads > 0) __builtin_amdgcn_sched_group_barrier(0x100, reads, 0);
-    if constexpr (loads > 0) __builtin_amdgcn_sched_group_barrier(0x10, loads, 0);
-    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-  });
-}
 
 template <class T, bool KCA, bool KCB, int EPI, int ACT, int BM, int BN, int WGM, int WGN>
 __global__ __launch_bounds__(64 * WGM * WGN, 2) void ffn_gemm(GemmArgs a) {

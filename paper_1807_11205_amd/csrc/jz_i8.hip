@@ -1,0 +1,307 @@
+// Products in 8-bit integers with a scale for each token and each channel (include/jz.h: jz_quantize_i8, jz_linear_i8, jz_ffn_i8_fwd).
+//
+//   scale = max |x| / 127 over a row,  q = x / scale to the nearest whole number (ties to even),   y[m][n] = RNE(sum over k of q_x q_w  *  s_x[m] s_w[n])
+//
+// The sums are int32 and exact, so no order or split of them matters.  Tokens are quantised by a launch of their own, a workgroup a row.  The gated block's h is kept in FP32
+// until it has codes: rounded to 16 bits first, three codes in a hundred would be another's neighbour.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "jz_internal.h"
+
+namespace {
+
+#include "jz_lds_dma.h"
+#include "jz_vec.h"
+#include "jz_ffn_gemm.h"
+#include "jz_mm_tile.h"
+
+int64_t i8_pitch(int64_t cols) { return (cols + 15) & ~int64_t(15); }
+
+// ---- codes --------------------------------------------------------------------------------------------------------------------
+struct QuantArgs {
+  const void* x;
+  signed char* q;
+  float* scale;
+  int64_t rows, ld, pitch;
+  int cols;
+};
+__device__ __forceinline__ unsigned magnitude8(f32x8 v) {  // NaN is larger than Inf, and Inf than every number
+  unsigned m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+  return m;
+}
+__device__ __forceinline__ unsigned long long codes8(f32x8 v, float s, int left) {
+  unsigned long long r = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float q = fminf(fmaxf(rintf(v[i] / s), -127.f), 127.f);
+    r |= (unsigned long long)(unsigned char)(i < left ? (int)q : 0) << (8 * i);
+  }
+  return r;
+}
+// A workgroup a row at a time; HOLD vectors of eight stay in a lane's registers, what is behind them is read twice.
+template <class T, int THREADS, int HOLD>
+__global__ __launch_bounds__(THREADS) void i8_quantize(QuantArgs a) {
+  __shared__ unsigned most[THREADS / 64];
+  const int t = threadIdx.x;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const T* const x = static_cast<const T*>(a.x) + row * a.ld;
+    auto get = [&](int64_t c) { return c + 8 <= a.cols ? load8(x + c) : load8(x + c, c < a.cols ? (int)(a.cols - c) : 0); };
+    typename Vec8<T>::V v[HOLD];
+    unsigned m = 0;
+#pragma unroll
+    for (int j = 0; j < HOLD; ++j) v[j] = get(((int64_t)j * THREADS + t) * 8);
+#pragma unroll
+    for (int j = 0; j < HOLD; ++j) m = max(m, magnitude8(widen8<T>(v[j])));
+    for (int64_t c = ((int64_t)HOLD * THREADS + t) * 8; c < a.cols; c += THREADS * 8) m = max(m, magnitude8(widen8<T>(get(c))));
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, d));
+    if ((t & 63) == 0) most[t >> 6] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) m = max(m, most[w]);
+    __syncthreads();
+    const bool fine = m < 0x7f800000u;
+    const float s = fine ? __uint_as_float(m) / 127.f : NAN;  // a row with Inf or NaN: every result of it is NaN
+    if (t == 0) a.scale[row] = s;
+    const bool none = !(s > 0.f);
+    signed char* const q = a.q + row * a.pitch;
+    auto put = [&](int64_t c, typename Vec8<T>::V w) {
+      if (c < a.pitch) *reinterpret_cast<unsigned long long*>(q + c) = none ? 0ull : codes8(widen8<T>(w), s, c < a.cols ? (int)(a.cols - c) : 0);
+    };
+#pragma unroll
+    for (int j = 0; j < HOLD; ++j) put(((int64_t)j * THREADS + t) * 8, v[j]);
+    for (int64_t c = ((int64_t)HOLD * THREADS + t) * 8; c < a.pitch; c += THREADS * 8) put(c, get(c));
+  }
+}
+template <class T>
+int quantize(const QuantArgs& a, hipStream_t st) {
+  const unsigned grid = (unsigned)std::min<int64_t>(a.rows, 1 << 20);
+  if (a.pitch <= 64 * 8 * 4) i8_quantize<T, 64, 4><<<grid, 64, 0, st>>>(a);
+  else i8_quantize<T, 256, 4><<<grid, 256, 0, st>>>(a);
+  return jz::launch_status();
+}
+int quantize(int dtype, const QuantArgs& a, hipStream_t st) {
+  if (a.rows == 0) return JZ_OK;
+  return dtype == JZ_F32 ? quantize<float>(a, st) : dtype == JZ_F16 ? quantize<_Float16>(a, st) : quantize<__bf16>(a, st);
+}
+
+// ---- products -----------------------------------------------------------------------------------------------------------------
+struct I8Out {
+  const float *sx, *sw, *su;  // scales of the tokens and of the channels (su: of the interleaved matrix)
+  void* y;
+  int64_t M, N, ld;
+  int act;
+};
+template <class T>
+struct I8Store : I8Out {
+  template <class S>
+  __device__ __forceinline__ void strip(const S& s, const MmTile&, int64_t m0, int64_t n0, int lane) const {
+    constexpr int PER = S::COLS / 8;
+#pragma unroll 1
+    for (int i = lane; i < 32 * PER; i += 64) {
+      const int row = i / PER, c = i % PER * 8;
+      const int64_t m = m0 + row, n = n0 + c;
+      if (m >= M || n >= N) continue;
+      const int left = N - n < 8 ? (int)(N - n) : 8;
+      int v[8];
+      s.row8(row, c, v);
+      const float r = sx[m];
+      const f32x8 w = load8(sw + n, left);
+      f32x8 f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = (float)v[e] * (r * w[e]);
+      store8(static_cast<T*>(y) + m * ld + n, narrow8<T>(f), left);
+    }
+  }
+};
+// gate and up alternate by 32 columns; h in FP32
+struct I8Glu : I8Out {
+  template <class S>
+  __device__ __forceinline__ void strip(const S& s, const MmTile&, int64_t m0, int64_t n0, int lane) const {
+    constexpr int PER = S::COLS / 16;
+#pragma unroll 1
+    for (int i = lane; i < 32 * PER; i += 64) {
+      const int row = i / PER, c = i % PER, from = (c >> 2) * 64 + (c & 3) * 8;
+      const int64_t m = m0 + row, n = n0 / 2 + c * 8;
+      if (m >= M || n >= N) continue;
+      const int left = N - n < 8 ? (int)(N - n) : 8;
+      int g[8], u[8];
+      s.row8(row, from, g);
+      s.row8(row, from + 32, u);
+      const float r = sx[m];
+      const f32x8 wg = load8(sw + n, left), wu = load8(su + n, left);
+      f32x8 h;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[e] = act_fwd(act, (float)g[e] * (r * wg[e])) * ((float)u[e] * (r * wu[e]));
+      store8(static_cast<float*>(y) + m * ld + n, h, left);
+    }
+  }
+};
+
+MmArgs i8_args(const signed char* x, int64_t M, const void* w0, const void* w1, int64_t N, int64_t K) {
+  MmArgs a = {};
+  const int64_t pitch = i8_pitch(K);
+  a.a = {{x, x}, M, pitch, 0};
+  a.b = {{w0, w1 ? w1 : w0}, N, pitch, 0};
+  a.row_bytes = pitch;
+  return a;
+}
+template <class T>
+int i8_product(const MmArgs& a, const I8Out& o, hipStream_t st) {
+  I8Store<T> e;
+  static_cast<I8Out&>(e) = o;
+  if ((o.M + 255) / 256 * ((o.N + 255) / 256) >= 160) return mm_launch<ElemI8, I8Store<T>, 256, false>(a, e, o.M, o.N, 1, st);
+  if ((o.M + 127) / 128 * ((o.N + 127) / 128) >= 256) return mm_launch<ElemI8, I8Store<T>, 128, false>(a, e, o.M, o.N, 1, st);
+  return mm_launch<ElemI8, I8Store<T>, 64, false>(a, e, o.M, o.N, 1, st);
+}
+int i8_glu(const MmArgs& a, const I8Out& o, hipStream_t st) {
+  I8Glu e;
+  static_cast<I8Out&>(e) = o;
+  const int64_t cols = (o.N + 31) / 32 * 64;
+  if ((o.M + 255) / 256 * ((cols + 255) / 256) >= 160) return mm_launch<ElemI8, I8Glu, 256, true>(a, e, o.M, cols, 1, st);
+  return mm_launch<ElemI8, I8Glu, 128, true>(a, e, o.M, cols, 1, st);
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------------------
+struct I8Tensor {
+  const void* p;
+  size_t bytes, align;
+  bool out;
+};
+int look_over(const I8Tensor* t, int n, const void* ws, size_t ws_bytes) {
+  for (int i = 0; i < n; ++i)
+    if (reinterpret_cast<uintptr_t>(t[i].p) & (t[i].align - 1)) return JZ_ERR_ALIGN;
+  for (int i = 0; i < n; ++i) {
+    if (jz::overlaps(t[i].p, t[i].bytes, ws, ws_bytes)) return JZ_ERR_ALIAS;
+    for (int j = i + 1; j < n; ++j)
+      if ((t[i].out || t[j].out) && jz::overlaps(t[i].p, t[i].bytes, t[j].p, t[j].bytes)) return JZ_ERR_ALIAS;
+  }
+  return JZ_OK;
+}
+size_t elem(int dtype) { return dtype == JZ_F32 ? 4 : 2; }
+size_t span_of(int64_t rows, int64_t cols, int64_t ld, size_t each) { return rows ? ((size_t)(rows - 1) * ld + cols) * each : 0; }
+size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
+
+// the sums of K products of codes fit int32 up to here: 127^2 K < 2^31
+constexpr int64_t I8_MOST = 131072;
+constexpr int64_t I8_ROWS = int64_t(1) << 31, I8_ELEMENTS = int64_t(1) << 38;
+
+struct I8Shape {
+  int64_t M, K, N, ldx, ldy;
+};
+int i8_shape(const jz_linear_i8_desc* d, I8Shape* s) {
+  if (!d) return JZ_ERR_NULL;
+  if (d->rows < 0 || d->in_features <= 0 || d->out_features <= 0 || d->dtype < JZ_F16 || d->dtype > JZ_F32) return JZ_ERR_SHAPE;
+  *s = {d->rows, d->in_features, d->out_features, d->x_stride ? d->x_stride : d->in_features, d->y_stride ? d->y_stride : d->out_features};
+  if (s->ldx < s->K || s->ldy < s->N) return JZ_ERR_SHAPE;
+  if (s->K > I8_MOST || s->N > (1 << 24) || std::max(s->ldx, s->ldy) > (1 << 24) || s->M > I8_ROWS) return JZ_ERR_UNSUPPORTED;
+  if (std::max(s->M * std::max(s->ldx, s->ldy), s->N * s->K) > I8_ELEMENTS) return JZ_ERR_UNSUPPORTED;
+  return JZ_OK;
+}
+struct I8Room {  // of M rows of codes
+  size_t scales, total;
+  I8Room(int64_t M, int64_t K) : scales(round256((size_t)M * i8_pitch(K))), total(scales + round256((size_t)M * 4)) {}
+};
+int ffn_i8_shape(const jz_ffn_desc* d, I8Shape* s, int64_t* F) {
+  if (!d) return JZ_ERR_NULL;
+  if (d->rows < 0 || d->in_features <= 0 || d->hidden <= 0 || d->out_features <= 0 || d->act < JZ_ACT_SILU || d->act > JZ_ACT_RELU || d->dtype < JZ_F16 || d->dtype > JZ_F32)
+    return JZ_ERR_SHAPE;
+  *s = {d->rows, d->in_features, d->out_features, d->x_stride ? d->x_stride : d->in_features, d->y_stride ? d->y_stride : d->out_features};
+  *F = d->hidden;
+  if (s->ldx < s->K || s->ldy < s->N) return JZ_ERR_SHAPE;
+  if (d->dtype == JZ_F32 || s->K > I8_MOST || *F > I8_MOST || s->N > (1 << 24) || std::max(s->ldx, s->ldy) > (1 << 24) || s->M > I8_ROWS) return JZ_ERR_UNSUPPORTED;
+  if (std::max(std::max(s->M * std::max(std::max(s->ldx, s->ldy), *F), s->N * *F), *F * s->K) > I8_ELEMENTS) return JZ_ERR_UNSUPPORTED;
+  return JZ_OK;
+}
+
+}  // namespace
+
+extern "C" int jz_quantize_i8(int64_t rows, int cols, int dtype, const void* x, int64_t x_stride, void* q, float* scale, void* hip_stream) {
+  if (rows < 0 || cols <= 0 || dtype < JZ_F16 || dtype > JZ_F32) return JZ_ERR_SHAPE;
+  const int64_t ld = x_stride ? x_stride : cols;
+  if (ld < cols) return JZ_ERR_SHAPE;
+  if (rows > I8_ROWS || ld > (1 << 24) || rows * ld > I8_ELEMENTS) return JZ_ERR_UNSUPPORTED;
+  if (rows == 0) return JZ_OK;
+  if (!x || !q || !scale) return JZ_ERR_NULL;
+  const I8Tensor t[] = {{x, span_of(rows, cols, ld, elem(dtype)), 16, false}, {q, (size_t)rows * i8_pitch(cols), 16, true}, {scale, (size_t)rows * 4, 16, true}};
+  const int rc = look_over(t, 3, nullptr, 0);
+  if (rc != JZ_OK) return rc;
+  return quantize(dtype, {x, static_cast<signed char*>(q), scale, rows, ld, i8_pitch(cols), cols}, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" int jz_linear_i8_workspace_bytes(const jz_linear_i8_desc* d, size_t* bytes) {
+  if (!bytes) return JZ_ERR_NULL;
+  I8Shape s;
+  const int rc = i8_shape(d, &s);
+  if (rc != JZ_OK) return rc;
+  *bytes = I8Room(s.M, s.K).total;
+  return JZ_OK;
+}
+
+extern "C" int jz_linear_i8(const jz_linear_i8_desc* d, const void* x, const void* wq, const float* w_scale, void* y, void* ws, size_t ws_bytes, void* hip_stream) {
+  I8Shape s;
+  int rc = i8_shape(d, &s);
+  if (rc != JZ_OK) return rc;
+  if (!wq || !w_scale || (s.M && (!x || !y))) return JZ_ERR_NULL;
+  if (s.M == 0) return JZ_OK;
+  const I8Room room(s.M, s.K);
+  if (!ws || ws_bytes < room.total) return JZ_ERR_WORKSPACE;
+  if (!jz::aligned16(ws)) return JZ_ERR_ALIGN;
+  const I8Tensor t[] = {{x, span_of(s.M, s.K, s.ldx, elem(d->dtype)), 16, false}, {wq, (size_t)s.N * i8_pitch(s.K), 16, false}, {w_scale, (size_t)s.N * 4, 16, false},
+                        {y, span_of(s.M, s.N, s.ldy, elem(d->dtype)), 16, true}};
+  rc = look_over(t, 4, ws, ws_bytes);
+  if (rc != JZ_OK) return rc;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  signed char* const q = static_cast<signed char*>(ws);
+  float* const sx = reinterpret_cast<float*>(q + room.scales);
+  rc = quantize(d->dtype, {x, q, sx, s.M, s.ldx, i8_pitch(s.K), (int)s.K}, st);
+  if (rc != JZ_OK) return rc;
+  const MmArgs a = i8_args(q, s.M, wq, nullptr, s.N, s.K);
+  const I8Out o = {sx, w_scale, nullptr, y, s.M, s.N, s.ldy, 0};
+  return d->dtype == JZ_F32 ? i8_product<float>(a, o, st) : d->dtype == JZ_F16 ? i8_product<_Float16>(a, o, st) : i8_product<__bf16>(a, o, st);
+}
+
+extern "C" int jz_ffn_i8_workspace_bytes(const jz_ffn_desc* d, size_t* bytes) {
+  if (!bytes) return JZ_ERR_NULL;
+  I8Shape s;
+  int64_t F;
+  const int rc = ffn_i8_shape(d, &s, &F);
+  if (rc != JZ_OK) return rc;
+  *bytes = I8Room(s.M, s.K).total + I8Room(s.M, F).total + round256((size_t)s.M * F * 4);
+  return JZ_OK;
+}
+
+extern "C" int jz_ffn_i8_fwd(const jz_ffn_desc* d, const void* x, const void* wq_gate, const float* s_gate, const void* wq_up, const float* s_up, const void* wq_down,
+                             const float* s_down, void* y, void* ws, size_t ws_bytes, void* hip_stream) {
+  I8Shape s;
+  int64_t F;
+  int rc = ffn_i8_shape(d, &s, &F);
+  if (rc != JZ_OK) return rc;
+  if (!wq_gate || !s_gate || !wq_up || !s_up || !wq_down || !s_down || (s.M && (!x || !y))) return JZ_ERR_NULL;
+  if (s.M == 0) return JZ_OK;
+  const I8Room rx(s.M, s.K), rh(s.M, F);
+  if (!ws || ws_bytes < rx.total + rh.total + round256((size_t)s.M * F * 4)) return JZ_ERR_WORKSPACE;
+  if (!jz::aligned16(ws)) return JZ_ERR_ALIGN;
+  const size_t w = (size_t)F * i8_pitch(s.K), f = (size_t)F * 4;
+  const I8Tensor t[] = {{x, span_of(s.M, s.K, s.ldx, 2), 16, false}, {wq_gate, w, 16, false}, {s_gate, f, 16, false}, {wq_up, w, 16, false}, {s_up, f, 16, false},
+                        {wq_down, (size_t)s.N * i8_pitch(F), 16, false}, {s_down, (size_t)s.N * 4, 16, false}, {y, span_of(s.M, s.N, s.ldy, 2), 16, true}};
+  rc = look_over(t, 8, ws, ws_bytes);
+  if (rc != JZ_OK) return rc;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  char* const b = static_cast<char*>(ws);
+  signed char *const qx = reinterpret_cast<signed char*>(b), *const qh = qx + rx.total;
+  float *const sx = reinterpret_cast<float*>(qx + rx.scales), *const sh = reinterpret_cast<float*>(qh + rh.scales), *const h = reinterpret_cast<float*>(b + rx.total + rh.total);
+  rc = quantize(d->dtype, {x, qx, sx, s.M, s.ldx, i8_pitch(s.K), (int)s.K}, st);
+  if (rc == JZ_OK) rc = i8_glu(i8_args(qx, s.M, wq_gate, wq_up, F, s.K), {sx, s_gate, s_up, h, s.M, F, F, d->act}, st);
+  if (rc == JZ_OK) rc = quantize(JZ_F32, {h, qh, sh, s.M, F, i8_pitch(F), (int)F}, st);
+  if (rc != JZ_OK) return rc;
+  const MmArgs a = i8_args(qh, s.M, wq_down, nullptr, s.N, F);
+  const I8Out o = {sh, s_down, nullptr, y, s.M, s.N, s.ldy, 0};
+  return d->dtype == JZ_F16 ? i8_product<_Float16>(a, o, st) : i8_product<__bf16>(a, o, st);
+}

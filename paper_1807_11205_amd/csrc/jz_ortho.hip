@@ -1,0 +1,491 @@
+// Orthogonalised updates (include/jz.h: jz_orthogonalize, jz_muon_mp_update): Newton-Schulz products on the matrix instructions.
+//
+//   X = G / (||G|| + eps)  (transposed where G has more rows than columns: m <= n),   steps times   A = X X^T,  B = a I + b A + c A^2,  X <- B X
+//
+// Every step applies s -> a s + b s^3 + c s^5 to the singular values and leaves the singular vectors.  Small values grow by a (3.4) a step, and what is lost of them early
+// grows with them; hence 22 bits an element, as two FP16 parts (jz_mm_tile.h), and FP32 sums.  Matrices are scaled by 2^11: values up to 31 are in FP16's range, and
+// the low part of an element of 2^-12, the size that a normalised 4096 x 4096 matrix has, still has its bits.  A and B are symmetric: only tiles on and below the diagonal are
+// computed, and stored twice.  X is kept in both orders, since it is an operand along both of its sides.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "jz_internal.h"
+
+namespace {
+
+#include "jz_lds_dma.h"
+#include "jz_vec.h"
+#include "jz_tile_schedule.h"
+#include "jz_mm_tile.h"
+
+constexpr float SCALE = 2048.f;
+constexpr int PAD = 32;      // sides of the matrices in the workspace are multiples of this, zeros behind their ends
+constexpr int PARTS = 64;    // workgroups that share a matrix's sum of squares
+
+// eight columns from col (a multiple of 8) on of a row of parts: 64 bytes of high parts of 32 columns, then their low parts
+__device__ __forceinline__ void store_parts(char* row, int64_t col, const float (&v)[8]) {
+  f16x8 hi, lo;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    hi[i] = (_Float16)v[i];
+    lo[i] = (_Float16)(v[i] - (float)hi[i]);
+  }
+  char* const p = row + (col >> 5) * 128 + (col & 31) * 2;
+  *reinterpret_cast<f16x8*>(p) = hi;
+  *reinterpret_cast<f16x8*>(p + 64) = lo;
+}
+__device__ __forceinline__ void load_parts(const char* row, int64_t col, float (&v)[8]) {
+  const char* const p = row + (col >> 5) * 128 + (col & 31) * 2;
+  const f16x8 hi = *reinterpret_cast<const f16x8*>(p), lo = *reinterpret_cast<const f16x8*>(p + 64);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (float)hi[i] + (float)lo[i];
+}
+
+// ---- the matrix itself ----------------------------------------------------------------------------------------------------------
+struct OrthoIn {
+  const void* x;        // [count][rows][cols], stride elements apart: the matrix, or gradients
+  float* momentum;      // of the update
+  float inv_s, mu;
+  const jz_loss_scale_state* state;
+  int nesterov;
+  int64_t count, rows, cols, stride;
+  double *sums, *inv;   // [count][PARTS]; [count]
+  float eps;
+  const int* skip;
+  int* found_inf;
+};
+// what is orthogonalised; g: the true gradient, v: the new momentum
+template <class T, bool MUON>
+struct OrthoValue {
+  const OrthoIn& a;
+  float inv_s;
+  __device__ __forceinline__ OrthoValue(const OrthoIn& a_) : a(a_), inv_s(MUON && a_.state ? 1.f / a_.state->scale : a_.inv_s) {}
+  __device__ __forceinline__ float get(int64_t i, float* g, float* v) const {
+    const float x = (float)static_cast<const T*>(a.x)[i];
+    if constexpr (!MUON) {
+      *g = *v = x;
+      return x;
+    } else {
+      *g = x * inv_s;
+      *v = a.mu * a.momentum[i] + *g;
+      return a.nesterov ? *g + a.mu * *v : *v;
+    }
+  }
+};
+
+// Partial sums of squares, in FP64; NaN where a gradient is not finite.
+template <class T, bool MUON>
+__global__ __launch_bounds__(256) void ortho_sumsq(OrthoIn a) {
+  __shared__ double lds[4];
+  const OrthoValue<T, MUON> in(a);
+  const int64_t n = a.rows * a.cols, base = (int64_t)blockIdx.y * a.stride;
+  double s = 0.;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += PARTS * 256) {
+    float g, v;
+    const double u = in.get(base + i, &g, &v);
+    s += u * u;
+    if (MUON && !(fabsf(g) < INFINITY)) s = NAN;
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) a.sums[(int64_t)blockIdx.y * PARTS + blockIdx.x] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+
+// Each matrix's factor; of the update, whether anything is to be done.  One workgroup, a wavefront a matrix.
+template <bool MUON>
+__global__ __launch_bounds__(1024) void ortho_factors(OrthoIn a) {
+  __shared__ int bad;
+  if (threadIdx.x == 0) bad = MUON && a.skip && *a.skip;
+  __syncthreads();
+  for (int64_t b = threadIdx.x >> 6; b < a.count; b += 16) {
+    double s = a.sums[b * PARTS + (threadIdx.x & 63)];
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) {
+      const double norm = sqrt(s) + (double)a.eps;
+      a.inv[b] = norm == 0. ? 0. : (double)SCALE / norm;
+      if (MUON && !(s < INFINITY)) bad = 1;
+    }
+  }
+  __syncthreads();
+  if (MUON && threadIdx.x == 0) *a.found_inf = bad;
+}
+
+// The matrix in parts, in both orders: r [rows][cols], c [cols][rows].  A tile of 64 x 64 a workgroup.
+struct OrthoParts {
+  char *r, *c;
+  int64_t rp, cp;  // padded sides
+};
+template <class T, bool MUON>
+__global__ __launch_bounds__(256) void ortho_parts(OrthoIn a, OrthoParts o) {
+  __shared__ float tile[64][65];
+  if (MUON && *a.found_inf) return;
+  const OrthoValue<T, MUON> in(a);
+  const int64_t across = (o.cp + 63) / 64, down = (o.rp + 63) / 64, of = blockIdx.x / (across * down), t = blockIdx.x - of * across * down;
+  const int64_t r0 = t / across * 64, c0 = t % across * 64, base = of * a.stride;
+  const double inv = a.inv[of];
+  for (int i = threadIdx.x; i < 64 * 64; i += 256) {
+    const int64_t r = r0 + i / 64, c = c0 + i % 64;
+    float u = 0.f;
+    if (r < a.rows && c < a.cols) {
+      float g, v;
+      u = (float)((double)in.get(base + r * a.cols + c, &g, &v) * inv);
+      if (MUON) a.momentum[base + r * a.cols + c] = v;
+    }
+    tile[i / 64][i % 64] = u;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 64 * 8; i += 256) {
+    const int row = i / 8, col = i % 8 * 8;
+    float v[8];
+    if (r0 + row < o.rp && c0 + col < o.cp) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = tile[row][col + e];
+      store_parts(o.r + (of * o.rp + r0 + row) * o.cp * 4, c0 + col, v);
+    }
+    if (c0 + row < o.cp && r0 + col < o.rp) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = tile[col + e][row];
+      store_parts(o.c + (of * o.cp + c0 + row) * o.rp * 4, r0 + col, v);
+    }
+  }
+}
+
+// ---- products -------------------------------------------------------------------------------------------------------------------
+// [rows][cols] of parts
+struct Parts {
+  char* p;
+  int64_t rows, cols;
+  __device__ __forceinline__ char* row(int64_t of, int64_t r) const { return p + (of * rows + r) * cols * 4; }
+};
+template <class S>
+__device__ __forceinline__ void store_rows(const S& s, const Parts& to, int64_t of, int64_t m0, int64_t n0, int lane, float factor) {
+  constexpr int PER = S::COLS / 8;
+#pragma unroll 1
+  for (int i = lane; i < 32 * PER; i += 64) {
+    const int row = i / PER, c = i % PER * 8;
+    if (m0 + row >= to.rows || n0 + c >= to.cols) continue;
+    float v[8];
+    s.row8(row, c, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= factor;
+    store_parts(to.row(of, m0 + row), n0 + c, v);
+  }
+}
+template <class S>
+__device__ __forceinline__ void store_cols(const S& s, const Parts& to, int64_t of, int64_t m0, int64_t n0, int lane, float factor) {
+#pragma unroll 1
+  for (int i = lane; i < S::COLS * 4; i += 64) {
+    const int col = i / 4, r = i % 4 * 8;
+    if (n0 + col >= to.rows || m0 + r >= to.cols) continue;
+    float v[8];
+    s.col8(r, col, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= factor;
+    store_parts(to.row(of, n0 + col), m0 + r, v);
+  }
+}
+struct OrthoGram {  // A = X X^T
+  Parts a;
+  template <class S>
+  __device__ __forceinline__ void strip(const S& s, const MmTile& w, int64_t m0, int64_t n0, int lane) const {
+    store_rows(s, a, w.of, m0, n0, lane, 1.f / SCALE);
+    if (w.m != w.n) store_cols(s, a, w.of, m0, n0, lane, 1.f / SCALE);
+  }
+};
+struct OrthoPoly {  // B = ca I + cb A + cc A^2
+  Parts a, b;
+  float ca, cb, cc;
+  template <class S>
+  __device__ __forceinline__ void strip(const S& s, const MmTile& w, int64_t m0, int64_t n0, int lane) const {
+    constexpr int PER = S::COLS / 8;
+#pragma unroll 1
+    for (int i = lane; i < 32 * PER; i += 64) {
+      const int row = i / PER, c = i % PER * 8;
+      if (m0 + row >= a.rows || n0 + c >= a.cols) continue;
+      float v[8], u[8];
+      s.row8(row, c, v);
+      load_parts(a.row(w.of, m0 + row), n0 + c, u);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = fmaf(cc / SCALE, v[e], fmaf(cb, u[e], m0 + row == n0 + c + e ? ca * SCALE : 0.f));
+      s.set_row8(row, c, v);
+      store_parts(b.row(w.of, m0 + row), n0 + c, v);
+    }
+    if (w.m != w.n) store_cols(s, b, w.of, m0, n0, lane, 1.f);
+  }
+};
+struct OrthoApply {  // X <- B X
+  Parts x, xt;
+  template <class S>
+  __device__ __forceinline__ void strip(const S& s, const MmTile& w, int64_t m0, int64_t n0, int lane) const {
+    store_rows(s, x, w.of, m0, n0, lane, 1.f / SCALE);
+    store_cols(s, xt, w.of, m0, n0, lane, 1.f / SCALE);
+  }
+};
+template <class O>
+struct OrthoResult {  // the last B X, rounded once; transposed back where TALL was transposed
+  O* y;
+  int64_t m, n, stride;
+  bool tall;
+  template <class S>
+  __device__ __forceinline__ void strip(const S& s, const MmTile& w, int64_t m0, int64_t n0, int lane) const {
+    constexpr int PER = S::COLS / 8;
+    O* const to = y + w.of * stride;
+    float v[8];
+    f32x8 f;
+    if (!tall) {
+#pragma unroll 1
+      for (int i = lane; i < 32 * PER; i += 64) {
+        const int row = i / PER, c = i % PER * 8;
+        if (m0 + row >= m || n0 + c >= n) continue;
+        s.row8(row, c, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = v[e] * (1.f / (SCALE * SCALE));
+        store8(to + (m0 + row) * n + n0 + c, narrow8<O>(f), n - n0 - c < 8 ? (int)(n - n0 - c) : 8);
+      }
+    } else {
+#pragma unroll 1
+      for (int i = lane; i < S::COLS * 4; i += 64) {
+        const int col = i / 4, r = i % 4 * 8;
+        if (n0 + col >= n || m0 + r >= m) continue;
+        s.col8(r, col, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = v[e] * (1.f / (SCALE * SCALE));
+        store8(to + (n0 + col) * m + m0 + r, narrow8<O>(f), m - m0 - r < 8 ? (int)(m - m0 - r) : 8);
+      }
+    }
+  }
+};
+
+// ---- the update's last pass -------------------------------------------------------------------------------------------------------
+struct MuonApply {
+  const float* o;     // [count][rows cols], dense
+  float* w;
+  void* w16;
+  int64_t each, stride, all;
+  float lr, update_scale, wd;
+  const int* found_inf;
+};
+template <class T>
+__global__ __launch_bounds__(256) void muon_apply(MuonApply a) {
+  if (*a.found_inf) return;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.all; i += (int64_t)gridDim.x * 256) {
+    const int64_t b = i / a.each, at = b * a.stride + (i - b * a.each);
+    const float w = a.w[at];
+    float r = w - a.lr * (a.update_scale * a.o[i] + a.wd * w);
+    lds_pin(r);  // rounded to FP32 here: the copy is that value's, and not the 16-bit rounding of a fused multiply-add
+    a.w[at] = r;
+    static_cast<T*>(a.w16)[at] = (T)r;
+  }
+}
+
+// ---- host -------------------------------------------------------------------------------------------------------------------------
+struct OrthoShape {
+  int64_t count, rows, cols, stride, m, n, mp, np;
+  bool tall;
+};
+int ortho_shape(const jz_ortho_desc* d, OrthoShape* s) {
+  if (!d) return JZ_ERR_NULL;
+  if (d->count < 0 || d->rows <= 0 || d->cols <= 0 || d->dtype < JZ_F16 || d->dtype > JZ_F32 || d->out_dtype < JZ_F16 || d->out_dtype > JZ_F32 || d->steps < 1 ||
+      !(fabsf(d->a) < INFINITY) || !(fabsf(d->b) < INFINITY) || !(fabsf(d->c) < INFINITY) || !(d->eps >= 0.f && d->eps < INFINITY))
+    return JZ_ERR_SHAPE;
+  const int64_t each = (int64_t)d->rows * d->cols;
+  *s = {d->count, d->rows, d->cols, d->stride ? d->stride : each, std::min(d->rows, d->cols), std::max(d->rows, d->cols), 0, 0, d->rows > d->cols};
+  if (s->stride < each) return JZ_ERR_SHAPE;
+  s->mp = (s->m + PAD - 1) / PAD * PAD;
+  s->np = (s->n + PAD - 1) / PAD * PAD;
+  if (s->n > (1 << 17) || d->steps > 64 || s->count > 65535 || s->stride > int64_t(1) << 35 || s->count * s->stride > int64_t(1) << 35 || s->count * s->mp * s->np > int64_t(1) << 35)
+    return JZ_ERR_UNSUPPORTED;
+  return JZ_OK;
+}
+size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
+struct OrthoLayout {
+  size_t sums, inv, x, xt[2], a, b, total;
+  explicit OrthoLayout(const OrthoShape& s) {
+    size_t o = 0;
+    auto room = [&](size_t bytes) {
+      const size_t at = o;
+      o += round256(bytes);
+      return at;
+    };
+    const size_t wide = (size_t)s.count * s.mp * s.np * 4, square = (size_t)s.count * s.mp * s.mp * 4;
+    sums = room((size_t)s.count * PARTS * 8);
+    inv = room((size_t)s.count * 8);
+    x = room(wide);
+    xt[0] = room(wide);
+    xt[1] = room(wide);
+    a = room(square);
+    b = room(square);
+    total = o;
+  }
+};
+
+template <class Epi>
+int ortho_product(const Parts& p, const Parts& q, bool symmetric, int64_t count, const int* skip, const Epi& e, hipStream_t st) {
+  MmArgs a = {};
+  a.a = {{p.p, p.p}, p.rows, p.cols * 4, p.rows * p.cols * 4};
+  a.b = {{q.p, q.p}, q.rows, q.cols * 4, q.rows * q.cols * 4};
+  a.row_bytes = p.cols * 4;
+  a.symmetric = symmetric;
+  a.skip = skip;
+  auto tiles = [&](int64_t t) {
+    const int64_t m = (p.rows + t - 1) / t, n = (q.rows + t - 1) / t;
+    return (symmetric ? m * (m + 1) / 2 : m * n) * count;
+  };
+  if (tiles(256) >= 200) return mm_launch<ElemSplit, Epi, 256, false>(a, e, p.rows, q.rows, count, st);
+  if (tiles(128) >= 200) return mm_launch<ElemSplit, Epi, 128, false>(a, e, p.rows, q.rows, count, st);
+  return mm_launch<ElemSplit, Epi, 64, false>(a, e, p.rows, q.rows, count, st);
+}
+
+template <class T, bool MUON>
+int ortho_begin(const OrthoIn& in, const OrthoShape& s, const OrthoParts& o, hipStream_t st) {
+  ortho_sumsq<T, MUON><<<dim3(PARTS, (unsigned)s.count), 256, 0, st>>>(in);
+  ortho_factors<MUON><<<1, 1024, 0, st>>>(in);
+  const int64_t tiles = (o.rp + 63) / 64 * ((o.cp + 63) / 64) * s.count;
+  ortho_parts<T, MUON><<<(unsigned)tiles, 256, 0, st>>>(in, o);
+  return jz::launch_status();
+}
+
+template <class O>
+int ortho_steps(const jz_ortho_desc* d, const OrthoShape& s, const OrthoLayout& L, char* b, O* y, int64_t y_stride, const int* skip, hipStream_t st) {
+  const Parts x = {b + L.x, s.mp, s.np}, A = {b + L.a, s.mp, s.mp}, B = {b + L.b, s.mp, s.mp};
+  for (int i = 0; i < d->steps; ++i) {
+    const Parts xt = {b + L.xt[i & 1], s.np, s.mp}, next = {b + L.xt[!(i & 1)], s.np, s.mp};
+    int rc = ortho_product(x, x, true, s.count, skip, OrthoGram{A}, st);
+    if (rc == JZ_OK) rc = ortho_product(A, A, true, s.count, skip, OrthoPoly{A, B, d->a, d->b, d->c}, st);
+    if (rc != JZ_OK) return rc;
+    if (i + 1 < d->steps) rc = ortho_product(B, xt, false, s.count, skip, OrthoApply{x, next}, st);
+    else rc = ortho_product(B, xt, false, s.count, skip, OrthoResult<O>{y, s.m, s.n, y_stride, s.tall}, st);
+    if (rc != JZ_OK) return rc;
+  }
+  return JZ_OK;
+}
+OrthoParts begin_parts(const OrthoShape& s, const OrthoLayout& L, char* b) {
+  if (s.tall) return {b + L.xt[0], b + L.x, s.np, s.mp};
+  return {b + L.x, b + L.xt[0], s.mp, s.np};
+}
+size_t bytes_of(int dtype) { return dtype == JZ_F32 ? 4 : 2; }
+size_t batch_bytes(const OrthoShape& s, size_t each) { return s.count ? ((size_t)(s.count - 1) * s.stride + s.rows * s.cols) * each : 0; }
+
+}  // namespace
+
+extern "C" int jz_orthogonalize_workspace_bytes(const jz_ortho_desc* d, size_t* bytes) {
+  if (!bytes) return JZ_ERR_NULL;
+  OrthoShape s;
+  const int rc = ortho_shape(d, &s);
+  if (rc != JZ_OK) return rc;
+  *bytes = s.count ? OrthoLayout(s).total : 0;
+  return JZ_OK;
+}
+
+extern "C" int jz_orthogonalize(const jz_ortho_desc* d, const void* x, void* y, void* ws, size_t ws_bytes, void* hip_stream) {
+  OrthoShape s;
+  int rc = ortho_shape(d, &s);
+  if (rc != JZ_OK) return rc;
+  if (s.count == 0) return JZ_OK;
+  if (!x || !y) return JZ_ERR_NULL;
+  const OrthoLayout L(s);
+  if (!ws || ws_bytes < L.total) return JZ_ERR_WORKSPACE;
+  if (!jz::aligned16(x) || !jz::aligned16(y) || !jz::aligned16(ws)) return JZ_ERR_ALIGN;
+  const size_t nx = batch_bytes(s, bytes_of(d->dtype)), ny = batch_bytes(s, bytes_of(d->out_dtype));
+  if (jz::overlaps(x, nx, y, ny) || jz::overlaps(x, nx, ws, ws_bytes) || jz::overlaps(y, ny, ws, ws_bytes)) return JZ_ERR_ALIAS;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  char* const b = static_cast<char*>(ws);
+  OrthoIn in = {};
+  in.x = x;
+  in.count = s.count;
+  in.rows = s.rows;
+  in.cols = s.cols;
+  in.stride = s.stride;
+  in.sums = reinterpret_cast<double*>(b + L.sums);
+  in.inv = reinterpret_cast<double*>(b + L.inv);
+  in.eps = d->eps;
+  const OrthoParts o = begin_parts(s, L, b);
+  rc = d->dtype == JZ_F32 ? ortho_begin<float, false>(in, s, o, st) : d->dtype == JZ_F16 ? ortho_begin<_Float16, false>(in, s, o, st) : ortho_begin<__bf16, false>(in, s, o, st);
+  if (rc != JZ_OK) return rc;
+  if (d->out_dtype == JZ_F32) return ortho_steps(d, s, L, b, static_cast<float*>(y), s.stride, nullptr, st);
+  if (d->out_dtype == JZ_F16) return ortho_steps(d, s, L, b, static_cast<_Float16*>(y), s.stride, nullptr, st);
+  return ortho_steps(d, s, L, b, static_cast<__bf16*>(y), s.stride, nullptr, st);
+}
+
+namespace {
+int muon_shape(const jz_ortho_desc* d, OrthoShape* s) {
+  const int rc = ortho_shape(d, s);
+  if (rc != JZ_OK) return rc;
+  if (d->dtype != d->out_dtype) return JZ_ERR_SHAPE;
+  return d->dtype == JZ_F32 ? JZ_ERR_UNSUPPORTED : JZ_OK;
+}
+}  // namespace
+
+extern "C" int jz_muon_mp_update_workspace_bytes(const jz_ortho_desc* d, size_t* bytes) {
+  if (!bytes) return JZ_ERR_NULL;
+  OrthoShape s;
+  const int rc = muon_shape(d, &s);
+  if (rc != JZ_OK) return rc;
+  *bytes = OrthoLayout(s).total;
+  return JZ_OK;
+}
+
+extern "C" int jz_muon_mp_update(const jz_ortho_desc* d, const jz_muon_hparams* hp, const jz_loss_scale_state* state_dev, const int* skip_dev, float* master_w, float* momentum,
+                                 const void* grad16, void* weight16, int* found_inf_dev, void* ws, size_t ws_bytes, void* hip_stream) {
+  OrthoShape s;
+  int rc = muon_shape(d, &s);
+  if (rc != JZ_OK) return rc;
+  if (!hp || !found_inf_dev || (s.count && (!master_w || !momentum || !grad16 || !weight16))) return JZ_ERR_NULL;
+  for (float v : {hp->lr, hp->momentum, hp->weight_decay, hp->update_scale})
+    if (!(fabsf(v) < INFINITY)) return JZ_ERR_SHAPE;
+  if (!state_dev && !(hp->loss_scale > 0.f && hp->loss_scale < 3.0e38f)) return JZ_ERR_SHAPE;
+  const OrthoLayout L(s);
+  if (s.count && (!ws || ws_bytes < L.total)) return JZ_ERR_WORKSPACE;
+  if (!jz::aligned16(master_w) || !jz::aligned16(momentum) || !jz::aligned16(grad16) || !jz::aligned16(weight16) || !jz::aligned16(ws) ||
+      (reinterpret_cast<uintptr_t>(found_inf_dev) & 3) || (reinterpret_cast<uintptr_t>(skip_dev) & 3) || (reinterpret_cast<uintptr_t>(state_dev) & 7))
+    return JZ_ERR_ALIGN;
+  const size_t n = batch_bytes(s, 1);
+  const struct {
+    const void* p;
+    size_t bytes;
+  } t[] = {{master_w, 4 * n}, {momentum, 4 * n}, {weight16, 2 * n}, {found_inf_dev, 4}, {grad16, 2 * n}, {skip_dev, 4}, {state_dev, sizeof(*state_dev)}, {ws, ws_bytes}};
+  for (int i = 0; i < 4; ++i)  // what is written, against everything
+    for (int j = i + 1; j < 8; ++j)
+      if (jz::overlaps(t[i].p, t[i].bytes, t[j].p, t[j].bytes)) return JZ_ERR_ALIAS;
+  for (int j = 4; j < 7; ++j)
+    if (jz::overlaps(t[j].p, t[j].bytes, ws, ws_bytes)) return JZ_ERR_ALIAS;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  char* const b = static_cast<char*>(ws);
+  OrthoIn in = {};
+  in.x = grad16;
+  in.momentum = momentum;
+  in.inv_s = state_dev ? 1.f : 1.f / hp->loss_scale;
+  in.mu = hp->momentum;
+  in.state = state_dev;
+  in.nesterov = hp->nesterov != 0;
+  in.count = s.count;
+  in.rows = s.rows;
+  in.cols = s.cols;
+  in.stride = s.stride;
+  in.sums = reinterpret_cast<double*>(b + L.sums);
+  in.inv = reinterpret_cast<double*>(b + L.inv);
+  in.eps = d->eps;
+  in.skip = skip_dev;
+  in.found_inf = found_inf_dev;
+  if (s.count == 0) {  // the flag alone
+    ortho_factors<true><<<1, 1024, 0, st>>>(in);
+    return jz::launch_status();
+  }
+  const OrthoParts o = begin_parts(s, L, b);
+  rc = d->dtype == JZ_F16 ? ortho_begin<_Float16, true>(in, s, o, st) : ortho_begin<__bf16, true>(in, s, o, st);
+  if (rc != JZ_OK) return rc;
+  float* const result = reinterpret_cast<float*>(b + L.x);  // the last product reads B and the other order of X
+  rc = ortho_steps(d, s, L, b, result, s.rows * s.cols, found_inf_dev, st);
+  if (rc != JZ_OK) return rc;
+  const MuonApply a = {result, master_w, weight16, s.rows * s.cols, s.stride, s.rows * s.cols * s.count, hp->lr, hp->update_scale, hp->weight_decay, found_inf_dev};
+  const unsigned grid = (unsigned)std::min<int64_t>((a.all + 255) / 256, 1 << 16);
+  if (d->dtype == JZ_F16) muon_apply<_Float16><<<grid, 256, 0, st>>>(a);
+  else muon_apply<__bf16><<<grid, 256, 0, st>>>(a);
+  return jz::launch_status();
+}

@@ -1,0 +1,213 @@
+"""Products in 8-bit integers against their definition: codes and scales bit for bit, sums exact, so that a result has three roundings of FP32 (the sum to FP32, the product of the
+scales, their product) and its own.  The gated block: codes of h that lie within FP32's error of a border may be the neighbour's (oracle.tokens.ffn_i8 says how much that is)."""
+import numpy as np
+import pytest
+import torch
+
+from jzt_blocks import DEV, E32, ROUND, TINY, TYPES, check, nans, randn, wide
+from oracle import tokens
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def jz():
+    from paper_1807_11205_amd import api
+    api.lib()
+    assert torch.cuda.is_available()
+    return api
+
+
+def quantized(jz, x, stride=0):
+    rows, cols = x.shape
+    q, s = torch.full((rows, jz.i8_pitch(cols)), 99, dtype=torch.int8, device=DEV), nans(rows, torch.float32)
+    jz.jz_quantize_i8(rows, cols, x, q, s, stride)
+    return q, s
+
+
+def same_codes(jz, x, q, s):
+    rq, rs = tokens.quantize(x.detach().cpu().float().numpy())
+    got = q.cpu().numpy()
+    assert np.array_equal(got[:, :x.shape[1]], rq) and not got[:, x.shape[1]:].any()
+    assert np.array_equal(s.cpu().numpy(), rs, equal_nan=True)
+    return rq, rs
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (1, 16), (5, 17), (2, 2048), (4, 2049), (3, 8193), (2, 20000), (700, 96)])
+def test_codes(jz, dtype, rows, cols):
+    g = np.random.default_rng([1, rows, cols])
+    x = randn(g, (rows, cols), TYPES[dtype], 3.0)
+    x[0, : cols // 2] *= 1e-3
+    q, s = quantized(jz, x)
+    same_codes(jz, x, q, s)
+
+
+def test_codes_of_odd_rows(jz):
+    x = torch.zeros((10, 33), dtype=torch.float32, device=DEV)
+    g = np.random.default_rng(2)
+    x[1] = randn(g, (33,), torch.float32) * 2.0 ** -140            # subnormal, scale and all
+    x[2, 5] = 190 * 2.0 ** -149                                    # its scale rounds down by a third
+    x[3, 7] = float("inf")
+    x[4, 0] = float("nan")
+    x[5] = torch.arange(33, device=DEV) + 0.5                      # ties, with the next
+    x[5, 32] = 127.0
+    x[6] = 3.4e38
+    x[7] = -x[6]
+    x[8, 32] = 2.0 ** -149                                         # scale 0
+    x[9, 3], x[9, 4] = float("-inf"), float("nan")
+    q, s = quantized(jz, x)
+    same_codes(jz, x, q, s)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_codes_of_strided_rows(jz, dtype):
+    g = np.random.default_rng(3)
+    big = randn(g, (9, 300), TYPES[dtype])
+    x = big[:, :131]
+    q, s = quantized(jz, x, 300)
+    same_codes(jz, x, q, s)
+
+
+def linear(jz, x, wq, s, N, x_stride=0, y=None, y_stride=0):
+    M, K = x.shape
+    d = jz.linear_i8_desc(M, K, N, jz.dtype_of(x.dtype), x_stride, y_stride)
+    ws = torch.full((jz.jz_linear_i8_workspace_bytes(d),), 0x5a, dtype=torch.uint8, device=DEV)
+    y = nans((M, N), x.dtype) if y is None else y
+    jz.jz_linear_i8(d, x, wq, s, y, ws)
+    torch.cuda.synchronize()
+    return y
+
+
+SIZES = [(1, 1, 1), (1, 64, 48), (1, 4096, 40), (2, 17, 3), (16, 128, 16), (17, 129, 65), (24, 2048, 700), (33, 100, 33), (64, 1000, 257), (65, 1000, 257), (100, 16, 8), (128, 128, 128),
+         (129, 640, 200), (300, 257, 1000), (777, 1001, 270), (1030, 2049, 640), (513, 64, 5000)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("M,K,N", SIZES)
+def test_linear(jz, dtype, M, K, N):
+    g = np.random.default_rng([4, M, K, N])
+    x = randn(g, (M, K), TYPES[dtype])
+    wq, s = quantized(jz, randn(g, (N, K), torch.float32, K ** -0.5))
+    y = linear(jz, x, wq, s, N)
+    q, sx = tokens.quantize(x.cpu().float().numpy())
+    ref = tokens.linear_i8(q, sx, wq.cpu().numpy()[:, :K], s.cpu().numpy())
+    check(y, ref, np.abs(ref), 3.01, "y")
+
+
+@pytest.mark.parametrize("M,K,N", [(5, 130, 40), (70, 130, 300), (2100, 140, 2300), (6000, 24, 3000)])
+def test_linear_strided(jz, M, K, N):
+    """Rows of x and y inside wider ones; the large ones go to the large tile."""
+    g = np.random.default_rng([5, M])
+    x = randn(g, (M, K + 7), torch.float16)[:, :K]
+    wq, s = quantized(jz, randn(g, (N, K), torch.float32))
+    room = torch.full((M, N + 9), 3.0, dtype=torch.float16, device=DEV)
+    y = linear(jz, x, wq, s, N, K + 7, room[:, :N], N + 9)
+    q, sx = tokens.quantize(x.cpu().float().numpy())
+    some = np.unique(np.concatenate([np.arange(min(M, 40)), np.arange(M - min(M, 40), M), g.integers(0, M, 100)]))
+    ref = tokens.linear_i8(q[some], sx[some], wq.cpu().numpy()[:, :K], s.cpu().numpy())
+    check(y[torch.from_numpy(some).to(DEV)].contiguous(), ref, np.abs(ref), 3.01, "y")
+    assert bool((room[:, N:] == 3).all())
+
+
+@pytest.mark.parametrize("M", [1, 40, 200, 3000])
+def test_largest_sums(jz, M):
+    """in_features as large as int32 allows, every product 127 x 127; signs that alternate add up to nothing."""
+    K, N = 131072, 17
+    x = torch.full((M, K), 2.0, dtype=torch.float16, device=DEV)
+    w = torch.full((N, K), 127, dtype=torch.int8, device=DEV)
+    w[1] = -127
+    w[2, ::2] = -127
+    y = linear(jz, x, w, torch.full((N,), 2.0 ** -20, dtype=torch.float32, device=DEV), N).double()
+    want = 127.0 * 127 * K * (float(np.float32(2.0) / np.float32(127)) * 2.0 ** -20)
+    assert bool((y[:, 2] == 0).all()) and torch.equal(y[:, 1], -y[:, 0]) and abs(float(y[0, 0]) - want) <= (2.0 ** -11 + 3.01 * E32) * want
+    assert bool((y[:, [0, 3, 16]] == y[0, 0]).all())
+
+
+def test_rows_that_are_not_finite(jz):
+    g = np.random.default_rng(6)
+    for M in (4, 90):
+        x = randn(g, (M, 50), torch.float16)
+        x[1, 3], x[3, 49] = float("inf"), float("nan")
+        x[2] = 0
+        w = randn(g, (30, 50), torch.float32)
+        w[7, 7] = float("nan")
+        w[8] = 0
+        y = linear(jz, x, *quantized(jz, w), 30)
+        bad = torch.isnan(y)
+        want = torch.zeros((M, 30), dtype=torch.bool, device=DEV)
+        want[[1, 3]] = True
+        want[:, 7] = True
+        assert torch.equal(bad, want) and bool((y[2][~want[2]] == 0).all()) and bool((y[0, 8] == 0).all())
+
+
+def ffn(jz, x, ws_, D, F, O, act, x_stride=0):
+    M = x.shape[0]
+    d = jz.ffn_desc(M, D, F, O, act, jz.dtype_of(x.dtype), x_stride)
+    ws = torch.full((jz.jz_ffn_i8_workspace_bytes(d),), 0x5a, dtype=torch.uint8, device=DEV)
+    y = nans((M, O), x.dtype)
+    jz.jz_ffn_i8_fwd(d, x, *ws_, y, ws)
+    torch.cuda.synchronize()
+    return y
+
+
+ACTS = ["silu", "gelu", "gelu_tanh", "relu"]
+
+
+@pytest.mark.parametrize("M,D,F,O", [(1, 64, 96, 32), (3, 65, 33, 7), (24, 256, 700, 130), (64, 100, 200, 60), (65, 100, 200, 60), (200, 300, 515, 129), (1100, 72, 1030, 48), (2900, 40, 2100, 24)])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("act", range(4))
+def test_block(jz, M, D, F, O, dtype, act):
+    g = np.random.default_rng([7, M, D, F, act])
+    x = randn(g, (M, D), TYPES[dtype], 1.5)
+    w = []
+    for a, b in ((F, D), (F, D), (O, F)):
+        w += list(quantized(jz, randn(g, (a, b), torch.float32, b ** -0.5)))
+    y = ffn(jz, x, w, D, F, O, act)
+    host = [(w[i].cpu().numpy()[:, :c], w[i + 1].cpu().numpy()) for i, c in ((0, D), (2, D), (4, F))]
+    ref, off = tokens.ffn_i8(*tokens.quantize(x.cpu().float().numpy()), *host, ACTS[act])
+    bound = ROUND[y.dtype] * np.abs(ref) + (1 + ROUND[y.dtype]) * (3.01 * E32 * np.abs(ref) + off) + TINY[y.dtype]
+    assert np.all(np.abs(wide(y) - ref) <= bound)
+
+
+def test_block_of_strided_rows(jz):
+    g = np.random.default_rng(8)
+    x = randn(g, (50, 90), torch.bfloat16)
+    w = []
+    for a, b in ((48, 64), (48, 64), (40, 48)):
+        w += list(quantized(jz, randn(g, (a, b), torch.float32)))
+    assert torch.equal(ffn(jz, x[:, :64], w, 64, 48, 40, 0, 90), ffn(jz, x[:, :64].contiguous(), w, 64, 48, 40, 0))
+
+
+@pytest.mark.parametrize("M", [2, 150])
+def test_in_a_graph_and_on_another_stream(jz, M):
+    g = np.random.default_rng(9)
+    D, F, O = 128, 320, 96
+    x = randn(g, (M, D), torch.float16)
+    w = []
+    for a, b in ((F, D), (F, D), (O, F)):
+        w += list(quantized(jz, randn(g, (a, b), torch.float32, b ** -0.5)))
+    d = jz.ffn_desc(M, D, F, O)
+    ws = torch.empty(jz.jz_ffn_i8_workspace_bytes(d), dtype=torch.uint8, device=DEV)
+    y, again = nans((M, O), torch.float16), nans((M, O), torch.float16)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    jz.jz_ffn_i8_fwd(d, x, *w, y, ws, stream=side)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        jz.jz_ffn_i8_fwd(d, x, *w, again, ws)
+    for k in range(4):
+        if k:
+            x.copy_(randn(g, (M, D), torch.float16))
+            jz.jz_ffn_i8_fwd(d, x, *w, y, ws)
+        again.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, again), k
+
+
+def test_without_rows(jz):
+    wq, s = quantized(jz, torch.ones((8, 16), device=DEV))
+    assert linear(jz, torch.empty((0, 16), dtype=torch.float16, device=DEV), wq, s, 8).shape == (0, 8)
+    jz.jz_quantize_i8(0, 5, torch.empty((0, 5), device=DEV), torch.empty((0, 16), dtype=torch.int8, device=DEV), torch.empty(0, device=DEV))

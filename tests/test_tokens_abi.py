@@ -1,0 +1,217 @@
+"""Refusals of the embedding, orthogonalisation and 8-bit entry points, found on the host before anything is launched (no GPU needed)."""
+import ctypes
+import math
+import os
+
+import pytest
+
+A = 0x100000000000      # addresses that are never followed: every call here is refused, or has nothing to do
+STEP = 1 << 40
+
+
+@pytest.fixture(scope="module")
+def jz():
+    from paper_1807_11205_amd import api
+    if not os.path.exists(api.LIB_PATH):
+        from paper_1807_11205_amd import build
+        build.build()
+    return api
+
+
+def places(names, over):
+    at = {k: A + i * STEP for i, k in enumerate(names)}
+    at.update(over)
+    return at
+
+
+def spread(d, over):
+    for k in list(over):
+        if hasattr(d, k) and k not in ("momentum",):
+            setattr(d, k, over.pop(k))
+
+
+def size(jz, name, d):
+    n = ctypes.c_size_t(0)
+    return getattr(jz.lib(), name)(ctypes.byref(d), ctypes.byref(n)), n.value
+
+
+# ---- embedding --------------------------------------------------------------------------------------------------------
+def embed(jz, forward, ws_bytes=None, accumulate=0, **over):
+    d = jz.embed_desc(50, 100, 64)
+    spread(d, over)
+    at = places(["ids", "table", "out", "dout", "dtable", "ws"], over)
+    if forward:
+        return jz.lib().jz_embed_fwd(ctypes.byref(d), at["ids"], at["table"], at["out"], None)
+    n = size(jz, "jz_embed_bwd_workspace_bytes", d)[1]
+    return jz.lib().jz_embed_bwd(ctypes.byref(d), at["ids"], at["dout"], accumulate, at["dtable"], at["ws"], n if ws_bytes is None else ws_bytes, None)
+
+
+@pytest.mark.parametrize("forward", [True, False])
+def test_embedding_descriptors(jz, forward):
+    for bad in (dict(tokens=-1), dict(vocab=0), dict(vocab=-5), dict(channels=0), dict(dtype=3), dict(dtype=-1), dict(out_dtype=3), dict(out_dtype=-1), dict(scale=math.nan),
+                dict(scale=math.inf), dict(out_stride=63), dict(out_stride=-1)):
+        assert embed(jz, forward, **dict(bad)) == jz.JZ_ERR_SHAPE, bad
+    for bad in (dict(out_dtype=1), dict(dtype=2, out_dtype=0), dict(channels=(1 << 24) + 1), dict(out_stride=(1 << 24) + 1), dict(tokens=1 << 31),
+                dict(tokens=1 << 30, out_stride=257), dict(vocab=1 << 30, channels=257)):
+        assert embed(jz, forward, **dict(bad)) == jz.JZ_ERR_UNSUPPORTED, bad
+
+
+def test_embedding_arguments(jz):
+    for k in ("ids", "table", "out"):
+        assert embed(jz, True, **{k: None}) == jz.JZ_ERR_NULL, k
+        assert embed(jz, True, **{k: A + 9 * STEP + 2}) == jz.JZ_ERR_ALIGN, k
+    assert embed(jz, True, out=A + STEP + 16) == embed(jz, True, out=A) == embed(jz, True, out=A + STEP - 16) == jz.JZ_ERR_ALIAS
+    assert embed(jz, True, tokens=0, ids=None, out=None) == jz.JZ_OK
+    for k in ("ids", "dout", "dtable"):
+        assert embed(jz, False, **{k: None}) == jz.JZ_ERR_NULL, k
+        assert embed(jz, False, **{k: A + 9 * STEP + 2}) == jz.JZ_ERR_ALIGN, k
+    assert embed(jz, False, ws=A + 9 * STEP + 8) == jz.JZ_ERR_ALIGN
+    n = size(jz, "jz_embed_bwd_workspace_bytes", jz.embed_desc(50, 100, 64))[1]
+    assert embed(jz, False, ws=None) == embed(jz, False, ws_bytes=n - 1) == jz.JZ_ERR_WORKSPACE
+    for bad in (dict(dtable=A + 3 * STEP), dict(dtable=A), dict(dtable=A + 5 * STEP), dict(ws=A + 3 * STEP + 64), dict(ws=A + 160)):
+        assert embed(jz, False, **bad) == jz.JZ_ERR_ALIAS, bad
+    assert embed(jz, False, accumulate=1, tokens=0, ids=None, dout=None) == jz.JZ_OK
+    assert size(jz, "jz_embed_bwd_workspace_bytes", jz.embed_desc(-1, 1, 1))[0] == jz.JZ_ERR_SHAPE
+    L = jz.lib()
+    assert L.jz_embed_bwd_workspace_bytes(None, ctypes.byref(ctypes.c_size_t(0))) == L.jz_embed_bwd_workspace_bytes(ctypes.byref(jz.embed_desc(1, 1, 1)), None) == jz.JZ_ERR_NULL
+    assert L.jz_embed_fwd(None, A, A, A, None) == jz.JZ_ERR_NULL
+
+
+# ---- orthogonalisation ------------------------------------------------------------------------------------------------
+def ortho(jz, ws_bytes=None, **over):
+    d = jz.ortho_desc(2, 40, 60)
+    spread(d, over)
+    at = places(["x", "y", "ws"], over)
+    n = size(jz, "jz_orthogonalize_workspace_bytes", d)[1]
+    return jz.lib().jz_orthogonalize(ctypes.byref(d), at["x"], at["y"], at["ws"], n if ws_bytes is None else ws_bytes, None)
+
+
+def test_orthogonalisation(jz):
+    for bad in (dict(count=-1), dict(rows=0), dict(cols=-2), dict(dtype=3), dict(out_dtype=-1), dict(steps=0), dict(a=math.nan), dict(b=math.inf), dict(c=-math.inf), dict(eps=-1.0),
+                dict(eps=math.nan), dict(eps=math.inf), dict(stride=2399), dict(stride=-1)):
+        assert ortho(jz, **dict(bad)) == jz.JZ_ERR_SHAPE, bad
+    for bad in (dict(rows=(1 << 17) + 1), dict(cols=1 << 18), dict(steps=65), dict(count=65536), dict(stride=(1 << 35) + 1), dict(stride=(1 << 34) + 1),
+                dict(rows=1 << 17, cols=1 << 17, count=3)):
+        assert ortho(jz, **dict(bad)) == jz.JZ_ERR_UNSUPPORTED, bad
+    assert ortho(jz, x=None) == ortho(jz, y=None) == jz.JZ_ERR_NULL
+    n = size(jz, "jz_orthogonalize_workspace_bytes", jz.ortho_desc(2, 40, 60))[1]
+    assert ortho(jz, ws=None) == ortho(jz, ws_bytes=n - 1) == jz.JZ_ERR_WORKSPACE
+    for k in ("x", "y", "ws"):
+        assert ortho(jz, **{k: A + 9 * STEP + 8}) == jz.JZ_ERR_ALIGN, k
+    for bad in (dict(y=A), dict(y=A + 4784), dict(stride=4000, y=A + 8000 + 16), dict(ws=A + STEP), dict(x=A + 2 * STEP + 64)):
+        assert ortho(jz, **bad) == jz.JZ_ERR_ALIAS, bad
+    assert ortho(jz, count=0, x=None, y=None, ws=None) == jz.JZ_OK
+    L = jz.lib()
+    for f in (L.jz_orthogonalize_workspace_bytes, L.jz_muon_mp_update_workspace_bytes):
+        assert f(None, ctypes.byref(ctypes.c_size_t(0))) == f(ctypes.byref(jz.ortho_desc(1, 1, 1)), None) == jz.JZ_ERR_NULL
+
+
+def muon(jz, ws_bytes=None, hp=None, **over):
+    d = jz.ortho_desc(2, 40, 60)
+    spread(d, over)
+    at = places(["state", "skip", "master", "momentum", "grad", "weight", "flag", "ws"], over)
+    n = size(jz, "jz_muon_mp_update_workspace_bytes", d)[1]
+    h = jz.muon_hparams(**(hp or {}))
+    return jz.lib().jz_muon_mp_update(ctypes.byref(d), ctypes.byref(h), at["state"], at["skip"], at["master"], at["momentum"], at["grad"], at["weight"], at["flag"], at["ws"],
+                                      n if ws_bytes is None else ws_bytes, None)
+
+
+def test_muon(jz):
+    assert muon(jz, rows=0) == muon(jz, out_dtype=1) == jz.JZ_ERR_SHAPE and muon(jz, dtype=2, out_dtype=2) == muon(jz, steps=100) == jz.JZ_ERR_UNSUPPORTED
+    for bad in (dict(lr=math.nan), dict(momentum=math.inf), dict(weight_decay=math.nan), dict(update_scale=math.inf)):
+        assert muon(jz, hp=bad) == jz.JZ_ERR_SHAPE, bad
+    for s in (0.0, -1.0, math.inf, math.nan):
+        assert muon(jz, hp=dict(loss_scale=s), state=None) == jz.JZ_ERR_SHAPE, s
+    for k in ("master", "momentum", "grad", "weight", "flag"):
+        assert muon(jz, **{k: None}) == jz.JZ_ERR_NULL, k
+    n = size(jz, "jz_muon_mp_update_workspace_bytes", jz.ortho_desc(2, 40, 60))[1]
+    assert muon(jz, ws=None) == muon(jz, ws_bytes=n - 1) == jz.JZ_ERR_WORKSPACE
+    for k, by in (("state", 4), ("skip", 2), ("master", 8), ("momentum", 8), ("grad", 8), ("weight", 8), ("flag", 2), ("ws", 8)):
+        assert muon(jz, **{k: A + 20 * STEP + by}) == jz.JZ_ERR_ALIGN, k
+    names = ["state", "skip", "master", "momentum", "grad", "weight", "flag", "ws"]
+    reach = dict(state=8, skip=4, master=19200, momentum=19200, grad=9600, weight=9600, flag=4, ws=n)
+    for i, p in enumerate(names):
+        for q in names[i + 1:]:
+            if p in ("state", "skip", "grad") and q in ("state", "skip", "grad"):
+                continue                                                # both only read
+            assert muon(jz, **{q: A + i * STEP}) == jz.JZ_ERR_ALIAS, (p, q)
+            if reach[p] >= 32:
+                assert muon(jz, **{q: A + i * STEP + (reach[p] - 1) // 16 * 16}) == jz.JZ_ERR_ALIAS, (p, q)
+
+
+# ---- 8-bit integers ---------------------------------------------------------------------------------------------------
+def test_quantize(jz):
+    def f(rows=5, cols=33, dtype=0, x=A, stride=0, q=A + STEP, s=A + 2 * STEP):
+        return jz.lib().jz_quantize_i8(rows, cols, dtype, x, stride, q, s, None)
+    assert f(rows=-1) == f(cols=0) == f(dtype=3) == f(dtype=-1) == f(stride=32) == f(stride=-1) == jz.JZ_ERR_SHAPE
+    assert f(rows=(1 << 31) + 1) == f(stride=(1 << 24) + 1) == f(cols=(1 << 24) + 1) == f(rows=1 << 31, cols=129) == jz.JZ_ERR_UNSUPPORTED
+    assert f(x=None) == f(q=None) == f(s=None) == jz.JZ_ERR_NULL
+    assert f(x=A + 8) == f(q=A + STEP + 4) == f(s=A + 2 * STEP + 4) == jz.JZ_ERR_ALIGN
+    assert f(q=A) == f(s=A + STEP + 224) == f(q=A + 256) == jz.JZ_ERR_ALIAS
+    assert f(rows=0, x=None, q=None, s=None) == jz.JZ_OK
+
+
+def linear(jz, ws_bytes=None, **over):
+    d = jz.linear_i8_desc(9, 50, 70)
+    spread(d, over)
+    at = places(["x", "wq", "s", "y", "ws"], over)
+    n = size(jz, "jz_linear_i8_workspace_bytes", d)[1]
+    return jz.lib().jz_linear_i8(ctypes.byref(d), at["x"], at["wq"], at["s"], at["y"], at["ws"], n if ws_bytes is None else ws_bytes, None)
+
+
+def test_linear(jz):
+    for bad in (dict(rows=-1), dict(in_features=0), dict(out_features=-1), dict(dtype=3), dict(x_stride=49), dict(y_stride=69)):
+        assert linear(jz, **dict(bad)) == jz.JZ_ERR_SHAPE, bad
+    for bad in (dict(in_features=131073), dict(out_features=(1 << 24) + 1), dict(rows=(1 << 31) + 1), dict(x_stride=(1 << 24) + 1), dict(rows=1 << 31, y_stride=129),
+                dict(in_features=131072, out_features=1 << 22)):
+        assert linear(jz, **dict(bad)) == jz.JZ_ERR_UNSUPPORTED, bad
+    n = size(jz, "jz_linear_i8_workspace_bytes", jz.linear_i8_desc(9, 50, 70))[1]
+    assert linear(jz, ws=None) == linear(jz, ws_bytes=n - 1) == jz.JZ_ERR_WORKSPACE
+    for k in ("x", "wq", "s", "y"):
+        assert linear(jz, **{k: None}) == jz.JZ_ERR_NULL, k
+        assert linear(jz, **{k: A + 9 * STEP + 8}) == jz.JZ_ERR_ALIGN, k
+    assert linear(jz, ws=A + 9 * STEP + 8) == jz.JZ_ERR_ALIGN
+    for bad in (dict(y=A), dict(y=A + STEP + 69 * 64), dict(y=A + 2 * STEP + 272), dict(ws=A + 16), dict(ws=A + 3 * STEP)):
+        assert linear(jz, **bad) == jz.JZ_ERR_ALIAS, bad
+    assert linear(jz, rows=0, x=None, y=None, ws=None) == jz.JZ_OK
+    L = jz.lib()
+    assert L.jz_linear_i8_workspace_bytes(None, ctypes.byref(ctypes.c_size_t(0))) == L.jz_linear_i8_workspace_bytes(ctypes.byref(jz.linear_i8_desc(1, 1, 1)), None) == jz.JZ_ERR_NULL
+
+
+def block(jz, ws_bytes=None, **over):
+    d = jz.ffn_desc(9, 50, 70, 30)
+    spread(d, over)
+    names = ["x", "qg", "sg", "qu", "su", "qd", "sd", "y", "ws"]
+    at = places(names, over)
+    n = size(jz, "jz_ffn_i8_workspace_bytes", d)[1]
+    return jz.lib().jz_ffn_i8_fwd(ctypes.byref(d), *(at[k] for k in names), n if ws_bytes is None else ws_bytes, None)
+
+
+def test_block(jz):
+    for bad in (dict(rows=-1), dict(in_features=0), dict(hidden=0), dict(out_features=-1), dict(dtype=3), dict(act=4), dict(act=-1), dict(x_stride=49), dict(y_stride=29)):
+        assert block(jz, **dict(bad)) == jz.JZ_ERR_SHAPE, bad
+    for bad in (dict(dtype=2), dict(in_features=131073), dict(hidden=131073), dict(out_features=(1 << 24) + 1), dict(rows=(1 << 31) + 1), dict(rows=1 << 31, hidden=129)):
+        assert block(jz, **dict(bad)) == jz.JZ_ERR_UNSUPPORTED, bad
+    n = size(jz, "jz_ffn_i8_workspace_bytes", jz.ffn_desc(9, 50, 70, 30))[1]
+    assert block(jz, ws=None) == block(jz, ws_bytes=n - 1) == jz.JZ_ERR_WORKSPACE
+    for k in ("x", "qg", "sg", "qu", "su", "qd", "sd", "y"):
+        assert block(jz, **{k: None}) == jz.JZ_ERR_NULL, k
+        assert block(jz, **{k: A + 19 * STEP + 8}) == jz.JZ_ERR_ALIGN, k
+    for i in range(7):
+        assert block(jz, y=A + i * STEP) == block(jz, ws=A + i * STEP) == jz.JZ_ERR_ALIAS, i
+    assert block(jz, ws=A + 7 * STEP) == jz.JZ_ERR_ALIAS
+    assert block(jz, rows=0, x=None, y=None, ws=None) == jz.JZ_OK
+
+
+def test_what_the_binding_refuses(jz):
+    import torch
+    for t in (torch.zeros(4, 8), torch.zeros((4, 8), dtype=torch.float16)):         # not on the GPU
+        with pytest.raises(TypeError):
+            jz.jz_embed_fwd(jz.embed_desc(4, 4, 8), torch.zeros(4, dtype=torch.int32), t, t)
+        with pytest.raises(TypeError):
+            jz.jz_orthogonalize(jz.ortho_desc(1, 4, 8), t, t, None)
+        with pytest.raises(TypeError):
+            jz.jz_quantize_i8(4, 8, t, t, t)
+    with pytest.raises(TypeError):
+        jz.jz_quantize_i8(4, 8, torch.zeros((4, 8), dtype=torch.float64), None, None)
+    assert [jz.i8_pitch(n) for n in (1, 16, 17, 4096)] == [16, 16, 32, 4096]
