@@ -441,8 +441,8 @@ int jz_embed_bwd(const jz_embed_desc* desc, const int* ids_dev, const void* dout
 /* Orthogonalised updates of weight matrices, beside LARS for those that are no matrices.  For each of `count` matrices [rows][cols], `stride` elements apart (0: dense):
  *   X = G / (||G||_F + eps),  then `steps` times   X <- a X + (b A + c A^2) X,  A = X X^T       (X^T in X's place where rows > cols)
  * a Newton-Schulz iteration: every singular value s of X goes to a s + b s^3 + c s^5 each time, the singular vectors stay.  With a, b, c = 3.4445, -4.7750, 2.0315 and
- * five steps the values that are not tiny end near 1 (0.7 to 1.2).  a, b, c finite, and such that every element of X, A and b A + c A^2 + a I stays below 31 in magnitude
- * (results are Inf or NaN otherwise: the products take 22 bits of every element, as two FP16 parts).  Sums are FP32, ||G|| is added up in FP64.
+ * five steps the values that are not tiny end near 1 (0.7 to 1.2).  a, b, c finite, and such that the singular values stay below 5 and |a + b t + c t^2| below
+ * max(1, |a|) <= 30 over their squares t (results may be Inf or NaN otherwise: the products take 22 bits of every element, as two FP16 parts).  Sums are FP32, ||G|| is added up in FP64.
  *   jz_orthogonalize   x (dtype) -> y (out_dtype), each JZ_F16, JZ_BF16 or JZ_F32, one rounding.  A matrix of zeros gives zeros; one with Inf or NaN NaNs.
  *   jz_muon_mp_update  one optimiser step in mixed precision; grad16 and weight16 have dtype == out_dtype == JZ_F16 or JZ_BF16:
  *       g = float(grad16) / S,  v <- momentum v + g,  u = g + momentum v where nesterov, else v,  O = the iteration's result for u (FP32)

@@ -44,28 +44,31 @@ __device__ __forceinline__ unsigned long long codes8(f32x8 v, float s, int left)
   }
   return r;
 }
-// A workgroup a row at a time; HOLD vectors of eight stay in a lane's registers, what is behind them is read twice.
-template <class T, int THREADS, int HOLD>
-__global__ __launch_bounds__(THREADS) void i8_quantize(QuantArgs a) {
-  __shared__ unsigned most[THREADS / 64];
-  const int t = threadIdx.x;
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+// A row at a time by a wavefront (WIDE: by the workgroup); HOLD vectors of eight stay in a lane's registers, what is behind them is read twice.
+template <class T, bool WIDE, int HOLD>
+__global__ __launch_bounds__(256) void i8_quantize(QuantArgs a) {
+  constexpr int LANES_ = WIDE ? 256 : 64;
+  __shared__ unsigned most[4];
+  const int t = WIDE ? threadIdx.x : threadIdx.x & 63;
+  for (int64_t row = WIDE ? blockIdx.x : (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < a.rows; row += (int64_t)gridDim.x * (WIDE ? 1 : 4)) {
     const T* const x = static_cast<const T*>(a.x) + row * a.ld;
     auto get = [&](int64_t c) { return c + 8 <= a.cols ? load8(x + c) : load8(x + c, c < a.cols ? (int)(a.cols - c) : 0); };
     typename Vec8<T>::V v[HOLD];
     unsigned m = 0;
 #pragma unroll
-    for (int j = 0; j < HOLD; ++j) v[j] = get(((int64_t)j * THREADS + t) * 8);
+    for (int j = 0; j < HOLD; ++j) v[j] = get(((int64_t)j * LANES_ + t) * 8);
 #pragma unroll
     for (int j = 0; j < HOLD; ++j) m = max(m, magnitude8(widen8<T>(v[j])));
-    for (int64_t c = ((int64_t)HOLD * THREADS + t) * 8; c < a.cols; c += THREADS * 8) m = max(m, magnitude8(widen8<T>(get(c))));
+    for (int64_t c = ((int64_t)HOLD * LANES_ + t) * 8; c < a.cols; c += LANES_ * 8) m = max(m, magnitude8(widen8<T>(get(c))));
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, d));
-    if ((t & 63) == 0) most[t >> 6] = m;
-    __syncthreads();
+    if constexpr (WIDE) {
+      if ((t & 63) == 0) most[t >> 6] = m;
+      __syncthreads();
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) m = max(m, most[w]);
-    __syncthreads();
+      for (int w = 0; w < 4; ++w) m = max(m, most[w]);
+      __syncthreads();
+    }
     const bool fine = m < 0x7f800000u;
     const float s = fine ? __uint_as_float(m) / 127.f : NAN;  // a row with Inf or NaN: every result of it is NaN
     if (t == 0) a.scale[row] = s;
@@ -75,21 +78,25 @@ __global__ __launch_bounds__(THREADS) void i8_quantize(QuantArgs a) {
       if (c < a.pitch) *reinterpret_cast<unsigned long long*>(q + c) = none ? 0ull : codes8(widen8<T>(w), s, c < a.cols ? (int)(a.cols - c) : 0);
     };
 #pragma unroll
-    for (int j = 0; j < HOLD; ++j) put(((int64_t)j * THREADS + t) * 8, v[j]);
-    for (int64_t c = ((int64_t)HOLD * THREADS + t) * 8; c < a.pitch; c += THREADS * 8) put(c, get(c));
+    for (int j = 0; j < HOLD; ++j) put(((int64_t)j * LANES_ + t) * 8, v[j]);
+    for (int64_t c = ((int64_t)HOLD * LANES_ + t) * 8; c < a.pitch; c += LANES_ * 8) put(c, get(c));
   }
 }
+// A wavefront a row where it can hold it and there are rows for the whole chip, else a workgroup a row.
 template <class T>
 int quantize(const QuantArgs& a, hipStream_t st) {
-  const unsigned grid = (unsigned)std::min<int64_t>(a.rows, 1 << 20);
-  if (a.pitch <= 64 * 8 * 4) i8_quantize<T, 64, 4><<<grid, 64, 0, st>>>(a);
-  else i8_quantize<T, 256, 4><<<grid, 256, 0, st>>>(a);
+  auto grid = [&](int64_t rows_each) { return (unsigned)std::min<int64_t>((a.rows + rows_each - 1) / rows_each, 1 << 20); };
+  if (a.pitch <= 64 * 8 * 4) i8_quantize<T, false, 4><<<grid(4), 256, 0, st>>>(a);
+  else if (a.pitch <= 64 * 8 * 8 && a.rows >= 1024) i8_quantize<T, false, 8><<<grid(4), 256, 0, st>>>(a);
+  else i8_quantize<T, true, 4><<<grid(1), 256, 0, st>>>(a);
   return jz::launch_status();
 }
 int quantize(int dtype, const QuantArgs& a, hipStream_t st) {
   if (a.rows == 0) return JZ_OK;
   return dtype == JZ_F32 ? quantize<float>(a, st) : dtype == JZ_F16 ? quantize<_Float16>(a, st) : quantize<__bf16>(a, st);
 }
+
+#include "jz_i8_few.h"
 
 // ---- products -----------------------------------------------------------------------------------------------------------------
 struct I8Out {
@@ -166,6 +173,58 @@ int i8_glu(const MmArgs& a, const I8Out& o, hipStream_t st) {
   const int64_t cols = (o.N + 31) / 32 * 64;
   if ((o.M + 255) / 256 * ((cols + 255) / 256) >= 160) return mm_launch<ElemI8, I8Glu, 256, true>(a, e, o.M, cols, 1, st);
   return mm_launch<ElemI8, I8Glu, 128, true>(a, e, o.M, cols, 1, st);
+}
+
+// Few rows.  Codes of the tokens: from q and sx, or, where x is given, made in every workgroup.
+constexpr int64_t FEW_TOKENS = 64;
+bool few_quantize(int64_t M, int64_t K) { return M <= 4 && M * i8_pitch(K) <= FEW_CODES; }
+template <class X, class Y, bool GLU, int TT, bool QUANTIZE>
+int few_launch(const FewArgs& a, hipStream_t st) {
+  // as many wavefronts as LDS holds, in one workgroup a compute unit or, where there are more of them, several
+  constexpr int W = GLU && TT == 4 ? 4 : 8, CH = (TT == 1 || QUANTIZE) && !GLU ? 2 : 1;
+  const unsigned grid = (unsigned)((a.N + 15) / 16);
+  if (grid <= 256 || W == 4) i8_few<X, Y, GLU, TT, W, CH, QUANTIZE><<<grid, 64 * W, 0, st>>>(a);
+  else i8_few<X, Y, GLU, TT, 4, CH, QUANTIZE><<<grid, 256, 0, st>>>(a);
+  return jz::launch_status();
+}
+template <class X, class Y, bool GLU>
+int few_product(const FewArgs& a, hipStream_t st) {
+  if (a.x) return few_launch<X, Y, GLU, 1, true>(a, st);
+  return a.M <= 16 ? few_launch<float, Y, GLU, 1, false>(a, st) : a.M <= 32 ? few_launch<float, Y, GLU, 2, false>(a, st) : few_launch<float, Y, GLU, 4, false>(a, st);
+}
+
+// ---- the calls ------------------------------------------------------------------------------------------------------------------
+struct Rows {  // tokens as they come, and room for their codes
+  const void* x;
+  int dtype;
+  int64_t M, K, ld;
+  signed char* q;
+  float* s;
+};
+template <class X, class Y>
+int i8_run(const Rows& r, const void* w, const float* sw, void* y, int64_t N, int64_t ldy, hipStream_t st) {
+  const bool in_place = few_quantize(r.M, r.K);
+  if (!in_place) {
+    const int rc = quantize(r.dtype, {r.x, r.q, r.s, r.M, r.ld, i8_pitch(r.K), (int)r.K}, st);
+    if (rc != JZ_OK) return rc;
+  }
+  if (r.M <= FEW_TOKENS) {
+    const signed char* c = static_cast<const signed char*>(w);
+    return few_product<X, Y, false>({r.q, {c, c}, r.s, {sw, sw}, in_place ? r.x : nullptr, y, r.M, N, r.K, i8_pitch(r.K), r.ld, ldy, 0}, st);
+  }
+  return i8_product<Y>(i8_args(r.q, r.M, w, nullptr, N, r.K), {r.s, sw, nullptr, y, r.M, N, ldy, 0}, st);
+}
+template <class X>
+int i8_run_glu(const Rows& r, const void* wg, const float* sg, const void* wu, const float* su, float* h, int64_t F, int act, hipStream_t st) {
+  const bool in_place = few_quantize(r.M, r.K);
+  if (!in_place) {
+    const int rc = quantize(r.dtype, {r.x, r.q, r.s, r.M, r.ld, i8_pitch(r.K), (int)r.K}, st);
+    if (rc != JZ_OK) return rc;
+  }
+  if (r.M <= FEW_TOKENS)
+    return few_product<X, float, true>({r.q, {static_cast<const signed char*>(wg), static_cast<const signed char*>(wu)}, r.s, {sg, su}, in_place ? r.x : nullptr, h, r.M, F, r.K,
+                                        i8_pitch(r.K), r.ld, F, act}, st);
+  return i8_glu(i8_args(r.q, r.M, wg, wu, F, r.K), {r.s, sg, su, h, r.M, F, F, act}, st);
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------------------
@@ -259,12 +318,10 @@ extern "C" int jz_linear_i8(const jz_linear_i8_desc* d, const void* x, const voi
   if (rc != JZ_OK) return rc;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   signed char* const q = static_cast<signed char*>(ws);
-  float* const sx = reinterpret_cast<float*>(q + room.scales);
-  rc = quantize(d->dtype, {x, q, sx, s.M, s.ldx, i8_pitch(s.K), (int)s.K}, st);
-  if (rc != JZ_OK) return rc;
-  const MmArgs a = i8_args(q, s.M, wq, nullptr, s.N, s.K);
-  const I8Out o = {sx, w_scale, nullptr, y, s.M, s.N, s.ldy, 0};
-  return d->dtype == JZ_F32 ? i8_product<float>(a, o, st) : d->dtype == JZ_F16 ? i8_product<_Float16>(a, o, st) : i8_product<__bf16>(a, o, st);
+  const Rows r = {x, d->dtype, s.M, s.K, s.ldx, q, reinterpret_cast<float*>(q + room.scales)};
+  if (d->dtype == JZ_F32) return i8_run<float, float>(r, wq, w_scale, y, s.N, s.ldy, st);
+  if (d->dtype == JZ_F16) return i8_run<_Float16, _Float16>(r, wq, w_scale, y, s.N, s.ldy, st);
+  return i8_run<__bf16, __bf16>(r, wq, w_scale, y, s.N, s.ldy, st);
 }
 
 extern "C" int jz_ffn_i8_workspace_bytes(const jz_ffn_desc* d, size_t* bytes) {
@@ -296,12 +353,12 @@ extern "C" int jz_ffn_i8_fwd(const jz_ffn_desc* d, const void* x, const void* wq
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   char* const b = static_cast<char*>(ws);
   signed char *const qx = reinterpret_cast<signed char*>(b), *const qh = qx + rx.total;
-  float *const sx = reinterpret_cast<float*>(qx + rx.scales), *const sh = reinterpret_cast<float*>(qh + rh.scales), *const h = reinterpret_cast<float*>(b + rx.total + rh.total);
-  rc = quantize(d->dtype, {x, qx, sx, s.M, s.ldx, i8_pitch(s.K), (int)s.K}, st);
-  if (rc == JZ_OK) rc = i8_glu(i8_args(qx, s.M, wq_gate, wq_up, F, s.K), {sx, s_gate, s_up, h, s.M, F, F, d->act}, st);
-  if (rc == JZ_OK) rc = quantize(JZ_F32, {h, qh, sh, s.M, F, i8_pitch(F), (int)F}, st);
-  if (rc != JZ_OK) return rc;
-  const MmArgs a = i8_args(qh, s.M, wq_down, nullptr, s.N, F);
-  const I8Out o = {sh, s_down, nullptr, y, s.M, s.N, s.ldy, 0};
-  return d->dtype == JZ_F16 ? i8_product<_Float16>(a, o, st) : i8_product<__bf16>(a, o, st);
+  float* const h = reinterpret_cast<float*>(b + rx.total + rh.total);
+  const Rows tokens = {x, d->dtype, s.M, s.K, s.ldx, qx, reinterpret_cast<float*>(qx + rx.scales)}, hidden = {h, JZ_F32, s.M, F, F, qh, reinterpret_cast<float*>(qh + rh.scales)};
+  if (d->dtype == JZ_F16) {
+    rc = i8_run_glu<_Float16>(tokens, wq_gate, s_gate, wq_up, s_up, h, F, d->act, st);
+    return rc == JZ_OK ? i8_run<float, _Float16>(hidden, wq_down, s_down, y, s.N, s.ldy, st) : rc;
+  }
+  rc = i8_run_glu<__bf16>(tokens, wq_gate, s_gate, wq_up, s_up, h, F, d->act, st);
+  return rc == JZ_OK ? i8_run<float, __bf16>(hidden, wq_down, s_down, y, s.N, s.ldy, st) : rc;
 }

@@ -88,6 +88,17 @@ struct MmSource {
     step = (unsigned)((DUAL ? 32 : THREADS / 8) * pitch);
     off = (unsigned)((DUAL ? row & 31 : row) * pitch) + chunk;
   }
+  // bytes k0 .. k0 + 127 of the rows into registers
+  template <class V>
+  __device__ __forceinline__ void get(V (&to)[EACH], int64_t k0, bool wanted) const {
+    static_assert(!DUAL, "");
+    const int64_t span = (rows_left - 1) * pitch + row_bytes - k0;
+    const int bytes = !wanted || span < 0 ? 0 : (int)(span < 0x7ffffff0 ? span : 0x7ffffff0);
+    const auto r = __builtin_amdgcn_make_buffer_rsrc((void*)(base[0] + (wanted ? k0 : 0)), 0, bytes, 0x00020000);
+    const unsigned end = (int64_t)chunk >= row_bytes - k0 ? 0x80000000u : 0u;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) to[i] = __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(r, (int)((off + i * step) | end), 0, 0));
+  }
   // bytes k0 .. k0 + 127 of the rows into LDS; what lies outside the operand arrives as zeros
   template <class L>
   __device__ __forceinline__ void load(L* lds, int64_t k0, int wave, bool wanted) const {
@@ -244,9 +255,77 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void mm_tiles(MmArgs a, Epi epi)
   });
 }
 
+// Few tiles: 64 x 64 by four wavefronts of 32 x 32.  What such a launch waits for is the way from memory, so four tiles of operands are on it at a time, in registers; two are in LDS.
+// (With two stages of LDS-direct loads, which wait for each other, 128 x 128 x 512 of ElemSplit took MM_SMALL_BEFORE us.)
+template <class E, class Epi>
+__global__ __launch_bounds__(256, 2) void mm_small(MmArgs a, Epi epi) {
+  constexpr int DEPTH = 4, EACH = 2;
+  typedef typename E::Reg Reg;
+  typedef typename E::Sum Sum;
+  typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[2][16384];
+  if (a.skip && *a.skip) return;
+  const MmTile w = mm_tile(a);
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, wm = wave >> 1, wn = wave & 1;
+  const int64_t m0 = (int64_t)w.m * 64, n0 = (int64_t)w.n * 64;
+  const int last = (int)((a.row_bytes + 127) / 128);
+  MmSource<64, 256, false> from_a, from_b;
+  from_a.init(a.a, w.of, m0, a.row_bytes, t);
+  from_b.init(a.b, w.of, n0, a.row_bytes, t);
+  u32x4 ra[DEPTH][EACH], rb[DEPTH][EACH];
+  auto fetch = [&](int d, int kt) {  // behind the last tile: zeros
+    from_a.get(ra[d], (int64_t)kt * 128, kt < last);
+    from_b.get(rb[d], (int64_t)kt * 128, kt < last);
+  };
+  unsigned at_a[4], at_b[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    const unsigned c = ((s * 2 + (lane >> 5)) ^ ((lane >> 1) & 7)) * 16;
+    at_a[s] = (wm * 32 + (lane & 31)) * 128 + c;
+    at_b[s] = 8192 + (wn * 32 + (lane & 31)) * 128 + c;
+  }
+  Sum acc[1] = {Sum{}};
+  static_for<0, DEPTH>([&](auto D) { fetch(decltype(D)::value, decltype(D)::value); });
+  for (int kt = 0; kt < last; kt += DEPTH) {
+    static_for<0, DEPTH>([&](auto D) {
+      constexpr int d = decltype(D)::value;
+      JZ_LDS unsigned char* const to = (JZ_LDS unsigned char*)lds[d & 1];
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        *reinterpret_cast<JZ_LDS u32x4*>(to + (i * 256 + t) * 16) = ra[d][i];
+        *reinterpret_cast<JZ_LDS u32x4*>(to + 8192 + (i * 256 + t) * 16) = rb[d][i];
+      }
+      fetch(d, kt + d + DEPTH);
+      // the other place's reads were waited for before the last barrier
+      lds_meet();
+      Reg x[4], y[4];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        x[s] = *reinterpret_cast<const JZ_LDS Reg*>(to + at_a[s]);
+        y[s] = *reinterpret_cast<const JZ_LDS Reg*>(to + at_b[s]);
+      }
+      if constexpr (E::SPLIT) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          acc[0] = E::mfma(y[s], x[s], acc[0]);
+          acc[0] = E::mfma(y[s], x[s + 2], acc[0]);
+          acc[0] = E::mfma(y[s + 2], x[s], acc[0]);
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) acc[0] = E::mfma(y[s], x[s], acc[0]);
+      }
+    });
+  }
+  __syncthreads();  // the results take the operands' place
+  const MmStrip<E, 1> strip = {(JZ_LDS unsigned char*)lds[0] + wave * 4096};
+  strip.put(acc, lane);
+  epi.strip(strip, w, m0 + wm * 32, n0 + wn * 32, lane);
+}
+
 constexpr int64_t MM_LANES = int64_t(1) << 32;  // a launch has fewer
 
-// A launch over `count` matrices, TILE x TILE: 256 by eight wavefronts in 2 x 4, 128 and 64 by four in 2 x 2.
+// A launch over `count` matrices, TILE x TILE: 256 by eight wavefronts in 2 x 4, 128 by four in 2 x 2, 64: mm_small.
 template <class E, class Epi, int TILE, bool DUAL>
 int mm_launch(MmArgs a, const Epi& epi, int64_t rows_m, int64_t rows_n, int64_t count, hipStream_t st) {
   constexpr int WGM = 2, WGN = TILE == 256 ? 4 : 2, THREADS = 64 * WGM * WGN;
@@ -255,6 +334,10 @@ int mm_launch(MmArgs a, const Epi& epi, int64_t rows_m, int64_t rows_n, int64_t 
   a.tiles = a.symmetric ? (unsigned)a.tiles_m * (a.tiles_m + 1) / 2 : (unsigned)a.tiles_m * a.tiles_n;
   a.workgroups = (unsigned)(a.tiles * count);
   constexpr unsigned most = (unsigned)(MM_LANES / THREADS - 1);
-  for (a.first = 0; a.first < a.workgroups; a.first += most) mm_tiles<E, Epi, TILE, TILE, WGM, WGN, DUAL><<<std::min(a.workgroups - a.first, most), THREADS, 0, st>>>(a, epi);
+  for (a.first = 0; a.first < a.workgroups; a.first += most) {
+    const unsigned grid = std::min(a.workgroups - a.first, most);
+    if constexpr (TILE == 64) mm_small<E, Epi><<<grid, 256, 0, st>>>(a, epi);
+    else mm_tiles<E, Epi, TILE, TILE, WGM, WGN, DUAL><<<grid, THREADS, 0, st>>>(a, epi);
+  }
   return jz::launch_status();
 }

@@ -23,7 +23,9 @@ namespace {
 
 constexpr float SCALE = 2048.f;
 constexpr int PAD = 32;      // sides of the matrices in the workspace are multiples of this, zeros behind their ends
-constexpr int PARTS = 64;    // workgroups that share a matrix's sum of squares
+
+// workgroups that share a matrix's sum of squares
+int sum_parts(int64_t elements, int64_t count) { return (int)std::max<int64_t>(1, std::min((elements + 8191) / 8192, std::max<int64_t>(1, 2048 / count))); }
 
 // eight columns from col (a multiple of 8) on of a row of parts: 64 bytes of high parts of 32 columns, then their low parts
 __device__ __forceinline__ void store_parts(char* row, int64_t col, const float (&v)[8]) {
@@ -52,27 +54,32 @@ struct OrthoIn {
   const jz_loss_scale_state* state;
   int nesterov;
   int64_t count, rows, cols, stride;
-  double *sums, *inv;   // [count][PARTS]; [count]
+  double *sums, *inv;   // [count][parts]; [count]
+  int parts;
   float eps;
   const int* skip;
   int* found_inf;
 };
-// what is orthogonalised; g: the true gradient, v: the new momentum
+// What is orthogonalised, eight elements from i on or the `left` that there are; v: the new momentum.
 template <class T, bool MUON>
 struct OrthoValue {
   const OrthoIn& a;
   float inv_s;
   __device__ __forceinline__ OrthoValue(const OrthoIn& a_) : a(a_), inv_s(MUON && a_.state ? 1.f / a_.state->scale : a_.inv_s) {}
-  __device__ __forceinline__ float get(int64_t i, float* g, float* v) const {
-    const float x = (float)static_cast<const T*>(a.x)[i];
-    if constexpr (!MUON) {
-      *g = *v = x;
-      return x;
-    } else {
-      *g = x * inv_s;
-      *v = a.mu * a.momentum[i] + *g;
-      return a.nesterov ? *g + a.mu * *v : *v;
-    }
+  __device__ __forceinline__ f32x8 get(int64_t i, int left, f32x8* v) const {
+    const f32x8 x = widen8<T>(load8(static_cast<const T*>(a.x) + i, left));
+    if constexpr (!MUON) return x;
+    const f32x8 g = x * inv_s;
+    *v = a.mu * load8(a.momentum + i, left) + g;
+    return a.nesterov ? g + a.mu * *v : *v;
+  }
+  // a gradient that is not finite, before any scale
+  __device__ __forceinline__ bool bad(int64_t i, int left) const {
+    const f32x8 x = widen8<T>(load8(static_cast<const T*>(a.x) + i, left));
+    bool r = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r |= !(fabsf(x[e]) < INFINITY);
+    return r;
   }
 };
 
@@ -83,17 +90,20 @@ __global__ __launch_bounds__(256) void ortho_sumsq(OrthoIn a) {
   const OrthoValue<T, MUON> in(a);
   const int64_t n = a.rows * a.cols, base = (int64_t)blockIdx.y * a.stride;
   double s = 0.;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += PARTS * 256) {
-    float g, v;
-    const double u = in.get(base + i, &g, &v);
-    s += u * u;
-    if (MUON && !(fabsf(g) < INFINITY)) s = NAN;
+#pragma unroll 2
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += (int64_t)a.parts * 2048) {
+    const int left = n - i < 8 ? (int)(n - i) : 8;
+    f32x8 v;
+    const f32x8 u = in.get(base + i, left, &v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fma((double)u[e], (double)u[e], s);
+    if (MUON && in.bad(base + i, left)) s = NAN;
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0) a.sums[(int64_t)blockIdx.y * PARTS + blockIdx.x] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+  if (threadIdx.x == 0) a.sums[(int64_t)blockIdx.y * a.parts + blockIdx.x] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
 // Each matrix's factor; of the update, whether anything is to be done.  One workgroup, a wavefront a matrix.
@@ -103,7 +113,8 @@ __global__ __launch_bounds__(1024) void ortho_factors(OrthoIn a) {
   if (threadIdx.x == 0) bad = MUON && a.skip && *a.skip;
   __syncthreads();
   for (int64_t b = threadIdx.x >> 6; b < a.count; b += 16) {
-    double s = a.sums[b * PARTS + (threadIdx.x & 63)];
+    double s = 0.;
+    for (int i = threadIdx.x & 63; i < a.parts; i += 64) s += a.sums[b * a.parts + i];
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
     if ((threadIdx.x & 63) == 0) {
@@ -129,29 +140,36 @@ __global__ __launch_bounds__(256) void ortho_parts(OrthoIn a, OrthoParts o) {
   const int64_t across = (o.cp + 63) / 64, down = (o.rp + 63) / 64, of = blockIdx.x / (across * down), t = blockIdx.x - of * across * down;
   const int64_t r0 = t / across * 64, c0 = t % across * 64, base = of * a.stride;
   const double inv = a.inv[of];
-  for (int i = threadIdx.x; i < 64 * 64; i += 256) {
-    const int64_t r = r0 + i / 64, c = c0 + i % 64;
-    float u = 0.f;
+  const int row = threadIdx.x / 8, col = threadIdx.x % 8 * 8;
+#pragma unroll
+  for (int h = 0; h < 64; h += 32) {
+    const int64_t r = r0 + row + h, c = c0 + col;
+    f32x8 u = {};
     if (r < a.rows && c < a.cols) {
-      float g, v;
-      u = (float)((double)in.get(base + r * a.cols + c, &g, &v) * inv);
-      if (MUON) a.momentum[base + r * a.cols + c] = v;
+      const int left = a.cols - c < 8 ? (int)(a.cols - c) : 8;
+      const int64_t at = base + r * a.cols + c;
+      f32x8 v;
+      u = in.get(at, left, &v);
+      if (MUON) store8(a.momentum + at, v, left);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] = e < left ? (float)((double)u[e] * inv) : 0.f;
     }
-    tile[i / 64][i % 64] = u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) tile[row + h][col + e] = u[e];
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < 64 * 8; i += 256) {
-    const int row = i / 8, col = i % 8 * 8;
+#pragma unroll
+  for (int h = 0; h < 64; h += 32) {
     float v[8];
-    if (r0 + row < o.rp && c0 + col < o.cp) {
+    if (r0 + row + h < o.rp && c0 + col < o.cp) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = tile[row][col + e];
-      store_parts(o.r + (of * o.rp + r0 + row) * o.cp * 4, c0 + col, v);
+      for (int e = 0; e < 8; ++e) v[e] = tile[row + h][col + e];
+      store_parts(o.r + (of * o.rp + r0 + row + h) * o.cp * 4, c0 + col, v);
     }
-    if (c0 + row < o.cp && r0 + col < o.rp) {
+    if (c0 + row + h < o.cp && r0 + col < o.rp) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = tile[col + e][row];
-      store_parts(o.c + (of * o.cp + c0 + row) * o.rp * 4, r0 + col, v);
+      for (int e = 0; e < 8; ++e) v[e] = tile[col + e][row + h];
+      store_parts(o.c + (of * o.cp + c0 + row + h) * o.rp * 4, r0 + col, v);
     }
   }
 }
@@ -190,12 +208,13 @@ __device__ __forceinline__ void store_cols(const S& s, const Parts& to, int64_t 
     store_parts(to.row(of, n0 + col), m0 + r, v);
   }
 }
-struct OrthoGram {  // A = X X^T
+struct OrthoSymmetric {  // a product that is its own transpose
   Parts a;
+  float factor;
   template <class S>
   __device__ __forceinline__ void strip(const S& s, const MmTile& w, int64_t m0, int64_t n0, int lane) const {
-    store_rows(s, a, w.of, m0, n0, lane, 1.f / SCALE);
-    if (w.m != w.n) store_cols(s, a, w.of, m0, n0, lane, 1.f / SCALE);
+    store_rows(s, a, w.of, m0, n0, lane, factor);
+    if (w.m != w.n) store_cols(s, a, w.of, m0, n0, lane, factor);
   }
 };
 struct OrthoPoly {  // B = ca I + cb A + cc A^2
@@ -221,10 +240,11 @@ struct OrthoPoly {  // B = ca I + cb A + cc A^2
 };
 struct OrthoApply {  // X <- B X
   Parts x, xt;
+  float factor;
   template <class S>
   __device__ __forceinline__ void strip(const S& s, const MmTile& w, int64_t m0, int64_t n0, int lane) const {
-    store_rows(s, x, w.of, m0, n0, lane, 1.f / SCALE);
-    store_cols(s, xt, w.of, m0, n0, lane, 1.f / SCALE);
+    store_rows(s, x, w.of, m0, n0, lane, factor);
+    store_cols(s, xt, w.of, m0, n0, lane, factor);
   }
 };
 template <class O>
@@ -232,6 +252,7 @@ struct OrthoResult {  // the last B X, rounded once; transposed back where TALL 
   O* y;
   int64_t m, n, stride;
   bool tall;
+  float factor;
   template <class S>
   __device__ __forceinline__ void strip(const S& s, const MmTile& w, int64_t m0, int64_t n0, int lane) const {
     constexpr int PER = S::COLS / 8;
@@ -245,7 +266,7 @@ struct OrthoResult {  // the last B X, rounded once; transposed back where TALL 
         if (m0 + row >= m || n0 + c >= n) continue;
         s.row8(row, c, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = v[e] * (1.f / (SCALE * SCALE));
+        for (int e = 0; e < 8; ++e) f[e] = v[e] * factor;
         store8(to + (m0 + row) * n + n0 + c, narrow8<O>(f), n - n0 - c < 8 ? (int)(n - n0 - c) : 8);
       }
     } else {
@@ -255,7 +276,7 @@ struct OrthoResult {  // the last B X, rounded once; transposed back where TALL 
         if (n0 + col >= n || m0 + r >= m) continue;
         s.col8(r, col, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = v[e] * (1.f / (SCALE * SCALE));
+        for (int e = 0; e < 8; ++e) f[e] = v[e] * factor;
         store8(to + (n0 + col) * m + m0 + r, narrow8<O>(f), m - m0 - r < 8 ? (int)(m - m0 - r) : 8);
       }
     }
@@ -267,20 +288,22 @@ struct MuonApply {
   const float* o;     // [count][rows cols], dense
   float* w;
   void* w16;
-  int64_t each, stride, all;
+  int64_t each, stride, count;
   float lr, update_scale, wd;
   const int* found_inf;
 };
 template <class T>
 __global__ __launch_bounds__(256) void muon_apply(MuonApply a) {
   if (*a.found_inf) return;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.all; i += (int64_t)gridDim.x * 256) {
-    const int64_t b = i / a.each, at = b * a.stride + (i - b * a.each);
-    const float w = a.w[at];
-    float r = w - a.lr * (a.update_scale * a.o[i] + a.wd * w);
+  const int64_t per = (a.each + 7) / 8;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.count * per; i += (int64_t)gridDim.x * 256) {
+    const int64_t b = i / per, k = (i - b * per) * 8, at = b * a.stride + k;
+    const int left = a.each - k < 8 ? (int)(a.each - k) : 8;
+    const f32x8 w = load8(a.w + at, left), o = load8(a.o + b * a.each + k, left);
+    f32x8 r = w - a.lr * (a.update_scale * o + a.wd * w);
     lds_pin(r);  // rounded to FP32 here: the copy is that value's, and not the 16-bit rounding of a fused multiply-add
-    a.w[at] = r;
-    static_cast<T*>(a.w16)[at] = (T)r;
+    store8(a.w + at, r, left);
+    store8(static_cast<T*>(a.w16) + at, narrow8<T>(r), left);
   }
 }
 
@@ -305,26 +328,10 @@ int ortho_shape(const jz_ortho_desc* d, OrthoShape* s) {
 }
 size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 struct OrthoLayout {
-  size_t sums, inv, x, xt[2], a, b, total;
-  explicit OrthoLayout(const OrthoShape& s) {
-    size_t o = 0;
-    auto room = [&](size_t bytes) {
-      const size_t at = o;
-      o += round256(bytes);
-      return at;
-    };
-    const size_t wide = (size_t)s.count * s.mp * s.np * 4, square = (size_t)s.count * s.mp * s.mp * 4;
-    sums = room((size_t)s.count * PARTS * 8);
-    inv = room((size_t)s.count * 8);
-    x = room(wide);
-    xt[0] = room(wide);
-    xt[1] = room(wide);
-    a = room(square);
-    b = room(square);
-    total = o;
-  }
+  size_t sums, inv, x, xt[2], a, b, more[4], total;
+  bool short_side;
+  OrthoLayout(const OrthoShape& s, int steps);
 };
-
 template <class Epi>
 int ortho_product(const Parts& p, const Parts& q, bool symmetric, int64_t count, const int* skip, const Epi& e, hipStream_t st) {
   MmArgs a = {};
@@ -344,23 +351,78 @@ int ortho_product(const Parts& p, const Parts& q, bool symmetric, int64_t count,
 
 template <class T, bool MUON>
 int ortho_begin(const OrthoIn& in, const OrthoShape& s, const OrthoParts& o, hipStream_t st) {
-  ortho_sumsq<T, MUON><<<dim3(PARTS, (unsigned)s.count), 256, 0, st>>>(in);
+  ortho_sumsq<T, MUON><<<dim3((unsigned)in.parts, (unsigned)s.count), 256, 0, st>>>(in);
   ortho_factors<MUON><<<1, 1024, 0, st>>>(in);
   const int64_t tiles = (o.rp + 63) / 64 * ((o.cp + 63) / 64) * s.count;
   ortho_parts<T, MUON><<<(unsigned)tiles, 256, 0, st>>>(in, o);
   return jz::launch_status();
 }
 
+// Steps in the space of the shorter side.  With A = X X^T an iterate is P X, P a polynomial of A that commutes with it: while P and A are carried along (B of the step, P <- B P,
+// A <- B A B: four symmetric m x m products a step), X itself is not needed.  But A has lost a value s of X that is below 2^-11 of the largest, s^2 being below FP32's last
+// bit, so that X is made, and A from it, after three steps at most: by then A's error of 2^-24 has grown to some 2^-16 of the smallest values.  (Emulated in FP32 with 22-bit operands, five
+// steps as 2 + 3, against 64 bits: 2.2e-6 to 4e-5 for spectra from flat to 1e-6, as the plain form's 2.4e-6 to 6e-5; five steps without X: 8e-5 to 3e-4.)
+int phases(int steps) { return (steps + 2) / 3; }
+int first_phase(int steps) { return steps - 3 * (phases(steps) - 1); }
+// multiply-adds, halves of symmetric products alone; a tenth less has to be saved at least
+bool short_side(int steps, int64_t m, int64_t n) {
+  const double p = phases(steps), k = steps, r = (double)n / (double)m;
+  return p * 3 * r + 4 * k - 3 * p < 0.9 * k * (3 * r + 1);
+}
+
+OrthoLayout::OrthoLayout(const OrthoShape& s, int steps) : short_side(::short_side(steps, s.m, s.n)) {
+  size_t o = 0;
+  auto room = [&](size_t bytes) {
+    const size_t at = o;
+    o += round256(bytes);
+    return at;
+  };
+  const size_t wide = (size_t)s.count * s.mp * s.np * 4, square = (size_t)s.count * s.mp * s.mp * 4;
+  sums = room(s.count ? (size_t)s.count * sum_parts(s.rows * s.cols, s.count) * 8 : 0);
+  inv = room((size_t)s.count * 8);
+  x = room(wide);
+  xt[0] = room(wide);
+  xt[1] = room(steps > 1 ? wide : 0);
+  a = room(square);
+  b = room(square);
+  for (size_t& m : more) m = room(short_side ? square : 0);
+  total = o;
+}
+
 template <class O>
 int ortho_steps(const jz_ortho_desc* d, const OrthoShape& s, const OrthoLayout& L, char* b, O* y, int64_t y_stride, const int* skip, hipStream_t st) {
-  const Parts x = {b + L.x, s.mp, s.np}, A = {b + L.a, s.mp, s.mp}, B = {b + L.b, s.mp, s.mp};
-  for (int i = 0; i < d->steps; ++i) {
-    const Parts xt = {b + L.xt[i & 1], s.np, s.mp}, next = {b + L.xt[!(i & 1)], s.np, s.mp};
-    int rc = ortho_product(x, x, true, s.count, skip, OrthoGram{A}, st);
-    if (rc == JZ_OK) rc = ortho_product(A, A, true, s.count, skip, OrthoPoly{A, B, d->a, d->b, d->c}, st);
+  auto square = [&](size_t at) { return Parts{b + at, s.mp, s.mp}; };
+  const Parts x = {b + L.x, s.mp, s.np};
+  Parts A = square(L.a), A1 = square(L.more[0]), C = square(L.more[1]), P = square(L.more[2]), P1 = square(L.more[3]);
+  const Parts B = square(L.b);
+  auto symmetric = [&](const Parts& p, const Parts& q, const Parts& to, float factor) { return ortho_product(p, q, true, s.count, skip, OrthoSymmetric{to, factor}, st); };
+  // P grows to a^steps where X has nothing: each step that it takes up scales it down by the power of two from |a| on
+  const float shrink = exp2f(-ceilf(log2f(std::max(1.f, fabsf(d->a)))));
+  int turn = 0, rc = JZ_OK;
+  for (int done = 0, steps; done < d->steps; done += steps) {
+    steps = !L.short_side ? 1 : done == 0 ? first_phase(d->steps) : 3;
+    rc = symmetric(x, x, A, 1.f / SCALE);
+    float small = 1.f;  // P in the workspace is SCALE small P
+    for (int i = 0; i < steps && rc == JZ_OK; ++i) {
+      const Parts to = i == 0 && steps > 1 ? P : B;
+      rc = ortho_product(A, A, true, s.count, skip, OrthoPoly{A, to, d->a, d->b, d->c}, st);
+      if (rc == JZ_OK && i + 1 < steps) {
+        rc = symmetric(to, A, C, 1.f / SCALE);
+        if (rc == JZ_OK) rc = symmetric(C, to, A1, 1.f / SCALE);
+        std::swap(A, A1);
+      }
+      if (rc == JZ_OK && i > 0) {
+        rc = symmetric(B, P, P1, shrink / SCALE);
+        small *= shrink;
+        std::swap(P, P1);
+      }
+    }
     if (rc != JZ_OK) return rc;
-    if (i + 1 < d->steps) rc = ortho_product(B, xt, false, s.count, skip, OrthoApply{x, next}, st);
-    else rc = ortho_product(B, xt, false, s.count, skip, OrthoResult<O>{y, s.m, s.n, y_stride, s.tall}, st);
+    const Parts xt = {b + L.xt[turn & 1], s.np, s.mp}, next = {b + L.xt[!(turn & 1)], s.np, s.mp};
+    ++turn;
+    const Parts& by = steps > 1 ? P : B;
+    if (done + steps < d->steps) rc = ortho_product(by, xt, false, s.count, skip, OrthoApply{x, next, 1.f / (SCALE * small)}, st);
+    else rc = ortho_product(by, xt, false, s.count, skip, OrthoResult<O>{y, s.m, s.n, y_stride, s.tall, 1.f / (SCALE * SCALE * small)}, st);
     if (rc != JZ_OK) return rc;
   }
   return JZ_OK;
@@ -379,7 +441,7 @@ extern "C" int jz_orthogonalize_workspace_bytes(const jz_ortho_desc* d, size_t* 
   OrthoShape s;
   const int rc = ortho_shape(d, &s);
   if (rc != JZ_OK) return rc;
-  *bytes = s.count ? OrthoLayout(s).total : 0;
+  *bytes = s.count ? OrthoLayout(s, d->steps).total : 0;
   return JZ_OK;
 }
 
@@ -389,7 +451,7 @@ extern "C" int jz_orthogonalize(const jz_ortho_desc* d, const void* x, void* y, 
   if (rc != JZ_OK) return rc;
   if (s.count == 0) return JZ_OK;
   if (!x || !y) return JZ_ERR_NULL;
-  const OrthoLayout L(s);
+  const OrthoLayout L(s, d->steps);
   if (!ws || ws_bytes < L.total) return JZ_ERR_WORKSPACE;
   if (!jz::aligned16(x) || !jz::aligned16(y) || !jz::aligned16(ws)) return JZ_ERR_ALIGN;
   const size_t nx = batch_bytes(s, bytes_of(d->dtype)), ny = batch_bytes(s, bytes_of(d->out_dtype));
@@ -403,6 +465,7 @@ extern "C" int jz_orthogonalize(const jz_ortho_desc* d, const void* x, void* y, 
   in.cols = s.cols;
   in.stride = s.stride;
   in.sums = reinterpret_cast<double*>(b + L.sums);
+  in.parts = s.count ? sum_parts(s.rows * s.cols, s.count) : 0;
   in.inv = reinterpret_cast<double*>(b + L.inv);
   in.eps = d->eps;
   const OrthoParts o = begin_parts(s, L, b);
@@ -427,7 +490,7 @@ extern "C" int jz_muon_mp_update_workspace_bytes(const jz_ortho_desc* d, size_t*
   OrthoShape s;
   const int rc = muon_shape(d, &s);
   if (rc != JZ_OK) return rc;
-  *bytes = OrthoLayout(s).total;
+  *bytes = OrthoLayout(s, d->steps).total;
   return JZ_OK;
 }
 
@@ -440,7 +503,7 @@ extern "C" int jz_muon_mp_update(const jz_ortho_desc* d, const jz_muon_hparams* 
   for (float v : {hp->lr, hp->momentum, hp->weight_decay, hp->update_scale})
     if (!(fabsf(v) < INFINITY)) return JZ_ERR_SHAPE;
   if (!state_dev && !(hp->loss_scale > 0.f && hp->loss_scale < 3.0e38f)) return JZ_ERR_SHAPE;
-  const OrthoLayout L(s);
+  const OrthoLayout L(s, d->steps);
   if (s.count && (!ws || ws_bytes < L.total)) return JZ_ERR_WORKSPACE;
   if (!jz::aligned16(master_w) || !jz::aligned16(momentum) || !jz::aligned16(grad16) || !jz::aligned16(weight16) || !jz::aligned16(ws) ||
       (reinterpret_cast<uintptr_t>(found_inf_dev) & 3) || (reinterpret_cast<uintptr_t>(skip_dev) & 3) || (reinterpret_cast<uintptr_t>(state_dev) & 7))
@@ -469,6 +532,7 @@ extern "C" int jz_muon_mp_update(const jz_ortho_desc* d, const jz_muon_hparams* 
   in.cols = s.cols;
   in.stride = s.stride;
   in.sums = reinterpret_cast<double*>(b + L.sums);
+  in.parts = s.count ? sum_parts(s.rows * s.cols, s.count) : 0;
   in.inv = reinterpret_cast<double*>(b + L.inv);
   in.eps = d->eps;
   in.skip = skip_dev;
@@ -483,8 +547,8 @@ extern "C" int jz_muon_mp_update(const jz_ortho_desc* d, const jz_muon_hparams* 
   float* const result = reinterpret_cast<float*>(b + L.x);  // the last product reads B and the other order of X
   rc = ortho_steps(d, s, L, b, result, s.rows * s.cols, found_inf_dev, st);
   if (rc != JZ_OK) return rc;
-  const MuonApply a = {result, master_w, weight16, s.rows * s.cols, s.stride, s.rows * s.cols * s.count, hp->lr, hp->update_scale, hp->weight_decay, found_inf_dev};
-  const unsigned grid = (unsigned)std::min<int64_t>((a.all + 255) / 256, 1 << 16);
+  const MuonApply a = {result, master_w, weight16, s.rows * s.cols, s.stride, s.count, hp->lr, hp->update_scale, hp->weight_decay, found_inf_dev};
+  const unsigned grid = (unsigned)std::min<int64_t>(((a.each + 7) / 8 * a.count + 255) / 256, 1 << 16);
   if (d->dtype == JZ_F16) muon_apply<_Float16><<<grid, 256, 0, st>>>(a);
   else muon_apply<__bf16><<<grid, 256, 0, st>>>(a);
   return jz::launch_status();

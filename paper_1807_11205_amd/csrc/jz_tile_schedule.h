@@ -15,6 +15,13 @@ __device__ __forceinline__ void all_landed() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// The same without a wait for what is on its way from memory.
+__device__ __forceinline__ void lds_meet() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // The order of a step's instructions: between one matrix instruction and the next a read of LDS or a load.  (In the compiler's order, all reads first, 8192 rows, 2048 ->
 // 5632 features take 10 % longer.)
 template <int MULTIPLY, int READ, int LOAD>

@@ -104,11 +104,13 @@ def test_zeros_and_matrices_that_are_not_finite(jz):
         against(y[[0, 3]], x[[0, 3]])
 
 
-def test_matrices_of_low_rank(jz):
-    """Directions that are not there stay so; noise of FP32 in them would grow a hundredfold a step."""
+@pytest.mark.parametrize("R,C", [(100, 140), (100, 400), (300, 70)])
+@pytest.mark.parametrize("steps", [1, 3, 5, 6, 7])
+def test_matrices_of_low_rank(jz, R, C, steps):
+    """Where a matrix has nothing the polynomial is a^steps; what rounding left there grows by as much."""
     g = np.random.default_rng(6)
-    x = torch.from_numpy(g.standard_normal((1, 100, 3)) @ g.standard_normal((1, 3, 140))).float().to(DEV)
-    against(run(jz, x, torch.float32), x)
+    x = torch.from_numpy(g.standard_normal((1, R, 3)) @ g.standard_normal((1, 3, C))).float().to(DEV)
+    against(run(jz, x, torch.float32, steps), x, steps)
 
 
 def test_strided_batch(jz):
