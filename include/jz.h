@@ -417,8 +417,8 @@ int jz_ffn_bwd(const jz_ffn_desc* desc, const void* x, const void* w_gate, const
  * Embedding lookup and the gradient of its table, for networks whose rows are tokens:
  *   jz_embed_fwd   out[t] = RNE( scale * table[ids[t]] )                           table [vocab][channels], out [tokens][channels]
  *   jz_embed_bwd   dtable[v] = RNE( scale * sum over t with ids[t] == v of dout[t]  [+ dtable[v]] )
- * ids: DEVICE int32 [tokens], 4-byte aligned.  A token outside [0, vocab) (a masked place) gets a row of zeros, and its row of dout is not
- * read.  The sum of a row is FP32, in an order that tokens and their positions alone decide (positions are sorted by token on the
+ * ids: DEVICE int32 [tokens], 4-byte aligned.  A token outside [0, vocab) (a masked place) gets a row of zeros, and its row of dout counts
+ * nowhere, whatever it holds.  The sum of a row is FP32, in an order that tokens and their positions alone decide (positions are sorted by token on the
  * device, stably): bit-identical from run to run.  accumulate == 0: every row of dtable is written, zeros where no token stands.  accumulate != 0:
  * only rows with tokens are, each read, added to in FP32 and rounded once more: for a table that is also the classifier's matrix, whose gradient is
  * there already.

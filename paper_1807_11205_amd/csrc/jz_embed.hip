@@ -16,6 +16,7 @@ namespace {
 #include "jz_vec.h"
 #include "jz_sort.h"
 
+constexpr int ZERO_EACH = 16384;    // elements of the table that a workgroup looks at
 constexpr int EMBED_GRID = 1 << 16;  // workgroups at most: each takes further turns
 
 // ---- lookup -----------------------------------------------------------------------------------------------------------------
@@ -69,6 +70,8 @@ __global__ __launch_bounds__(256) void embed_lookup(LookupArgs a) {
   }
 }
 
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+
 // ---- gradient ---------------------------------------------------------------------------------------------------------------
 // The sorted positions are cut into pieces of `piece`.  Where a token's places begin, its piece adds them up, to the end of the next piece at most; if there are more
 // of them (a frequent token), every further piece leaves a partial sum of its own, and embed_join adds those up in order.  A thread has eight channels; `lanes`
@@ -82,7 +85,7 @@ struct SumArgs {
   unsigned *n_long, *long_list; // pieces where such a token begins
   int64_t tokens, ld, pieces;
   int vocab, channels, piece, lanes, slices, accumulate;
-  int64_t sum_blocks, zero_blocks, zero_rows;
+  int64_t sum_blocks, zero_blocks;
   float scale;
 };
 
@@ -100,47 +103,33 @@ __device__ __forceinline__ void finish_row(const SumArgs& a, unsigned key, int c
   store8(p, narrow8<G>(v), left);
 }
 
+// The sorted places of a piece and of the next one, and the tokens before: [0] one place, [1] a piece and one place before.
+struct Window {
+  unsigned *key, *pos;
+  unsigned before[2];
+};
 template <class O, class G>
-__device__ void sum_piece(const SumArgs& a, int64_t piece, int c) {
-  const int64_t s = piece * a.piece, T = a.tokens;
-  const int64_t own_end = s + a.piece < T ? s + a.piece : T, far_end = own_end + a.piece < T ? own_end + a.piece : T;
+__device__ __forceinline__ void sum_piece(const SumArgs& a, int64_t piece, int c, const Window& w) {
+  constexpr int U = sizeof(O) == 4 ? 4 : 8;  // rows on their way at a time
+  const int64_t rest = a.tokens - piece * a.piece;
+  const int own_end = rest < a.piece ? (int)rest : a.piece, far_end = rest < 2 * a.piece ? (int)rest : 2 * a.piece;
   const int left = a.channels - c < 8 ? a.channels - c : 8;
-  int64_t i = s;
-  const unsigned first = a.keys[s];
+  int i = 0;
+  const unsigned first = w.key[0], last = w.key[own_end - 1];
   if (first >= (unsigned)a.vocab) return;  // tokens outside the table come last
   bool head = false;                       // a token's further part
-  if (s > 0 && a.keys[s - 1] == first) {
-    head = s > a.piece && a.keys[s - a.piece - 1] == first;
+  if (w.before[0] == first) {
+    head = w.before[1] == first;
     if (!head)  // it began in the piece before, which adds this piece's places too
-      while (i < own_end && a.keys[i] == first) ++i;
+      while (i < own_end && w.key[i] == first) ++i;
   }
+  if (i >= own_end) return;
+  const bool all_head = head && last == first;  // nothing of the piece is its own: the next piece's places are another's
+  const int end = all_head ? own_end : far_end;
   const O* const dout = static_cast<const O*>(a.dout) + c;
-  while (i < own_end) {
-    const unsigned key = a.keys[i];
-    if (key >= (unsigned)a.vocab) return;
-    const int64_t end = head ? own_end : far_end;
-    f32x8 sum = {};
-    for (;;) {  // four places at a time
-      int n = 1;
-      unsigned at[4];
-      at[0] = a.pos[i];
-#pragma unroll
-      for (int u = 1; u < 4; ++u) {
-        const bool more = n == u && i + u < end && a.keys[i + u] == key;
-        at[u] = more ? a.pos[i + u] : at[0];
-        n += more;
-      }
-      f32x8 v[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) v[u] = row8(dout + (int64_t)at[u] * a.ld, left);
-      sum += v[0];
-      if (n > 1) sum += v[1];
-      if (n > 2) sum += v[2];
-      if (n > 3) sum += v[3];
-      i += n;
-      if (n < 4 || i >= end || a.keys[i] != key) break;
-    }
-    const bool goes_on = i == end && i < T && a.keys[i] == key;
+  unsigned key = w.key[i];
+  f32x8 sum = {};
+  auto flush = [&](bool goes_on) {
     if (head || goes_on) {
       store8(a.partial + (piece * 2 + !head) * a.channels + c, sum, left);
       if (!head && c == 0) a.long_list[atomicAdd(a.n_long, 1u)] = (unsigned)piece;  // their order is of no consequence: each has a row of its own
@@ -148,24 +137,91 @@ __device__ void sum_piece(const SumArgs& a, int64_t piece, int c) {
       finish_row<G>(a, key, c, left, sum);
     }
     head = false;
+  };
+  // does the token at the end of what is looked at go on behind it?  (behind two pieces: the place after the window is a third's first)
+  auto goes_on = [&](int at) { return at == end && !all_head && rest > end && a.keys[piece * a.piece + end] == key; };
+  for (;;) {
+    unsigned k[U];
+    typename Vec8<O>::V v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = i + u < end ? i + u : end - 1;
+      k[u] = w.key[at];
+      const bool mine = i + u < end && k[u] < (unsigned)a.vocab && (i + u < own_end || k[u] == last);
+      if (!mine) k[u] = ~0u;
+      // in the place of one that is not its own a row that it reads anyway, and does not add
+      const O* const p = dout + (int64_t)w.pos[mine ? at : i] * a.ld;
+      v[u] = left >= 8 ? load8(p) : load8(p, left);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (k[u] != key) {
+        flush(goes_on(i + u));  // what stopped it: another token, the end of the next piece, or of all
+        if (k[u] == ~0u) return;
+        key = k[u];
+        sum = f32x8{};
+      }
+      sum += widen8<O>(v[u]);
+    }
+    i += U;
+    if (i >= end) {
+      flush(goes_on(end));
+      return;
+    }
   }
 }
 
 template <class O, class G>
-__global__ __launch_bounds__(256) void embed_sum(SumArgs a) {
+__global__ __launch_bounds__(256, 4) void embed_sum(SumArgs a) {
+  __shared__ unsigned keys[32 * 64], pos[32 * 64];  // of each worker: two pieces
   const int per = 256 / a.lanes, mine = threadIdx.x / a.lanes, lane = threadIdx.x % a.lanes;
-  for (int64_t b = blockIdx.x; b < a.sum_blocks + a.zero_blocks; b += gridDim.x) {
+  const int64_t blocks = a.sum_blocks + a.zero_blocks;
+  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
     if (b < a.sum_blocks) {
       const int64_t w = b * per + mine, piece = w / a.slices;
       const int c = ((int)(w - piece * a.slices) * a.lanes + lane) * 8;
-      if (piece < a.pieces && c < a.channels) sum_piece<O, G>(a, piece, c);
-    } else {  // rows of the table without a token
-      const int64_t row0 = (b - a.sum_blocks) * a.zero_rows, vecs = (a.channels + 7) / 8;
-      const int64_t rows = a.vocab - row0 < a.zero_rows ? a.vocab - row0 : a.zero_rows;
-      for (int64_t i = threadIdx.x; i < rows * vecs; i += 256) {
-        const int64_t r = i / vecs, c = (i - r * vecs) * 8;
-        if (a.used[row0 + r]) continue;
-        store8(static_cast<G*>(a.dtable) + (row0 + r) * a.channels + c, typename Vec8<G>::V{}, (int)(a.channels - c < 8 ? a.channels - c : 8));
+      const int64_t at = piece * a.piece;
+      Window win = {keys + mine * 2 * a.piece, pos + mine * 2 * a.piece, {~0u, ~0u}};
+      __syncthreads();  // the previous turn's reads
+      if (piece < a.pieces) {
+        for (int j = lane; j < 2 * a.piece && at + j < a.tokens; j += a.lanes) {
+          win.key[j] = a.keys[at + j];
+          win.pos[j] = a.pos[at + j];
+        }
+        if (piece > 0) win.before[0] = a.keys[at - 1];
+        if (piece > 1) win.before[1] = a.keys[at - a.piece - 1];
+      }
+      __syncthreads();
+      if (piece < a.pieces && c < a.channels) sum_piece<O, G>(a, piece, c, win);
+    } else {  // what lies in rows of the table without a token, in vectors on 16 bytes whatever the channels are
+      const int64_t all = (int64_t)a.vocab * a.channels, e0 = (b - a.sum_blocks) * ZERO_EACH, row0 = e0 / a.channels;
+      const int n = (int)(all - e0 < ZERO_EACH ? all - e0 : ZERO_EACH);
+      const unsigned off = (unsigned)(e0 - row0 * a.channels), D = (unsigned)a.channels;
+      G* const to = static_cast<G*>(a.dtable) + e0;
+      const unsigned char* const used = a.used + row0;
+      constexpr int EACH = ZERO_EACH / (256 * 8);
+      unsigned char busy[EACH], next[EACH];  // of the row that a vector begins in, and where one ends inside the vector of the next: does it have a token?  All asked for together
+      unsigned ends[EACH];
+#pragma unroll
+      for (int j = 0; j < EACH; ++j) {
+        const unsigned i = (j * 256 + threadIdx.x) * 8, row = (off + i) / D;
+        ends[j] = (row + 1) * D - (off + i);
+        busy[j] = (int)i < n ? used[row] : 1;
+        next[j] = ends[j] < 8 && (int)(i + ends[j]) < n ? used[row + 1] : 1;
+      }
+#pragma unroll
+      for (int j = 0; j < EACH; ++j) {
+        const int i = (j * 256 + threadIdx.x) * 8;
+        if (ends[j] >= 8) {
+          if (!busy[j]) store8(to + i, typename Vec8<G>::V{});
+        } else if (D >= 8) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (i + e < n && !(e < (int)ends[j] ? busy[j] : next[j])) to[i + e] = (G)0.f;
+        } else {
+          for (int e = 0; e < 8 && i + e < n; ++e)
+            if (!used[(off + i + e) / D]) to[i + e] = (G)0.f;
+        }
       }
     }
   }
@@ -183,20 +239,23 @@ __global__ __launch_bounds__(512) void embed_join(SumArgs a) {
     for (unsigned i = blockIdx.x; i < n; i += gridDim.x) {
       const int64_t from = a.long_list[i];
       const unsigned key = a.keys[(from + 1) * a.piece];  // the next piece's places are all the token's
-      int64_t lo = from + 2, hi = a.pieces;               // first piece that does not begin with it
+      int64_t lo = from + 2, hi = a.pieces;               // first piece that does not begin with it: 64 places are looked at at a time
       while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
-        if (a.keys[mid * a.piece] == key) lo = mid + 1;
-        else hi = mid;
+        const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const int with = __popcll(__ballot(at < hi && a.keys[at * a.piece] == key));
+        if (with == 0) break;
+        const int64_t known = lo + (with - 1) * step + 1;  // the last that has it is before this one
+        hi = known + step - 1 < hi ? known + step - 1 : hi;
+        lo = known;
       }
       const int64_t parts = lo - (from + 2), each = (parts + 7) / 8, b = wave * each, e = b + each < parts ? b + each : parts;
       f32x4 sum = {0.f, 0.f, 0.f, 0.f};
       auto add = [&](const float* p) {
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (k < left) v[k] = p[k];
-        sum += v;
+        if (left == 4) {
+          sum += *reinterpret_cast<const f32x4_any*>(p);
+          return;
+        }
+        for (int k = 0; k < left; ++k) sum[k] += p[k];
       };
       if (left > 0) {
         if (wave == 0) add(a.partial + (from * 2 + 1) * a.channels + c);
@@ -362,8 +421,7 @@ extern "C" int jz_embed_bwd(const jz_embed_desc* d, const int* ids, const void* 
   a.scale = d->scale;
   const int64_t per = 256 / p.lanes;
   a.sum_blocks = (p.pieces * p.slices + per - 1) / per;
-  a.zero_rows = std::max<int64_t>(1, 16384 / s.D);
-  a.zero_blocks = accumulate ? 0 : (s.V + a.zero_rows - 1) / a.zero_rows;
+  a.zero_blocks = accumulate ? 0 : ((int64_t)s.V * s.D + ZERO_EACH - 1) / ZERO_EACH;
   if (d->dtype == JZ_F32) return sums<float, float>(a, st);
   if (d->dtype == JZ_F16) return d->out_dtype == JZ_F32 ? sums<float, _Float16>(a, st) : sums<_Float16, _Float16>(a, st);
   return d->out_dtype == JZ_F32 ? sums<float, __bf16>(a, st) : sums<__bf16, __bf16>(a, st);

@@ -2,8 +2,9 @@
 //
 // A token outside [0, vocab) gets the key `vocab` and so comes last.  Within a wavefront equal digits find each other by ballots, a lane's rank among them is the
 // number of lower lanes with its digit, and a counter for each wavefront and digit carries the count from one 64 to the next: no order depends on who comes first.
-// Up to 16384 tokens one workgroup does it all in LDS (one launch; 50000 different tokens are 16 bits, two passes).  Beyond, each pass is three launches: counts of the
-// digits in tiles of 4096, their running sums over the tiles, and the move.
+// Up to 16384 tokens are sorted as runs of 1024 in LDS, and the runs joined: two launches.  (One workgroup for all of them was bound by what one compute unit can do: 16384 tokens of 50000, 35 us by
+// ballots, 46 with counters for each thread and digit.)  Beyond, each pass is three launches: counts of the digits in tiles of 4096, their running sums over the tiles, and the
+// move.
 // On the way `used` (one byte for each token of the vocabulary, or NULL) is cleared and then set where a token occurs, and *counter is cleared.
 #pragma once
 
@@ -11,7 +12,7 @@ constexpr int SORT_BITS = 9, SORT_RADIX = 1 << SORT_BITS, SORT_TILE = 4096;
 constexpr int64_t SORT_SMALL = 16384;
 
 struct SortLayout {
-  int passes, bits;  // of a digit
+  int all_bits, passes, bits;  // of a key; passes of the large form and bits of their digits
   int64_t tiles;
   size_t keys[2], pos[2], counts, totals, total;
 };
@@ -19,6 +20,7 @@ inline SortLayout sort_layout(int64_t n, int vocab) {
   SortLayout L;
   int bits = 1;
   while (bits < 32 && (int64_t(1) << bits) <= vocab) ++bits;  // the largest key is `vocab`
+  L.all_bits = bits;
   L.passes = (bits + SORT_BITS - 1) / SORT_BITS;
   L.bits = (bits + L.passes - 1) / L.passes;
   L.tiles = n > SORT_SMALL ? (n + SORT_TILE - 1) / SORT_TILE : 0;
@@ -31,8 +33,8 @@ inline SortLayout sort_layout(int64_t n, int vocab) {
   const size_t list = (size_t)n * 4;
   L.keys[0] = room(list);
   L.pos[0] = room(list);
-  L.keys[1] = L.tiles ? room(list) : 0;
-  L.pos[1] = L.tiles ? room(list) : 0;
+  L.keys[1] = n > 1024 ? room(list) : 0;
+  L.pos[1] = n > 1024 ? room(list) : 0;
   L.counts = room((size_t)L.tiles * SORT_RADIX * 4);
   L.totals = room(L.tiles ? SORT_RADIX * 4 : 0);
   L.total = o;
@@ -45,7 +47,7 @@ struct SortArgs {
   unsigned *keys, *pos, *counts, *totals, *counter;
   unsigned char* used;               // cleared in the first pass, set in the last
   int64_t n, tiles;
-  int vocab, shift, bits, passes;
+  int vocab, shift, bits, all_bits;
   bool first, last;
 };
 
@@ -84,64 +86,89 @@ __device__ __forceinline__ unsigned exclusive_sum(unsigned v, unsigned* lds) {
   return base + s - v;
 }
 
-// Everything in one workgroup: EACH keys a thread, in order: wavefront, turn, lane.  Keys behind the last are the largest there are and stay behind it.
-template <int EACH>
-__global__ __launch_bounds__(1024) void sort_small(SortArgs a) {
-  constexpr int N = 1024 * EACH;
-  __shared__ unsigned keys[N];
-  __shared__ unsigned short pos[N];
+// Runs of 1024 positions, a workgroup each, one key a thread: sorted by itself in LDS.  Keys behind the last are the largest there are and stay behind it.
+__global__ __launch_bounds__(1024) void sort_runs(SortArgs a) {
+  __shared__ unsigned keys[1024], pos[1024];
   __shared__ unsigned count[16][SORT_RADIX], start[SORT_RADIX], scan[16];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, radix = 1 << a.bits;
-  unsigned k[EACH], p[EACH];
-#pragma unroll
-  for (int j = 0; j < EACH; ++j) {
-    p[j] = wave * (64 * EACH) + j * 64 + lane;
-    k[j] = p[j] < a.n ? sort_key(a.ids[p[j]], a.vocab) : ~0u;
-  }
-  if (t == 0) *a.counter = 0;
+  const int t = threadIdx.x, wave = t >> 6, radix = 1 << a.bits;
+  const int64_t i = (int64_t)blockIdx.x * 1024 + t;
+  unsigned k = i < a.n ? sort_key(a.ids[i], a.vocab) : ~0u, p = (unsigned)i;
   if (a.used)
-    for (int64_t i = (int64_t)t * 16; i < a.vocab; i += 1024 * 16) *reinterpret_cast<uint4*>(a.used + i) = uint4{0, 0, 0, 0};  // whole: its room ends on 256 bytes
-  for (int pass = 0; pass < a.passes; ++pass) {
-    const int shift = pass * a.bits;
-    for (int i = t; i < 16 * SORT_RADIX; i += 1024) count[i / SORT_RADIX][i % SORT_RADIX] = 0;
+    for (int64_t u = i * 16; u < a.vocab; u += (int64_t)gridDim.x * 1024 * 16) *reinterpret_cast<uint4*>(a.used + u) = uint4{0, 0, 0, 0};  // whole: its room ends on 256 bytes
+  if (i == 0) *a.counter = 0;
+  for (int shift = 0; shift < a.all_bits; shift += a.bits) {
+    for (int c = t; c < 16 * radix; c += 1024) count[c >> a.bits][c & (radix - 1)] = 0;
     __syncthreads();
-    unsigned r[EACH];
-#pragma unroll
-    for (int j = 0; j < EACH; ++j) r[j] = rank_in_wave(k[j] >> shift & (radix - 1), a.bits, count[wave]);
+    const unsigned d = k >> shift & (radix - 1), r = rank_in_wave(d, a.bits, count[wave]);
     __syncthreads();
     unsigned all = 0;
-    if (t < radix)
+    if (t < radix) {
+      unsigned c[16];
+#pragma unroll
+      for (int w = 0; w < 16; ++w) c[w] = count[w][t];
+#pragma unroll
       for (int w = 0; w < 16; ++w) {
-        const unsigned c = count[w][t];
         count[w][t] = all;
-        all += c;
+        all += c[w];
       }
+    }
     const unsigned before = exclusive_sum<16>(all, scan);
     if (t < radix) start[t] = before;
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < EACH; ++j) {
-      const unsigned d = k[j] >> shift & (radix - 1), to = start[d] + count[wave][d] + r[j];
-      keys[to] = k[j];
-      pos[to] = (unsigned short)p[j];
-    }
+    const unsigned to = start[d] + count[wave][d] + r;
+    keys[to] = k;
+    pos[to] = p;
     __syncthreads();
+    k = keys[t];
+    p = pos[t];
+  }
+  if (i < a.n) {
+    a.keys[i] = k;
+    a.pos[i] = p;
+    if (a.tiles == 1 && a.used && k < (unsigned)a.vocab) a.used[k] = 1;  // one run: this workgroup alone has cleared it, before the barriers above
+  }
+}
+
+// Up to 16 runs into one list: a key's place is its place in its run and the number of keys before it in each other run, by bisection; equal keys of earlier runs come first.
+__global__ __launch_bounds__(256) void sort_merge(SortArgs a) {
+  __shared__ __attribute__((aligned(16))) unsigned keys[SORT_SMALL];
+  const int runs = (int)a.tiles, t = threadIdx.x;
+  const int64_t i = (int64_t)blockIdx.x * 256 + t;
+  const unsigned mine = i < a.n ? a.keys_in[i] : ~0u, p = i < a.n ? a.pos_in[i] : 0;
+  for (int j = t * 4; j < runs * 1024; j += 1024) {
+    uint4 v = {~0u, ~0u, ~0u, ~0u};
+    if (j + 3 < a.n) v = *reinterpret_cast<const uint4*>(a.keys_in + j);
+    else {
+      if (j < a.n) v.x = a.keys_in[j];
+      if (j + 1 < a.n) v.y = a.keys_in[j + 1];
+      if (j + 2 < a.n) v.z = a.keys_in[j + 2];
+    }
+    *reinterpret_cast<uint4*>(keys + j) = v;
+  }
+  __syncthreads();
+  if (i >= a.n) return;
+  const int run = (int)(i >> 10);
+  unsigned to = (unsigned)(i & 1023);
+  for (int q0 = 0; q0 < runs; q0 += 4) {  // four bisections at a time
+    unsigned at[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int j = 0; j < EACH; ++j) {
-      const int i = wave * (64 * EACH) + j * 64 + lane;
-      k[j] = keys[i];
-      p[j] = pos[i];
+    for (int s = 512; s > 0; s >>= 1)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int of = q0 + q < runs ? q0 + q : 0;
+        if (keys[of * 1024 + at[q] + s - 1] < mine + (of < run ? 1u : 0u)) at[q] += s;
+      }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int of = q0 + q;
+      if (of >= runs || of == run) continue;
+      if (keys[of * 1024 + at[q]] < mine + (of < run ? 1u : 0u)) ++at[q];
+      to += at[q];
     }
   }
-#pragma unroll
-  for (int j = 0; j < EACH; ++j) {
-    const int i = wave * (64 * EACH) + j * 64 + lane;
-    if (i < a.n) {
-      a.keys[i] = k[j];
-      a.pos[i] = p[j];
-      if (a.used && k[j] < (unsigned)a.vocab) a.used[k[j]] = 1;  // cleared before the barriers above
-    }
-  }
+  a.keys[to] = mine;
+  a.pos[to] = p;
+  if (a.used && mine < (unsigned)a.vocab) a.used[mine] = 1;
 }
 
 __global__ __launch_bounds__(256) void sort_count(SortArgs a) {
@@ -240,17 +267,25 @@ inline int sort_tokens(const SortLayout& L, const int* ids, int64_t n, int vocab
   a.tiles = L.tiles;
   a.vocab = vocab;
   a.bits = L.bits;
-  a.passes = L.passes;
+  a.all_bits = L.all_bits;
   a.used = used;
   a.counter = counter;
   a.counts = list(L.counts);
   a.totals = list(L.totals);
   if (n <= SORT_SMALL) {
+    const unsigned runs = (unsigned)std::max<int64_t>(1, (n + 1023) / 1024);
+    a.tiles = runs;
     a.keys = list(L.keys[0]);
     a.pos = list(L.pos[0]);
-    if (n <= 1024) sort_small<1><<<1, 1024, 0, st>>>(a);
-    else if (n <= 4096) sort_small<4><<<1, 1024, 0, st>>>(a);
-    else sort_small<16><<<1, 1024, 0, st>>>(a);
+    sort_runs<<<runs, 1024, 0, st>>>(a);
+    if (runs > 1) {
+      if (jz::launch_status() != JZ_OK) return JZ_ERR_LAUNCH;
+      a.keys_in = a.keys;
+      a.pos_in = a.pos;
+      a.keys = list(L.keys[1]);
+      a.pos = list(L.pos[1]);
+      sort_merge<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(a);
+    }
     *keys = a.keys;
     *pos = a.pos;
     return jz::launch_status();
