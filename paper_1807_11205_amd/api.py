@@ -1109,11 +1109,14 @@ def _workspace_bytes(name, desc) -> int:
     return n.value
 
 
+_current_device = _get_device if _get_device is not None else torch.cuda.current_device
+
+
 def _here(*tensors):
     """Launches go to the current device: tensors that lie on another are refused."""
     for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != torch.cuda.current_device():
-            raise ValueError("a tensor is on device %d, the current one is %d" % (t.get_device(), torch.cuda.current_device()))
+        if t is not None and t.is_cuda and t.get_device() != _current_device():
+            raise ValueError("a tensor is on device %d, the current one is %d" % (t.get_device(), _current_device()))
 
 
 def embed_desc(tokens: int, vocab: int, channels: int, dtype: int = JZ_F16, out_dtype: Optional[int] = None, scale: float = 1.0, out_stride: int = 0) -> jz_embed_desc:

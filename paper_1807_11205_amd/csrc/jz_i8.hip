@@ -105,25 +105,31 @@ struct I8Out {
   int64_t M, N, ld;
   int act;
 };
+// A lane has the same eight columns in every row that it stores; its scales are asked for together, from places that exist, before the first is needed.  (A load in each turn of the
+// loop was waited for in each: I8_EPILOGUE_BEFORE.)
 template <class T>
 struct I8Store : I8Out {
   template <class S>
   __device__ __forceinline__ void strip(const S& s, const MmTile&, int64_t m0, int64_t n0, int lane) const {
-    constexpr int PER = S::COLS / 8;
-#pragma unroll 1
-    for (int i = lane; i < 32 * PER; i += 64) {
-      const int row = i / PER, c = i % PER * 8;
-      const int64_t m = m0 + row, n = n0 + c;
-      if (m >= M || n >= N) continue;
-      const int left = N - n < 8 ? (int)(N - n) : 8;
+    constexpr int PER = S::COLS / 8, TURNS = PER / 2, EACH = 64 / PER;
+    const int c = lane % PER * 8, row0 = lane / PER;
+    const int64_t n = n0 + c;
+    const int left = N - n < 8 ? (int)(N - n) : 8;
+    float r[TURNS];
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) r[t] = sx[m0 + row0 + t * EACH < M ? m0 + row0 + t * EACH : M - 1];
+    if (left <= 0) return;
+    const f32x8 w = load8(sw + n, left);
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) {
+      const int row = row0 + t * EACH;
+      const int64_t m = m0 + row;
       int v[8];
       s.row8(row, c, v);
-      const float r = sx[m];
-      const f32x8 w = load8(sw + n, left);
       f32x8 f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = (float)v[e] * (r * w[e]);
-      store8(static_cast<T*>(y) + m * ld + n, narrow8<T>(f), left);
+      for (int e = 0; e < 8; ++e) f[e] = (float)v[e] * (r[t] * w[e]);
+      if (m < M) store8(static_cast<T*>(y) + m * ld + n, narrow8<T>(f), left);
     }
   }
 };
@@ -131,22 +137,26 @@ struct I8Store : I8Out {
 struct I8Glu : I8Out {
   template <class S>
   __device__ __forceinline__ void strip(const S& s, const MmTile&, int64_t m0, int64_t n0, int lane) const {
-    constexpr int PER = S::COLS / 16;
-#pragma unroll 1
-    for (int i = lane; i < 32 * PER; i += 64) {
-      const int row = i / PER, c = i % PER, from = (c >> 2) * 64 + (c & 3) * 8;
-      const int64_t m = m0 + row, n = n0 / 2 + c * 8;
-      if (m >= M || n >= N) continue;
-      const int left = N - n < 8 ? (int)(N - n) : 8;
+    constexpr int PER = S::COLS / 16, TURNS = PER / 2, EACH = 64 / PER;
+    const int c = lane % PER, from = (c >> 2) * 64 + (c & 3) * 8, row0 = lane / PER;
+    const int64_t n = n0 / 2 + c * 8;
+    const int left = N - n < 8 ? (int)(N - n) : 8;
+    float r[TURNS];
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) r[t] = sx[m0 + row0 + t * EACH < M ? m0 + row0 + t * EACH : M - 1];
+    if (left <= 0) return;
+    const f32x8 wg = load8(sw + n, left), wu = load8(su + n, left);
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) {
+      const int row = row0 + t * EACH;
+      const int64_t m = m0 + row;
       int g[8], u[8];
       s.row8(row, from, g);
       s.row8(row, from + 32, u);
-      const float r = sx[m];
-      const f32x8 wg = load8(sw + n, left), wu = load8(su + n, left);
       f32x8 h;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) h[e] = act_fwd(act, (float)g[e] * (r * wg[e])) * ((float)u[e] * (r * wu[e]));
-      store8(static_cast<float*>(y) + m * ld + n, h, left);
+      for (int e = 0; e < 8; ++e) h[e] = act_fwd(act, (float)g[e] * (r[t] * wg[e])) * ((float)u[e] * (r[t] * wu[e]));
+      if (m < M) store8(static_cast<float*>(y) + m * ld + n, h, left);
     }
   }
 };

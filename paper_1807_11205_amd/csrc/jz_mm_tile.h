@@ -323,12 +323,86 @@ __global__ __launch_bounds__(256, 2) void mm_small(MmArgs a, Epi epi) {
   epi.strip(strip, w, m0 + wm * 32, n0 + wn * 32, lane);
 }
 
+// Fewer still, and short sums: 32 x 32 by eight wavefronts that share k, 64 bytes of it at a time each, straight into the registers that the matrix instructions take; four such pieces are on
+// their way at a time, and nobody waits for another but for the sums, which meet in LDS and are added in the wavefronts' order.
+template <class E, class Epi>
+__global__ __launch_bounds__(512, 2) void mm_tiny(MmArgs a, Epi epi) {
+  constexpr int WAVES = 8, U = 4;
+  typedef typename E::Reg Reg;
+  typedef typename E::Sum Sum;
+  typedef MmStrip<E, 1> Strip;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[WAVES][4096];
+  if (a.skip && *a.skip) return;
+  const MmTile w = mm_tile(a);
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int64_t m0 = (int64_t)w.m * 32, n0 = (int64_t)w.n * 32;
+  auto source = [&](const MmOperand& o, int64_t row0) {
+    const int64_t span = (o.rows - row0 - 1) * o.pitch + a.row_bytes;
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(static_cast<const char*>(o.p[0]) + w.of * o.of + row0 * o.pitch), 0, (int)(span < 0x7ffffff0 ? span : 0x7ffffff0), 0x00020000);
+  };
+  const auto from_a = source(a.a, m0), from_b = source(a.b, n0);
+  const unsigned row_a = (unsigned)((lane & 31) * a.a.pitch), row_b = (unsigned)((lane & 31) * a.b.pitch);
+  const int units = (int)((a.row_bytes + 63) / 64);
+  struct Piece {
+    Reg a[2], b[2];
+  };
+  auto get = [&](Piece& p, int u) {  // behind the end: zeros
+    // ElemSplit: 16 k of high parts and, 64 bytes on, their low parts; ElemI8: 64 k
+    const unsigned j = u & 1, k0 = (unsigned)(u >> 1) * 128, h = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const unsigned k = k0 + (E::SPLIT ? (2 * j + h) * 16 + i * 64 : (4 * j + 2 * i + h) * 16);
+      const unsigned end = k >= (unsigned)a.row_bytes ? 0x80000000u : 0u;
+      p.a[i] = __builtin_bit_cast(Reg, __builtin_amdgcn_raw_buffer_load_b128(from_a, (int)((row_a + k) | end), 0, 0));
+      p.b[i] = __builtin_bit_cast(Reg, __builtin_amdgcn_raw_buffer_load_b128(from_b, (int)((row_b + k) | end), 0, 0));
+    }
+  };
+  Sum acc[1] = {Sum{}};
+  auto multiply = [&](const Piece& p) {
+    if constexpr (E::SPLIT) {
+      acc[0] = E::mfma(p.b[0], p.a[0], acc[0]);
+      acc[0] = E::mfma(p.b[0], p.a[1], acc[0]);
+      acc[0] = E::mfma(p.b[1], p.a[0], acc[0]);
+    } else {
+      acc[0] = E::mfma(p.b[0], p.a[0], acc[0]);
+      acc[0] = E::mfma(p.b[1], p.a[1], acc[0]);
+    }
+  };
+  Piece p[2][U];
+  auto ask = [&](Piece (&to)[U], int u0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) get(to[u], u0 + u * WAVES);
+  };
+  ask(p[0], wave);
+  for (int u0 = wave; u0 < units; u0 += 2 * U * WAVES) {
+    ask(p[1], u0 + U * WAVES);
+#pragma unroll
+    for (int u = 0; u < U; ++u) multiply(p[0][u]);
+    if (u0 + U * WAVES >= units) break;
+    ask(p[0], u0 + 2 * U * WAVES);
+#pragma unroll
+    for (int u = 0; u < U; ++u) multiply(p[1][u]);
+  }
+  Strip{(JZ_LDS unsigned char*)lds[wave]}.put(acc, lane);
+  __syncthreads();
+  if (t < 256) {
+    typedef typename Strip::V4 V4;
+    JZ_LDS V4* const mine = reinterpret_cast<JZ_LDS V4*>((JZ_LDS unsigned char*)lds[0] + t * 16);
+    V4 v = *mine;
+#pragma unroll
+    for (int q = 1; q < WAVES; ++q) v += mine[q * 256];
+    *mine = v;
+  }
+  __syncthreads();
+  if (wave == 0) epi.strip(Strip{(JZ_LDS unsigned char*)lds[0]}, w, m0, n0, lane);
+}
+
 constexpr int64_t MM_LANES = int64_t(1) << 32;  // a launch has fewer
 
-// A launch over `count` matrices, TILE x TILE: 256 by eight wavefronts in 2 x 4, 128 by four in 2 x 2, 64: mm_small.
+// A launch over `count` matrices, TILE x TILE: 256 by eight wavefronts in 2 x 4, 128 by four in 2 x 2, 64: mm_small, 32: mm_tiny.
 template <class E, class Epi, int TILE, bool DUAL>
 int mm_launch(MmArgs a, const Epi& epi, int64_t rows_m, int64_t rows_n, int64_t count, hipStream_t st) {
-  constexpr int WGM = 2, WGN = TILE == 256 ? 4 : 2, THREADS = 64 * WGM * WGN;
+  constexpr int WGM = 2, WGN = TILE == 256 ? 4 : 2, THREADS = TILE == 32 ? 512 : 64 * WGM * WGN;
   a.tiles_m = (int)((rows_m + TILE - 1) / TILE);
   a.tiles_n = (int)((rows_n + TILE - 1) / TILE);
   a.tiles = a.symmetric ? (unsigned)a.tiles_m * (a.tiles_m + 1) / 2 : (unsigned)a.tiles_m * a.tiles_n;
@@ -336,7 +410,8 @@ int mm_launch(MmArgs a, const Epi& epi, int64_t rows_m, int64_t rows_n, int64_t 
   constexpr unsigned most = (unsigned)(MM_LANES / THREADS - 1);
   for (a.first = 0; a.first < a.workgroups; a.first += most) {
     const unsigned grid = std::min(a.workgroups - a.first, most);
-    if constexpr (TILE == 64) mm_small<E, Epi><<<grid, 256, 0, st>>>(a, epi);
+    if constexpr (TILE == 32) mm_tiny<E, Epi><<<grid, 512, 0, st>>>(a, epi);
+    else if constexpr (TILE == 64) mm_small<E, Epi><<<grid, 256, 0, st>>>(a, epi);
     else mm_tiles<E, Epi, TILE, TILE, WGM, WGN, DUAL><<<grid, THREADS, 0, st>>>(a, epi);
   }
   return jz::launch_status();

@@ -183,29 +183,31 @@ struct Parts {
 };
 template <class S>
 __device__ __forceinline__ void store_rows(const S& s, const Parts& to, int64_t of, int64_t m0, int64_t n0, int lane, float factor) {
-  constexpr int PER = S::COLS / 8;
-#pragma unroll 1
-  for (int i = lane; i < 32 * PER; i += 64) {
-    const int row = i / PER, c = i % PER * 8;
-    if (m0 + row >= to.rows || n0 + c >= to.cols) continue;
+  constexpr int PER = S::COLS / 8, EACH = 64 / PER;
+  const int c = lane % PER * 8;
+  char* const p = to.row(of, m0);
+  if (n0 + c >= to.cols) return;
+#pragma unroll
+  for (int row = lane / PER; row < 32; row += EACH) {
     float v[8];
     s.row8(row, c, v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= factor;
-    store_parts(to.row(of, m0 + row), n0 + c, v);
+    if (m0 + row < to.rows) store_parts(p + row * to.cols * 4, n0 + c, v);
   }
 }
 template <class S>
 __device__ __forceinline__ void store_cols(const S& s, const Parts& to, int64_t of, int64_t m0, int64_t n0, int lane, float factor) {
-#pragma unroll 1
-  for (int i = lane; i < S::COLS * 4; i += 64) {
-    const int col = i / 4, r = i % 4 * 8;
-    if (n0 + col >= to.rows || m0 + r >= to.cols) continue;
+  const int r = lane % 4 * 8;
+  char* const p = to.row(of, n0);
+  if (m0 + r >= to.cols) return;
+#pragma unroll
+  for (int col = lane / 4; col < S::COLS; col += 16) {
     float v[8];
     s.col8(r, col, v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= factor;
-    store_parts(to.row(of, n0 + col), m0 + r, v);
+    if (n0 + col < to.rows) store_parts(p + col * to.cols * 4, m0 + r, v);
   }
 }
 struct OrthoSymmetric {  // a product that is its own transpose
@@ -222,18 +224,21 @@ struct OrthoPoly {  // B = ca I + cb A + cc A^2
   float ca, cb, cc;
   template <class S>
   __device__ __forceinline__ void strip(const S& s, const MmTile& w, int64_t m0, int64_t n0, int lane) const {
-    constexpr int PER = S::COLS / 8;
-#pragma unroll 1
-    for (int i = lane; i < 32 * PER; i += 64) {
-      const int row = i / PER, c = i % PER * 8;
-      if (m0 + row >= a.rows || n0 + c >= a.cols) continue;
-      float v[8], u[8];
-      s.row8(row, c, v);
-      load_parts(a.row(w.of, m0 + row), n0 + c, u);
+    constexpr int PER = S::COLS / 8, EACH = 64 / PER, TURNS = 32 / EACH;
+    const int c = lane % PER * 8, row0 = lane / PER;
+    const int64_t n = n0 + c < a.cols ? n0 + c : 0;
+    float u[TURNS][8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = fmaf(cc / SCALE, v[e], fmaf(cb, u[e], m0 + row == n0 + c + e ? ca * SCALE : 0.f));
+    for (int t = 0; t < TURNS; ++t) load_parts(a.row(w.of, m0 + row0 + t * EACH < a.rows ? m0 + row0 + t * EACH : 0), n, u[t]);  // together, before the first is needed
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) {
+      const int row = row0 + t * EACH;
+      float v[8];
+      s.row8(row, c, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = fmaf(cc / SCALE, v[e], fmaf(cb, u[t][e], m0 + row == n0 + c + e ? ca * SCALE : 0.f));
       s.set_row8(row, c, v);
-      store_parts(b.row(w.of, m0 + row), n0 + c, v);
+      if (m0 + row < a.rows && n0 + c < a.cols) store_parts(b.row(w.of, m0 + row), n0 + c, v);
     }
     if (w.m != w.n) store_cols(s, b, w.of, m0, n0, lane, 1.f);
   }
@@ -282,6 +287,8 @@ struct OrthoResult {  // the last B X, rounded once; transposed back where TALL 
     }
   }
 };
+
+#include "jz_ortho_chain.h"
 
 // ---- the update's last pass -------------------------------------------------------------------------------------------------------
 struct MuonApply {
@@ -346,6 +353,7 @@ int ortho_product(const Parts& p, const Parts& q, bool symmetric, int64_t count,
   };
   if (tiles(256) >= 200) return mm_launch<ElemSplit, Epi, 256, false>(a, e, p.rows, q.rows, count, st);
   if (tiles(128) >= 200) return mm_launch<ElemSplit, Epi, 128, false>(a, e, p.rows, q.rows, count, st);
+  if (tiles(32) <= 512 && a.row_bytes <= 4096) return mm_launch<ElemSplit, Epi, 32, false>(a, e, p.rows, q.rows, count, st);
   return mm_launch<ElemSplit, Epi, 64, false>(a, e, p.rows, q.rows, count, st);
 }
 
@@ -364,8 +372,9 @@ int ortho_begin(const OrthoIn& in, const OrthoShape& s, const OrthoParts& o, hip
 // steps as 2 + 3, against 64 bits: 2.2e-6 to 4e-5 for spectra from flat to 1e-6, as the plain form's 2.4e-6 to 6e-5; five steps without X: 8e-5 to 3e-4.)
 int phases(int steps) { return (steps + 2) / 3; }
 int first_phase(int steps) { return steps - 3 * (phases(steps) - 1); }
-// multiply-adds, halves of symmetric products alone; a tenth less has to be saved at least
+// multiply-adds, halves of symmetric products alone; a tenth less has to be saved at least.  Where a phase is one launch (jz_ortho_chain.h) there are fewer of those too.
 bool short_side(int steps, int64_t m, int64_t n) {
+  if (m <= CHAIN_SIDE) return true;
   const double p = phases(steps), k = steps, r = (double)n / (double)m;
   return p * 3 * r + 4 * k - 3 * p < 0.9 * k * (3 * r + 1);
 }
@@ -403,18 +412,24 @@ int ortho_steps(const jz_ortho_desc* d, const OrthoShape& s, const OrthoLayout& 
     steps = !L.short_side ? 1 : done == 0 ? first_phase(d->steps) : 3;
     rc = symmetric(x, x, A, 1.f / SCALE);
     float small = 1.f;  // P in the workspace is SCALE small P
-    for (int i = 0; i < steps && rc == JZ_OK; ++i) {
-      const Parts to = i == 0 && steps > 1 ? P : B;
-      rc = ortho_product(A, A, true, s.count, skip, OrthoPoly{A, to, d->a, d->b, d->c}, st);
-      if (rc == JZ_OK && i + 1 < steps) {
-        rc = symmetric(to, A, C, 1.f / SCALE);
-        if (rc == JZ_OK) rc = symmetric(C, to, A1, 1.f / SCALE);
-        std::swap(A, A1);
-      }
-      if (rc == JZ_OK && i > 0) {
-        rc = symmetric(B, P, P1, shrink / SCALE);
-        small *= shrink;
-        std::swap(P, P1);
+    if (s.mp <= CHAIN_SIDE) {
+      for (int i = 1; i < steps; ++i) small *= shrink;
+      if (rc == JZ_OK) rc = ortho_chain_launch({A, {steps > 1 ? P : B, P1}, steps, d->a, d->b, d->c, shrink, skip}, s.count, st);
+      if ((steps - 1) & 1) std::swap(P, P1);
+    } else {
+      for (int i = 0; i < steps && rc == JZ_OK; ++i) {
+        const Parts to = i == 0 && steps > 1 ? P : B;
+        rc = ortho_product(A, A, true, s.count, skip, OrthoPoly{A, to, d->a, d->b, d->c}, st);
+        if (rc == JZ_OK && i + 1 < steps) {
+          rc = symmetric(to, A, C, 1.f / SCALE);
+          if (rc == JZ_OK) rc = symmetric(C, to, A1, 1.f / SCALE);
+          std::swap(A, A1);
+        }
+        if (rc == JZ_OK && i > 0) {
+          rc = symmetric(B, P, P1, shrink / SCALE);
+          small *= shrink;
+          std::swap(P, P1);
+        }
       }
     }
     if (rc != JZ_OK) return rc;
