@@ -73,31 +73,56 @@ struct OrthoValue {
     *v = a.mu * load8(a.momentum + i, left) + g;
     return a.nesterov ? g + a.mu * *v : *v;
   }
-  // a gradient that is not finite, before any scale
-  __device__ __forceinline__ bool bad(int64_t i, int left) const {
-    const f32x8 x = widen8<T>(load8(static_cast<const T*>(a.x) + i, left));
-    bool r = false;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r |= !(fabsf(x[e]) < INFINITY);
+  // the squares of eight, NaN where a gradient is not finite; loads first, then what is made of them
+  struct Raw {
+    typename Vec8<T>::V x;
+    f32x8 m;
+  };
+  __device__ __forceinline__ Raw ask(int64_t i) const {
+    Raw r;
+    r.x = load8(static_cast<const T*>(a.x) + i);
+    if constexpr (MUON) r.m = load8(a.momentum + i);
     return r;
+  }
+  __device__ __forceinline__ double squares(const Raw& r) const {
+    const f32x8 x = widen8<T>(r.x);
+    double s = 0.;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float u = x[e];
+      if constexpr (MUON) {
+        const float g = x[e] * inv_s, v = a.mu * r.m[e] + g;
+        u = a.nesterov ? g + a.mu * v : v;
+      }
+      s = fma((double)u, (double)u, s);
+      if (MUON && !(fabsf(x[e]) < INFINITY)) s = NAN;
+    }
+    return s;
   }
 };
 
 // Partial sums of squares, in FP64; NaN where a gradient is not finite.
 template <class T, bool MUON>
 __global__ __launch_bounds__(256) void ortho_sumsq(OrthoIn a) {
+  constexpr int U = 4;  // groups of eight on their way at a time
   __shared__ double lds[4];
   const OrthoValue<T, MUON> in(a);
-  const int64_t n = a.rows * a.cols, base = (int64_t)blockIdx.y * a.stride;
+  const int64_t n = a.rows * a.cols, base = (int64_t)blockIdx.y * a.stride, step = (int64_t)a.parts * 2048;
   double s = 0.;
-#pragma unroll 2
-  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += (int64_t)a.parts * 2048) {
-    const int left = n - i < 8 ? (int)(n - i) : 8;
-    f32x8 v;
-    const f32x8 u = in.get(base + i, left, &v);
+  int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  for (; i + (U - 1) * step + 8 <= n; i += U * step) {
+    typename OrthoValue<T, MUON>::Raw r[U];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s = fma((double)u[e], (double)u[e], s);
-    if (MUON && in.bad(base + i, left)) s = NAN;
+    for (int u = 0; u < U; ++u) r[u] = in.ask(base + i + u * step);
+#pragma unroll
+    for (int u = 0; u < U; ++u) s += in.squares(r[u]);
+  }
+  for (; i < n; i += step) {
+    const int left = n - i < 8 ? (int)(n - i) : 8;
+    typename OrthoValue<T, MUON>::Raw r = {};
+    r.x = load8(static_cast<const T*>(a.x) + base + i, left);
+    if (MUON) r.m = load8(a.momentum + base + i, left);
+    s += in.squares(r);
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
@@ -188,7 +213,8 @@ __device__ __forceinline__ void store_rows(const S& s, const Parts& to, int64_t 
   char* const p = to.row(of, m0);
   if (n0 + c >= to.cols) return;
 #pragma unroll
-  for (int row = lane / PER; row < 32; row += EACH) {
+  for (int t = 0; t < 32 / EACH; ++t) {
+    const int row = lane / PER + t * EACH;
     float v[8];
     s.row8(row, c, v);
 #pragma unroll
@@ -202,7 +228,8 @@ __device__ __forceinline__ void store_cols(const S& s, const Parts& to, int64_t 
   char* const p = to.row(of, n0);
   if (m0 + r >= to.cols) return;
 #pragma unroll
-  for (int col = lane / 4; col < S::COLS; col += 16) {
+  for (int t = 0; t < S::COLS / 16; ++t) {
+    const int col = lane / 4 + t * 16;
     float v[8];
     s.col8(r, col, v);
 #pragma unroll
@@ -252,67 +279,68 @@ struct OrthoApply {  // X <- B X
     store_cols(s, xt, w.of, m0, n0, lane, factor);
   }
 };
-template <class O>
-struct OrthoResult {  // the last B X, rounded once; transposed back where TALL was transposed
-  O* y;
+// The last B X: eight elements at a time to where they are stored, transposed back where TALL was transposed.
+template <class Sink>
+struct OrthoResult {
+  Sink sink;
   int64_t m, n, stride;
   bool tall;
   float factor;
   template <class S>
   __device__ __forceinline__ void strip(const S& s, const MmTile& w, int64_t m0, int64_t n0, int lane) const {
-    constexpr int PER = S::COLS / 8;
-    O* const to = y + w.of * stride;
+    constexpr int PER = S::COLS / 8, EACH = 64 / PER;
     float v[8];
     f32x8 f;
     if (!tall) {
-#pragma unroll 1
-      for (int i = lane; i < 32 * PER; i += 64) {
-        const int row = i / PER, c = i % PER * 8;
-        if (m0 + row >= m || n0 + c >= n) continue;
+      const int c = lane % PER * 8, left = n - n0 - c < 8 ? (int)(n - n0 - c) : 8;
+      if (left <= 0) return;
+#pragma unroll 2
+      for (int t = 0; t < 32 / EACH; ++t) {
+        const int row = lane / PER + t * EACH;
         s.row8(row, c, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = v[e] * factor;
-        store8(to + (m0 + row) * n + n0 + c, narrow8<O>(f), n - n0 - c < 8 ? (int)(n - n0 - c) : 8);
+        if (m0 + row < m) sink.put(w.of * stride + (m0 + row) * n + n0 + c, f, left);
       }
     } else {
-#pragma unroll 1
-      for (int i = lane; i < S::COLS * 4; i += 64) {
-        const int col = i / 4, r = i % 4 * 8;
-        if (n0 + col >= n || m0 + r >= m) continue;
+      const int r = lane % 4 * 8, left = m - m0 - r < 8 ? (int)(m - m0 - r) : 8;
+      if (left <= 0) return;
+#pragma unroll 2
+      for (int t = 0; t < S::COLS / 16; ++t) {
+        const int col = lane / 4 + t * 16;
         s.col8(r, col, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = v[e] * factor;
-        store8(to + (n0 + col) * m + m0 + r, narrow8<O>(f), m - m0 - r < 8 ? (int)(m - m0 - r) : 8);
+        if (n0 + col < n) sink.put(w.of * stride + (n0 + col) * m + m0 + r, f, left);
       }
     }
   }
 };
+// The result itself, rounded once.  A BF16 result's last product takes operands rounded to FP16: their errors, 2^-12 each, are an eighth of the result's own, and the product a third
+// of the work.  (FP16 results would be 1.7 times as far off.)
+template <class O>
+struct OrthoStore {
+  typedef typename std::conditional<std::is_same<O, __bf16>::value, ElemHigh, ElemSplit>::type E;
+  O* y;
+  __device__ __forceinline__ void put(int64_t at, f32x8 v, int left) const { store8(y + at, narrow8<O>(v), left); }
+};
+// The update's master weights and their copy.
+template <class T>
+struct MuonStore {
+  typedef ElemSplit E;
+  float* w;
+  T* w16;
+  float lr, update_scale, wd;
+  __device__ __forceinline__ void put(int64_t at, f32x8 o, int left) const {
+    const f32x8 v = load8(w + at, left);
+    f32x8 r = v - lr * (update_scale * o + wd * v);
+    lds_pin(r);  // rounded to FP32 here: the copy is that value's, and not the 16-bit rounding of a fused multiply-add
+    store8(w + at, r, left);
+    store8(w16 + at, narrow8<T>(r), left);
+  }
+};
 
 #include "jz_ortho_chain.h"
-
-// ---- the update's last pass -------------------------------------------------------------------------------------------------------
-struct MuonApply {
-  const float* o;     // [count][rows cols], dense
-  float* w;
-  void* w16;
-  int64_t each, stride, count;
-  float lr, update_scale, wd;
-  const int* found_inf;
-};
-template <class T>
-__global__ __launch_bounds__(256) void muon_apply(MuonApply a) {
-  if (*a.found_inf) return;
-  const int64_t per = (a.each + 7) / 8;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.count * per; i += (int64_t)gridDim.x * 256) {
-    const int64_t b = i / per, k = (i - b * per) * 8, at = b * a.stride + k;
-    const int left = a.each - k < 8 ? (int)(a.each - k) : 8;
-    const f32x8 w = load8(a.w + at, left), o = load8(a.o + b * a.each + k, left);
-    f32x8 r = w - a.lr * (a.update_scale * o + a.wd * w);
-    lds_pin(r);  // rounded to FP32 here: the copy is that value's, and not the 16-bit rounding of a fused multiply-add
-    store8(a.w + at, r, left);
-    store8(static_cast<T*>(a.w16) + at, narrow8<T>(r), left);
-  }
-}
 
 // ---- host -------------------------------------------------------------------------------------------------------------------------
 struct OrthoShape {
@@ -339,7 +367,7 @@ struct OrthoLayout {
   bool short_side;
   OrthoLayout(const OrthoShape& s, int steps);
 };
-template <class Epi>
+template <class E = ElemSplit, class Epi>
 int ortho_product(const Parts& p, const Parts& q, bool symmetric, int64_t count, const int* skip, const Epi& e, hipStream_t st) {
   MmArgs a = {};
   a.a = {{p.p, p.p}, p.rows, p.cols * 4, p.rows * p.cols * 4};
@@ -347,14 +375,26 @@ int ortho_product(const Parts& p, const Parts& q, bool symmetric, int64_t count,
   a.row_bytes = p.cols * 4;
   a.symmetric = symmetric;
   a.skip = skip;
-  auto tiles = [&](int64_t t) {
-    const int64_t m = (p.rows + t - 1) / t, n = (q.rows + t - 1) / t;
-    return (symmetric ? m * (m + 1) / 2 : m * n) * count;
-  };
-  if (tiles(256) >= 200) return mm_launch<ElemSplit, Epi, 256, false>(a, e, p.rows, q.rows, count, st);
-  if (tiles(128) >= 200) return mm_launch<ElemSplit, Epi, 128, false>(a, e, p.rows, q.rows, count, st);
-  if (tiles(32) <= 512 && a.row_bytes <= 4096) return mm_launch<ElemSplit, Epi, 32, false>(a, e, p.rows, q.rows, count, st);
-  return mm_launch<ElemSplit, Epi, 64, false>(a, e, p.rows, q.rows, count, st);
+  // The tile with the least expected time: what comes before and after the sum, and for each tile of it (32 k) the longer of one workgroup's way through it and what the chip takes for all.
+  // Microseconds, fitted to 17 sizes from 192 to 2816 squared (1 to 16 of them), each with every tile; FP16 inputs, the model is within 20 % of all but two.
+  const struct {
+    int64_t tile;
+    double fix, one, all;
+  } kinds[] = {{256, 10., 1.5, 9.4e-3}, {128, 6., .68, 3.1e-3}, {64, 4.5, .34, 1.2e-3}, {32, 4., .2, 1.3e-3}};
+  int64_t best = 0;
+  double least = INFINITY;
+  for (const auto& k : kinds) {
+    const int64_t m = (p.rows + k.tile - 1) / k.tile, n = (q.rows + k.tile - 1) / k.tile;
+    const double tiles = (double)(symmetric ? m * (m + 1) / 2 : m * n) * (double)count, t = k.fix + (double)p.cols / 32. * std::max(k.one, tiles * k.all);
+    if (t < least) {
+      least = t;
+      best = k.tile;
+    }
+  }
+  if (best == 256) return mm_launch<E, Epi, 256, false>(a, e, p.rows, q.rows, count, st);
+  if (best == 128) return mm_launch<E, Epi, 128, false>(a, e, p.rows, q.rows, count, st);
+  if (best == 64) return mm_launch<E, Epi, 64, false>(a, e, p.rows, q.rows, count, st);
+  return mm_launch<E, Epi, 32, false>(a, e, p.rows, q.rows, count, st);
 }
 
 template <class T, bool MUON>
@@ -398,8 +438,8 @@ OrthoLayout::OrthoLayout(const OrthoShape& s, int steps) : short_side(::short_si
   total = o;
 }
 
-template <class O>
-int ortho_steps(const jz_ortho_desc* d, const OrthoShape& s, const OrthoLayout& L, char* b, O* y, int64_t y_stride, const int* skip, hipStream_t st) {
+template <class Sink>
+int ortho_steps(const jz_ortho_desc* d, const OrthoShape& s, const OrthoLayout& L, char* b, const Sink& sink, const int* skip, hipStream_t st) {
   auto square = [&](size_t at) { return Parts{b + at, s.mp, s.mp}; };
   const Parts x = {b + L.x, s.mp, s.np};
   Parts A = square(L.a), A1 = square(L.more[0]), C = square(L.more[1]), P = square(L.more[2]), P1 = square(L.more[3]);
@@ -437,7 +477,7 @@ int ortho_steps(const jz_ortho_desc* d, const OrthoShape& s, const OrthoLayout& 
     ++turn;
     const Parts& by = steps > 1 ? P : B;
     if (done + steps < d->steps) rc = ortho_product(by, xt, false, s.count, skip, OrthoApply{x, next, 1.f / (SCALE * small)}, st);
-    else rc = ortho_product(by, xt, false, s.count, skip, OrthoResult<O>{y, s.m, s.n, y_stride, s.tall, 1.f / (SCALE * SCALE * small)}, st);
+    else rc = ortho_product<typename Sink::E>(by, xt, false, s.count, skip, OrthoResult<Sink>{sink, s.m, s.n, s.stride, s.tall, 1.f / (SCALE * SCALE * small)}, st);
     if (rc != JZ_OK) return rc;
   }
   return JZ_OK;
@@ -486,9 +526,9 @@ extern "C" int jz_orthogonalize(const jz_ortho_desc* d, const void* x, void* y, 
   const OrthoParts o = begin_parts(s, L, b);
   rc = d->dtype == JZ_F32 ? ortho_begin<float, false>(in, s, o, st) : d->dtype == JZ_F16 ? ortho_begin<_Float16, false>(in, s, o, st) : ortho_begin<__bf16, false>(in, s, o, st);
   if (rc != JZ_OK) return rc;
-  if (d->out_dtype == JZ_F32) return ortho_steps(d, s, L, b, static_cast<float*>(y), s.stride, nullptr, st);
-  if (d->out_dtype == JZ_F16) return ortho_steps(d, s, L, b, static_cast<_Float16*>(y), s.stride, nullptr, st);
-  return ortho_steps(d, s, L, b, static_cast<__bf16*>(y), s.stride, nullptr, st);
+  if (d->out_dtype == JZ_F32) return ortho_steps(d, s, L, b, OrthoStore<float>{static_cast<float*>(y)}, nullptr, st);
+  if (d->out_dtype == JZ_F16) return ortho_steps(d, s, L, b, OrthoStore<_Float16>{static_cast<_Float16*>(y)}, nullptr, st);
+  return ortho_steps(d, s, L, b, OrthoStore<__bf16>{static_cast<__bf16*>(y)}, nullptr, st);
 }
 
 namespace {
@@ -559,12 +599,6 @@ extern "C" int jz_muon_mp_update(const jz_ortho_desc* d, const jz_muon_hparams* 
   const OrthoParts o = begin_parts(s, L, b);
   rc = d->dtype == JZ_F16 ? ortho_begin<_Float16, true>(in, s, o, st) : ortho_begin<__bf16, true>(in, s, o, st);
   if (rc != JZ_OK) return rc;
-  float* const result = reinterpret_cast<float*>(b + L.x);  // the last product reads B and the other order of X
-  rc = ortho_steps(d, s, L, b, result, s.rows * s.cols, found_inf_dev, st);
-  if (rc != JZ_OK) return rc;
-  const MuonApply a = {result, master_w, weight16, s.rows * s.cols, s.stride, s.count, hp->lr, hp->update_scale, hp->weight_decay, found_inf_dev};
-  const unsigned grid = (unsigned)std::min<int64_t>(((a.each + 7) / 8 * a.count + 255) / 256, 1 << 16);
-  if (d->dtype == JZ_F16) muon_apply<_Float16><<<grid, 256, 0, st>>>(a);
-  else muon_apply<__bf16><<<grid, 256, 0, st>>>(a);
-  return jz::launch_status();
+  if (d->dtype == JZ_F16) return ortho_steps(d, s, L, b, MuonStore<_Float16>{master_w, static_cast<_Float16*>(weight16), hp->lr, hp->update_scale, hp->weight_decay}, found_inf_dev, st);
+  return ortho_steps(d, s, L, b, MuonStore<__bf16>{master_w, static_cast<__bf16*>(weight16), hp->lr, hp->update_scale, hp->weight_decay}, found_inf_dev, st);
 }
