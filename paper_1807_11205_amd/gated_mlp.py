@@ -25,6 +25,8 @@ EPS = 1e-5
 
 
 class GatedMLP:
+    vocab, fc, i8 = 0, "w_fc", None     # without a vocabulary, a classifier of its own, no codes
+
     def __init__(self, rows: int, width: int, hidden: int, classes: int, blocks: int, scale: float = 0.5, max_norm: float = 1.0, seed: int = 1,
                  initial_loss_scale: float = 1024.0, hparams: Optional[dict] = None, policy: Optional[dict] = None, device: str = "cuda:0", vocab: int = 0,
                  embed_scale: float = 1.0, tied: bool = False, optimizer: str = "lars", muon: Optional[dict] = None):
