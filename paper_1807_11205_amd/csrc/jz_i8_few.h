@@ -15,7 +15,7 @@ struct FewArgs {
   int64_t M, N, K, pitch, ldx, ldy;
   int act;
 };
-constexpr int FEW_CODES = 16384;  // bytes of codes that a workgroup makes itself
+constexpr int FEW_CODES = 8192;  // bytes of codes that a workgroup makes itself
 
 template <class X, class Y, bool GLU, int TT, int WAVES, int CH, bool QUANTIZE>
 __global__ __launch_bounds__(64 * WAVES) void i8_few(FewArgs a) {

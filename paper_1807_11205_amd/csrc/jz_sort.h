@@ -129,37 +129,45 @@ __global__ __launch_bounds__(1024) void sort_runs(SortArgs a) {
   }
 }
 
-// Up to 16 runs into one list: a key's place is its place in its run and the number of keys before it in each other run, by bisection; equal keys of earlier runs come first.
+// Up to RUNS runs into one list: a key's place is its place in its run and the number of keys before it in each other run, by bisection; equal keys of earlier runs come first.
+template <int RUNS>
 __global__ __launch_bounds__(256) void sort_merge(SortArgs a) {
-  __shared__ __attribute__((aligned(16))) unsigned keys[SORT_SMALL];
+  __shared__ __attribute__((aligned(16))) unsigned keys[RUNS * 1024];
   const int runs = (int)a.tiles, t = threadIdx.x;
   const int64_t i = (int64_t)blockIdx.x * 256 + t;
   const unsigned mine = i < a.n ? a.keys_in[i] : ~0u, p = i < a.n ? a.pos_in[i] : 0;
-  for (int j = t * 4; j < runs * 1024; j += 1024) {
-    uint4 v = {~0u, ~0u, ~0u, ~0u};
-    if (j + 3 < a.n) v = *reinterpret_cast<const uint4*>(a.keys_in + j);
-    else {
-      if (j < a.n) v.x = a.keys_in[j];
-      if (j + 1 < a.n) v.y = a.keys_in[j + 1];
-      if (j + 2 < a.n) v.z = a.keys_in[j + 2];
-    }
-    *reinterpret_cast<uint4*>(keys + j) = v;
+  const int n = (int)a.n, end = (n - 1) & ~3;  // the last four there are: a list's room ends on 256 bytes
+  uint4 v[RUNS];
+#pragma unroll
+  for (int j = 0; j < RUNS; ++j) {  // asked for together
+    const int at = j * 1024 + t * 4;
+    v[j] = *reinterpret_cast<const uint4*>(a.keys_in + (at < end ? at : end));
+  }
+#pragma unroll
+  for (int j = 0; j < RUNS; ++j) {
+    const int at = j * 1024 + t * 4;
+    if (at >= n) v[j].x = ~0u;
+    if (at + 1 >= n) v[j].y = ~0u;
+    if (at + 2 >= n) v[j].z = ~0u;
+    if (at + 3 >= n) v[j].w = ~0u;
+    *reinterpret_cast<uint4*>(keys + at) = v[j];
   }
   __syncthreads();
   if (i >= a.n) return;
   const int run = (int)(i >> 10);
   unsigned to = (unsigned)(i & 1023);
-  for (int q0 = 0; q0 < runs; q0 += 4) {  // four bisections at a time
-    unsigned at[4] = {0, 0, 0, 0};
+  constexpr int Q = RUNS < 8 ? RUNS : 8;  // bisections at a time
+  for (int q0 = 0; q0 < runs; q0 += Q) {
+    unsigned at[Q] = {};
 #pragma unroll
     for (int s = 512; s > 0; s >>= 1)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < Q; ++q) {
         const int of = q0 + q < runs ? q0 + q : 0;
         if (keys[of * 1024 + at[q] + s - 1] < mine + (of < run ? 1u : 0u)) at[q] += s;
       }
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < Q; ++q) {
       const int of = q0 + q;
       if (of >= runs || of == run) continue;
       if (keys[of * 1024 + at[q]] < mine + (of < run ? 1u : 0u)) ++at[q];
@@ -284,7 +292,9 @@ inline int sort_tokens(const SortLayout& L, const int* ids, int64_t n, int vocab
       a.pos_in = a.pos;
       a.keys = list(L.keys[1]);
       a.pos = list(L.pos[1]);
-      sort_merge<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(a);
+      const unsigned grid = (unsigned)((n + 255) / 256);
+      if (runs <= 4) sort_merge<4><<<grid, 256, 0, st>>>(a);
+      else sort_merge<16><<<grid, 256, 0, st>>>(a);
     }
     *keys = a.keys;
     *pos = a.pos;
