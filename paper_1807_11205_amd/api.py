@@ -934,7 +934,7 @@ def jz_conv2d_bwd_data_block_end_bwd(desc, dy16, w16, dyb16, bn_x16, y_out16, ga
 # ---------------------------------------------------------------------------------------------
 def _invoke(name: str, words, stream):
     """An entry point called with integers and addresses (None: NULL) by the binding's native part."""
-    st = _host.invoke(_address(name), tuple(w or 0 for w in words), _stream(stream))
+    st = _host.invoke(_address(name), words, _stream(stream))
     if st:      # JZ_OK is 0
         raise JzError(st, name)
 
@@ -1114,9 +1114,13 @@ _current_device = _get_device if _get_device is not None else torch.cuda.current
 
 def _here(*tensors):
     """Launches go to the current device: tensors that lie on another are refused."""
+    here = None
     for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != _current_device():
-            raise ValueError("a tensor is on device %d, the current one is %d" % (t.get_device(), _current_device()))
+        if t is not None and t.is_cuda:
+            if here is None:
+                here = _current_device()
+            if t.get_device() != here:
+                raise ValueError("a tensor is on device %d, the current one is %d" % (t.get_device(), here))
 
 
 def embed_desc(tokens: int, vocab: int, channels: int, dtype: int = JZ_F16, out_dtype: Optional[int] = None, scale: float = 1.0, out_stride: int = 0) -> jz_embed_desc:

@@ -111,7 +111,7 @@ PyObject* conv(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(status);
 }
 
-// invoke(function, (integers and addresses ...), stream) -> status: an entry point without floating-point arguments, at most 24 before the stream
+// invoke(function, (integers and addresses ...), stream) -> status: an entry point without floating-point arguments, at most 24 before the stream; None is NULL
 template <size_t... I>
 int spread(uint64_t fn, const uint64_t* v, std::index_sequence<I...>) {
   return reinterpret_cast<int (*)(decltype((void)I, uint64_t())...)>(fn)(v[I]...);
@@ -129,7 +129,10 @@ PyObject* invoke(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   const Py_ssize_t m = PyTuple_GET_SIZE(a[1]);
   uint64_t v[MOST + 1];
-  for (Py_ssize_t i = 0; i < m; ++i) v[i] = PyLong_AsUnsignedLongLongMask(PyTuple_GET_ITEM(a[1], i));
+  for (Py_ssize_t i = 0; i < m; ++i) {
+    PyObject* const o = PyTuple_GET_ITEM(a[1], i);
+    v[i] = o == Py_None ? 0 : PyLong_AsUnsignedLongLongMask(o);
+  }
   v[m] = PyLong_AsUnsignedLongLongMask(a[2]);
   const uint64_t fn = PyLong_AsUnsignedLongLong(a[0]);
   if (PyErr_Occurred()) return nullptr;
