@@ -8,6 +8,8 @@
 //     ElemSplit  32 k of an FP32 value v as hi = FP16(v) (chunks 0-3) and lo = FP16(v - hi) (chunks 4-7), 22 bits together.  A product is hi hi + hi lo + lo hi: three
 //                instructions for each two reads of an operand, so that the matrix instructions and not LDS are what the loop waits for
 //     ElemHigh   the same operands, of which only the high parts are loaded: products of FP16 numbers
+// Bound, 256 x 256: the matrix instructions.  16384 rows 4096 -> 12288 of ElemI8 in 712 us, 2.3 POP/s (the library's product of 8192^3 2.1); ElemSplit, 4096 x 4096 times 4096 x 12288, 914 us,
+// 1.35 PFLOP/s of matrix instructions (FP16 library 1.36), which are busy 68 % of 1.6 GHz; 16 products of 1024^3 that fill 160 of the compute units 82 us, 20 of them results on their way.
 // Sums are in exchanged order (B's rows first): register 4 j + i of a lane holds row lane % 32, column 8 j + 4 (lane / 32) + i.
 #pragma once
 
@@ -47,6 +49,7 @@ struct MmArgs {
   unsigned workgroups, first;
   bool symmetric;          // only tiles on and below the diagonal
   const int* skip;         // or NULL: nothing is done where it is not 0
+  int splits;              // mm_tiny: workgroups that share a tile's sum, each with results of its own (w.of counts matrices times splits)
 };
 
 // Where a workgroup's tile lies.  Consecutive workgroups land on different XCDs, each with an L2 of its own, so every XCD gets a run of tiles; within it four rows of
@@ -269,7 +272,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void mm_tiles(MmArgs a, Epi epi)
 }
 
 // Few tiles: 64 x 64 by four wavefronts of 32 x 32.  What such a launch waits for is the way from memory, so four tiles of operands are on it at a time, in registers; two are in LDS.
-// (With two stages of LDS-direct loads, which wait for each other, 128 x 128 x 512 of ElemSplit took MM_SMALL_BEFORE us.)
+// (X X^T of 128 x 512, ElemSplit: 10.6 us with two stages of LDS-direct loads, which wait for each other, 8.5 so.)
 template <class E, class Epi>
 __global__ __launch_bounds__(256, 2) void mm_small(MmArgs a, Epi epi) {
   constexpr int DEPTH = 4, EACH = 2;
@@ -339,7 +342,8 @@ __global__ __launch_bounds__(256, 2) void mm_small(MmArgs a, Epi epi) {
 }
 
 // Fewer still, and short sums: 32 x 32 by eight wavefronts that share k, 64 bytes of it at a time each, straight into the registers that the matrix instructions take; four such pieces are on
-// their way at a time, and nobody waits for another but for the sums, which meet in LDS and are added in the wavefronts' order.
+// their way at a time, and nobody waits for another but for the sums, which meet in LDS and are added in the wavefronts' order.  X X^T of 128 x 512 7.4 us, 352 x 352 x 352 7 (mm_small 8.4).
+// Four of them are what any launch takes here that reads what the launch before it wrote.
 template <class E, class Epi>
 __global__ __launch_bounds__(512, 2) void mm_tiny(MmArgs a, Epi epi) {
   constexpr int WAVES = 8, U = 4;
@@ -351,24 +355,25 @@ __global__ __launch_bounds__(512, 2) void mm_tiny(MmArgs a, Epi epi) {
   const MmTile w = mm_tile(a);
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int64_t m0 = (int64_t)w.m * 32, n0 = (int64_t)w.n * 32;
+  const unsigned matrix = w.of / a.splits, part = w.of - matrix * a.splits;
   auto source = [&](const MmOperand& o, int64_t row0) {
     const int64_t span = (o.rows - row0 - 1) * o.pitch + a.row_bytes;
-    return __builtin_amdgcn_make_buffer_rsrc((void*)(static_cast<const char*>(o.p[0]) + w.of * o.of + row0 * o.pitch), 0, (int)(span < 0x7ffffff0 ? span : 0x7ffffff0), 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(static_cast<const char*>(o.p[0]) + matrix * o.of + row0 * o.pitch), 0, (int)(span < 0x7ffffff0 ? span : 0x7ffffff0), 0x00020000);
   };
   const auto from_a = source(a.a, m0), from_b = source(a.b, n0);
   const unsigned row_a = (unsigned)((lane & 31) * a.a.pitch), row_b = (unsigned)((lane & 31) * a.b.pitch);
-  const int units = (int)((a.row_bytes + 63) / 64);
+  const int all = (int)((a.row_bytes + 63) / 64), first = (int)((int64_t)all * part / a.splits), units = (int)((int64_t)all * (part + 1) / a.splits);
   struct Piece {
     Reg a[2], b[2];
   };
   auto get = [&](Piece& p, int u) {  // behind the end: zeros
     // ElemSplit: 16 k of high parts and, 64 bytes on, their low parts; ElemI8: 64 k
-    const unsigned j = u & 1, k0 = (unsigned)(u >> 1) * 128, h = lane >> 5;
+    const unsigned j = u & 1, k0 = (unsigned)(u >> 1) * 128, h = lane >> 5, behind = u >= units ? 0x80000000u : 0u;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       if (E::HIGH && i) break;
       const unsigned k = k0 + (E::SPLIT ? (2 * j + h) * 16 + i * 64 : (4 * j + 2 * i + h) * 16);
-      const unsigned end = k >= (unsigned)a.row_bytes ? 0x80000000u : 0u;
+      const unsigned end = k >= (unsigned)a.row_bytes ? 0x80000000u : behind;
       p.a[i] = __builtin_bit_cast(Reg, __builtin_amdgcn_raw_buffer_load_b128(from_a, (int)((row_a + k) | end), 0, 0));
       p.b[i] = __builtin_bit_cast(Reg, __builtin_amdgcn_raw_buffer_load_b128(from_b, (int)((row_b + k) | end), 0, 0));
     }
@@ -391,8 +396,8 @@ __global__ __launch_bounds__(512, 2) void mm_tiny(MmArgs a, Epi epi) {
 #pragma unroll
     for (int u = 0; u < U; ++u) get(to[u], u0 + u * WAVES);
   };
-  ask(p[0], wave);
-  for (int u0 = wave; u0 < units; u0 += 2 * U * WAVES) {
+  ask(p[0], first + wave);
+  for (int u0 = first + wave; u0 < units; u0 += 2 * U * WAVES) {
     ask(p[1], u0 + U * WAVES);
 #pragma unroll
     for (int u = 0; u < U; ++u) multiply(p[0][u]);
@@ -424,7 +429,8 @@ int mm_launch(MmArgs a, const Epi& epi, int64_t rows_m, int64_t rows_n, int64_t 
   a.tiles_m = (int)((rows_m + TILE - 1) / TILE);
   a.tiles_n = (int)((rows_n + TILE - 1) / TILE);
   a.tiles = a.symmetric ? (unsigned)a.tiles_m * (a.tiles_m + 1) / 2 : (unsigned)a.tiles_m * a.tiles_n;
-  a.workgroups = (unsigned)(a.tiles * count);
+  a.workgroups = (unsigned)(a.tiles * count) * (a.splits > 1 ? a.splits : 1);
+  if (a.splits < 1) a.splits = 1;
   constexpr unsigned most = (unsigned)(MM_LANES / THREADS - 1);
   for (a.first = 0; a.first < a.workgroups; a.first += most) {
     const unsigned grid = std::min(a.workgroups - a.first, most);

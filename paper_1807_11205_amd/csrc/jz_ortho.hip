@@ -6,6 +6,9 @@
 // grows with them; hence 22 bits an element, as two FP16 parts (jz_mm_tile.h), and FP32 sums.  Matrices are scaled by 2^11: values up to 31 are in FP16's range, and
 // the low part of an element of 2^-12, the size that a normalised 4096 x 4096 matrix has, still has its bits.  A and B are symmetric: only tiles on and below the diagonal are
 // computed, and stored twice.  X is kept in both orders, since it is an operand along both of its sides.
+//
+// Bound: the matrix instructions with large matrices (4096 x 12288, BF16: 5.8 ms, 1.0 PFLOP/s of them; 16 of 2816 x 1024, the whole update: 2.2 ms, 0.2 of it memory's around the products), with
+// small ones the launches, each of which waits for the one before (128 x 512: nine, 87 us; three of 1001 x 333: twenty, 150 us).
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -101,7 +104,7 @@ struct OrthoValue {
   }
 };
 
-// Partial sums of squares, in FP64; NaN where a gradient is not finite.
+// Partial sums of squares, in FP64; NaN where a gradient is not finite.  Memory: 16 x 2816 x 1024 gradients and momenta 68 us (4.1 TB/s).
 template <class T, bool MUON>
 __global__ __launch_bounds__(256) void ortho_sumsq(OrthoIn a) {
   constexpr int U = 4;  // groups of eight on their way at a time
@@ -152,7 +155,7 @@ __global__ __launch_bounds__(1024) void ortho_factors(OrthoIn a) {
   if (MUON && threadIdx.x == 0) *a.found_inf = bad;
 }
 
-// The matrix in parts, in both orders: r [rows][cols], c [cols][rows].  A tile of 64 x 64 a workgroup.
+// The matrix in parts, in both orders: r [rows][cols], c [cols][rows].  A tile of 64 x 64 a workgroup.  Memory: as above 144 us for 830 MB.
 struct OrthoParts {
   char *r, *c;
   int64_t rp, cp;  // padded sides
@@ -162,7 +165,8 @@ __global__ __launch_bounds__(256) void ortho_parts(OrthoIn a, OrthoParts o) {
   __shared__ float tile[64][65];
   if (MUON && *a.found_inf) return;
   const OrthoValue<T, MUON> in(a);
-  const int64_t across = (o.cp + 63) / 64, down = (o.rp + 63) / 64, of = blockIdx.x / (across * down), t = blockIdx.x - of * across * down;
+  const int64_t across = (o.cp + 63) / 64, down = (o.rp + 63) / 64;
+  const int64_t id = gridDim.x - 1 - blockIdx.x, of = id / (across * down), t = id - of * across * down;  // what was squared last is still in the last-level cache
   const int64_t r0 = t / across * 64, c0 = t % across * 64, base = of * a.stride;
   const double inv = a.inv[of];
   const int row = threadIdx.x / 8, col = threadIdx.x % 8 * 8;
@@ -244,6 +248,35 @@ struct OrthoSymmetric {  // a product that is its own transpose
   __device__ __forceinline__ void strip(const S& s, const MmTile& w, int64_t m0, int64_t n0, int lane) const {
     store_rows(s, a, w.of, m0, n0, lane, factor);
     if (w.m != w.n) store_cols(s, a, w.of, m0, n0, lane, factor);
+  }
+};
+struct OrthoSums {  // sums as they are, a tile on and one below the diagonal
+  float* p;
+  int64_t side;
+  float factor;
+  template <class S>
+  __device__ __forceinline__ void strip(const S& s, const MmTile& w, int64_t m0, int64_t n0, int lane) const {
+    constexpr int PER = S::COLS / 8, EACH = 64 / PER;
+    float* const to = p + w.of * side * side;
+    float v[8];
+    f32x8 f;
+#pragma unroll
+    for (int t = 0; t < 32 / EACH; ++t) {
+      const int row = lane / PER + t * EACH, c = lane % PER * 8;
+      s.row8(row, c, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = v[e] * factor;
+      if (m0 + row < side && n0 + c < side) store8(to + (m0 + row) * side + n0 + c, f);
+    }
+    if (w.m == w.n) return;
+#pragma unroll
+    for (int t = 0; t < S::COLS / 16; ++t) {
+      const int col = lane / 4 + t * 16, r = lane % 4 * 8;
+      s.col8(r, col, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = v[e] * factor;
+      if (n0 + col < side && m0 + r < side) store8(to + (n0 + col) * side + m0 + r, f);
+    }
   }
 };
 struct OrthoPoly {  // B = ca I + cb A + cc A^2
@@ -397,6 +430,23 @@ int ortho_product(const Parts& p, const Parts& q, bool symmetric, int64_t count,
   return mm_launch<E, Epi, 32, false>(a, e, p.rows, q.rows, count, st);
 }
 
+// X X^T of a narrow X: as many workgroups to a tile as keep eight tiles of the sum (256 k) each and do not fill the chip.  Two phases of
+// 64 x 4096: 109 us with one, 62 so; 16 of 2693 x 80: 128 and 109.
+int gram_splits(const OrthoShape& s) {
+  const int64_t tiles = s.mp / 32 * (s.mp / 32 + 1) / 2 * std::max<int64_t>(1, s.count);
+  return (int)std::max<int64_t>(1, std::min(std::min<int64_t>(16, s.np / 256), 256 / tiles));
+}
+int ortho_gram_sums(const Parts& x, int64_t count, int splits, const int* skip, const OrthoSums& e, hipStream_t st) {
+  if (splits == 1) return ortho_product(x, x, true, count, skip, e, st);
+  MmArgs a = {};
+  a.a = a.b = {{x.p, x.p}, x.rows, x.cols * 4, x.rows * x.cols * 4};
+  a.row_bytes = x.cols * 4;
+  a.symmetric = true;
+  a.skip = skip;
+  a.splits = splits;
+  return mm_launch<ElemSplit, OrthoSums, 32, false>(a, e, x.rows, x.rows, count, st);
+}
+
 template <class T, bool MUON>
 int ortho_begin(const OrthoIn& in, const OrthoShape& s, const OrthoParts& o, hipStream_t st) {
   ortho_sumsq<T, MUON><<<dim3((unsigned)in.parts, (unsigned)s.count), 256, 0, st>>>(in);
@@ -432,9 +482,9 @@ OrthoLayout::OrthoLayout(const OrthoShape& s, int steps) : short_side(::short_si
   x = room(wide);
   xt[0] = room(wide);
   xt[1] = room(steps > 1 ? wide : 0);
-  a = room(square);
+  a = room(s.mp <= CHAIN_SIDE ? square * gram_splits(s) : square);
   b = room(square);
-  for (size_t& m : more) m = room(short_side ? square : 0);
+  for (int i = 0; i < 4; ++i) more[i] = room(short_side && (i > 1 || s.mp > CHAIN_SIDE) ? square : 0);  // narrow ones have A, A B in LDS
   total = o;
 }
 
@@ -450,13 +500,16 @@ int ortho_steps(const jz_ortho_desc* d, const OrthoShape& s, const OrthoLayout& 
   int turn = 0, rc = JZ_OK;
   for (int done = 0, steps; done < d->steps; done += steps) {
     steps = !L.short_side ? 1 : done == 0 ? first_phase(d->steps) : 3;
-    rc = symmetric(x, x, A, 1.f / SCALE);
     float small = 1.f;  // P in the workspace is SCALE small P
     if (s.mp <= CHAIN_SIDE) {
       for (int i = 1; i < steps; ++i) small *= shrink;
-      if (rc == JZ_OK) rc = ortho_chain_launch({A, {steps > 1 ? P : B, P1}, steps, d->a, d->b, d->c, shrink, skip}, s.count, st);
+      float* const sums = reinterpret_cast<float*>(b + L.a);
+      const int splits = gram_splits(s);
+      rc = ortho_gram_sums(x, s.count, splits, skip, OrthoSums{sums, s.mp, 1.f / SCALE}, st);
+      if (rc == JZ_OK) rc = ortho_chain_launch({sums, {steps > 1 ? P : B, P1}, splits, steps, d->a, d->b, d->c, shrink, skip}, s.count, st);
       if ((steps - 1) & 1) std::swap(P, P1);
     } else {
+      rc = symmetric(x, x, A, 1.f / SCALE);
       for (int i = 0; i < steps && rc == JZ_OK; ++i) {
         const Parts to = i == 0 && steps > 1 ? P : B;
         rc = ortho_product(A, A, true, s.count, skip, OrthoPoly{A, to, d->a, d->b, d->c}, st);

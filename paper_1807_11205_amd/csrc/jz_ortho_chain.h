@@ -3,15 +3,17 @@
 //
 // Such a product is a microsecond's work, but as a launch of its own takes five: what the launch before wrote has to come back from memory.  Here A and B of a step stay in LDS, in parts as
 // everywhere: 128 rows of 512 bytes, 16-byte chunk c of a row at c ^ (row % 16), so that the operands' reads of 32 rows meet on no bank.  P, the third matrix, is an operand once a step
-// and lies in the workspace.  Eight wavefronts in 2 x 4, each 64 x 32 of the result; symmetric results are computed whole, since storing a tile twice would cost what its products save.
+// and lies in the workspace.  X X^T itself is a launch before, several workgroups to a tile where X is long: they leave sums in FP32.  Eight wavefronts in 2 x 4, each 64 x 32 of the result;
+// symmetric results are computed whole, since storing a tile twice would cost what its products save.
 // 128 x 128: 3.5 us a product, of which the matrix instructions and the reads of LDS, 48 each a wavefront, take 1.5 side by side, the results' way through the registers and LDS and
 // four barriers a step the rest.  (Sixteen wavefronts of 32 x 32 spill; reads placed among the products by hand change nothing.)
 #pragma once
 
 constexpr int CHAIN_SIDE = 128;
 struct ChainArgs {
-  Parts a, p[2];  // the last P: p[(steps - 1) % 2]
-  int steps;
+  const float* a;  // [matrix][splits][side][side]: A as the sums that share its product left it, in FP32
+  Parts p[2];      // the last P: p[(steps - 1) % 2]
+  int splits, steps;
   float ca, cb, cc, shrink;
   const int* skip;
 };
@@ -25,10 +27,16 @@ __global__ __launch_bounds__(512, 2) void ortho_chain(ChainArgs a) {
   const int64_t of = blockIdx.x;
   const bool busy = wm * 64 < SIDE && wn * 32 < SIDE;
   auto at = [](int row, int chunk) { return row * ROW + ((chunk ^ (row & 15)) * 16); };
-  const char* const from = a.a.row(of, 0);
-  for (int i = t; i < SIDE * SIDE / 4; i += 512) {
-    const int row = i / (SIDE / 4), c = i % (SIDE / 4);
-    *reinterpret_cast<JZ_LDS f16x8*>((JZ_LDS unsigned char*)s0 + at(row, c)) = *reinterpret_cast<const f16x8*>(from + row * (SIDE * 4) + c * 16);
+  const float* const from = a.a + of * a.splits * (SIDE * SIDE);
+  for (int i = t; i < SIDE * SIDE / 8; i += 512) {
+    const int row = i / (SIDE / 8), c = i % (SIDE / 8);
+    f32x8 v = load8(from + i * 8);
+#pragma unroll 4
+    for (int s = 1; s < a.splits; ++s) v += load8(from + s * (SIDE * SIDE) + i * 8);
+    const f16x8 hi = __builtin_convertvector(v, f16x8), lo = __builtin_convertvector(v - __builtin_convertvector(hi, f32x8), f16x8);
+    JZ_LDS unsigned char* const l = (JZ_LDS unsigned char*)s0;
+    *reinterpret_cast<JZ_LDS f16x8*>(l + at(row, c / 4 * 8 + c % 4)) = hi;
+    *reinterpret_cast<JZ_LDS f16x8*>(l + at(row, c / 4 * 8 + c % 4 + 4)) = lo;
   }
   __syncthreads();
   typedef mm_f32x16 Sum;
@@ -133,7 +141,7 @@ __global__ __launch_bounds__(512, 2) void ortho_chain(ChainArgs a) {
 
 inline int ortho_chain_launch(const ChainArgs& a, int64_t count, hipStream_t st) {
   const unsigned grid = (unsigned)count;
-  switch (a.a.rows / 32) {
+  switch (a.p[0].rows / 32) {
     case 1: ortho_chain<1><<<grid, 512, 0, st>>>(a); break;
     case 2: ortho_chain<2><<<grid, 512, 0, st>>>(a); break;
     case 3: ortho_chain<3><<<grid, 512, 0, st>>>(a); break;

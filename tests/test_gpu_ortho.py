@@ -72,6 +72,16 @@ def test_larger_tiles(jz, B, R, C):
     against(run(jz, x, torch.float32), x)
 
 
+@pytest.mark.parametrize("B,R,C", [(1, 20, 9000), (16, 2693, 80), (2, 31000, 5), (3, 100, 777), (600, 33, 70), (1, 128, 4103)])
+def test_narrow_ones(jz, B, R, C):
+    """Long sums that several workgroups share, and many short ones; in the same order every time."""
+    g = np.random.default_rng([8, B, R, C])
+    x = matrices(g, B, R, C, torch.bfloat16)
+    y = run(jz, x, torch.float32)
+    against(y, x)
+    assert torch.equal(y, run(jz, x, torch.float32))
+
+
 @pytest.mark.parametrize("steps", [1, 2, 3, 8])
 def test_steps_and_coefficients(jz, steps):
     g = np.random.default_rng(3)

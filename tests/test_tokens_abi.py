@@ -101,6 +101,9 @@ def test_orthogonalisation(jz):
     for bad in (dict(y=A), dict(y=A + 4784), dict(stride=4000, y=A + 8000 + 16), dict(ws=A + STEP), dict(x=A + 2 * STEP + 64)):
         assert ortho(jz, **bad) == jz.JZ_ERR_ALIAS, bad
     assert ortho(jz, count=0, x=None, y=None, ws=None) == jz.JZ_OK
+    for sizes in ((0, 40, 60), (0, 60, 16), (0, 500, 600)):
+        assert size(jz, "jz_orthogonalize_workspace_bytes", jz.ortho_desc(*sizes)) == (jz.JZ_OK, 0)
+        assert size(jz, "jz_muon_mp_update_workspace_bytes", jz.ortho_desc(*sizes))[0] == jz.JZ_OK
     L = jz.lib()
     for f in (L.jz_orthogonalize_workspace_bytes, L.jz_muon_mp_update_workspace_bytes):
         assert f(None, ctypes.byref(ctypes.c_size_t(0))) == f(ctypes.byref(jz.ortho_desc(1, 1, 1)), None) == jz.JZ_ERR_NULL
