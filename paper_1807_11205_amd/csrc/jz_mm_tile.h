@@ -134,7 +134,7 @@ struct MmStrip {
   typedef typename E::Val V;
   typedef V V4 __attribute__((ext_vector_type(4)));
   __device__ __forceinline__ JZ_LDS V4* chunk(int row, int c) const { return reinterpret_cast<JZ_LDS V4*>(lds + row * PITCH + ((c ^ (row & MASK)) * 16)); }
-  __device__ __forceinline__ void put(const typename E::Sum (&s)[TN], int lane) const {
+  __device__ __forceinline__ void put(const typename E::Sum* s, int lane) const {
     static_for<0, TN * 4>([&](auto I) {
       constexpr int y = decltype(I)::value / 4, j = decltype(I)::value % 4;
       *chunk(lane & 31, y * 8 + j * 2 + (lane >> 5)) = V4{s[y][4 * j], s[y][4 * j + 1], s[y][4 * j + 2], s[y][4 * j + 3]};
@@ -157,9 +157,10 @@ struct MmStrip {
   }
 };
 
-// epi.strip(strip, tile, m, n, lane): what becomes of rows m .. m + 31 and columns n .. n + TN * 32 - 1 of a matrix
+// epi.strip(strip, tile, m, n, lane): what becomes of rows m .. m + 31 and columns n .. n + COLS - 1 of a matrix; a wavefront with an odd number of sums across (192 x 192) hands them out one by one.
+// 192 x 192: four wavefronts with 144 registers of sums each, one on a SIMD; 54 matrix instructions for 24 reads of LDS, a third fewer for each product than 128 x 128 has.
 template <class E, class Epi, int BM, int BN, int WGM, int WGN, bool DUAL>
-__global__ __launch_bounds__(64 * WGM * WGN, 2) void mm_tiles(MmArgs a, Epi epi) {
+__global__ __launch_bounds__(64 * WGM * WGN, BM == 192 ? 1 : 2) void mm_tiles(MmArgs a, Epi epi) {
   constexpr int THREADS = 64 * WGM * WGN, TM = BM / WGM / 32, TN = BN / WGN / 32, READS = TM + TN;
   typedef typename E::Reg Reg;
   typedef typename E::Sum Sum;
@@ -261,13 +262,13 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void mm_tiles(MmArgs a, Epi epi)
     multiply(q, q);
   }
   all_landed();  // zeros too: the results take the operands' place
-  constexpr int STRIP = 32 * TN * 128, FIT = SA::BYTES / STRIP;
+  constexpr int WIDE = TN % 2 ? 1 : TN, STRIP = 32 * WIDE * 128, FIT = SA::BYTES / STRIP;
   static_assert(FIT >= 1 && 2 * FIT >= WGM * WGN, "the results pass through the place of A");
-  const MmStrip<E, TN> strip = {(JZ_LDS unsigned char*)(wave < FIT ? a0 + wave * STRIP : a1 + (wave - FIT) * STRIP)};
-  static_for<0, TM>([&](auto X) {
-    constexpr int x = decltype(X)::value;
-    strip.put(acc[x], lane);
-    epi.strip(strip, w, m0 + (wm * TM + x) * 32, n0 + wn * TN * 32, lane);
+  const MmStrip<E, WIDE> strip = {(JZ_LDS unsigned char*)(wave < FIT ? a0 + wave * STRIP : a1 + (wave - FIT) * STRIP)};
+  static_for<0, TM * TN / WIDE>([&](auto I) {
+    constexpr int x = decltype(I)::value / (TN / WIDE), y = decltype(I)::value % (TN / WIDE) * WIDE;
+    strip.put(&acc[x][y], lane);
+    epi.strip(strip, w, m0 + (wm * TM + x) * 32, n0 + (wn * TN + y) * 32, lane);
   });
 }
 
@@ -422,9 +423,10 @@ __global__ __launch_bounds__(512, 2) void mm_tiny(MmArgs a, Epi epi) {
 
 constexpr int64_t MM_LANES = int64_t(1) << 32;  // a launch has fewer
 
-// A launch over `count` matrices, TILE x TILE: 256 by eight wavefronts in 2 x 4, 128 by four in 2 x 2, 64: mm_small, 32: mm_tiny.
+// A launch over `count` matrices, TILE x TILE: 256 by eight wavefronts in 2 x 4, 192 and 128 by four in 2 x 2, 64: mm_small, 32: mm_tiny.
 template <class E, class Epi, int TILE, bool DUAL>
 int mm_launch(MmArgs a, const Epi& epi, int64_t rows_m, int64_t rows_n, int64_t count, hipStream_t st) {
+  static_assert(!DUAL || TILE != 192, "");
   constexpr int WGM = 2, WGN = TILE == 256 ? 4 : 2, THREADS = TILE == 32 ? 512 : 64 * WGM * WGN;
   a.tiles_m = (int)((rows_m + TILE - 1) / TILE);
   a.tiles_n = (int)((rows_n + TILE - 1) / TILE);

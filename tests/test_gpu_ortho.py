@@ -72,6 +72,15 @@ def test_larger_tiles(jz, B, R, C):
     against(run(jz, x, torch.float32), x)
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("B,R,C", [(16, 900, 880), (1, 2700, 2690)])
+def test_tiles_of_192(jz, B, R, C, out):
+    """Symmetric products (the first) and the last one (the second) of the size for which neither 256 nor 128 fill the chip."""
+    g = np.random.default_rng([9, B, R, C])
+    x = matrices(g, B, R, C, torch.bfloat16)
+    against(run(jz, x, TYPES[out], steps=2), x, steps=2)
+
+
 @pytest.mark.parametrize("B,R,C", [(1, 20, 9000), (16, 2693, 80), (2, 31000, 5), (3, 100, 777), (600, 33, 70), (1, 128, 4103)])
 def test_narrow_ones(jz, B, R, C):
     """Long sums that several workgroups share, and many short ones; in the same order every time."""
