@@ -173,23 +173,33 @@ MmArgs i8_args(const signed char* x, int64_t M, const void* w0, const void* w1, 
   a.row_bytes = pitch;
   return a;
 }
+// Fitted to 20 sizes from 128 x 1024 x 1024 to 5000 x 8000 x 5000, each with every tile; FP16, microseconds, without the quantising launch, 256 / 192 / 128 / 64: 4096^3 61 78 71 116,
+// 1500 rows 4096 -> 6000 50 43 57 70, 3000 rows 2048 -> 3000 31 27 34 40, 2048 rows 4096 -> 4096 50 42 37 65, 1500^3 26 21 16 14; with that launch, the last 32, 512 rows 8192 -> 1024 87 - 54 32 43,
+// 128 rows 1024 -> 1024 23 - 17 16 13.
+constexpr MmTime I8_TIMES[] = {{256, 0., 10., 1.07, .75, 3.1e-3, 256, 1.},
+                               {192, 0., 9.5, .84, .62, 1.7e-3, 256, .97},
+                               {128, 7., 0., .64, .5, .95e-3, 512, .97},
+                               {64, 6., 0., .34, 0., .88e-3, 256, .97},
+                               {32, 5., 0., .2, 0., 1.1e-3, 256, .97}};
+// Two products and the activation: 128 only where it is expected to take a seventh less (4096 rows 2048 -> 5632 and back, all of it: 204 us with 256, 231 with 128, which the model has 3 % ahead).
+constexpr MmTime GLU_TIMES[] = {I8_TIMES[0], {128, 7., 0., .64, .5, .95e-3, 512, .86}};
 template <class T>
 int i8_product(const MmArgs& a, const I8Out& o, hipStream_t st) {
   I8Store<T> e;
   static_cast<I8Out&>(e) = o;
-  // The largest tile that has one or nearly one for each compute unit, but 32 x 32 only where that is no more.  FP16, microseconds with the quantising launch, 256 / 128 / 64 / 32:
-  // 4096^3 83 93 137 530, 1024 rows 4096 -> 4096 55 37 44 140, 512 rows 8192 -> 1024 87 54 32 43, 777 rows 1001 -> 2730 27 20 19 28, 128 rows 1024 -> 1024 23 17 16 13.
-  auto tiles = [&](int64_t t) { return (o.M + t - 1) / t * ((o.N + t - 1) / t); };
-  if (tiles(256) >= 160) return mm_launch<ElemI8, I8Store<T>, 256, false>(a, e, o.M, o.N, 1, st);
-  if (tiles(128) >= 256) return mm_launch<ElemI8, I8Store<T>, 128, false>(a, e, o.M, o.N, 1, st);
-  if (tiles(32) <= 256) return mm_launch<ElemI8, I8Store<T>, 32, false>(a, e, o.M, o.N, 1, st);
-  return mm_launch<ElemI8, I8Store<T>, 64, false>(a, e, o.M, o.N, 1, st);
+  switch (mm_tile_for(I8_TIMES, o.M, o.N, false, 1, a.row_bytes)) {
+    case 256: return mm_launch<ElemI8, I8Store<T>, 256, false>(a, e, o.M, o.N, 1, st);
+    case 192: return mm_launch<ElemI8, I8Store<T>, 192, false>(a, e, o.M, o.N, 1, st);
+    case 128: return mm_launch<ElemI8, I8Store<T>, 128, false>(a, e, o.M, o.N, 1, st);
+    case 64: return mm_launch<ElemI8, I8Store<T>, 64, false>(a, e, o.M, o.N, 1, st);
+  }
+  return mm_launch<ElemI8, I8Store<T>, 32, false>(a, e, o.M, o.N, 1, st);
 }
 int i8_glu(const MmArgs& a, const I8Out& o, hipStream_t st) {
   I8Glu e;
   static_cast<I8Out&>(e) = o;
   const int64_t cols = (o.N + 31) / 32 * 64;
-  if ((o.M + 255) / 256 * ((cols + 255) / 256) >= 160) return mm_launch<ElemI8, I8Glu, 256, true>(a, e, o.M, cols, 1, st);
+  if (mm_tile_for(GLU_TIMES, o.M, cols, false, 1, a.row_bytes) == 256) return mm_launch<ElemI8, I8Glu, 256, true>(a, e, o.M, cols, 1, st);
   return mm_launch<ElemI8, I8Glu, 128, true>(a, e, o.M, cols, 1, st);
 }
 

@@ -421,6 +421,30 @@ __global__ __launch_bounds__(512, 2) void mm_tiny(MmArgs a, Epi epi) {
   if (wave == 0) epi.strip(Strip{(JZ_LDS unsigned char*)lds[0]}, w, m0, n0, lane);
 }
 
+// The tile with the least expected time, in microseconds: a launch's own, what comes before and after the sums that a compute unit forms one after the other (`slots` workgroups at a time), and for
+// each 128 bytes of a sum how many turns there are and what all workgroups take of the chip, whose clock falls with the matrix instructions; few workgroups wait for memory alone.
+struct MmTime {
+  int64_t tile;
+  double launch, turn, least, each, all;
+  int slots;
+  double better;  // taken where it is that much of the time of the ones before
+};
+template <int N>
+int64_t mm_tile_for(const MmTime (&kinds)[N], int64_t rows_m, int64_t rows_n, bool symmetric, int64_t count, int64_t row_bytes) {
+  int64_t best = 0;
+  double least = INFINITY;
+  for (const MmTime& k : kinds) {
+    const int64_t m = (rows_m + k.tile - 1) / k.tile, n = (rows_n + k.tile - 1) / k.tile, tiles = (symmetric ? m * (m + 1) / 2 : m * n) * count;
+    const double turns = (double)((tiles + k.slots - 1) / k.slots);
+    const double t = k.launch + k.turn * turns + (double)((row_bytes + 127) / 128) * std::max(k.least, turns * k.each + (double)tiles * k.all);
+    if (best == 0 || t < least * k.better) {
+      least = t;
+      best = k.tile;
+    }
+  }
+  return best;
+}
+
 constexpr int64_t MM_LANES = int64_t(1) << 32;  // a launch has fewer
 
 // A launch over `count` matrices, TILE x TILE: 256 by eight wavefronts in 2 x 4, 192 and 128 by four in 2 x 2, 64: mm_small, 32: mm_tiny.

@@ -408,30 +408,20 @@ int ortho_product(const Parts& p, const Parts& q, bool symmetric, int64_t count,
   a.row_bytes = p.cols * 4;
   a.symmetric = symmetric;
   a.skip = skip;
-  // The tile with the least expected time: what comes before and after the sums that a compute unit forms one after the other (128: two at a time, so that the next hides it), and for each tile
-  // of a sum (32 k) how many a compute unit has of them and what all of them take of the chip, whose clock falls with the matrix instructions; few tiles wait for memory alone.  Microseconds,
-  // fitted to 25 sizes from 192 to 4096 squared (1 to 16 of them), each with every tile; FP16 inputs.  The model is within 10 % of most and its choice within 5 % of the best.  Smaller tiles
+  // Fitted to 25 sizes from 192 to 4096 squared (1 to 16 of them), each with every tile; FP16 inputs.  The model is within 10 % of most and its choice within 5 % of the best.  Smaller tiles
   // read the operands more often, which shows where they do not stay in the last-level cache (16 updates of 2816 x 1024: 2.14 ms with 256, 2.22 with the 128 that the model alone prefers for
-  // K = 1024), hence the 7 %.
-  // 192 is there for what fills the chip with neither 256 nor 128: the symmetric product of 4096 x 4096 is 136 tiles of 256, 241 us, 253 of 192, 200 us, or 528 of 128, 250 us; the whole of
-  // 4096 x 12288 in FP16 6.1 ms without it, 5.5 with.
-  const struct {
-    int64_t tile;
-    double fix, turn, least, each, all;
-  } kinds[] = {{256, 2., 12., 1.4, 1.1, 5.2e-3}, {192, 4., 12., .9, .66, 3.3e-3}, {128, 6., 0., .68, .38, 1.55e-3}, {64, 4.5, 0., .34, 0., 1.3e-3}, {32, 4., 0., .2, 0., 1.3e-3}};
-  int64_t best = 0;
-  double least = INFINITY;
-  for (const auto& k : kinds) {
-    const int64_t m = (p.rows + k.tile - 1) / k.tile, n = (q.rows + k.tile - 1) / k.tile, tiles = (symmetric ? m * (m + 1) / 2 : m * n) * count;
-    const double turns = (double)((tiles + 255) / 256);
-    const double t = k.fix + k.turn * turns + (double)p.cols / 32. * std::max(k.least, turns * k.each + (double)tiles * k.all);
-    if (t < least * (k.tile < 128 ? 1. : .93)) {
-      least = t;
-      best = k.tile;
-    }
+  // K = 1024), hence the 7 %.  192 is there for what fills the chip with neither 256 nor 128: the symmetric product of 4096 x 4096 is 136 tiles of 256, 241 us, 253 of 192, 200 us, or 528 of
+  // 128, 250 us; the whole of 4096 x 12288 in FP16 6.1 ms without it, 5.5 with.
+  static constexpr MmTime kinds[] = {{256, 2., 12., 1.4, 1.1, 5.2e-3, 256, 1.},
+                                     {192, 4., 12., .9, .66, 3.3e-3, 256, .93},
+                                     {128, 6., 0., .68, .38, 1.55e-3, 256, .93},
+                                     {64, 4.5, 0., .34, 0., 1.3e-3, 256, 1.},
+                                     {32, 4., 0., .2, 0., 1.3e-3, 256, 1.}};
+  const int64_t best = mm_tile_for(kinds, p.rows, q.rows, symmetric, count, p.cols * 4);
+  if constexpr (!std::is_same<Epi, OrthoSums>::value) {  // those have 128 rows at most: as many tiles of 128, and each takes less
+    if (best == 256) return mm_launch<E, Epi, 256, false>(a, e, p.rows, q.rows, count, st);
+    if (best == 192) return mm_launch<E, Epi, 192, false>(a, e, p.rows, q.rows, count, st);
   }
-  if (best == 256) return mm_launch<E, Epi, 256, false>(a, e, p.rows, q.rows, count, st);
-  if (best == 192) return mm_launch<E, Epi, 192, false>(a, e, p.rows, q.rows, count, st);
   if (best == 128) return mm_launch<E, Epi, 128, false>(a, e, p.rows, q.rows, count, st);
   if (best == 64) return mm_launch<E, Epi, 64, false>(a, e, p.rows, q.rows, count, st);
   return mm_launch<E, Epi, 32, false>(a, e, p.rows, q.rows, count, st);

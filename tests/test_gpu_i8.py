@@ -110,6 +110,19 @@ def test_linear_strided(jz, M, K, N):
     assert bool((room[:, N:] == 3).all())
 
 
+@pytest.mark.parametrize("M,K,N", [(4000, 1000, 4001), (1500, 1500, 6000), (3001, 2050, 3003), (1800, 600, 2000), (1537, 4096, 4100)])
+def test_linear_of_many_rows(jz, M, K, N):
+    """Each large tile, with an end inside the last ones."""
+    g = np.random.default_rng([9, M])
+    x = randn(g, (M, K), torch.bfloat16)
+    wq, s = quantized(jz, randn(g, (N, K), torch.float32))
+    y = linear(jz, x, wq, s, N)
+    q, sx = tokens.quantize(x.cpu().float().numpy())
+    some = np.unique(np.concatenate([np.arange(40), np.arange(M - 300, M), g.integers(0, M, 100)]))
+    ref = tokens.linear_i8(q[some], sx[some], wq.cpu().numpy()[:, :K], s.cpu().numpy())
+    check(y[torch.from_numpy(some).to(DEV)].contiguous(), ref, np.abs(ref), 3.01, "y")
+
+
 @pytest.mark.parametrize("M", [1, 40, 200, 3000])
 def test_largest_sums(jz, M):
     """in_features as large as int32 allows, every product 127 x 127; signs that alternate add up to nothing."""
@@ -168,6 +181,23 @@ def test_block(jz, M, D, F, O, dtype, act):
     ref, off = tokens.ffn_i8(*tokens.quantize(x.cpu().float().numpy()), *host, ACTS[act])
     bound = ROUND[y.dtype] * np.abs(ref) + (1 + ROUND[y.dtype]) * (3.01 * E32 * np.abs(ref) + off) + TINY[y.dtype]
     assert np.all(np.abs(wide(y) - ref) <= bound)
+
+
+def test_block_of_many_rows(jz):
+    """The large tile of two products."""
+    M, D, F, O = 1500, 1500, 3001, 40
+    g = np.random.default_rng([10, M])
+    x = randn(g, (M, D), torch.float16)
+    w = []
+    for a, b in ((F, D), (F, D), (O, F)):
+        w += list(quantized(jz, randn(g, (a, b), torch.float32, b ** -0.5)))
+    y = ffn(jz, x, w, D, F, O, 0)
+    host = [(w[i].cpu().numpy()[:, :c], w[i + 1].cpu().numpy()) for i, c in ((0, D), (2, D), (4, F))]
+    q, sx = tokens.quantize(x.cpu().float().numpy())
+    some = np.unique(np.concatenate([np.arange(40), np.arange(M - 260, M), g.integers(0, M, 60)]))
+    ref, off = tokens.ffn_i8(q[some], sx[some], *host, ACTS[0])
+    bound = ROUND[y.dtype] * np.abs(ref) + (1 + ROUND[y.dtype]) * (3.01 * E32 * np.abs(ref) + off) + TINY[y.dtype]
+    assert np.all(np.abs(wide(y[torch.from_numpy(some).to(DEV)]) - ref) <= bound)
 
 
 def test_block_of_strided_rows(jz):
