@@ -442,13 +442,14 @@ int jz_embed_bwd(const jz_embed_desc* desc, const int* ids_dev, const void* dout
  *   X = G / (||G||_F + eps),  then `steps` times   X <- a X + (b A + c A^2) X,  A = X X^T       (X^T in X's place where rows > cols)
  * a Newton-Schulz iteration: every singular value s of X goes to a s + b s^3 + c s^5 each time, the singular vectors stay.  With a, b, c = 3.4445, -4.7750, 2.0315 and
  * five steps the values that are not tiny end near 1 (0.7 to 1.2).  a, b, c finite, and such that the singular values stay below 5 and |a + b t + c t^2| below
- * max(1, |a|) <= 30 over their squares t (results may be Inf or NaN otherwise: the products take 22 bits of every element, as two FP16 parts).  Sums are FP32, ||G|| is added up in FP64.
+ * max(1, |a|) <= 30 over their squares t (results may be Inf or NaN otherwise: the products take 22 bits of every element, as two FP16 parts,
+ * and of one below 2^-14 what is above 2^-36, so that a G whose norm is far below eps keeps fewer).  Sums are FP32, ||G|| is added up in FP64.
  *   jz_orthogonalize   x (dtype) -> y (out_dtype), each JZ_F16, JZ_BF16 or JZ_F32, one rounding.  A matrix of zeros gives zeros; one with Inf or NaN NaNs.
  *   jz_muon_mp_update  one optimiser step in mixed precision; grad16 and weight16 have dtype == out_dtype == JZ_F16 or JZ_BF16:
  *       g = float(grad16) / S,  v <- momentum v + g,  u = g + momentum v where nesterov, else v,  O = the iteration's result for u (FP32)
  *       w <- w - lr (update_scale O + weight_decay w),   weight16 = RNE(w)
  *     S is state_dev->scale when state_dev (DEVICE, as in jz_lars_mp_update_dyn) is not NULL, else hp->loss_scale.  update_scale is the caller's choice, usually
- *     sqrt(max(1, rows / cols)).  *found_inf_dev (DEVICE int): 1 if a gradient is Inf or NaN, or if skip_dev (DEVICE int, may be NULL: another
+ *     sqrt(max(1, rows / cols)).  *found_inf_dev (DEVICE int): 1 if a gradient, or the momentum that it would leave, is Inf or NaN, or if skip_dev (DEVICE int, may be NULL: another
  *     call's flag, as of jz_grad_clip) is not 0, else 0; with 1 nothing else is written.  Call it before jz_lars_mp_update_dyn, which adjusts the scale.  found_inf_dev may be the
  *     `nonfinite` of a LARS sink (jz_lars_sumsq_sink, after jz_lars_begin_step) of a tensor that no kernel fills, so that the presummed LARS update of the other
  *     parameters is skipped, and the scale lowered, together with this one.

@@ -1131,7 +1131,7 @@ def embed_desc(tokens: int, vocab: int, channels: int, dtype: int = JZ_F16, out_
 def jz_embed_fwd(desc: jz_embed_desc, ids, table, out, stream=None):
     """out[t] = scale * table[ids[t]]; zeros where ids[t] is outside the table."""
     d = desc
-    _here(table, out)
+    _here(ids, table, out)
     _invoke("jz_embed_fwd", (ctypes.addressof(d), _ids(ids, d.tokens), _dev_ptr(table, _type(d.dtype), d.vocab * d.channels, "table"),
                               _rows_ptr(out, _type(d.out_dtype), d.tokens, d.channels, d.out_stride, "out")), stream)
 
@@ -1143,7 +1143,7 @@ def jz_embed_bwd_workspace_bytes(desc: jz_embed_desc) -> int:
 def jz_embed_bwd(desc: jz_embed_desc, ids, dout, dtable, ws, accumulate: bool = False, stream=None):
     """dtable[v] = scale * sum of dout[t] over the places t of token v; accumulate: added to what is there, rows without a token left as they are."""
     d = desc
-    _here(dout, dtable, ws)
+    _here(ids, dout, dtable, ws)
     wp, wn = _ws(ws)
     _invoke("jz_embed_bwd", (ctypes.addressof(d), _ids(ids, d.tokens), _rows_ptr(dout, _type(d.out_dtype), d.tokens, d.channels, d.out_stride, "dout"), int(bool(accumulate)),
                               _dev_ptr(dtable, _type(d.dtype), d.vocab * d.channels, "dtable"), wp, wn), stream)
@@ -1190,7 +1190,7 @@ def jz_muon_mp_update(desc: jz_ortho_desc, hp: jz_muon_hparams, master, momentum
     """The momentum, the orthogonalised update of the FP32 master weights and their 16-bit copy.  state: the device-resident loss scale (else hp.loss_scale); skip: another
     call's overflow flag (int32[1]); found_inf: int32[1], or the address of a flag (as jz_lars_sumsq_sink gives them)."""
     t, f = _type(desc.dtype), torch.float32
-    _here(master, grad16, ws)
+    _here(master, momentum, grad16, weight16, ws, state, skip, None if isinstance(found_inf, int) else found_inf)
     wp, wn = _ws(ws)
     _invoke("jz_muon_mp_update", (ctypes.addressof(desc), ctypes.addressof(hp), _ls_state(state) if state is not None else 0, _flag(skip) if skip is not None else 0,
                                    _matrices_ptr(master, f, desc, "master"), _matrices_ptr(momentum, f, desc, "momentum"), _matrices_ptr(grad16, t, desc, "grad16"),
@@ -1208,7 +1208,7 @@ def _codes_ptr(t, rows, cols, what):
 
 def jz_quantize_i8(rows: int, cols: int, x, q, scale, x_stride: int = 0, stream=None):
     """Codes (int8 [rows, i8_pitch(cols)], zeros behind column cols) and scales (float32 [rows]) of the rows of x."""
-    _here(x, q)
+    _here(x, q, scale)
     _invoke("jz_quantize_i8", (rows, cols, dtype_of(x.dtype), _rows_ptr(x, x.dtype, rows, cols, x_stride, "x"), x_stride, _codes_ptr(q, rows, cols, "q"),
                                 _dev_ptr(scale, torch.float32, rows, "scale")), stream)
 
@@ -1224,7 +1224,7 @@ def jz_linear_i8_workspace_bytes(desc: jz_linear_i8_desc) -> int:
 def jz_linear_i8(desc: jz_linear_i8_desc, x, wq, w_scale, y, ws=None, stream=None):
     """y = x w^T with x quantised row by row and w in codes [out_features, i8_pitch(in_features)] with a scale for each row."""
     d, t = desc, _type(desc.dtype)
-    _here(x, wq, y, ws)
+    _here(x, wq, w_scale, y, ws)
     wp, wn = _ws(ws)
     _invoke("jz_linear_i8", (ctypes.addressof(d), _rows_ptr(x, t, d.rows, d.in_features, d.x_stride, "x"), _codes_ptr(wq, d.out_features, d.in_features, "wq"),
                               _dev_ptr(w_scale, torch.float32, d.out_features, "w_scale"), _rows_ptr(y, t, d.rows, d.out_features, d.y_stride, "y"), wp, wn), stream)
@@ -1238,7 +1238,7 @@ def jz_ffn_i8_fwd(desc: jz_ffn_desc, x, wq_gate, s_gate, wq_up, s_up, wq_down, s
     """The gated block with its three matrices in codes, each with a scale for each row."""
     d, t, f = desc, _type(desc.dtype), torch.float32
     M, D, F, O = d.rows, d.in_features, d.hidden, d.out_features
-    _here(x, wq_gate, y, ws)
+    _here(x, wq_gate, s_gate, wq_up, s_up, wq_down, s_down, y, ws)
     wp, wn = _ws(ws)
     _invoke("jz_ffn_i8_fwd", (ctypes.addressof(d), _rows_ptr(x, t, M, D, d.x_stride, "x"), _codes_ptr(wq_gate, F, D, "wq_gate"), _dev_ptr(s_gate, f, F, "s_gate"),
                                _codes_ptr(wq_up, F, D, "wq_up"), _dev_ptr(s_up, f, F, "s_up"), _codes_ptr(wq_down, O, F, "wq_down"), _dev_ptr(s_down, f, O, "s_down"),

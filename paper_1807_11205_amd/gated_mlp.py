@@ -154,6 +154,8 @@ class GatedMLP:
     # ---- the step ------------------------------------------------------------------------------------------------------
     def set_batch(self, x: torch.Tensor, labels: torch.Tensor, stream=None):
         """r_0 (float32 [rows, width]) and the classes of the rows, copied on the stream of the step that takes them."""
+        if self.vocab:
+            raise ValueError("the network's rows are tokens: set_tokens")
         with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
             self.r[0].copy_(x)
             self.labels.copy_(labels)
@@ -230,6 +232,8 @@ class GatedMLP:
         prepare_answers_i8.  x is as the current stream leaves it; the logits are ready once `stream` is (None: the current one)."""
         if i8 and self.i8 is None:
             raise ValueError("prepare_answers_i8 comes first")
+        if self.vocab and x.is_floating_point():
+            raise ValueError("the network's rows are tokens")
         current = torch.cuda.current_stream(self.device)
         if stream is None or api._stream(stream) == api._stream(current):
             return self._answer(x, i8)

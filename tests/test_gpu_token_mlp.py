@@ -166,6 +166,23 @@ def test_what_is_refused(jz):
         GatedMLP(8, 64, 64, 16, 1).set_tokens(torch.zeros(8, dtype=torch.int32), torch.zeros(8, dtype=torch.int32))
 
 
+def test_tokens_and_rows_are_not_mixed_up(jz):
+    from paper_1807_11205_amd.gated_mlp import GatedMLP
+    m = GatedMLP(8, 64, 64, 16, 1, vocab=24)
+    with pytest.raises(ValueError):
+        m.set_batch(torch.zeros(8, 64), torch.zeros(8, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        m.answer(torch.zeros(8, 64, device=m.device))
+    with pytest.raises(ValueError):
+        m.answer(torch.zeros(8, device=m.device))
+    with pytest.raises(ValueError):
+        m.answer(torch.zeros(8, dtype=torch.int32, device=m.device), i8=True)
+    m.prepare_answers_i8()
+    ids = torch.tensor([3, 0, 23, 24, -1, 3], device=m.device)
+    for i8 in (False, True):
+        assert torch.equal(m.answer(ids, i8=i8), m.answer(ids.to(torch.int32), i8=i8))
+
+
 def test_without_blocks(jz):
     from paper_1807_11205_amd.gated_mlp import GatedMLP
     m = GatedMLP(16, 64, 64, 16, 0, vocab=16, tied=True, optimizer="muon")
