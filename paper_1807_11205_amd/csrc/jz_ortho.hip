@@ -134,6 +134,10 @@ __global__ __launch_bounds__(256) void ortho_sumsq(OrthoIn a) {
   if (threadIdx.x == 0) a.sums[(int64_t)blockIdx.y * a.parts + blockIdx.x] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
+__device__ __forceinline__ double ortho_factor(double s, float eps) {
+  const double norm = sqrt(s) + (double)eps;
+  return norm == 0. ? 0. : (double)SCALE / norm;
+}
 // Each matrix's factor; of the update, whether anything is to be done.  One workgroup, a wavefront a matrix.
 template <bool MUON>
 __global__ __launch_bounds__(1024) void ortho_factors(OrthoIn a) {
@@ -142,12 +146,12 @@ __global__ __launch_bounds__(1024) void ortho_factors(OrthoIn a) {
   __syncthreads();
   for (int64_t b = threadIdx.x >> 6; b < a.count; b += 16) {
     double s = 0.;
+#pragma unroll 8
     for (int i = threadIdx.x & 63; i < a.parts; i += 64) s += a.sums[b * a.parts + i];
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
     if ((threadIdx.x & 63) == 0) {
-      const double norm = sqrt(s) + (double)a.eps;
-      a.inv[b] = norm == 0. ? 0. : (double)SCALE / norm;
+      a.inv[b] = ortho_factor(s, a.eps);
       if (MUON && !(s < INFINITY)) bad = 1;
     }
   }
@@ -160,15 +164,43 @@ struct OrthoParts {
   char *r, *c;
   int64_t rp, cp;  // padded sides
 };
-template <class T, bool MUON>
+// FOLD: few sums, which every workgroup adds up by itself instead of a launch of one: 3 of 1001 x 333 161 and so 159 us, the update of 16 of 64 x 200 60.5 and 58.2.
+constexpr int ORTHO_FOLD = 1024;
+template <class T, bool MUON, bool FOLD>
 __global__ __launch_bounds__(256) void ortho_parts(OrthoIn a, OrthoParts o) {
   __shared__ float tile[64][65];
-  if (MUON && *a.found_inf) return;
+  if (MUON && !FOLD && *a.found_inf) return;
   const OrthoValue<T, MUON> in(a);
   const int64_t across = (o.cp + 63) / 64, down = (o.rp + 63) / 64;
   const int64_t id = gridDim.x - 1 - blockIdx.x, of = id / (across * down), t = id - of * across * down;  // what was squared last is still in the last-level cache
   const int64_t r0 = t / across * 64, c0 = t % across * 64, base = of * a.stride;
-  const double inv = a.inv[of];
+  double inv;
+  if constexpr (FOLD) {
+    __shared__ double mine[4];
+    __shared__ int bad[4];
+    const int all = (int)a.count * a.parts, from = (int)of * a.parts;
+    double s = 0.;
+    bool wrong = MUON && a.skip && *a.skip;
+    for (int i = threadIdx.x; i < a.parts; i += 256) s += a.sums[from + i];
+    if (MUON)
+      for (int i = threadIdx.x; i < all; i += 256) wrong |= !(a.sums[i] < INFINITY);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
+    wrong = __any(wrong);
+    if ((threadIdx.x & 63) == 0) {
+      mine[threadIdx.x >> 6] = s;
+      bad[threadIdx.x >> 6] = wrong;
+    }
+    __syncthreads();
+    inv = ortho_factor((mine[0] + mine[1]) + (mine[2] + mine[3]), a.eps);
+    if (MUON) {
+      wrong = bad[0] | bad[1] | bad[2] | bad[3];
+      if (blockIdx.x == 0 && threadIdx.x == 0) *a.found_inf = wrong;
+      if (wrong) return;
+    }
+  } else {
+    inv = a.inv[of];
+  }
   const int row = threadIdx.x / 8, col = threadIdx.x % 8 * 8;
 #pragma unroll
   for (int h = 0; h < 64; h += 32) {
@@ -447,9 +479,13 @@ int ortho_gram_sums(const Parts& x, int64_t count, int splits, const int* skip, 
 template <class T, bool MUON>
 int ortho_begin(const OrthoIn& in, const OrthoShape& s, const OrthoParts& o, hipStream_t st) {
   ortho_sumsq<T, MUON><<<dim3((unsigned)in.parts, (unsigned)s.count), 256, 0, st>>>(in);
-  ortho_factors<MUON><<<1, 1024, 0, st>>>(in);
   const int64_t tiles = (o.rp + 63) / 64 * ((o.cp + 63) / 64) * s.count;
-  ortho_parts<T, MUON><<<(unsigned)tiles, 256, 0, st>>>(in, o);
+  if (s.count * in.parts <= ORTHO_FOLD) {
+    ortho_parts<T, MUON, true><<<(unsigned)tiles, 256, 0, st>>>(in, o);
+  } else {
+    ortho_factors<MUON><<<1, 1024, 0, st>>>(in);
+    ortho_parts<T, MUON, false><<<(unsigned)tiles, 256, 0, st>>>(in, o);
+  }
   return jz::launch_status();
 }
 

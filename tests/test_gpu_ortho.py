@@ -221,6 +221,26 @@ def test_an_overflow_leaves_everything(jz, how):
     check_muon(s, before, HP, 64.0)
 
 
+@pytest.mark.parametrize("how", ["inf", "skip"])
+def test_an_overflow_of_many_sums(jz, how):
+    """More partial sums than a workgroup adds up by itself."""
+    g = np.random.default_rng(11)
+    s = muon_state(g, 2, 2100, 2050, torch.float16, 64.0)
+    x = float(s["grad16"][1, 7, 2049])
+    if how != "skip":
+        s["grad16"][1, 7, 2049] = float(how)
+    before = {k: v.clone() for k, v in s.items()}
+    skip = torch.full((1,), int(how == "skip"), dtype=torch.int32, device=DEV)
+    assert muon(jz, s, HP, 64.0, skip=skip) == 1
+    for k in ("momentum", "master"):
+        assert torch.equal(s[k], before[k]), k
+    assert bool(torch.isnan(s["weight16"]).all())
+    skip.zero_()
+    s["grad16"][1, 7, 2049] = x
+    assert muon(jz, s, HP, 64.0, skip=skip) == 0
+    assert torch.equal(s["weight16"], s["master"].half()) and bool((s["master"] != before["master"]).any(2).all())
+
+
 def test_without_matrices(jz):
     d = jz.ortho_desc(0, 8, 8)
     e, f = torch.empty((0, 8, 8), dtype=torch.float16, device=DEV), torch.empty((0, 8, 8), device=DEV)
