@@ -7,7 +7,7 @@
 //     ElemI8     128 int8 of k; a step is one 32x32x32 matrix instruction, sums are int32 and exact
 //     ElemSplit  32 k of an FP32 value v as hi = FP16(v) (chunks 0-3) and lo = FP16(v - hi) (chunks 4-7), 22 bits together.  A product is hi hi + hi lo + lo hi: three
 //                instructions for each two reads of an operand, so that the matrix instructions and not LDS are what the loop waits for
-//     ElemHigh   the same operands, of which only the high parts are loaded: products of FP16 numbers
+//     ElemHalf   64 k as FP16
 // Bound, 256 x 256: the matrix instructions.  16384 rows 4096 -> 12288 of ElemI8 in 712 us, 2.3 POP/s (the library's product of 8192^3 2.1); ElemSplit, 4096 x 4096 times 4096 x 12288, 914 us,
 // 1.35 PFLOP/s of matrix instructions (FP16 library 1.36), which are busy 68 % of 1.6 GHz; 16 products of 1024^3 that fill 160 of the compute units 82 us, 20 of them results on their way.
 // Sums are in exchanged order (B's rows first): register 4 j + i of a lane holds row lane % 32, column 8 j + 4 (lane / 32) + i.
@@ -22,20 +22,20 @@ struct ElemI8 {
   typedef i32x4 Reg;
   typedef i32x16 Sum;
   typedef int Val;
-  static constexpr bool SPLIT = false, HIGH = false;
+  static constexpr bool SPLIT = false;
   static __device__ __forceinline__ Sum mfma(Reg a, Reg b, Sum c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
 };
-template <bool HIGH_>
-struct ElemParts {
+template <bool SPLIT_>
+struct ElemFp16 {
   typedef f16x8 Reg;
   typedef mm_f32x16 Sum;
   typedef float Val;
-  static constexpr bool SPLIT = true, HIGH = HIGH_;
+  static constexpr bool SPLIT = SPLIT_;
   static __device__ __forceinline__ Sum mfma(Reg a, Reg b, Sum c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
-typedef ElemParts<false> ElemSplit;
-typedef ElemParts<true> ElemHigh;
+typedef ElemFp16<true> ElemSplit;
+typedef ElemFp16<false> ElemHalf;
 
 struct MmOperand {
   const void* p[2];        // [1]: the matrix interleaved with [0], 32 rows by 32 rows (B only)
@@ -84,9 +84,8 @@ struct MmSource {
   const char* base[2];
   int64_t pitch, rows_left, row_bytes;
   unsigned off, step, chunk;
-  unsigned never;  // a chunk that is not wanted: an offset outside
 
-  __device__ __forceinline__ void init(const MmOperand& o, int64_t of, int64_t row0, int64_t row_bytes_, int t, bool high) {
+  __device__ __forceinline__ void init(const MmOperand& o, int64_t of, int64_t row0, int64_t row_bytes_, int t) {
     pitch = o.pitch;
     row_bytes = row_bytes_;
     rows_left = o.rows - row0;
@@ -94,7 +93,6 @@ struct MmSource {
     base[1] = static_cast<const char*>(o.p[DUAL ? 1 : 0]) + of * o.of + row0 * pitch;
     const int row = t >> 3;
     chunk = (((t & 7) ^ ((row >> 1) & 7)) * 16);
-    never = high && chunk >= 64 ? 0x80000000u : 0u;
     step = (unsigned)((DUAL ? 32 : THREADS / 8) * pitch);
     off = (unsigned)((DUAL ? row & 31 : row) * pitch) + chunk;
   }
@@ -105,7 +103,7 @@ struct MmSource {
     const int64_t span = (rows_left - 1) * pitch + row_bytes - k0;
     const int bytes = !wanted || span < 0 ? 0 : (int)(span < 0x7ffffff0 ? span : 0x7ffffff0);
     const auto r = __builtin_amdgcn_make_buffer_rsrc((void*)(base[0] + (wanted ? k0 : 0)), 0, bytes, 0x00020000);
-    const unsigned end = (int64_t)chunk >= row_bytes - k0 ? 0x80000000u : never;
+    const unsigned end = (int64_t)chunk >= row_bytes - k0 ? 0x80000000u : 0u;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) to[i] = __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(r, (int)((off + i * step) | end), 0, 0));
   }
@@ -116,7 +114,7 @@ struct MmSource {
     const int bytes = !wanted || span < 0 ? 0 : (int)(span < 0x7ffffff0 ? span : 0x7ffffff0);
     const auto r0 = __builtin_amdgcn_make_buffer_rsrc((void*)(base[0] + skip), 0, bytes, 0x00020000);
     const auto r1 = __builtin_amdgcn_make_buffer_rsrc((void*)(base[1] + skip), 0, bytes, 0x00020000);
-    const unsigned end = (int64_t)chunk >= row_bytes - k0 ? 0x80000000u : never;  // a row's end inside the tile
+    const unsigned end = (int64_t)chunk >= row_bytes - k0 ? 0x80000000u : 0u;  // a row's end inside the tile
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       const bool second = DUAL && (THREADS == 256 ? i & 1 : wave >> 2);  // 256 threads bring 32 rows at a time, 512 threads 64
@@ -175,8 +173,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 192 ? 1 : 2) void mm_tiles(Mm
   const int last = (int)((a.row_bytes + 127) / 128);
   SA from_a;
   SB from_b;
-  from_a.init(a.a, w.of, m0, a.row_bytes, t, E::HIGH);
-  from_b.init(a.b, w.of, DUAL ? n0 / 2 : n0, a.row_bytes, t, E::HIGH);
+  from_a.init(a.a, w.of, m0, a.row_bytes, t);
+  from_b.init(a.b, w.of, DUAL ? n0 / 2 : n0, a.row_bytes, t);
   auto fetch = [&](auto* la, auto* lb, int kt) {  // behind the last tile: zeros, so that there is no branch among the products
     from_a.load(la, (int64_t)kt * 128, wave, kt < last);
     from_b.load(lb, (int64_t)kt * 128, wave, kt < last);
@@ -215,13 +213,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 192 ? 1 : 2) void mm_tiles(Mm
     all_landed();
     read(la, lb, 0, p);
     fetch(na, nb, kt + 1);
-    if constexpr (E::HIGH) {
-      multiply(q, q);
-      spread_out<MULT, READS, LOADS>();
-      read(la, lb, 1, q);
-      multiply(p, p);
-      spread_out<MULT, READS, 0>();
-    } else if constexpr (E::SPLIT) {
+    if constexpr (E::SPLIT) {
       // q, r: the second half's hi and lo
       multiply(r, q);
       multiply(q, r);
@@ -255,7 +247,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 192 ? 1 : 2) void mm_tiles(Mm
     tile(a0, b0, a1, b1, kt);
     if (kt + 1 < last) tile(a1, b1, a0, b0, kt + 1);
   }
-  if constexpr (E::SPLIT && !E::HIGH) {
+  if constexpr (E::SPLIT) {
     multiply(r, q);
     multiply(q, r);
   } else {
@@ -287,8 +279,8 @@ __global__ __launch_bounds__(256, 2) void mm_small(MmArgs a, Epi epi) {
   const int64_t m0 = (int64_t)w.m * 64, n0 = (int64_t)w.n * 64;
   const int last = (int)((a.row_bytes + 127) / 128);
   MmSource<64, 256, false> from_a, from_b;
-  from_a.init(a.a, w.of, m0, a.row_bytes, t, E::HIGH);
-  from_b.init(a.b, w.of, n0, a.row_bytes, t, E::HIGH);
+  from_a.init(a.a, w.of, m0, a.row_bytes, t);
+  from_b.init(a.b, w.of, n0, a.row_bytes, t);
   u32x4 ra[DEPTH][EACH], rb[DEPTH][EACH];
   auto fetch = [&](int d, int kt) {  // behind the last tile: zeros
     from_a.get(ra[d], (int64_t)kt * 128, kt < last);
@@ -317,7 +309,7 @@ __global__ __launch_bounds__(256, 2) void mm_small(MmArgs a, Epi epi) {
       lds_meet();
       Reg x[4], y[4];
 #pragma unroll
-      for (int s = 0; s < (E::HIGH ? 2 : 4); ++s) {
+      for (int s = 0; s < 4; ++s) {
         x[s] = *reinterpret_cast<const JZ_LDS Reg*>(to + at_a[s]);
         y[s] = *reinterpret_cast<const JZ_LDS Reg*>(to + at_b[s]);
       }
@@ -325,10 +317,8 @@ __global__ __launch_bounds__(256, 2) void mm_small(MmArgs a, Epi epi) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           acc[0] = E::mfma(y[s], x[s], acc[0]);
-          if constexpr (!E::HIGH) {
-            acc[0] = E::mfma(y[s], x[s + 2], acc[0]);
-            acc[0] = E::mfma(y[s + 2], x[s], acc[0]);
-          }
+          acc[0] = E::mfma(y[s], x[s + 2], acc[0]);
+          acc[0] = E::mfma(y[s + 2], x[s], acc[0]);
         }
       } else {
 #pragma unroll
@@ -368,11 +358,10 @@ __global__ __launch_bounds__(512, 2) void mm_tiny(MmArgs a, Epi epi) {
     Reg a[2], b[2];
   };
   auto get = [&](Piece& p, int u) {  // behind the end: zeros
-    // ElemSplit: 16 k of high parts and, 64 bytes on, their low parts; ElemI8: 64 k
+    // ElemSplit: 16 k of high parts and, 64 bytes on, their low parts; the others: 64 bytes of k
     const unsigned j = u & 1, k0 = (unsigned)(u >> 1) * 128, h = lane >> 5, behind = u >= units ? 0x80000000u : 0u;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      if (E::HIGH && i) break;
       const unsigned k = k0 + (E::SPLIT ? (2 * j + h) * 16 + i * 64 : (4 * j + 2 * i + h) * 16);
       const unsigned end = k >= (unsigned)a.row_bytes ? 0x80000000u : behind;
       p.a[i] = __builtin_bit_cast(Reg, __builtin_amdgcn_raw_buffer_load_b128(from_a, (int)((row_a + k) | end), 0, 0));
@@ -383,10 +372,8 @@ __global__ __launch_bounds__(512, 2) void mm_tiny(MmArgs a, Epi epi) {
   auto multiply = [&](const Piece& p) {
     if constexpr (E::SPLIT) {
       acc[0] = E::mfma(p.b[0], p.a[0], acc[0]);
-      if constexpr (!E::HIGH) {
-        acc[0] = E::mfma(p.b[0], p.a[1], acc[0]);
-        acc[0] = E::mfma(p.b[1], p.a[0], acc[0]);
-      }
+      acc[0] = E::mfma(p.b[0], p.a[1], acc[0]);
+      acc[0] = E::mfma(p.b[1], p.a[0], acc[0]);
     } else {
       acc[0] = E::mfma(p.b[0], p.a[0], acc[0]);
       acc[0] = E::mfma(p.b[1], p.a[1], acc[0]);

@@ -72,6 +72,15 @@ def test_larger_tiles(jz, B, R, C):
     against(run(jz, x, torch.float32), x)
 
 
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 5, 7])
+@pytest.mark.parametrize("B,R,C", [(3, 100, 140), (5, 31, 33), (2, 150, 260), (3, 260, 150), (2, 140, 1400), (1, 600, 590)])
+def test_bf16_results(jz, steps, B, R, C):
+    """The operands of the last product rounded to FP16, 2^-12 each: with BF16's own rounding, half a step at most and a third of its square on average, below half a step."""
+    g = np.random.default_rng([12, steps, B, R, C])
+    x = matrices(g, B, R, C, torch.float32)
+    against(run(jz, x, torch.bfloat16, steps=steps), x, steps=steps)
+
+
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 @pytest.mark.parametrize("B,R,C", [(16, 900, 880), (1, 2700, 2690)])
 def test_tiles_of_192(jz, B, R, C, out):
