@@ -19,6 +19,15 @@ namespace {
 constexpr int ZERO_EACH = 16384;    // elements of the table that a workgroup looks at
 constexpr int EMBED_GRID = 1 << 16;  // workgroups at most: each takes further turns
 
+// What is written past the caches: results of half of the last-level cache and more, of which the next launch would find little there, and rows of the table that stand there stay.  Lookup of
+// 268 MB in BF16 85.4 us with ordinary stores, 81.0 so, of 262 MB out of 3000 rows 82 and 58, of 134 MB in FP32 43 and 30; the zeros of a table of 205 MB 144.7 and 137.9 with the lookup and all
+// (in FP32, two halves of every 32 bytes that go by themselves, 548 and 740: not those).
+constexpr size_t STREAM_BYTES = size_t(128) << 20;
+template <class T>
+__device__ __forceinline__ void stream8(T* p, typename Vec8<T>::V v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<typename Vec8<T>::U*>(p));
+}
+
 // ---- lookup -----------------------------------------------------------------------------------------------------------------
 struct LookupArgs {
   const int* ids;
@@ -29,14 +38,25 @@ struct LookupArgs {
   float scale;
 };
 
-// Groups of eight channels; a row's last group ends with the row, so that it overlaps its neighbour where channels are no multiple of 8 (both store the
-// same values).  FEW: less than eight channels.
-template <class T, class O, bool FEW>
+// Channels that a lane stores at a time: FP32 rows past the caches 16 bytes, since the two halves of 32 would go their ways by themselves.
+template <class T, class O>
+constexpr int lookup_each(bool stream) {
+  return sizeof(O) == 4 && (stream || sizeof(T) == 4) ? 4 : 8;
+}
+// Groups of EACH channels; a row's last group ends with the row, so that it overlaps its neighbour where channels are no multiple of it (both store the same
+// values).  FEW: less than eight channels.  STREAM: past the caches.
+template <class T, class O, bool FEW, bool STREAM>
 __global__ __launch_bounds__(256) void embed_lookup(LookupArgs a) {
-  constexpr int U = 4;  // loads in flight
-  const int64_t per = (a.channels + 7) / 8, all = a.tokens * per;
+  constexpr int EACH = FEW ? 8 : lookup_each<T, O>(STREAM), U = 32 / EACH;  // U: loads in flight
+  typedef T In __attribute__((ext_vector_type(EACH)));
+  typedef O Out __attribute__((ext_vector_type(EACH)));
+  typedef float F32 __attribute__((ext_vector_type(EACH)));
+  typedef In InAny __attribute__((aligned(sizeof(T))));
+  typedef Out OutAny __attribute__((aligned(sizeof(O))));
+  const int64_t per = (a.channels + EACH - 1) / EACH, all = a.tokens * per;
+  const bool small = EACH == 4 && all < int64_t(1) << 32;  // indexes of 32 bits divide faster, which those of 8 hide (84 us for 81 with it)
   for (int64_t base = (int64_t)blockIdx.x * (256 * U); base < all; base += (int64_t)gridDim.x * (256 * U)) {
-    typename Vec8<T>::V v[U];
+    In v[U];
     int64_t to[U];
     bool there[U];
 #pragma unroll
@@ -44,17 +64,18 @@ __global__ __launch_bounds__(256) void embed_lookup(LookupArgs a) {
       const int64_t i = base + u * 256 + threadIdx.x;
       to[u] = -1;
       there[u] = false;
-      v[u] = {};
+      v[u] = In{};
       if (i < all) {
-        const int64_t t = i / per;
-        int64_t c = (i - t * per) * 8;
-        if (!FEW && c + 8 > a.channels) c = a.channels - 8;
+        const int64_t t = small ? (unsigned)i / (unsigned)per : i / per;
+        int64_t c = (i - t * per) * EACH;
+        if (!FEW && c + EACH > a.channels) c = a.channels - EACH;
         const int id = a.ids[t];
         there[u] = (unsigned)id < (unsigned)a.vocab;
         to[u] = t * a.ld + c;
         if (there[u]) {
           const T* p = static_cast<const T*>(a.table) + (int64_t)id * a.channels + c;
-          v[u] = FEW ? load8(p, a.channels) : load8(p);
+          if constexpr (FEW) v[u] = load8(p, a.channels);
+          else v[u] = *reinterpret_cast<const InAny*>(p);
         }
       }
     }
@@ -62,10 +83,11 @@ __global__ __launch_bounds__(256) void embed_lookup(LookupArgs a) {
     for (int u = 0; u < U; ++u) {
       if (to[u] < 0) continue;
       // a token outside the table: zeros, also with a scale that is not finite
-      const typename Vec8<O>::V r = there[u] ? narrow8<O>(widen8<T>(v[u]) * a.scale) : typename Vec8<O>::V{};
+      const Out r = there[u] ? __builtin_convertvector(__builtin_convertvector(v[u], F32) * a.scale, Out) : Out{};
       O* p = static_cast<O*>(a.out) + to[u];
-      if (FEW) store8(p, r, a.channels);
-      else store8(p, r);
+      if constexpr (FEW) store8(p, r, a.channels);
+      else if constexpr (STREAM) __builtin_nontemporal_store(r, reinterpret_cast<OutAny*>(p));
+      else *reinterpret_cast<OutAny*>(p) = r;
     }
   }
 }
@@ -77,7 +99,7 @@ typedef f32x4 f32x4_any __attribute__((aligned(4)));
 // of them (a frequent token), every further piece leaves a partial sum of its own, and embed_join adds those up in order.  A thread has eight channels; `lanes`
 // threads (a power of two) have a row or, of a wide one, a slice.
 //
-// Bound: memory.  16384 tokens, 50001 x 2048, FP32 -> FP16: 77 us for 340 MB (4.4 TB/s), 17.5 us of sorting before and 8 of joining behind; 1777 tokens, 32003 x 1001, BF16: 17 us for 68 MB.
+// Bound: memory.  16384 tokens, 50001 x 2048, FP32 -> FP16: 66 us for 340 MB (5.1 TB/s), 14 us of sorting before and 8 of joining behind; 1777 tokens, 32003 x 1001, BF16: 17 us for 68 MB.
 // Blocks that add up come first, those that clear behind them (taking turns: 114 us); 128 registers a lane, so that four workgroups are on a compute unit (without the bound 202: 80 and 24 us).
 // Pieces are longer where there are more of them: 8 places, 16 from 4096 tokens and 32 from 32768, that is 512 workers or more for the chip and a partial sum for 16 rows or more.
 struct SumArgs {
@@ -112,7 +134,7 @@ struct Window {
   unsigned *key, *pos;
   unsigned before[2];
 };
-template <class O, class G>
+template <class O, class G, bool ONCE>
 __device__ __forceinline__ void sum_piece(const SumArgs& a, int64_t piece, int c, const Window& w) {
   constexpr int U = sizeof(O) == 4 ? 4 : 8;  // rows on their way at a time
   const int64_t rest = a.tokens - piece * a.piece;
@@ -155,7 +177,8 @@ __device__ __forceinline__ void sum_piece(const SumArgs& a, int64_t piece, int c
       if (!mine) k[u] = ~0u;
       // in the place of one that is not its own a row that it reads anyway, and does not add
       const O* const p = dout + (int64_t)w.pos[mine ? at : i] * a.ld;
-      v[u] = left >= 8 ? load8(p) : load8(p, left);
+      if constexpr (ONCE) v[u] = left >= 8 ? (typename Vec8<O>::V)__builtin_nontemporal_load(reinterpret_cast<const typename Vec8<O>::U*>(p)) : load8(p, left);
+      else v[u] = left >= 8 ? load8(p) : load8(p, left);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -175,7 +198,10 @@ __device__ __forceinline__ void sum_piece(const SumArgs& a, int64_t piece, int c
   }
 }
 
-template <class O, class G>
+// STREAM: rows without a token are written past the caches.  ONCE: rows of dout do not stay in them either, where they are half of the last-level cache together, whole lines, and FP32 only in one
+// slice, whose halves of lines come at once: 16384 tokens, 50001 x 2048, FP32 134 us without it, 126 so, 60000 of 20000 x 1024 203 and 180, 32000 of 50000 x 4096 in BF16 278 and 272; but 30000 of
+// 60000 x 4096 in FP32 425 and 430, of 60000 x 3000 338 and 362, 1777 of 32003 x 1001 in BF16 38.5 and 48.
+template <class O, class G, bool STREAM, bool ONCE>
 __global__ __launch_bounds__(256, 4) void embed_sum(SumArgs a) {
   __shared__ unsigned keys[32 * 64], pos[32 * 64];  // of each worker: two pieces
   const int per = 256 / a.lanes, mine = threadIdx.x / a.lanes, lane = threadIdx.x % a.lanes;
@@ -196,7 +222,7 @@ __global__ __launch_bounds__(256, 4) void embed_sum(SumArgs a) {
         if (piece > 1) win.before[1] = a.keys[at - a.piece - 1];
       }
       __syncthreads();
-      if (piece < a.pieces && c < a.channels) sum_piece<O, G>(a, piece, c, win);
+      if (piece < a.pieces && c < a.channels) sum_piece<O, G, ONCE>(a, piece, c, win);
     } else {  // what lies in rows of the table without a token, in vectors on 16 bytes whatever the channels are
       const int64_t all = (int64_t)a.vocab * a.channels, e0 = (b - a.sum_blocks) * ZERO_EACH, row0 = e0 / a.channels;
       const int n = (int)(all - e0 < ZERO_EACH ? all - e0 : ZERO_EACH);
@@ -217,7 +243,9 @@ __global__ __launch_bounds__(256, 4) void embed_sum(SumArgs a) {
       for (int j = 0; j < EACH; ++j) {
         const int i = (j * 256 + threadIdx.x) * 8;
         if (ends[j] >= 8) {
-          if (!busy[j]) store8(to + i, typename Vec8<G>::V{});
+          if (busy[j]) continue;
+          if constexpr (STREAM) stream8(to + i, typename Vec8<G>::V{});
+          else store8(to + i, typename Vec8<G>::V{});
         } else if (D >= 8) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -342,20 +370,30 @@ EmbedLayout embed_layout(const EmbedShape& s) {
 
 template <class T, class O>
 void lookup(const LookupArgs& a, hipStream_t st) {
-  const int64_t vecs = a.tokens * ((a.channels + 7) / 8);
-  const unsigned grid = (unsigned)std::min<int64_t>((vecs + 1023) / 1024, EMBED_GRID);
-  if (a.channels < 8) embed_lookup<T, O, true><<<grid, 256, 0, st>>>(a);
-  else embed_lookup<T, O, false><<<grid, 256, 0, st>>>(a);
+  const bool few = a.channels < 8, stream = !few && (size_t)a.tokens * a.channels * sizeof(O) >= STREAM_BYTES;
+  const int64_t each = few ? 8 : lookup_each<T, O>(stream), vecs = a.tokens * ((a.channels + each - 1) / each), of = 256 * 32 / each;
+  const unsigned grid = (unsigned)std::min<int64_t>((vecs + of - 1) / of, EMBED_GRID);
+  if (few) embed_lookup<T, O, true, false><<<grid, 256, 0, st>>>(a);
+  else if (stream) embed_lookup<T, O, false, true><<<grid, 256, 0, st>>>(a);
+  else embed_lookup<T, O, false, false><<<grid, 256, 0, st>>>(a);
 }
 
+template <class O, class G, bool STREAM>
+void sum_launch(const SumArgs& a, hipStream_t st) {
+  const unsigned grid = (unsigned)std::min<int64_t>(a.sum_blocks + a.zero_blocks, int64_t(1) << 23);
+  if (grid == 0) return;
+  const bool lines = a.ld * sizeof(O) % 128 == 0 && reinterpret_cast<uintptr_t>(a.dout) % 128 == 0;
+  if (lines && (sizeof(O) == 2 || a.slices == 1) && (size_t)a.tokens * a.channels * sizeof(O) >= STREAM_BYTES) embed_sum<O, G, STREAM, true><<<grid, 256, 0, st>>>(a);
+  else embed_sum<O, G, STREAM, false><<<grid, 256, 0, st>>>(a);
+}
 template <class O, class G>
 int sums(const SumArgs& a, hipStream_t st) {
-  const int64_t blocks = a.sum_blocks + a.zero_blocks;
-  if (blocks > 0) embed_sum<O, G><<<(unsigned)std::min<int64_t>(blocks, int64_t(1) << 23), 256, 0, st>>>(a);
+  if (sizeof(G) == 2 && (size_t)a.vocab * a.channels * sizeof(G) >= STREAM_BYTES) sum_launch<O, G, sizeof(G) == 2>(a, st);
+  else sum_launch<O, G, false>(a, st);
   if (jz::launch_status() != JZ_OK) return JZ_ERR_LAUNCH;
   if (a.tokens > 2 * a.piece) {
-    const dim3 grid((unsigned)std::min<int64_t>(a.pieces, 64), (unsigned)std::min<int64_t>((a.channels + 255) / 256, 64));
-    embed_join<G><<<grid, 512, 0, st>>>(a);
+    const dim3 join((unsigned)std::min<int64_t>(a.pieces, 64), (unsigned)std::min<int64_t>((a.channels + 255) / 256, 64));
+    embed_join<G><<<join, 512, 0, st>>>(a);
   }
   return jz::launch_status();
 }

@@ -220,3 +220,34 @@ def test_in_a_graph_and_on_another_stream(jz, T):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, again), k
+
+
+@pytest.mark.parametrize("types,T,D", [(("bf16", "bf16"), 16500, 4097), (("f16", "f32"), 16500, 2050), (("f32", "f32"), 8200, 4100), (("bf16", "f32"), 40000, 1003), (("f16", "f16"), 33000, 2048)])
+def test_lookups_past_the_caches(jz, types, T, D):
+    """Results of 128 MiB and more; half of a number is exact."""
+    V, dt, out = 3001, TYPES[types[0]], TYPES[types[1]]
+    g = torch.Generator(DEV).manual_seed(T)
+    table = torch.randint(-100, 101, (V, D), generator=g, device=DEV).to(dt)
+    ids = torch.randint(-2, V + 2, (T,), generator=g, device=DEV, dtype=torch.int32)
+    y = torch.full((T, D), 7.0, dtype=out, device=DEV)
+    jz.jz_embed_fwd(jz.embed_desc(T, V, D, jz.dtype_of(dt), jz.dtype_of(out), 0.5), ids, table, y)
+    there = (ids >= 0) & (ids < V)
+    assert torch.equal(y, torch.where(there[:, None], table[ids.clamp(0, V - 1).long()].to(out) * 0.5, torch.zeros((), dtype=out, device=DEV)))
+
+
+@pytest.mark.parametrize("types,T,V,D", [(("f16", "f32"), 33000, 70001, 1024), (("bf16", "bf16"), 34000, 17000, 4096), (("f16", "f32"), 18000, 20000, 4096), (("bf16", "f32"), 5000, 70001, 1001),
+                                         (("f32", "f32"), 70000, 40000, 512), (("f16", "f16"), 35000, 300, 2049), (("f16", "f16"), 33600, 400, 2048)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradients_past_the_caches(jz, types, T, V, D, accumulate):
+    """Tables and rows of 128 MiB and more; sums of whole numbers are exact."""
+    dt, out = TYPES[types[0]], TYPES[types[1]]
+    g = torch.Generator(DEV).manual_seed(T + V)
+    ids = torch.where(torch.rand(T, generator=g, device=DEV) < 0.01, torch.full((), V // 2, device=DEV), torch.randint(-2, V + 2, (T,), generator=g, device=DEV)).int()
+    dout = torch.randint(-1, 2, (T, D), generator=g, device=DEV).to(out)
+    before = torch.randint(-1, 2, (V, D), generator=g, device=DEV).to(dt) if accumulate else torch.full((V, D), float("nan"), dtype=dt, device=DEV)
+    got, d = before.clone(), jz.embed_desc(T, V, D, jz.dtype_of(dt), jz.dtype_of(out), 2.0)
+    jz.jz_embed_bwd(d, ids, dout, got, torch.full((jz.jz_embed_bwd_workspace_bytes(d),), 0x33, dtype=torch.uint8, device=DEV), accumulate=accumulate)
+    there = (ids >= 0) & (ids < V)
+    want = torch.zeros((V, D), device=DEV).index_add_(0, ids[there].long(), dout[there].float()) * 2
+    assert float(want.abs().max()) <= 250       # with one more, whole numbers in eight bits
+    assert torch.equal(got.float(), want + before.float() if accumulate else want)
