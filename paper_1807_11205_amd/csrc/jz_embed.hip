@@ -19,14 +19,9 @@ namespace {
 constexpr int ZERO_EACH = 16384;    // elements of the table that a workgroup looks at
 constexpr int EMBED_GRID = 1 << 16;  // workgroups at most: each takes further turns
 
-// What is written past the caches: results of half of the last-level cache and more, of which the next launch would find little there, and rows of the table that stand there stay.  Lookup of
+// Results of STREAM_BYTES and more are written past the caches: the next launch would find little of them there, and the table's rows stay.  Lookup of
 // 268 MB in BF16 85.4 us with ordinary stores, 81.0 so, of 262 MB out of 3000 rows 82 and 58, of 134 MB in FP32 43 and 30; the zeros of a table of 205 MB 144.7 and 137.9 with the lookup and all
 // (in FP32, two halves of every 32 bytes that go by themselves, 548 and 740: not those).
-constexpr size_t STREAM_BYTES = size_t(128) << 20;
-template <class T>
-__device__ __forceinline__ void stream8(T* p, typename Vec8<T>::V v) {
-  __builtin_nontemporal_store(v, reinterpret_cast<typename Vec8<T>::U*>(p));
-}
 
 // ---- lookup -----------------------------------------------------------------------------------------------------------------
 struct LookupArgs {

@@ -32,6 +32,12 @@ template <class T>
 __device__ __forceinline__ void store8(T* p, typename Vec8<T>::V v) {
   *reinterpret_cast<typename Vec8<T>::U*>(p) = v;
 }
+// past the caches: for results of half of the last-level cache and more, of which they would keep little
+constexpr size_t STREAM_BYTES = size_t(128) << 20;
+template <class T>
+__device__ __forceinline__ void stream8(T* p, typename Vec8<T>::V v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<typename Vec8<T>::U*>(p));
+}
 template <class T>
 __device__ __forceinline__ f32x8 widen8(typename Vec8<T>::V v) {
   return __builtin_convertvector(v, f32x8);

@@ -123,6 +123,21 @@ def test_linear_of_many_rows(jz, M, K, N):
     check(y[torch.from_numpy(some).to(DEV)].contiguous(), ref, np.abs(ref), 3.01, "y")
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("N,stride", [(8192, 0), (8195, 8224), (8195, 0)])
+def test_large_results(jz, dtype, N, stride):
+    """128 MiB and more of y, the same bits as a thousand rows at a time."""
+    M, K = 8200, 40
+    g = torch.Generator(DEV).manual_seed(N)
+    x = torch.randn((M, K), generator=g, device=DEV).to(TYPES[dtype])
+    wq, s = quantized(jz, torch.randn((N, K), generator=g, device=DEV))
+    room = torch.full((M, stride or N), 3.0, dtype=TYPES[dtype], device=DEV)
+    linear(jz, x, wq, s, N, y=room[:, :N], y_stride=stride)
+    for r in range(0, M, 1000):
+        assert torch.equal(room[r:r + 1000, :N], linear(jz, x[r:r + 1000].contiguous(), wq, s, N))
+    assert bool((room[:, N:] == 3).all())
+
+
 @pytest.mark.parametrize("M", [1, 40, 200, 3000])
 def test_largest_sums(jz, M):
     """in_features as large as int32 allows, every product 127 x 127; signs that alternate add up to nothing."""
