@@ -94,7 +94,7 @@ typedef f32x4 f32x4_any __attribute__((aligned(4)));
 // of them (a frequent token), every further piece leaves a partial sum of its own, and embed_join adds those up in order.  A thread has eight channels; `lanes`
 // threads (a power of two) have a row or, of a wide one, a slice.
 //
-// Bound: memory.  16384 tokens, 50001 x 2048, FP32 -> FP16: 66 us for 340 MB (5.1 TB/s), 14 us of sorting before and 8 of joining behind; 1777 tokens, 32003 x 1001, BF16: 17 us for 68 MB.
+// Bound: memory.  16384 tokens, 50001 x 2048, FP32 -> FP16: 73 us for 340 MB (4.7 TB/s), 13 us of sorting before and 7 of joining behind; 1777 tokens, 32003 x 1001, BF16: 17 us for 68 MB.
 // Blocks that add up come first, those that clear behind them (taking turns: 114 us); 128 registers a lane, so that four workgroups are on a compute unit (without the bound 202: 80 and 24 us).
 // Pieces are longer where there are more of them: 8 places, 16 from 4096 tokens and 32 from 32768, that is 512 workers or more for the chip and a partial sum for 16 rows or more.
 struct SumArgs {

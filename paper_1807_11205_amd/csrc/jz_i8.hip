@@ -7,7 +7,7 @@
 // until it has codes: rounded to 16 bits first, one code in 700 (FP16) or in 90 (BF16) would be its neighbour, which an answer in FP16 shows.
 //
 // Bound: with few rows the weights' way from memory (jz_i8_few.h), with many the matrix instructions (jz_mm_tile.h), in between two launches that wait for each other (9 us).
-// 16384 rows 4096 -> 12288 in BF16: 764 us, 52 of them codes (201 MB, 3.9 TB/s; a wavefront a row: a workgroup a row took 66).
+// 16384 rows 4096 -> 12288 in BF16: 725 to 760 us, 50 of them codes (201 MB, 3.9 TB/s; a wavefront a row: a workgroup a row took 66).
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -110,7 +110,7 @@ struct I8Out {
   int act;
 };
 // A lane has the same eight columns in every row that it stores; its scales are asked for together, from places that exist, before the first is needed.  (A load in each turn of the
-// loop was waited for in each: 16384 rows, 4096 -> 12288, 778 us and now 764.)
+// loop was waited for in each: 16384 rows, 4096 -> 12288, 778 us, so 764.)
 template <class T>
 struct I8Store : I8Out {
   bool stream;  // past the caches

@@ -3,13 +3,14 @@
 //
 // To the loads an operand is rows of bytes.  A tile of it is BM (BN) rows x 128 bytes, brought in by LDS-direct loads, two stages; 16-byte chunk c of a row lies at
 // c ^ (row / 2 % 8), so that neither the loads' writes nor the operands' reads meet on a bank.  An operand register is 16 bytes of a row for each lane: lane l has row l % 32 and
-// chunk 2 s + l / 32 in step s = 0 .. 3.  Two kinds of elements:
+// chunk 2 s + l / 32 in step s = 0 .. 3.  Three kinds of elements:
 //     ElemI8     128 int8 of k; a step is one 32x32x32 matrix instruction, sums are int32 and exact
 //     ElemSplit  32 k of an FP32 value v as hi = FP16(v) (chunks 0-3) and lo = FP16(v - hi) (chunks 4-7), 22 bits together.  A product is hi hi + hi lo + lo hi: three
 //                instructions for each two reads of an operand, so that the matrix instructions and not LDS are what the loop waits for
-//     ElemHalf   64 k as FP16
-// Bound, 256 x 256: the matrix instructions.  16384 rows 4096 -> 12288 of ElemI8 in 712 us, 2.3 POP/s (the library's product of 8192^3 2.1); ElemSplit, 4096 x 4096 times 4096 x 12288, 914 us,
-// 1.35 PFLOP/s of matrix instructions (FP16 library 1.36), which are busy 68 % of 1.6 GHz; 16 products of 1024^3 that fill 160 of the compute units 82 us, 20 of them results on their way.
+//     ElemHalf   64 k as FP16, a step one instruction
+// Bound, 256 x 256: the matrix instructions.  16384 rows 4096 -> 12288 of ElemI8 in 700 us, 2.3 POP/s (the library's product of 8192^3 2.1); ElemSplit, 4096 x 4096 times 4096 x 12288, 914 us,
+// 1.35 PFLOP/s of matrix instructions (FP16 library 1.36), which are busy 79 % of 1.6 GHz; the same of ElemHalf 345 us, 1.2 PFLOP/s; 16 products
+// of 1024^3 that fill 160 of the compute units 78 us, 20 of them results on their way.
 // Sums are in exchanged order (B's rows first): register 4 j + i of a lane holds row lane % 32, column 8 j + 4 (lane / 32) + i.
 #pragma once
 
