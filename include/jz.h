@@ -455,7 +455,7 @@ int jz_embed_bwd(const jz_embed_desc* desc, const int* ids_dev, const void* dout
  *     parameters is skipped, and the scale lowered, together with this one.
  * Sides up to 2^17, count up to 65535, count * stride and the padded matrices up to 2^35 elements, steps 1 to 64 (JZ_ERR_UNSUPPORTED beyond).  Outputs overlap
  * nothing (a batch reaches from its first element to its last).  The workspace holds the matrices in parts: 12 bytes an element and 8 to 24 for each of
- * the square of the shorter side; JZ_ERR_WORKSPACE with less than reported. */
+ * the square of the shorter side, up to 76 where that is at most 128; JZ_ERR_WORKSPACE with less than reported. */
 typedef struct {
   int64_t count;
   int rows, cols;
