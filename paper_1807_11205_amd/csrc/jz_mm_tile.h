@@ -7,9 +7,8 @@
 //     ElemI8     128 int8 of k; a step is one 32x32x32 matrix instruction, sums are int32 and exact
 //     ElemSplit  32 k of an FP32 value v as hi = FP16(v) (chunks 0-3) and lo = FP16(v - hi) (chunks 4-7), 22 bits together.  A product is hi hi + hi lo + lo hi: three
 //                instructions for each two reads of an operand, so that the matrix instructions and not LDS are what the loop waits for
-//     ElemHalf   64 k as FP16, a step one instruction
 // Bound, 256 x 256: the matrix instructions.  16384 rows 4096 -> 12288 of ElemI8 in 700 us, 2.3 POP/s (the library's product of 8192^3 2.1); ElemSplit, 4096 x 4096 times 4096 x 12288, 914 us,
-// 1.35 PFLOP/s of matrix instructions (FP16 library 1.36), which are busy 79 % of 1.6 GHz; the same of ElemHalf 345 us, 1.2 PFLOP/s; 16 products
+// 1.35 PFLOP/s of matrix instructions (FP16 library 1.36), which are busy 79 % of 1.6 GHz; 16 products
 // of 1024^3 that fill 160 of the compute units 78 us, 20 of them results on their way.
 // Sums are in exchanged order (B's rows first): register 4 j + i of a lane holds row lane % 32, column 8 j + 4 (lane / 32) + i.
 #pragma once
@@ -26,17 +25,13 @@ struct ElemI8 {
   static constexpr bool SPLIT = false;
   static __device__ __forceinline__ Sum mfma(Reg a, Reg b, Sum c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
 };
-template <bool SPLIT_>
-struct ElemFp16 {
+struct ElemSplit {
   typedef f16x8 Reg;
   typedef mm_f32x16 Sum;
   typedef float Val;
-  static constexpr bool SPLIT = SPLIT_;
+  static constexpr bool SPLIT = true;
   static __device__ __forceinline__ Sum mfma(Reg a, Reg b, Sum c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
-
-typedef ElemFp16<true> ElemSplit;
-typedef ElemFp16<false> ElemHalf;
 
 struct MmOperand {
   const void* p[2];        // [1]: the matrix interleaved with [0], 32 rows by 32 rows (B only)

@@ -7,7 +7,7 @@
 // the low part of an element of 2^-12, the size that a normalised 4096 x 4096 matrix has, still has its bits.  A and B are symmetric: only tiles on and below the diagonal are
 // computed, and stored twice.  X is kept in both orders, since it is an operand along both of its sides.
 //
-// Bound: the matrix instructions with large matrices (4096 x 12288, BF16: 5.1 ms, 1.13 PFLOP/s of them; 16 of 2816 x 1024, the whole update: 2.2 ms, 0.2 of it memory's around the products), with
+// Bound: the matrix instructions with large matrices (4096 x 12288, FP16 or BF16: 5.6 ms, 1.17 PFLOP/s of them; 16 of 2816 x 1024, the whole update: 2.2 ms, 0.2 of it memory's around the products), with
 // small ones the launches, each of which waits for the one before (128 x 512: nine, 87 us; three of 1001 x 333: twenty, 150 us).
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -30,18 +30,13 @@ constexpr int PAD = 32;      // sides of the matrices in the workspace are multi
 // workgroups that share a matrix's sum of squares
 int sum_parts(int64_t elements, int64_t count) { return (int)std::max<int64_t>(1, std::min((elements + 8191) / 8192, std::max<int64_t>(1, 2048 / count))); }
 
-// eight columns from col (a multiple of 8) on of a row of parts: 64 bytes of high parts of 32 columns, then their low parts; HALF: high parts alone
-template <bool HALF = false>
+// eight columns from col (a multiple of 8) on of a row of parts: 64 bytes of high parts of 32 columns, then their low parts
 __device__ __forceinline__ void store_parts(char* row, int64_t col, const float (&v)[8]) {
   f16x8 hi, lo;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     hi[i] = (_Float16)v[i];
     lo[i] = (_Float16)(v[i] - (float)hi[i]);
-  }
-  if (HALF) {
-    *reinterpret_cast<f16x8*>(row + col * 2) = hi;
-    return;
   }
   char* const p = row + (col >> 5) * 128 + (col & 31) * 2;
   *reinterpret_cast<f16x8*>(p) = hi;
@@ -168,7 +163,6 @@ __global__ __launch_bounds__(1024) void ortho_factors(OrthoIn a) {
 struct OrthoParts {
   char *r, *c;
   int64_t rp, cp;  // padded sides
-  bool r_half, c_half;
 };
 // FOLD: few sums, which every workgroup adds up by itself instead of a launch of one: 3 of 1001 x 333 161 and so 159 us, the update of 16 of 64 x 200 60.5 and 58.2.
 constexpr int ORTHO_FOLD = 1024;
@@ -231,37 +225,27 @@ __global__ __launch_bounds__(256) void ortho_parts(OrthoIn a, OrthoParts o) {
     if (r0 + row + h < o.rp && c0 + col < o.cp) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = tile[row + h][col + e];
-      char* const to = o.r + of * o.rp * o.cp * 4;
-      if (o.r_half) store_parts<true>(to + (r0 + row + h) * o.cp * 2, c0 + col, v);
-      else store_parts(to + (r0 + row + h) * o.cp * 4, c0 + col, v);
+      store_parts(o.r + (of * o.rp + r0 + row + h) * o.cp * 4, c0 + col, v);
     }
     if (c0 + row + h < o.cp && r0 + col < o.rp) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = tile[col + e][row + h];
-      char* const to = o.c + of * o.cp * o.rp * 4;
-      if (o.c_half) store_parts<true>(to + (c0 + row + h) * o.rp * 2, r0 + col, v);
-      else store_parts(to + (c0 + row + h) * o.rp * 4, r0 + col, v);
+      store_parts(o.c + (of * o.cp + c0 + row + h) * o.rp * 4, r0 + col, v);
     }
   }
 }
 
 // ---- products -------------------------------------------------------------------------------------------------------------------
-// [rows][cols] of parts, or of high parts alone: what the last product takes for a BF16 result.  Matrices lie equally far apart in both forms.
-struct Parts {
+struct Parts {  // [matrix][rows][cols]
   char* p;
   int64_t rows, cols;
-  bool half = false;
-  int64_t pitch() const { return cols * (half ? 2 : 4); }
-  template <bool HALF = false>
-  __device__ __forceinline__ char* row(int64_t of, int64_t r) const {
-    return p + (HALF ? of * rows * cols * 4 + r * cols * 2 : (of * rows + r) * cols * 4);
-  }
+  __device__ __forceinline__ char* row(int64_t of, int64_t r) const { return p + (of * rows + r) * cols * 4; }
 };
-template <bool HALF = false, class S>
+template <class S>
 __device__ __forceinline__ void store_rows(const S& s, const Parts& to, int64_t of, int64_t m0, int64_t n0, int lane, float factor) {
   constexpr int PER = S::COLS / 8, EACH = 64 / PER;
   const int c = lane % PER * 8;
-  char* const p = to.row<HALF>(of, m0);
+  char* const p = to.row(of, m0);
   if (n0 + c >= to.cols) return;
 #pragma unroll
   for (int t = 0; t < 32 / EACH; ++t) {
@@ -270,13 +254,13 @@ __device__ __forceinline__ void store_rows(const S& s, const Parts& to, int64_t 
     s.row8(row, c, v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= factor;
-    if (m0 + row < to.rows) store_parts<HALF>(p + row * to.cols * (HALF ? 2 : 4), n0 + c, v);
+    if (m0 + row < to.rows) store_parts(p + row * to.cols * 4, n0 + c, v);
   }
 }
-template <bool HALF = false, class S>
+template <class S>
 __device__ __forceinline__ void store_cols(const S& s, const Parts& to, int64_t of, int64_t m0, int64_t n0, int lane, float factor) {
   const int r = lane % 4 * 8;
-  char* const p = to.row<HALF>(of, n0);
+  char* const p = to.row(of, n0);
   if (m0 + r >= to.cols) return;
 #pragma unroll
   for (int t = 0; t < S::COLS / 16; ++t) {
@@ -285,17 +269,16 @@ __device__ __forceinline__ void store_cols(const S& s, const Parts& to, int64_t 
     s.col8(r, col, v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= factor;
-    if (n0 + col < to.rows) store_parts<HALF>(p + col * to.cols * (HALF ? 2 : 4), m0 + r, v);
+    if (n0 + col < to.rows) store_parts(p + col * to.cols * 4, m0 + r, v);
   }
 }
-template <bool HALF>
 struct OrthoSymmetric {  // a product that is its own transpose
   Parts a;
   float factor;
   template <class S>
   __device__ __forceinline__ void strip(const S& s, const MmTile& w, int64_t m0, int64_t n0, int lane) const {
-    store_rows<HALF>(s, a, w.of, m0, n0, lane, factor);
-    if (w.m != w.n) store_cols<HALF>(s, a, w.of, m0, n0, lane, factor);
+    store_rows(s, a, w.of, m0, n0, lane, factor);
+    if (w.m != w.n) store_cols(s, a, w.of, m0, n0, lane, factor);
   }
 };
 struct OrthoSums {  // sums as they are, a tile on and one below the diagonal
@@ -327,7 +310,6 @@ struct OrthoSums {  // sums as they are, a tile on and one below the diagonal
     }
   }
 };
-template <bool HALF>
 struct OrthoPoly {  // B = ca I + cb A + cc A^2
   Parts a, b;
   float ca, cb, cc;
@@ -347,19 +329,18 @@ struct OrthoPoly {  // B = ca I + cb A + cc A^2
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = fmaf(cc / SCALE, v[e], fmaf(cb, u[t][e], m0 + row == n0 + c + e ? ca * SCALE : 0.f));
       s.set_row8(row, c, v);
-      if (m0 + row < a.rows && n0 + c < a.cols) store_parts<HALF>(b.row<HALF>(w.of, m0 + row), n0 + c, v);
+      if (m0 + row < a.rows && n0 + c < a.cols) store_parts(b.row(w.of, m0 + row), n0 + c, v);
     }
-    if (w.m != w.n) store_cols<HALF>(s, b, w.of, m0, n0, lane, 1.f);
+    if (w.m != w.n) store_cols(s, b, w.of, m0, n0, lane, 1.f);
   }
 };
-template <bool HALF>
 struct OrthoApply {  // X <- B X
   Parts x, xt;
   float factor;
   template <class S>
   __device__ __forceinline__ void strip(const S& s, const MmTile& w, int64_t m0, int64_t n0, int lane) const {
     store_rows(s, x, w.of, m0, n0, lane, factor);
-    store_cols<HALF>(s, xt, w.of, m0, n0, lane, factor);
+    store_cols(s, xt, w.of, m0, n0, lane, factor);
   }
 };
 // The last B X: eight elements at a time to where they are stored, transposed back where TALL was transposed.
@@ -399,18 +380,16 @@ struct OrthoResult {
     }
   }
 };
-// The result itself, rounded once.  A BF16 result's last product takes operands rounded to FP16: their errors, 2^-12 each, are an eighth of the result's own, and the product a third
-// of the work; the launches before leave them so (read out of both parts: 5.28 and 5.08 ms for 4096 x 12288).  (FP16 results would be 1.7 times as far off.)
+// The result itself, rounded once.  (Operands rounded to FP16 in the last product of a BF16 result would save two thirds of it, 5.6 and 5.1 ms for 4096 x 12288, but P, up to 41 where X has
+// little, would count their errors that many times: with a matrix of low rank 1 to 2 % of the result.)
 template <class O>
 struct OrthoStore {
-  typedef typename std::conditional<std::is_same<O, __bf16>::value, ElemHalf, ElemSplit>::type E;
   O* y;
   __device__ __forceinline__ void put(int64_t at, f32x8 v, int left) const { store8(y + at, narrow8<O>(v), left); }
 };
 // The update's master weights and their copy.
 template <class T>
 struct MuonStore {
-  typedef ElemSplit E;
   float* w;
   T* w16;
   float lr, update_scale, wd;
@@ -450,12 +429,12 @@ struct OrthoLayout {
   bool short_side;
   OrthoLayout(const OrthoShape& s, int steps);
 };
-template <class E = ElemSplit, class Epi>
+template <class Epi>
 int ortho_product(const Parts& p, const Parts& q, bool symmetric, int64_t count, const int* skip, const Epi& e, hipStream_t st) {
   MmArgs a = {};
-  a.a = {{p.p, p.p}, p.rows, p.pitch(), p.rows * p.cols * 4};
-  a.b = {{q.p, q.p}, q.rows, q.pitch(), q.rows * q.cols * 4};
-  a.row_bytes = p.pitch();
+  a.a = {{p.p, p.p}, p.rows, p.cols * 4, p.rows * p.cols * 4};
+  a.b = {{q.p, q.p}, q.rows, q.cols * 4, q.rows * q.cols * 4};
+  a.row_bytes = p.cols * 4;
   a.symmetric = symmetric;
   a.skip = skip;
   // Fitted to 25 sizes from 192 to 4096 squared (1 to 16 of them), each with every tile; FP16 inputs.  The model is within 10 % of most and its choice within 5 % of the best.  Smaller tiles
@@ -469,12 +448,12 @@ int ortho_product(const Parts& p, const Parts& q, bool symmetric, int64_t count,
                                      {32, 4., 0., .2, 0., 1.3e-3, 256, 1.}};
   const int64_t best = mm_tile_for(kinds, p.rows, q.rows, symmetric, count, a.row_bytes);
   if constexpr (!std::is_same<Epi, OrthoSums>::value) {  // those have 128 rows at most: as many tiles of 128, and each takes less
-    if (best == 256) return mm_launch<E, Epi, 256, false>(a, e, p.rows, q.rows, count, st);
-    if (best == 192) return mm_launch<E, Epi, 192, false>(a, e, p.rows, q.rows, count, st);
+    if (best == 256) return mm_launch<ElemSplit, Epi, 256, false>(a, e, p.rows, q.rows, count, st);
+    if (best == 192) return mm_launch<ElemSplit, Epi, 192, false>(a, e, p.rows, q.rows, count, st);
   }
-  if (best == 128) return mm_launch<E, Epi, 128, false>(a, e, p.rows, q.rows, count, st);
-  if (best == 64) return mm_launch<E, Epi, 64, false>(a, e, p.rows, q.rows, count, st);
-  return mm_launch<E, Epi, 32, false>(a, e, p.rows, q.rows, count, st);
+  if (best == 128) return mm_launch<ElemSplit, Epi, 128, false>(a, e, p.rows, q.rows, count, st);
+  if (best == 64) return mm_launch<ElemSplit, Epi, 64, false>(a, e, p.rows, q.rows, count, st);
+  return mm_launch<ElemSplit, Epi, 32, false>(a, e, p.rows, q.rows, count, st);
 }
 
 // X X^T of a narrow X: as many workgroups to a tile as keep eight tiles of the sum (256 k) each and do not fill the chip.  Two phases of
@@ -545,33 +524,17 @@ int phase_steps(const OrthoLayout& L, int steps, int done) { return !L.short_sid
 
 template <class Sink>
 int ortho_steps(const jz_ortho_desc* d, const OrthoShape& s, const OrthoLayout& L, char* b, const Sink& sink, const int* skip, hipStream_t st) {
-  constexpr bool HALF = std::is_same<typename Sink::E, ElemHalf>::value;  // the last product's operands
   auto square = [&](size_t at) { return Parts{b + at, s.mp, s.mp}; };
   const Parts x = {b + L.x, s.mp, s.np};
   Parts A = square(L.a), A1 = square(L.more[0]), C = square(L.more[1]), P = square(L.more[2]), P1 = square(L.more[3]);
   const Parts B = square(L.b);
-  // HALF results where `half` says so, for sinks that take them
-  auto poly = [&](const Parts& p, const Parts& to, bool half) {
-    if constexpr (HALF)
-      if (half) return ortho_product(p, p, true, s.count, skip, OrthoPoly<true>{p, to, d->a, d->b, d->c}, st);
-    return ortho_product(p, p, true, s.count, skip, OrthoPoly<false>{p, to, d->a, d->b, d->c}, st);
-  };
-  auto symmetric = [&](const Parts& p, const Parts& q, const Parts& to, float factor, bool half = false) {
-    if constexpr (HALF)
-      if (half) return ortho_product(p, q, true, s.count, skip, OrthoSymmetric<true>{to, factor}, st);
-    return ortho_product(p, q, true, s.count, skip, OrthoSymmetric<false>{to, factor}, st);
-  };
-  auto apply = [&](const Parts& by, const Parts& xt, const Parts& to, const Parts& to_t, float factor, bool half) {
-    if constexpr (HALF)
-      if (half) return ortho_product(by, xt, false, s.count, skip, OrthoApply<true>{to, to_t, factor}, st);
-    return ortho_product(by, xt, false, s.count, skip, OrthoApply<false>{to, to_t, factor}, st);
-  };
+  auto symmetric = [&](const Parts& p, const Parts& q, const Parts& to, float factor) { return ortho_product(p, q, true, s.count, skip, OrthoSymmetric{to, factor}, st); };
   // P grows to a^steps where X has nothing: each step that it takes up scales it down by the power of two from |a| on
   const float shrink = exp2f(-ceilf(log2f(std::max(1.f, fabsf(d->a)))));
   int turn = 0, rc = JZ_OK;
   for (int done = 0, steps; done < d->steps; done += steps) {
     steps = phase_steps(L, d->steps, done);
-    const bool last = done + steps == d->steps, by_half = HALF && last, next_half = HALF && !last && done + steps + phase_steps(L, d->steps, done + steps) == d->steps;
+    const bool last = done + steps == d->steps;
     float small = 1.f;  // P in the workspace is SCALE small P
     if (s.mp <= CHAIN_SIDE) {
       for (int i = 1; i < steps; ++i) small *= shrink;
@@ -579,39 +542,38 @@ int ortho_steps(const jz_ortho_desc* d, const OrthoShape& s, const OrthoLayout& 
       const int splits = gram_splits(s);
       rc = ortho_gram_sums(x, s.count, splits, skip, OrthoSums{sums, s.mp, 1.f / SCALE}, st);
       const ChainArgs chain = {sums, {steps > 1 ? P : B, P1}, splits, steps, d->a, d->b, d->c, shrink, skip};
-      if (rc == JZ_OK) rc = by_half ? ortho_chain_launch<true>(chain, s.count, st) : ortho_chain_launch<false>(chain, s.count, st);
+      if (rc == JZ_OK) rc = ortho_chain_launch(chain, s.count, st);
       if ((steps - 1) & 1) std::swap(P, P1);
     } else {
       rc = symmetric(x, x, A, 1.f / SCALE);
       for (int i = 0; i < steps && rc == JZ_OK; ++i) {
         const Parts to = i == 0 && steps > 1 ? P : B;
-        rc = poly(A, to, by_half && steps == 1);
+        rc = ortho_product(A, A, true, s.count, skip, OrthoPoly{A, to, d->a, d->b, d->c}, st);
         if (rc == JZ_OK && i + 1 < steps) {
           rc = symmetric(to, A, C, 1.f / SCALE);
           if (rc == JZ_OK) rc = symmetric(C, to, A1, 1.f / SCALE);
           std::swap(A, A1);
         }
         if (rc == JZ_OK && i > 0) {
-          rc = symmetric(B, P, P1, shrink / SCALE, by_half && i + 1 == steps);
+          rc = symmetric(B, P, P1, shrink / SCALE);
           small *= shrink;
           std::swap(P, P1);
         }
       }
     }
     if (rc != JZ_OK) return rc;
-    const Parts xt = {b + L.xt[turn & 1], s.np, s.mp, by_half}, next = {b + L.xt[!(turn & 1)], s.np, s.mp, next_half};
+    const Parts xt = {b + L.xt[turn & 1], s.np, s.mp}, next = {b + L.xt[!(turn & 1)], s.np, s.mp};
     ++turn;
-    Parts by = steps > 1 ? P : B;
-    by.half = by_half;
-    if (!last) rc = apply(by, xt, x, next, 1.f / (SCALE * small), next_half);
-    else rc = ortho_product<typename Sink::E>(by, xt, false, s.count, skip, OrthoResult<Sink>{sink, s.m, s.n, s.stride, s.tall, 1.f / (SCALE * SCALE * small)}, st);
+    const Parts by = steps > 1 ? P : B;
+    if (!last) rc = ortho_product(by, xt, false, s.count, skip, OrthoApply{x, next, 1.f / (SCALE * small)}, st);
+    else rc = ortho_product(by, xt, false, s.count, skip, OrthoResult<Sink>{sink, s.m, s.n, s.stride, s.tall, 1.f / (SCALE * SCALE * small)}, st);
     if (rc != JZ_OK) return rc;
   }
   return JZ_OK;
 }
-OrthoParts begin_parts(const OrthoShape& s, const OrthoLayout& L, char* b, bool half) {  // half: X^T is an operand of the last product alone
-  if (s.tall) return {b + L.xt[0], b + L.x, s.np, s.mp, half, false};
-  return {b + L.x, b + L.xt[0], s.mp, s.np, false, half};
+OrthoParts begin_parts(const OrthoShape& s, const OrthoLayout& L, char* b) {
+  if (s.tall) return {b + L.xt[0], b + L.x, s.np, s.mp};
+  return {b + L.x, b + L.xt[0], s.mp, s.np};
 }
 size_t bytes_of(int dtype) { return dtype == JZ_F32 ? 4 : 2; }
 size_t batch_bytes(const OrthoShape& s, size_t each) { return s.count ? ((size_t)(s.count - 1) * s.stride + s.rows * s.cols) * each : 0; }
@@ -650,7 +612,7 @@ extern "C" int jz_orthogonalize(const jz_ortho_desc* d, const void* x, void* y, 
   in.parts = s.count ? sum_parts(s.rows * s.cols, s.count) : 0;
   in.inv = reinterpret_cast<double*>(b + L.inv);
   in.eps = d->eps;
-  const OrthoParts o = begin_parts(s, L, b, d->out_dtype == JZ_BF16 && phase_steps(L, d->steps, 0) == d->steps);
+  const OrthoParts o = begin_parts(s, L, b);
   rc = d->dtype == JZ_F32 ? ortho_begin<float, false>(in, s, o, st) : d->dtype == JZ_F16 ? ortho_begin<_Float16, false>(in, s, o, st) : ortho_begin<__bf16, false>(in, s, o, st);
   if (rc != JZ_OK) return rc;
   if (d->out_dtype == JZ_F32) return ortho_steps(d, s, L, b, OrthoStore<float>{static_cast<float*>(y)}, nullptr, st);
@@ -723,7 +685,7 @@ extern "C" int jz_muon_mp_update(const jz_ortho_desc* d, const jz_muon_hparams* 
     ortho_factors<true><<<1, 1024, 0, st>>>(in);
     return jz::launch_status();
   }
-  const OrthoParts o = begin_parts(s, L, b, false);
+  const OrthoParts o = begin_parts(s, L, b);
   rc = d->dtype == JZ_F16 ? ortho_begin<_Float16, true>(in, s, o, st) : ortho_begin<__bf16, true>(in, s, o, st);
   if (rc != JZ_OK) return rc;
   if (d->dtype == JZ_F16) return ortho_steps(d, s, L, b, MuonStore<_Float16>{master_w, static_cast<_Float16*>(weight16), hp->lr, hp->update_scale, hp->weight_decay}, found_inf_dev, st);

@@ -18,7 +18,7 @@ struct ChainArgs {
   const int* skip;
 };
 
-template <int KT, bool HALF>  // KT: the padded side / 32; HALF: the last P in high parts alone
+template <int KT>  // the padded side / 32
 __global__ __launch_bounds__(512, 2) void ortho_chain(ChainArgs a) {
   constexpr int SIDE = 32 * KT, ROW = 512;
   __shared__ __attribute__((aligned(1024))) unsigned char s0[CHAIN_SIDE * ROW], s1[CHAIN_SIDE * ROW];
@@ -86,13 +86,9 @@ __global__ __launch_bounds__(512, 2) void ortho_chain(ChainArgs a) {
     *reinterpret_cast<JZ_LDS f16x4*>(l + at(row, c)) = hi;
     *reinterpret_cast<JZ_LDS f16x4*>(l + at(row, c + 4)) = lo;
   };
-  auto store = [&](const Parts& to, int row, int col, f32x4 v, bool half) {
+  auto store = [&](const Parts& to, int row, int col, f32x4 v) {
     f16x4 hi, lo;
     split(v, &hi, &lo);
-    if (half) {
-      *reinterpret_cast<f16x4*>(to.row(of, 0) + (row * to.cols + col) * 2) = hi;  // inside the matrix's own place: others still read theirs
-      return;
-    }
     char* const p = to.row(of, row) + (col >> 5) * 128 + (col & 31) * 2;
     *reinterpret_cast<f16x4*>(p) = hi;
     *reinterpret_cast<f16x4*>(p + 64) = lo;
@@ -108,7 +104,7 @@ __global__ __launch_bounds__(512, 2) void ortho_chain(ChainArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) b[e] = fmaf(a.cc / SCALE, v[e], fmaf(a.cb, u[e], row == col + e ? a.ca * SCALE : 0.f));
       keep(s1, row, col, b);
-      if (i == 0) store(a.p[0], row, col, b, HALF && a.steps == 1);
+      if (i == 0) store(a.p[0], row, col, b);
     });
     if (i == 0 && a.steps == 1) return;
     __syncthreads();  // s1: B
@@ -128,7 +124,7 @@ __global__ __launch_bounds__(512, 2) void ortho_chain(ChainArgs a) {
           add(read(s1, wm * 64 + 32, j), y[j], s[1]);
         }
       }
-      each(s, [&](int row, int col, f32x4 v) { store(a.p[i & 1], row, col, v * (a.shrink / SCALE), HALF && i + 1 == a.steps); });
+      each(s, [&](int row, int col, f32x4 v) { store(a.p[i & 1], row, col, v * (a.shrink / SCALE)); });
     }
     if (i + 1 == a.steps) return;
     // A <- B A B
@@ -143,14 +139,13 @@ __global__ __launch_bounds__(512, 2) void ortho_chain(ChainArgs a) {
   }
 }
 
-template <bool HALF>
-int ortho_chain_launch(const ChainArgs& a, int64_t count, hipStream_t st) {
+inline int ortho_chain_launch(const ChainArgs& a, int64_t count, hipStream_t st) {
   const unsigned grid = (unsigned)count;
   switch (a.p[0].rows / 32) {
-    case 1: ortho_chain<1, HALF><<<grid, 512, 0, st>>>(a); break;
-    case 2: ortho_chain<2, HALF><<<grid, 512, 0, st>>>(a); break;
-    case 3: ortho_chain<3, HALF><<<grid, 512, 0, st>>>(a); break;
-    default: ortho_chain<4, HALF><<<grid, 512, 0, st>>>(a); break;
+    case 1: ortho_chain<1><<<grid, 512, 0, st>>>(a); break;
+    case 2: ortho_chain<2><<<grid, 512, 0, st>>>(a); break;
+    case 3: ortho_chain<3><<<grid, 512, 0, st>>>(a); break;
+    default: ortho_chain<4><<<grid, 512, 0, st>>>(a); break;
   }
   return jz::launch_status();
 }
