@@ -219,13 +219,34 @@ class GatedMLP:
 
     # ---- answers -------------------------------------------------------------------------------------------------------
     def prepare_answers_i8(self, stream=None):
-        """Codes and scales of all matrices as they are now, for answer(i8=True): again after every update that is to be seen."""
-        if self.i8 is None:
+        """Codes and scales of all matrices as `stream` (None: the current one) finds them, for answer(i8=True): again after every update that is to be seen.  Answers
+        that follow, on whatever stream, wait for the codes, and the codes for the answers before them.  In a capture both are left out, since a graph cannot wait for what is outside it:
+        there the order is the caller's."""
+        codes = self.i8
+        if codes is None:
             names = [n for n in self.shapes if n.startswith(("w_gate_", "w_up_", "w_down_"))] + [self.fc]
-            self.i8 = {n: (self._buf((self.shapes[n][0], api.i8_pitch(self.shapes[n][1])), torch.int8), self._buf(self.shapes[n][0], torch.float32)) for n in names}
+            codes = {n: (self._buf((self.shapes[n][0], api.i8_pitch(self.shapes[n][1])), torch.int8), self._buf(self.shapes[n][0], torch.float32)) for n in names}
             torch.cuda.current_stream(self.device).synchronize()
-        for n, (q, s) in self.i8.items():
-            api.jz_quantize_i8(*self.shapes[n], self._param(self.w16, n), q, s, stream=stream)
+            self.i8_written, self.i8_read = None, {}        # events: the last codes, and each stream's last answer
+        stream = self._stream_object(stream)
+        with torch.cuda.stream(stream):
+            captured = torch.cuda.is_current_stream_capturing()
+            if not captured:
+                for event in ([self.i8_written] if self.i8_written else []) + list(self.i8_read.values()):
+                    stream.wait_event(event)
+                self.i8_read = {}
+            for n, (q, s) in codes.items():
+                api.jz_quantize_i8(*self.shapes[n], self._param(self.w16, n), q, s)
+            if not captured:
+                self.i8_written = stream.record_event()
+        self.i8 = codes
+
+    def _stream_object(self, stream):
+        if stream is None:
+            return torch.cuda.current_stream(self.device)
+        if hasattr(stream, "cuda_stream"):
+            return stream
+        return torch.cuda.ExternalStream(int(stream), self.device) if int(stream) else torch.cuda.default_stream(self.device)
 
     def answer(self, x: torch.Tensor, stream=None, i8: bool = False) -> torch.Tensor:
         """Logits (float16) of the rows of x (float32 [any number of rows, width], or int32 tokens), nothing kept for a backward pass; i8: with the codes of
@@ -237,8 +258,7 @@ class GatedMLP:
         current = torch.cuda.current_stream(self.device)
         if stream is None or api._stream(stream) == api._stream(current):
             return self._answer(x, i8)
-        if not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(int(stream), self.device) if int(stream) else torch.cuda.default_stream(self.device)
+        stream = self._stream_object(stream)
         stream.wait_stream(current)
         with torch.cuda.stream(stream):         # copies, temporaries and launches all belong to it
             logits = self._answer(x, i8)
@@ -259,6 +279,9 @@ class GatedMLP:
             r = x.to(torch.float32).clone()
         logits = self._buf((rows, self.classes))
         if i8:
+            stream, captured = torch.cuda.current_stream(self.device), torch.cuda.is_current_stream_capturing()
+            if not captured:
+                stream.wait_event(self.i8_written)
             fc = api.linear_i8_desc(rows, D, self.classes, api.JZ_F16)
             ws = self._buf(max(16, api.jz_ffn_i8_workspace_bytes(ffn), api.jz_linear_i8_workspace_bytes(fc)), torch.uint8)
         else:
@@ -273,6 +296,8 @@ class GatedMLP:
             api.jz_norm_residual_fwd(around, r, y, m("w_post_%d" % i), m("gate_%d" % i), m("w_pre_%d" % (i + 1)), r, n, k1, k2)
         if i8:
             api.jz_linear_i8(fc, n, *self.i8[self.fc], logits, ws)
+            if not captured:
+                self.i8_read[stream.cuda_stream] = stream.record_event(self.i8_read.get(stream.cuda_stream))
         else:
             api.jz_gemm_fc(api.JZ_FWD, rows, D, self.classes, n, self._param(self.w16, self.fc), logits, ws)
         return logits
