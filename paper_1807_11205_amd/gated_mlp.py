@@ -24,13 +24,18 @@ from . import api
 EPS = 1e-5
 
 
+def _within_int32(t):
+    """Tokens or classes of 64 bits without their wrapping around: what int32 does not hold stays outside of every vocabulary, at -1 or 2^31 - 1."""
+    return t.clamp(-1, 2 ** 31 - 1) if t.dtype == torch.int64 else t
+
+
 class GatedMLP:
     vocab, fc, i8 = 0, "w_fc", None     # without a vocabulary, a classifier of its own, no codes
 
     def __init__(self, rows: int, width: int, hidden: int, classes: int, blocks: int, scale: float = 0.5, max_norm: float = 1.0, seed: int = 1,
                  initial_loss_scale: float = 1024.0, hparams: Optional[dict] = None, policy: Optional[dict] = None, device: str = "cuda:0", vocab: int = 0,
                  embed_scale: float = 1.0, tied: bool = False, optimizer: str = "lars", muon: Optional[dict] = None):
-        """vocab > 0: the rows are tokens (set_tokens; answer takes int32 tokens); tied: the classes are the vocabulary and the classifier's matrix is the embedding's table.
+        """vocab > 0: the rows are tokens (set_tokens; answer takes tokens too); tied: the classes are the vocabulary and the classifier's matrix is the embedding's table.
         muon: settings of the orthogonalised updates (lr, momentum, weight_decay, nesterov, steps)."""
         if width % 8 or hidden % 8 or classes % 8:
             raise ValueError("width, hidden and classes must be multiples of 8: tensors of the fused buffers start on 16 bytes")
@@ -153,20 +158,20 @@ class GatedMLP:
 
     # ---- the step ------------------------------------------------------------------------------------------------------
     def set_batch(self, x: torch.Tensor, labels: torch.Tensor, stream=None):
-        """r_0 (float32 [rows, width]) and the classes of the rows, copied on the stream of the step that takes them."""
+        """r_0 (float32 [rows, width]) and the classes of the rows (int32 or int64), copied on the stream of the step that takes them."""
         if self.vocab:
             raise ValueError("the network's rows are tokens: set_tokens")
         with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
             self.r[0].copy_(x)
-            self.labels.copy_(labels)
+            self.labels.copy_(_within_int32(labels))
 
     def set_tokens(self, ids: torch.Tensor, labels: torch.Tensor, stream=None):
-        """The rows' tokens (int32 [rows]; one outside the vocabulary is a row of zeros) and classes, as set_batch."""
+        """The rows' tokens (int32 or int64 [rows]; one outside the vocabulary is a row of zeros) and classes, as set_batch."""
         if not self.vocab:
             raise ValueError("the network has no vocabulary")
         with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
-            self.ids.copy_(ids)
-            self.labels.copy_(labels)
+            self.ids.copy_(_within_int32(ids))
+            self.labels.copy_(_within_int32(labels))
 
     def forward(self, stream=None):
         m = lambda n: self._param(self.master, n)
@@ -249,7 +254,7 @@ class GatedMLP:
         return torch.cuda.ExternalStream(int(stream), self.device) if int(stream) else torch.cuda.default_stream(self.device)
 
     def answer(self, x: torch.Tensor, stream=None, i8: bool = False) -> torch.Tensor:
-        """Logits (float16) of the rows of x (float32 [any number of rows, width], or int32 tokens), nothing kept for a backward pass; i8: with the codes of
+        """Logits (float16) of the rows of x (float32 [any number of rows, width], or tokens as set_tokens takes them), nothing kept for a backward pass; i8: with the codes of
         prepare_answers_i8.  x is as the current stream leaves it; the logits are ready once `stream` is (None: the current one)."""
         if i8 and self.i8 is None:
             raise ValueError("prepare_answers_i8 comes first")
@@ -274,7 +279,7 @@ class GatedMLP:
         n, y, k1, k2 = self._buf((rows, D)), self._buf((rows, D)), self._buf(rows, torch.float32), self._buf(rows, torch.float32)
         if self.vocab:
             r = self._buf((rows, D), torch.float32)
-            api.jz_embed_fwd(self._embed(rows), x.to(torch.int32).contiguous(), self._param(self.w16, "embed"), r)
+            api.jz_embed_fwd(self._embed(rows), _within_int32(x).to(torch.int32).contiguous(), self._param(self.w16, "embed"), r)
         else:
             r = x.to(torch.float32).clone()
         logits = self._buf((rows, self.classes))
