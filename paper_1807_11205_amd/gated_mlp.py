@@ -169,6 +169,10 @@ class GatedMLP:
         """The rows' tokens (int32 or int64 [rows]; one outside the vocabulary is a row of zeros) and classes, as set_batch."""
         if not self.vocab:
             raise ValueError("the network has no vocabulary")
+        if ids.is_floating_point():
+            raise ValueError("the network's rows are tokens")
+        if ids.shape != (self.rows,) or labels.shape != (self.rows,):
+            raise ValueError("a step takes %d tokens and as many classes" % self.rows)
         with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
             self.ids.copy_(_within_int32(ids))
             self.labels.copy_(_within_int32(labels))
