@@ -449,10 +449,12 @@ int jz_embed_bwd(const jz_embed_desc* desc, const int* ids_dev, const void* dout
  *       g = float(grad16) / S,  v <- momentum v + g,  u = g + momentum v where nesterov, else v,  O = the iteration's result for u (FP32)
  *       w <- w - lr (update_scale O + weight_decay w),   weight16 = RNE(w)
  *     S is state_dev->scale when state_dev (DEVICE, as in jz_lars_mp_update_dyn) is not NULL, else hp->loss_scale.  update_scale is the caller's choice, usually
- *     sqrt(max(1, rows / cols)).  *found_inf_dev (DEVICE int): 1 if a gradient, or the momentum that it would leave, is Inf or NaN, or if skip_dev (DEVICE int, may be NULL: another
+ *     sqrt(max(1, rows / cols)).  *found_inf_dev (DEVICE int): 1 if a gradient, or the v or u that it would lead to, is Inf or NaN, or if skip_dev (DEVICE int, may be NULL: another
  *     call's flag, as of jz_grad_clip) is not 0, else 0; with 1 nothing else is written.  Call it before jz_lars_mp_update_dyn, which adjusts the scale.  found_inf_dev may be the
  *     `nonfinite` of a LARS sink (jz_lars_sumsq_sink, after jz_lars_begin_step) of a tensor that no kernel fills, so that the presummed LARS update of the other
  *     parameters is skipped, and the scale lowered, together with this one.
+ *   jz_muon_mp_overflow  the flag of such an update alone, ahead of it: *found_inf_dev as above, nothing else but the workspace is written (as large as the update's).  Matrices of several shapes are one
+ *     step with it: the flags of all but the first shape, each call with the flag before as its skip_dev, then the updates in order, each with the flag before as its skip_dev.
  * Sides up to 2^17, count up to 65535, count * stride and the padded matrices up to 2^35 elements, steps 1 to 64 (JZ_ERR_UNSUPPORTED beyond).  Outputs overlap
  * nothing (a batch reaches from its first element to its last).  The workspace holds the matrices in parts: 12 bytes an element and 8 to 24 for each of
  * the square of the shorter side, up to 76 where that is at most 128; JZ_ERR_WORKSPACE with less than reported. */
@@ -471,6 +473,8 @@ typedef struct {
 int jz_orthogonalize_workspace_bytes(const jz_ortho_desc* desc, size_t* bytes);
 int jz_orthogonalize(const jz_ortho_desc* desc, const void* x, void* y, void* ws, size_t ws_bytes, void* hip_stream);
 int jz_muon_mp_update_workspace_bytes(const jz_ortho_desc* desc, size_t* bytes);
+int jz_muon_mp_overflow(const jz_ortho_desc* desc, const jz_muon_hparams* hp, const jz_loss_scale_state* state_dev, const int* skip_dev, const float* momentum,
+                        const void* grad16, int* found_inf_dev, void* ws, size_t ws_bytes, void* hip_stream);
 int jz_muon_mp_update(const jz_ortho_desc* desc, const jz_muon_hparams* hp, const jz_loss_scale_state* state_dev, const int* skip_dev, float* master_w,
                       float* momentum, const void* grad16, void* weight16, int* found_inf_dev, void* ws, size_t ws_bytes, void* hip_stream);
 

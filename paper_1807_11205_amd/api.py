@@ -51,7 +51,7 @@ EXPORTS = [
     "jz_norm_residual_fwd", "jz_norm_residual_bwd_workspace_bytes", "jz_norm_residual_bwd",
     "jz_ffn_fwd_workspace_bytes", "jz_ffn_fwd", "jz_ffn_bwd_workspace_bytes", "jz_ffn_bwd",
     "jz_embed_fwd", "jz_embed_bwd_workspace_bytes", "jz_embed_bwd",
-    "jz_orthogonalize_workspace_bytes", "jz_orthogonalize", "jz_muon_mp_update_workspace_bytes", "jz_muon_mp_update",
+    "jz_orthogonalize_workspace_bytes", "jz_orthogonalize", "jz_muon_mp_update_workspace_bytes", "jz_muon_mp_overflow", "jz_muon_mp_update",
     "jz_quantize_i8", "jz_linear_i8_workspace_bytes", "jz_linear_i8", "jz_ffn_i8_workspace_bytes", "jz_ffn_i8_fwd",
     "jz_status_string", "jz_version",
 ]
@@ -225,6 +225,7 @@ def lib() -> ctypes.CDLL:
         L.jz_embed_bwd.argtypes = [ep, vp, vp, ci, vp, vp, sz, vp]
         L.jz_orthogonalize_workspace_bytes.argtypes = L.jz_muon_mp_update_workspace_bytes.argtypes = [op, ctypes.POINTER(sz)]
         L.jz_orthogonalize.argtypes = [op, vp, vp, vp, sz, vp]
+        L.jz_muon_mp_overflow.argtypes = [op, ctypes.POINTER(jz_muon_hparams)] + [vp] * 6 + [sz, vp]
         L.jz_muon_mp_update.argtypes = [op, ctypes.POINTER(jz_muon_hparams)] + [vp] * 8 + [sz, vp]
         L.jz_quantize_i8.argtypes = [i64, ci, ci, vp, i64, vp, vp, vp]
         L.jz_linear_i8_workspace_bytes.argtypes = [lp, ctypes.POINTER(sz)]
@@ -1186,15 +1187,27 @@ def jz_muon_mp_update_workspace_bytes(desc: jz_ortho_desc) -> int:
     return _workspace_bytes("jz_muon_mp_update_workspace_bytes", desc)
 
 
+def _flag_or_address(flag):
+    return flag if flag is None or isinstance(flag, int) else _flag(flag)
+
+
+def jz_muon_mp_overflow(desc: jz_ortho_desc, hp: jz_muon_hparams, momentum, grad16, found_inf, ws, state: Optional[torch.Tensor] = None, skip=None, stream=None):
+    """found_inf: what jz_muon_mp_update would set there, for the updates of other matrices that are one step with this one's."""
+    _here(momentum, grad16, ws, state, *(None if isinstance(flag, int) else flag for flag in (skip, found_inf)))
+    wp, wn = _ws(ws)
+    _invoke("jz_muon_mp_overflow", (ctypes.addressof(desc), ctypes.addressof(hp), _ls_state(state) if state is not None else 0, _flag_or_address(skip),
+                                     _matrices_ptr(momentum, torch.float32, desc, "momentum"), _matrices_ptr(grad16, _type(desc.dtype), desc, "grad16"), _flag_or_address(found_inf), wp, wn), stream)
+
+
 def jz_muon_mp_update(desc: jz_ortho_desc, hp: jz_muon_hparams, master, momentum, grad16, weight16, found_inf, ws, state: Optional[torch.Tensor] = None, skip=None, stream=None):
     """The momentum, the orthogonalised update of the FP32 master weights and their 16-bit copy.  state: the device-resident loss scale (else hp.loss_scale); skip: another
-    call's overflow flag (int32[1]); found_inf: int32[1], or the address of a flag (as jz_lars_sumsq_sink gives them)."""
+    call's overflow flag; found_inf and skip: int32[1], or the address of a flag (as jz_lars_sumsq_sink gives them)."""
     t, f = _type(desc.dtype), torch.float32
-    _here(master, momentum, grad16, weight16, ws, state, skip, None if isinstance(found_inf, int) else found_inf)
+    _here(master, momentum, grad16, weight16, ws, state, *(None if isinstance(flag, int) else flag for flag in (skip, found_inf)))
     wp, wn = _ws(ws)
-    _invoke("jz_muon_mp_update", (ctypes.addressof(desc), ctypes.addressof(hp), _ls_state(state) if state is not None else 0, _flag(skip) if skip is not None else 0,
+    _invoke("jz_muon_mp_update", (ctypes.addressof(desc), ctypes.addressof(hp), _ls_state(state) if state is not None else 0, _flag_or_address(skip),
                                    _matrices_ptr(master, f, desc, "master"), _matrices_ptr(momentum, f, desc, "momentum"), _matrices_ptr(grad16, t, desc, "grad16"),
-                                   _matrices_ptr(weight16, t, desc, "weight16"), found_inf if isinstance(found_inf, int) else _flag(found_inf), wp, wn), stream)
+                                   _matrices_ptr(weight16, t, desc, "weight16"), _flag_or_address(found_inf), wp, wn), stream)
 
 
 def i8_pitch(cols: int) -> int:

@@ -475,8 +475,14 @@ int ortho_gram_sums(const Parts& x, int64_t count, int splits, const int* skip, 
 }
 
 template <class T, bool MUON>
+int ortho_norms(const OrthoIn& in, hipStream_t st) {
+  ortho_sumsq<T, MUON><<<dim3((unsigned)in.parts, (unsigned)in.count), 256, 0, st>>>(in);
+  return jz::launch_status();
+}
+template <class T, bool MUON>
 int ortho_begin(const OrthoIn& in, const OrthoShape& s, const OrthoParts& o, hipStream_t st) {
-  ortho_sumsq<T, MUON><<<dim3((unsigned)in.parts, (unsigned)s.count), 256, 0, st>>>(in);
+  const int rc = ortho_norms<T, MUON>(in, st);
+  if (rc != JZ_OK) return rc;
   const int64_t tiles = (o.rp + 63) / 64 * ((o.cp + 63) / 64) * s.count;
   if (s.count * in.parts <= ORTHO_FOLD) {
     ortho_parts<T, MUON, true><<<(unsigned)tiles, 256, 0, st>>>(in, o);
@@ -638,53 +644,89 @@ extern "C" int jz_muon_mp_update_workspace_bytes(const jz_ortho_desc* d, size_t*
   return JZ_OK;
 }
 
-extern "C" int jz_muon_mp_update(const jz_ortho_desc* d, const jz_muon_hparams* hp, const jz_loss_scale_state* state_dev, const int* skip_dev, float* master_w, float* momentum,
-                                 const void* grad16, void* weight16, int* found_inf_dev, void* ws, size_t ws_bytes, void* hip_stream) {
-  OrthoShape s;
-  int rc = muon_shape(d, &s);
+namespace {
+// What an update reads before it writes anything: the checks that both calls share, and the arguments of the first launches.
+int muon_in(const jz_ortho_desc* d, const jz_muon_hparams* hp, const jz_loss_scale_state* state_dev, const int* skip_dev, const float* momentum, const void* grad16, bool rest_there,
+            int* found_inf_dev, void* ws, size_t ws_bytes, OrthoShape* s, OrthoIn* in) {
+  const int rc = muon_shape(d, s);
   if (rc != JZ_OK) return rc;
-  if (!hp || !found_inf_dev || (s.count && (!master_w || !momentum || !grad16 || !weight16))) return JZ_ERR_NULL;
+  if (!hp || !found_inf_dev || (s->count && (!momentum || !grad16 || !rest_there))) return JZ_ERR_NULL;
   for (float v : {hp->lr, hp->momentum, hp->weight_decay, hp->update_scale})
     if (!(fabsf(v) < INFINITY)) return JZ_ERR_SHAPE;
   if (!state_dev && !(hp->loss_scale > 0.f && hp->loss_scale < 3.0e38f)) return JZ_ERR_SHAPE;
-  const OrthoLayout L(s, d->steps);
-  if (s.count && (!ws || ws_bytes < L.total)) return JZ_ERR_WORKSPACE;
-  if (!jz::aligned16(master_w) || !jz::aligned16(momentum) || !jz::aligned16(grad16) || !jz::aligned16(weight16) || !jz::aligned16(ws) ||
-      (reinterpret_cast<uintptr_t>(found_inf_dev) & 3) || (reinterpret_cast<uintptr_t>(skip_dev) & 3) || (reinterpret_cast<uintptr_t>(state_dev) & 7))
+  const OrthoLayout L(*s, d->steps);
+  if (s->count && (!ws || ws_bytes < L.total)) return JZ_ERR_WORKSPACE;
+  if (!jz::aligned16(momentum) || !jz::aligned16(grad16) || !jz::aligned16(ws) || (reinterpret_cast<uintptr_t>(found_inf_dev) & 3) || (reinterpret_cast<uintptr_t>(skip_dev) & 3) ||
+      (reinterpret_cast<uintptr_t>(state_dev) & 7))
     return JZ_ERR_ALIGN;
-  const size_t n = batch_bytes(s, 1);
-  const struct {
-    const void* p;
-    size_t bytes;
-  } t[] = {{master_w, 4 * n}, {momentum, 4 * n}, {weight16, 2 * n}, {found_inf_dev, 4}, {grad16, 2 * n}, {skip_dev, 4}, {state_dev, sizeof(*state_dev)}, {ws, ws_bytes}};
-  for (int i = 0; i < 4; ++i)  // what is written, against everything
-    for (int j = i + 1; j < 8; ++j)
-      if (jz::overlaps(t[i].p, t[i].bytes, t[j].p, t[j].bytes)) return JZ_ERR_ALIAS;
-  for (int j = 4; j < 7; ++j)
-    if (jz::overlaps(t[j].p, t[j].bytes, ws, ws_bytes)) return JZ_ERR_ALIAS;
-  hipStream_t st = static_cast<hipStream_t>(hip_stream);
   char* const b = static_cast<char*>(ws);
-  OrthoIn in = {};
-  in.x = grad16;
-  in.momentum = momentum;
-  in.inv_s = state_dev ? 1.f : 1.f / hp->loss_scale;
-  in.mu = hp->momentum;
-  in.state = state_dev;
-  in.nesterov = hp->nesterov != 0;
-  in.count = s.count;
-  in.rows = s.rows;
-  in.cols = s.cols;
-  in.stride = s.stride;
-  in.sums = reinterpret_cast<double*>(b + L.sums);
-  in.parts = s.count ? sum_parts(s.rows * s.cols, s.count) : 0;
-  in.inv = reinterpret_cast<double*>(b + L.inv);
-  in.eps = d->eps;
-  in.skip = skip_dev;
-  in.found_inf = found_inf_dev;
+  *in = {};
+  in->x = grad16;
+  in->momentum = const_cast<float*>(momentum);
+  in->inv_s = state_dev ? 1.f : 1.f / hp->loss_scale;
+  in->mu = hp->momentum;
+  in->state = state_dev;
+  in->nesterov = hp->nesterov != 0;
+  in->count = s->count;
+  in->rows = s->rows;
+  in->cols = s->cols;
+  in->stride = s->stride;
+  in->sums = reinterpret_cast<double*>(b + L.sums);
+  in->parts = s->count ? sum_parts(s->rows * s->cols, s->count) : 0;
+  in->inv = reinterpret_cast<double*>(b + L.inv);
+  in->eps = d->eps;
+  in->skip = skip_dev;
+  in->found_inf = found_inf_dev;
+  return JZ_OK;
+}
+struct Place {
+  const void* p;
+  size_t bytes;
+};
+// the first `written` of n places overlap nothing, and the workspace, the last of them, nothing either
+bool apart(const Place* t, int written, int n) {
+  for (int i = 0; i < n; ++i)
+    for (int j = i + 1; j < n; ++j)
+      if ((i < written || j == n - 1) && jz::overlaps(t[i].p, t[i].bytes, t[j].p, t[j].bytes)) return false;
+  return true;
+}
+}  // namespace
+
+extern "C" int jz_muon_mp_overflow(const jz_ortho_desc* d, const jz_muon_hparams* hp, const jz_loss_scale_state* state_dev, const int* skip_dev, const float* momentum, const void* grad16,
+                                   int* found_inf_dev, void* ws, size_t ws_bytes, void* hip_stream) {
+  OrthoShape s;
+  OrthoIn in;
+  const int rc = muon_in(d, hp, state_dev, skip_dev, momentum, grad16, true, found_inf_dev, ws, ws_bytes, &s, &in);
+  if (rc != JZ_OK) return rc;
+  const size_t n = batch_bytes(s, 1);
+  const Place t[] = {{found_inf_dev, 4}, {momentum, 4 * n}, {grad16, 2 * n}, {skip_dev, 4}, {state_dev, sizeof(*state_dev)}, {ws, ws_bytes}};
+  if (!apart(t, 1, 6)) return JZ_ERR_ALIAS;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (s.count) {
+    const int launched = d->dtype == JZ_F16 ? ortho_norms<_Float16, true>(in, st) : ortho_norms<__bf16, true>(in, st);
+    if (launched != JZ_OK) return launched;
+  }
+  ortho_factors<true><<<1, 1024, 0, st>>>(in);
+  return jz::launch_status();
+}
+
+extern "C" int jz_muon_mp_update(const jz_ortho_desc* d, const jz_muon_hparams* hp, const jz_loss_scale_state* state_dev, const int* skip_dev, float* master_w, float* momentum,
+                                 const void* grad16, void* weight16, int* found_inf_dev, void* ws, size_t ws_bytes, void* hip_stream) {
+  OrthoShape s;
+  OrthoIn in;
+  int rc = muon_in(d, hp, state_dev, skip_dev, momentum, grad16, master_w && weight16, found_inf_dev, ws, ws_bytes, &s, &in);
+  if (rc != JZ_OK) return rc;
+  if (!jz::aligned16(master_w) || !jz::aligned16(weight16)) return JZ_ERR_ALIGN;
+  const size_t n = batch_bytes(s, 1);
+  const Place t[] = {{master_w, 4 * n}, {momentum, 4 * n}, {weight16, 2 * n}, {found_inf_dev, 4}, {grad16, 2 * n}, {skip_dev, 4}, {state_dev, sizeof(*state_dev)}, {ws, ws_bytes}};
+  if (!apart(t, 4, 8)) return JZ_ERR_ALIAS;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (s.count == 0) {  // the flag alone
     ortho_factors<true><<<1, 1024, 0, st>>>(in);
     return jz::launch_status();
   }
+  const OrthoLayout L(s, d->steps);
+  char* const b = static_cast<char*>(ws);
   const OrthoParts o = begin_parts(s, L, b);
   rc = d->dtype == JZ_F16 ? ortho_begin<_Float16, true>(in, s, o, st) : ortho_begin<__bf16, true>(in, s, o, st);
   if (rc != JZ_OK) return rc;

@@ -11,8 +11,8 @@ One step = forward; softmax cross-entropy gradient times the loss scale; backwar
 by their global norm; the mixed-precision LARS update with the device-resident dynamic loss scale.  The residual stream and its gradient
 are FP32, everything between a block's norms FP16.  The norms' and gates' parameters are exempt from weight decay.
 
-With optimizer="muon" the blocks' matrices get orthogonalised updates instead, all of a shape in one call, and LARS has the other parameters; either skips the
-step when the other's gradients overflow.  Answers can also run with the matrices in 8-bit integers (prepare_answers_i8).
+With optimizer="muon" the blocks' matrices get orthogonalised updates instead, all of a shape in one call, and LARS has the other parameters; all of them skip the
+step where a gradient, or a matrix's momentum, overflows.  Answers can also run with the matrices in 8-bit integers (prepare_answers_i8).
 """
 from typing import Optional
 
@@ -106,7 +106,7 @@ class GatedMLP:
                 sink = api.jz_lars_sumsq_sink(self.ps, self.lars_ws, of_lars + k)
                 self.groups.append((desc, api.muon_hparams(update_scale=max(1.0, shape[0] / shape[1]) ** 0.5, **m), slice(a, b), sink.nonfinite))
                 ws = max(ws, api.jz_muon_mp_update_workspace_bytes(desc))
-            self.muon_ws = self._buf(ws, torch.uint8)
+            self.muon_ws, self.muon_found_inf = self._buf(ws, torch.uint8), self._buf(1, torch.int32)
 
         # clipping in place: every gradient of the fused buffer as a tensor of its own
         self.grad_list = api.GradList([self._param(self.grad, n) for n in self.shapes])
@@ -210,8 +210,13 @@ class GatedMLP:
         if self.muon:
             api.jz_lars_begin_step(self.ps, self.lars_ws, self.ls_state, stream)
             api.jz_lars_grad_sumsq(self.ps, 0, len(self.ps.flags), self.lars_ws, stream)
+            # one step over both shapes and LARS: the second shape's flag before the first is written, and each later update behind the flags of all before it
+            desc, hp, at, _ = self.groups[1]
+            skip = self.muon_found_inf
+            api.jz_muon_mp_overflow(desc, hp, self.momentum[at], self.grad[at], skip, self.muon_ws, self.ls_state, self.clip_found_inf, stream)
             for desc, hp, at, flag in self.groups:
-                api.jz_muon_mp_update(desc, hp, self.master[at], self.momentum[at], self.grad[at], self.w16[at], flag, self.muon_ws, self.ls_state, self.clip_found_inf, stream)
+                api.jz_muon_mp_update(desc, hp, self.master[at], self.momentum[at], self.grad[at], self.w16[at], flag, self.muon_ws, self.ls_state, skip, stream)
+                skip = flag
             api.jz_lars_mp_update_presummed_dyn(self.ps, self.hp, self.policy, self.ls_state, self.found_inf, self.lars_ws, stream)
             return
         api.jz_lars_mp_update_dyn(self.ps, self.hp, self.policy, self.ls_state, self.found_inf, self.lars_ws, stream)
