@@ -484,7 +484,8 @@ int jz_muon_mp_update(const jz_ortho_desc* desc, const jz_muon_hparams* hp, cons
  *   jz_quantize_i8   x [rows][cols] (x_stride elements apart, 0: dense; JZ_F16, JZ_BF16, JZ_F32) -> q, scale [rows] (FP32).  Codes lie in rows of
  *                    round16(cols) bytes, the multiple of 16 from cols on, zeros behind the last: the layout that the products want of weights.
  *   jz_linear_i8     y[m][n] = RNE( sum over k of q_x[m][k] q_w[n][k] * (s_x[m] s_w[n]) ): x is quantised row by row in the workspace; the sum is
- *                    int32 and exact.  x, y: dtype (all three).  in_features up to 131072 (what int32 holds).
+ *                    int32 and exact, the two products behind it are FP32 (so that scales whose product is no normal number of FP32 keep fewer bits, or give Inf or NaN).
+ *                    x, y: dtype (all three).  in_features up to 131072 (what int32 holds).
  *   jz_ffn_i8_fwd    the gated block of jz_ffn_fwd with all three matrices in codes: h = act(x W_gate^T) * (x W_up^T) in FP32 from the two products as above,
  *                    unrounded, then quantised row by row, y = RNE of the third.  dtype JZ_F16 or JZ_BF16; desc as for jz_ffn_fwd (dx_stride, dy_stride not used).
  * Any positive feature counts, rows >= 0 up to 2^31, other features and strides up to 2^24, a tensor up to 2^38 elements (JZ_ERR_UNSUPPORTED beyond).  Outputs overlap

@@ -8,7 +8,7 @@
 // computed, and stored twice.  X is kept in both orders, since it is an operand along both of its sides.
 //
 // Bound: the matrix instructions with large matrices (4096 x 12288, FP16 or BF16: 5.6 ms, 1.17 PFLOP/s of them; 16 of 2816 x 1024, the whole update: 2.2 ms, 0.2 of it memory's around the products), with
-// small ones the launches, each of which waits for the one before (128 x 512: nine, 87 us; three of 1001 x 333: twenty, 150 us).
+// small ones the launches, each of which waits for the one before (128 x 512: eight, 90 us; three of 1001 x 333: twenty, 158 us).
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -499,7 +499,8 @@ int ortho_begin(const OrthoIn& in, const OrthoShape& s, const OrthoParts& o, hip
 // steps as 2 + 3, against 64 bits: 2.2e-6 to 4e-5 for spectra from flat to 1e-6, as the plain form's 2.4e-6 to 6e-5; five steps without X: 8e-5 to 3e-4.)
 int phases(int steps) { return (steps + 2) / 3; }
 int first_phase(int steps) { return steps - 3 * (phases(steps) - 1); }
-// multiply-adds, halves of symmetric products alone; a tenth less has to be saved at least.  Where a phase is one launch (jz_ortho_chain.h) there are fewer of those too.
+// multiply-adds, halves of symmetric products alone; a tenth less has to be saved at least.  Where a phase is one launch (jz_ortho_chain.h) there are fewer of those too.  Launches are not weighed: this
+// way five steps are 18 products, with X itself 15, and by the tiles' model one matrix of 200 x 400 to 640 x 1000 takes 6 to 15 % longer this way (100 and 87 us, 181 and 167).
 bool short_side(int steps, int64_t m, int64_t n) {
   if (m <= CHAIN_SIDE) return true;
   const double p = phases(steps), k = steps, r = (double)n / (double)m;

@@ -4,7 +4,7 @@
 // number of lower lanes with its digit, and a counter for each wavefront and digit carries the count from one 64 to the next: no order depends on who comes first.
 // Up to 16384 tokens are sorted as runs of 1024 in LDS, and the runs joined: two launches.  (One workgroup for all of them was bound by what one compute unit can do: 16384 tokens of 50000, 35 us by
 // ballots, 46 with counters for each thread and digit.)  Beyond, each pass is three launches: counts of the digits in tiles of 4096, their running sums over the tiles, and the
-// move.
+// move; counts and moves are n / 4096 workgroups, so that short ones leave most of the chip idle (20000 tokens of 100000 x 64, two passes: 83 us for gradient and lookup, of 500 x 64, one pass: 57).
 // On the way `used` (one byte for each token of the vocabulary, or NULL) is cleared and then set where a token occurs, and *counter is cleared.
 #pragma once
 

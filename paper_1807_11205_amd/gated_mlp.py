@@ -7,6 +7,8 @@ for rows that come one at a time (sequencing and buffer bookkeeping only: every 
                r_{i+1} = r_i + scale gate_i norm(y) w_post_i,    n_{i+1} = norm(r_{i+1}) w_pre_{i+1}        one call
     logits = n_last W_fc^T         (tied: W_fc is E)
 
+Rows are independent of each other: nothing mixes them, so that with a vocabulary a row's logits depend on its one token alone (a bigram model, where the classes are the tokens that follow).
+
 One step = forward; softmax cross-entropy gradient times the loss scale; backward into the fused FP16 gradient buffer; clipping of all gradients
 by their global norm; the mixed-precision LARS update with the device-resident dynamic loss scale.  The residual stream and its gradient
 are FP32, everything between a block's norms FP16.  The norms' and gates' parameters are exempt from weight decay.
