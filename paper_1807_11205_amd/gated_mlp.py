@@ -16,6 +16,8 @@ are FP32, everything between a block's norms FP16.  The norms' and gates' parame
 With optimizer="muon" the blocks' matrices get orthogonalised updates instead, all of a shape in one call, and LARS has the other parameters; all of them skip the
 step where a gradient, or a matrix's momentum, overflows.  Answers can also run with the matrices in 8-bit integers (prepare_answers_i8).
 """
+import contextlib
+import threading
 from typing import Optional
 
 import numpy as np
@@ -138,7 +140,7 @@ class GatedMLP:
         if vocab:
             need.append(api.jz_embed_bwd_workspace_bytes(self.embed))
         self.ws = torch.zeros(max(16, *need), dtype=torch.uint8, device=self.device)
-        self.i8 = None
+        self.i8, self.i8_lock = None, threading.Lock()
         torch.cuda.current_stream(self.device).synchronize()    # whatever stream a step runs on, the buffers' fills are behind it
 
     # ---- buffers and parameter views --------------------------------------------------------------------------------
@@ -237,7 +239,11 @@ class GatedMLP:
     def prepare_answers_i8(self, stream=None):
         """Codes and scales of all matrices as `stream` (None: the current one) finds them, for answer(i8=True): again after every update that is to be seen.  Answers
         that follow, on whatever stream, wait for the codes, and the codes for the answers before them.  In a capture both are left out, since a graph cannot wait for what is outside it:
-        there the order is the caller's."""
+        there the order is the caller's.  Threads may call both: the launches of one call lie together."""
+        with self.i8_lock:
+            self._write_codes(stream)
+
+    def _write_codes(self, stream):
         codes = self.i8
         if codes is None:
             names = [n for n in self.shapes if n.startswith(("w_gate_", "w_up_", "w_down_"))] + [self.fc]
@@ -271,12 +277,13 @@ class GatedMLP:
             raise ValueError("prepare_answers_i8 comes first")
         if self.vocab and x.is_floating_point():
             raise ValueError("the network's rows are tokens")
-        current = torch.cuda.current_stream(self.device)
+        current, one = torch.cuda.current_stream(self.device), self.i8_lock if i8 else contextlib.nullcontext()
         if stream is None or api._stream(stream) == api._stream(current):
-            return self._answer(x, i8)
+            with one:
+                return self._answer(x, i8)
         stream = self._stream_object(stream)
         stream.wait_stream(current)
-        with torch.cuda.stream(stream):         # copies, temporaries and launches all belong to it
+        with one, torch.cuda.stream(stream):    # copies, temporaries and launches all belong to it
             logits = self._answer(x, i8)
         x.record_stream(stream)
         logits.record_stream(current)

@@ -1,6 +1,7 @@
 """Codes of the stack of gated blocks and the answers that read them, on streams of their own: what is ordered behind what (no GPU: every stream carries the set of the calls that
 are known to have ended before its next one, events and waits pass it on)."""
 import contextlib
+import threading
 
 import pytest
 import torch
@@ -71,6 +72,7 @@ def stack():
     m.shapes = {"%s_%d" % (n, i): (16, 32) if n == "w_down" else (32, 16) for n in ("w_gate", "w_up", "w_down") for i in range(2)}
     m.shapes["w_fc"] = (8, 16)
     m.master = m.w16 = torch.zeros(1)
+    m.i8_lock = threading.Lock()
     m._param = lambda buf, name: buf
     return m
 
@@ -113,3 +115,22 @@ def test_a_capture_waits_for_nothing_outside(monkeypatch):
     w.capturing = False
     m.answer(torch.zeros(3, 16), i8=True)       # waits for the codes of before the capture, as if that had not been
     assert set(range(7)) <= w.calls[-1][1]
+
+
+def test_codes_from_a_thread_wait_for_the_answer_that_is_being_launched(monkeypatch):
+    """One thread answers while another writes new codes: all launches of either lie together, and the later ones behind the earlier ones' event."""
+    w, m = World(monkeypatch), stack()
+    m.prepare_answers_i8()
+    first, thread = len(w.calls), []
+
+    def between(*a, stream=None, **k):      # in the middle of the answer
+        if not thread:
+            thread.append(threading.Thread(target=m.prepare_answers_i8, kwargs=dict(stream=8)))
+            thread[0].start()
+            thread[0].join(0.3)
+        w.call("jz_ffn_i8_fwd", stream)
+    monkeypatch.setattr(api, "jz_ffn_i8_fwd", between)
+    m.answer(torch.zeros(3, 16), 9, i8=True)
+    thread[0].join()
+    reads, new = w.since(first, *READS), w.since(first, "jz_quantize_i8")
+    assert len(reads) == 3 and len(new) == 7 and all(reads <= w.calls[n][1] for n in new)
