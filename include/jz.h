@@ -444,7 +444,8 @@ int jz_embed_bwd(const jz_embed_desc* desc, const int* ids_dev, const void* dout
  * five steps the values that are not tiny end near 1 (0.7 to 1.2).  a, b, c finite, and such that the singular values stay below 5 and |a + b t + c t^2| below
  * max(1, |a|) <= 30 over their squares t (results may be Inf or NaN otherwise: the products take 22 bits of every element, as two FP16 parts,
  * and of one below 2^-14 what is above 2^-36, so that a G whose norm is far below eps keeps fewer).  Sums are FP32, ||G|| is added up in FP64.
- *   jz_orthogonalize   x (dtype) -> y (out_dtype), each JZ_F16, JZ_BF16 or JZ_F32, one rounding.  A matrix of zeros gives zeros; one with Inf or NaN NaNs.
+ *   jz_orthogonalize   x (dtype) -> y (out_dtype), each JZ_F16, JZ_BF16 or JZ_F32, one rounding.  A result in JZ_F32 is as close as the formulas in FP32 are; for one of 16 bits, as for an
+ *     update, the steps are taken in polynomials of A where that is less work: errors up to five times as large, and well below the rounding.  A matrix of zeros gives zeros; one with Inf or NaN NaNs.
  *   jz_muon_mp_update  one optimiser step in mixed precision; grad16 and weight16 have dtype == out_dtype == JZ_F16 or JZ_BF16:
  *       g = float(grad16) / S,  v <- momentum v + g,  u = g + momentum v where nesterov, else v,  O = the iteration's result for u (FP32)
  *       w <- w - lr (update_scale O + weight_decay w),   weight16 = RNE(w)

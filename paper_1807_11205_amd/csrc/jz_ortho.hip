@@ -8,7 +8,7 @@
 // computed, and stored twice.  X is kept in both orders, since it is an operand along both of its sides.
 //
 // Bound: the matrix instructions with large matrices (4096 x 12288, FP16 or BF16: 5.6 ms, 1.17 PFLOP/s of them; 16 of 2816 x 1024, the whole update: 2.2 ms, 0.2 of it memory's around the products), with
-// small ones the launches, each of which waits for the one before (128 x 512: eight, 90 us; three of 1001 x 333: twenty, 158 us).
+// small ones the launches, each of which waits for the one before (128 x 512: eight, 90 us; three of 1001 x 333, FP32: seventeen, 171 us).
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -427,7 +427,7 @@ size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 struct OrthoLayout {
   size_t sums, inv, x, xt[2], a, b, more[4], total;
   bool short_side;
-  OrthoLayout(const OrthoShape& s, int steps);
+  OrthoLayout(const OrthoShape& s, const jz_ortho_desc* d);
 };
 template <class Epi>
 int ortho_product(const Parts& p, const Parts& q, bool symmetric, int64_t count, const int* skip, const Epi& e, hipStream_t st) {
@@ -497,17 +497,20 @@ int ortho_begin(const OrthoIn& in, const OrthoShape& s, const OrthoParts& o, hip
 // A <- B A B: four symmetric m x m products a step), X itself is not needed.  But A has lost a value s of X that is below 2^-11 of the largest, s^2 being below FP32's last
 // bit, so that X is made, and A from it, after three steps at most: by then A's error of 2^-24 has grown to some 2^-16 of the smallest values.  (Emulated in FP32 with 22-bit operands, five
 // steps as 2 + 3, against 64 bits: 2.2e-6 to 4e-5 for spectra from flat to 1e-6, as the plain form's 2.4e-6 to 6e-5; five steps without X: 8e-5 to 3e-4.)
+// Not for a result in FP32: in P the FP32 sums' errors of A grow with the square of what X's would, and where small values stand beside large ones that is more than FP32's own: normal
+// elements, 64 x 64 6.4e-6 where the formulas in FP32 have 1.2e-6, 128 x 128 7.4e-6 and 1.4e-6, 1024 x 2816 5.4e-6 and 2.6e-6; with steps of X itself 0.9e-6, 0.9e-6 and 2.1e-6.  It costs 128 x 512
+// 90 -> 113 us, 256 x 2048 153 -> 180, 4096 x 12288 5.8 -> 8.5 ms.  A result of 16 bits rounds 2e-4 of itself away or more, and an update's weights have O times lr.
 int phases(int steps) { return (steps + 2) / 3; }
 int first_phase(int steps) { return steps - 3 * (phases(steps) - 1); }
 // multiply-adds, halves of symmetric products alone; a tenth less has to be saved at least.  Where a phase is one launch (jz_ortho_chain.h) there are fewer of those too.  Launches are not weighed: this
-// way five steps are 18 products, with X itself 15, and by the tiles' model one matrix of 200 x 400 to 640 x 1000 takes 6 to 15 % longer this way (100 and 87 us, 181 and 167).
+// way five steps are 18 products, with X itself 15, and by the tiles' model one matrix of 200 x 400 to 640 x 1000 takes 6 to 15 % longer this way (100 and 87 us, 181 and 167; the last one, measured in FP32, 198 and 187).
 bool short_side(int steps, int64_t m, int64_t n) {
   if (m <= CHAIN_SIDE) return true;
   const double p = phases(steps), k = steps, r = (double)n / (double)m;
   return p * 3 * r + 4 * k - 3 * p < 0.9 * k * (3 * r + 1);
 }
 
-OrthoLayout::OrthoLayout(const OrthoShape& s, int steps) : short_side(::short_side(steps, s.m, s.n)) {
+OrthoLayout::OrthoLayout(const OrthoShape& s, const jz_ortho_desc* d) : short_side(d->out_dtype != JZ_F32 && ::short_side(d->steps, s.m, s.n)) {
   size_t o = 0;
   auto room = [&](size_t bytes) {
     const size_t at = o;
@@ -519,7 +522,7 @@ OrthoLayout::OrthoLayout(const OrthoShape& s, int steps) : short_side(::short_si
   inv = room((size_t)s.count * 8);
   x = room(wide);
   xt[0] = room(wide);
-  xt[1] = room(steps > 1 ? wide : 0);
+  xt[1] = room(d->steps > 1 ? wide : 0);
   a = room(s.mp <= CHAIN_SIDE ? square * gram_splits(s) : square);
   b = room(square);
   for (int i = 0; i < 4; ++i) more[i] = room(short_side && (i > 1 || s.mp > CHAIN_SIDE) ? square : 0);  // narrow ones have A, A B in LDS
@@ -592,7 +595,7 @@ extern "C" int jz_orthogonalize_workspace_bytes(const jz_ortho_desc* d, size_t* 
   OrthoShape s;
   const int rc = ortho_shape(d, &s);
   if (rc != JZ_OK) return rc;
-  *bytes = s.count ? OrthoLayout(s, d->steps).total : 0;
+  *bytes = s.count ? OrthoLayout(s, d).total : 0;
   return JZ_OK;
 }
 
@@ -602,7 +605,7 @@ extern "C" int jz_orthogonalize(const jz_ortho_desc* d, const void* x, void* y, 
   if (rc != JZ_OK) return rc;
   if (s.count == 0) return JZ_OK;
   if (!x || !y) return JZ_ERR_NULL;
-  const OrthoLayout L(s, d->steps);
+  const OrthoLayout L(s, d);
   if (!ws || ws_bytes < L.total) return JZ_ERR_WORKSPACE;
   if (!jz::aligned16(x) || !jz::aligned16(y) || !jz::aligned16(ws)) return JZ_ERR_ALIGN;
   const size_t nx = batch_bytes(s, bytes_of(d->dtype)), ny = batch_bytes(s, bytes_of(d->out_dtype));
@@ -641,7 +644,7 @@ extern "C" int jz_muon_mp_update_workspace_bytes(const jz_ortho_desc* d, size_t*
   OrthoShape s;
   const int rc = muon_shape(d, &s);
   if (rc != JZ_OK) return rc;
-  *bytes = OrthoLayout(s, d->steps).total;
+  *bytes = OrthoLayout(s, d).total;
   return JZ_OK;
 }
 
@@ -655,7 +658,7 @@ int muon_in(const jz_ortho_desc* d, const jz_muon_hparams* hp, const jz_loss_sca
   for (float v : {hp->lr, hp->momentum, hp->weight_decay, hp->update_scale})
     if (!(fabsf(v) < INFINITY)) return JZ_ERR_SHAPE;
   if (!state_dev && !(hp->loss_scale > 0.f && hp->loss_scale < 3.0e38f)) return JZ_ERR_SHAPE;
-  const OrthoLayout L(*s, d->steps);
+  const OrthoLayout L(*s, d);
   if (s->count && (!ws || ws_bytes < L.total)) return JZ_ERR_WORKSPACE;
   if (!jz::aligned16(momentum) || !jz::aligned16(grad16) || !jz::aligned16(ws) || (reinterpret_cast<uintptr_t>(found_inf_dev) & 3) || (reinterpret_cast<uintptr_t>(skip_dev) & 3) ||
       (reinterpret_cast<uintptr_t>(state_dev) & 7))
@@ -726,7 +729,7 @@ extern "C" int jz_muon_mp_update(const jz_ortho_desc* d, const jz_muon_hparams* 
     ortho_factors<true><<<1, 1024, 0, st>>>(in);
     return jz::launch_status();
   }
-  const OrthoLayout L(s, d->steps);
+  const OrthoLayout L(s, d);
   char* const b = static_cast<char*>(ws);
   const OrthoParts o = begin_parts(s, L, b);
   rc = d->dtype == JZ_F16 ? ortho_begin<_Float16, true>(in, s, o, st) : ortho_begin<__bf16, true>(in, s, o, st);
